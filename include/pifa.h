@@ -42,7 +42,8 @@ typedef enum {
   PIFA_ERR_RANK_DEFICIENT = -6,  /* W' = U V^T has fewer than r independent rows               */
   PIFA_ERR_WORKSPACE = -7,       /* workspace missing or smaller than pifa_workspace_size()    */
   PIFA_ERR_DEVICE_INDEX = -8,    /* a kernel met a pivot/non-pivot index outside [0, m)       */
-  PIFA_ERR_RANGE = -9            /* a Y_p value exceeded the fp16 range (C stored as fp16)      */
+  PIFA_ERR_RANGE = -9,           /* a Y_p value exceeded the fp16 range (C stored as fp16)      */
+  PIFA_ERR_CAPACITY = -10        /* page tables: more tokens, pages or columns than there are   */
 } pifa_status;
 
 /* Storage type of C. W_p, X and Y are always bf16. C may be bf16 or fp16 (both 2 bytes per
@@ -347,6 +348,143 @@ int pifa_m_reconstruct(const float* XXt, int64_t ldxx, const float* YtXt, int64_
 /* pifa_m_reconstruct_workspace_size -- bytes of device scratch pifa_m_reconstruct needs; negative
  * pifa_status on bad arguments. Pure host arithmetic. */
 int64_t pifa_m_reconstruct_workspace_size(int64_t m, int64_t n, int64_t r);
+
+/*
+ * Attention between the projections. A PIFA layer replaces a linear layer; the calls below are what lies between
+ * a decoder layer's q / k / v projections and its output projection when it serves or trains: page tables for a
+ * step's requests, rotary positions with the write into a paged key / value cache, and attention of each
+ * request's new tokens over its pages. The paper has no counterpart.
+ *
+ * The cache of one layer is two DEVICE buffers of `dtype` (a pifa_dtype), k_cache and v_cache, of `pages` pages
+ * of `page_size` tokens of `kv_heads` heads of `head_dim` elements; element e of head h of token o of page p is
+ * at p * page_stride + o * token_stride + h * head_stride + e in either buffer, so pages may hold tokens of
+ * heads or heads of tokens. A token's slot is p * page_size + o. Offsets are 64-bit.
+ * Activations are rows of heads: element e of head h of token t is at t * ld + h * head_dim + e.
+ * Alignment: bases 16 bytes, strides and leading dimensions multiples of 8 elements (PIFA_ERR_ALIGNMENT).
+ * The calls are asynchronous on cuda_stream, allocate nothing, take T == 0 (and B == 0) as a no-op, and can be captured into
+ * a CUDA graph: sizes that the host passes are capacities, lengths are read on the device.
+ */
+
+/*
+ * pifa_page_tables -- the tables of one step, from the requests' lengths.
+ *
+ *   cached_len   DEVICE, int32[B]: tokens of each request that are in the cache already.
+ *   new_len      DEVICE, int32[B]: tokens that this step adds (0 allowed). Negative lengths count as 0 and
+ *                latch PIFA_ERR_DEVICE_INDEX.
+ *   page_size    tokens per page, 1 to 65536.
+ *   free_pages   DEVICE, int32[n_free]: pages that may be handed out, in this order.
+ *   free_first   DEVICE, int32[1]: the first entry of free_pages that is still free.
+ *   table        DEVICE in/out, int32, B x cols, leading dimension ldt >= cols: row b holds request b's pages in
+ *                the order of its tokens. Entries [ceil(cached / page_size), ceil((cached + new) / page_size))
+ *                are written, request after request, with the next free pages; others are left as they are.
+ *   q_start      DEVICE out, int32[B + 1]: first row of each request's new tokens; q_start[B] is their number.
+ *   kv_len       DEVICE out, int32[B]: cached + new.
+ *   positions    DEVICE out, int32[T]: the position of each new token in its request; 0 in rows past q_start[B].
+ *   slots        DEVICE out, int64[T]: the slot of each new token; -1 in rows past q_start[B].
+ *   free_next    DEVICE out, int32[1]: free_first after this step.
+ *
+ *   B <= 4096 (PIFA_ERR_UNSUPPORTED). Where the new tokens exceed T, the pages n_free or a request's pages
+ *   cols, nothing is written out of bounds, tokens without a page get slot -1, free_next stops at n_free and
+ *   PIFA_ERR_CAPACITY is latched. A serving loop may pass kv_len = cached_len and free_next = free_first (each
+ *   exactly; they are written after every block has read them); outputs must not overlap otherwise.
+ */
+int pifa_page_tables(const int32_t* cached_len, const int32_t* new_len, int64_t B, int64_t page_size,
+                     const int32_t* free_pages, int64_t n_free, const int32_t* free_first,
+                     int32_t* table, int64_t cols, int64_t ldt,
+                     int32_t* q_start, int32_t* kv_len, int32_t* positions, int64_t* slots, int64_t T,
+                     int32_t* free_next, void* cuda_stream);
+
+/* Which elements of a head turn together: PIFA_ROPE_HALF pairs i with i + rot_dim / 2,
+ * PIFA_ROPE_INTERLEAVED 2 i with 2 i + 1 (i < rot_dim / 2). Elements from rot_dim on are not turned. */
+typedef enum { PIFA_ROPE_HALF = 0, PIFA_ROPE_INTERLEAVED = 1 } pifa_rope_layout;
+
+/* How pifa_rope_frequencies stretches frequencies for contexts `factor` times longer than `original`. */
+typedef enum {
+  PIFA_ROPE_SCALE_NONE = 0,
+  PIFA_ROPE_SCALE_LINEAR = 1, /* every frequency divided by factor                                      */
+  PIFA_ROPE_SCALE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)): the slowest pair divided by factor */
+  PIFA_ROPE_SCALE_BANDS = 3   /* by turns n within `original` positions: n >= high kept, n <= low divided by
+                                 factor, blended linearly in n between                                  */
+} pifa_rope_scaling;
+
+/*
+ * pifa_rope_frequencies -- HOST: the frequencies of rot_dim / 2 pairs, f_i = base^(-2 i / rot_dim) radians per
+ * position, scaled as `scaling` says, as whole multiples of 2^-64 turn: freq[i] = f_i / (2 pi) * 2^64. A phase
+ * is then position * freq[i] modulo 2^64, an integer product without an error that grows with the position.
+ *   freq         HOST out, int64[rot_dim / 2].
+ *   rot_dim      even, >= 2 (PIFA_ROPE_SCALE_BASE: >= 4). base > 1, factor >= 1, original > 0, 0 <= low < high
+ *                (the last four only where `scaling` uses them).
+ */
+int pifa_rope_frequencies(int64_t rot_dim, double base, int scaling, double factor, double original, double low,
+                          double high, int64_t* freq);
+
+/*
+ * pifa_rope -- rotary positions: each pair (x, y) of a head becomes scale (x cos a - y sin a, y cos a + x sin a),
+ * a = 2 pi position freq[i] / 2^64; with `inverse` the angle is -a, which is the gradient: dX from dY.
+ *   X            DEVICE, dtype, T rows of `heads` heads, leading dimension ldx >= heads * head_dim.
+ *   Y            DEVICE out, as X with ldy. Y may be X itself (ldx == ldy); it must not overlap X otherwise.
+ *   positions    DEVICE, int32[T].
+ *   freq         DEVICE, int64[rot_dim / 2] (pifa_rope_frequencies).
+ *   rot_dim      a multiple of 16 up to head_dim; head_dim a multiple of 16 up to 512 (PIFA_ERR_UNSUPPORTED).
+ *   scale        factor on the turned elements (1; some long-context methods raise it).
+ *   Numerics: fp32, rounded once to dtype.
+ */
+int pifa_rope(const void* X, int64_t T, int64_t heads, int64_t ldx, int64_t head_dim, int dtype,
+              const int32_t* positions, const int64_t* freq, int64_t rot_dim, int layout, float scale, int inverse,
+              void* Y, int64_t ldy, void* cuda_stream);
+
+/*
+ * pifa_rope_cache -- one launch between the projections and the attention: Q turned into Qr, K turned and stored
+ * at its tokens' slots of k_cache, V stored at the slots of v_cache.
+ *   Q, K, V      DEVICE, dtype, T rows of q_heads, kv_heads and kv_heads heads (ldq, ldk, ldv; they may be columns
+ *                of one projection's output).
+ *   positions    DEVICE, int32[T]; slots DEVICE, int64[T]: a slot of -1 stores nothing; others outside
+ *                [0, pages * page_size) store nothing and latch PIFA_ERR_DEVICE_INDEX. Slots of one call differ.
+ *   Qr           DEVICE out, ldqr; may be Q itself (ldqr == ldq), must not overlap an input otherwise.
+ *   freq, rot_dim, layout, scale as pifa_rope.
+ */
+int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T,
+                    int64_t q_heads, int64_t kv_heads, int64_t head_dim, int dtype,
+                    const int32_t* positions, const int64_t* slots,
+                    const int64_t* freq, int64_t rot_dim, int layout, float scale,
+                    void* Qr, int64_t ldqr, void* k_cache, void* v_cache, int64_t pages, int64_t page_size,
+                    int64_t page_stride, int64_t token_stride, int64_t head_stride, void* cuda_stream);
+
+/*
+ * pifa_paged_attention -- causal attention of each request's new tokens over its pages: with L = kv_len[b] and
+ * n = q_start[b + 1] - q_start[b], new token i of request b sees the keys j < L - n + i + 1, and
+ *   O = sum_j softmax_j(scale Q . K_j) V_j.
+ * Query head h reads key / value head h / (q_heads / kv_heads).
+ *
+ *   Q            DEVICE, dtype, T rows of q_heads heads, ldq. Rows [q_start[b], q_start[b + 1]) are request b's.
+ *   O            DEVICE out, as Q with ldo; must not overlap an input. A row that sees no key (L < n) gets zeros;
+ *                rows of no request are not written.
+ *   table        DEVICE, int32, B x cols, ldt: the pages of each request. Entries are read up to
+ *                ceil(kv_len / page_size). A request with kv_len > cols * page_size is cut to that and latches
+ *                PIFA_ERR_CAPACITY; keys of a page outside [0, pages) read as zeros and latch
+ *                PIFA_ERR_DEVICE_INDEX.
+ *   q_start      DEVICE, int32[B + 1], ascending from 0; kv_len DEVICE, int32[B].
+ *   max_q        at least every request's number of new tokens, at least 1 (host): picks the kernel. A request with more
+ *                latches PIFA_ERR_CAPACITY and its further rows are not written.
+ *   workspace    DEVICE scratch of pifa_paged_attention_workspace_size() bytes, 256-byte aligned, no
+ *                initialisation needed.
+ *   head_dim 64 or 128; page_size a power of two from 16 to 256; q_heads a multiple of kv_heads, at most 64 query heads to a
+ *   key / value head; B <= 4096 (PIFA_ERR_UNSUPPORTED).
+ *   What the cache holds past a request's kv_len, or in pages of no request, is not used, whatever its bits.
+ *   Numerics: fp32 scores, running maximum and sums; the weights enter the second product in dtype, scaled to at
+ *   most 1, O is rounded once. Results do not depend on the order in which blocks run.
+ */
+int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                         int dtype, const void* k_cache, const void* v_cache, int64_t pages, int64_t page_size,
+                         int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                         const int32_t* table, int64_t cols, int64_t ldt,
+                         const int32_t* q_start, const int32_t* kv_len, int64_t B, int64_t max_q, float scale,
+                         void* O, int64_t ldo, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* pifa_paged_attention_workspace_size -- bytes of device scratch pifa_paged_attention needs; negative
+ * pifa_status on bad arguments. */
+int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
+                                            int64_t max_q);
 
 /* pifa_validate_indices -- HOST copies: PIFA_OK iff pivot_idx (r entries) and nonpivot_idx
  * (m - r entries) are strictly ascending, inside [0, m) and disjoint (so together a partition

@@ -6,6 +6,7 @@
 #include <atomic>
 #include <mutex>
 #include <string>
+#include <utility>
 
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -105,6 +106,35 @@ int make_tmap_2d(CUtensorMap* map, int dtype, const void* base, int64_t rows, in
   return PIFA_OK;
 }
 
+int pifa_check_cache(const PifaCacheShape& c, int64_t least, int64_t most) {
+  const int64_t lim = (int64_t)1 << 31, far = (int64_t)1 << 46;
+  if (c.heads < 1 || c.heads > 65536 || c.dim < 1 || c.pages < 1 || c.pages >= lim || c.page_size < 1)
+    return pifa_fail(PIFA_ERR_INVALID_ARG, "cache: pages, page_size, heads or head_dim out of range");
+  if (c.page_size < least || c.page_size > most) return pifa_fail(PIFA_ERR_UNSUPPORTED, "cache: page_size not supported");
+  if (c.page_stride < 0 || c.token_stride < 0 || c.head_stride < 0 || c.page_stride >= far || c.token_stride >= lim ||
+      c.head_stride >= lim)
+    return pifa_fail(PIFA_ERR_INVALID_ARG, "cache: a stride out of range");
+  if ((c.page_stride | c.token_stride | c.head_stride) & 7)
+    return pifa_fail(PIFA_ERR_ALIGNMENT, "cache: strides must be multiples of 8 elements");
+  // elements of different heads, tokens and pages differ: sorted by stride, each steps over all of the ones below
+  struct { int64_t n, stride; } d[3] = {{c.heads, c.head_stride}, {c.page_size, c.token_stride}, {c.pages, c.page_stride}};
+  for (int i = 0; i < 3; ++i)
+    for (int j = 0; j < i; ++j)
+      if (d[i].stride < d[j].stride) std::swap(d[i], d[j]);
+  int64_t extent = c.dim;
+  for (const auto& x : d) {
+    if (x.n == 1) continue;
+    if (x.stride < extent) return pifa_fail(PIFA_ERR_INVALID_ARG, "cache: strides make elements overlap");
+    if (x.stride > ((int64_t)1 << 60) / x.n) return pifa_fail(PIFA_ERR_INVALID_ARG, "cache: too large");
+    extent += (x.n - 1) * x.stride;
+  }
+  return PIFA_OK;
+}
+
+PifaSpan pifa_cache_span(const void* base, const PifaCacheShape& c) {
+  return pifa_span(base, 1, (c.pages - 1) * c.page_stride + (c.page_size - 1) * c.token_stride + (c.heads - 1) * c.head_stride + c.dim, 0, 2);
+}
+
 // ---- public API ---------------------------------------------------------------------------------
 extern "C" {
 
@@ -130,6 +160,7 @@ const char* pifa_status_string(int status) {
     case PIFA_ERR_WORKSPACE: return "PIFA_ERR_WORKSPACE";
     case PIFA_ERR_DEVICE_INDEX: return "PIFA_ERR_DEVICE_INDEX";
     case PIFA_ERR_RANGE: return "PIFA_ERR_RANGE";
+    case PIFA_ERR_CAPACITY: return "PIFA_ERR_CAPACITY";
     default: return "PIFA_ERR_UNKNOWN";
   }
 }

@@ -80,6 +80,17 @@ inline bool pifa_spans_overlap(PifaSpan a, PifaSpan b) {
   return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
 }
 
+// ---- paged key / value caches (api.cpp) ---------------------------------------------------------
+// Element counts and strides of a cache's two buffers, as the entry points take them.
+struct PifaCacheShape {
+  int64_t pages, page_size, heads, dim;
+  int64_t page_stride, token_stride, head_stride;
+};
+// PIFA_OK, or the failure, for sizes and strides; page_size in [least, most].
+int pifa_check_cache(const PifaCacheShape& c, int64_t least, int64_t most);
+// The bytes from the first to the last element of one buffer.
+PifaSpan pifa_cache_span(const void* base, const PifaCacheShape& c);
+
 // ---- decode (decode.cu) ----------------------------------------------------------------------
 int64_t decode_workspace_bytes(const PifaShape& s);
 int launch_decode(const PifaShape& s, const PifaPointers& p, int* status, cudaStream_t stream);

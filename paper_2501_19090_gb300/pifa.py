@@ -7,6 +7,7 @@ missing or unloadable library raises -- there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -27,6 +28,7 @@ PIFA_ERR_RANK_DEFICIENT = -6
 PIFA_ERR_WORKSPACE = -7
 PIFA_ERR_DEVICE_INDEX = -8
 PIFA_ERR_RANGE = -9
+PIFA_ERR_CAPACITY = -10
 
 PIFA_DTYPE_BF16 = 0
 PIFA_DTYPE_FP16 = 1
@@ -41,6 +43,14 @@ PIFA_DECODE_GRID_WAVES = 1
 PIFA_DECODE_GRID_PERSISTENT = 2
 PIFA_DECODE_GRID_SPLITK = 3
 
+PIFA_ROPE_HALF = 0
+PIFA_ROPE_INTERLEAVED = 1
+
+PIFA_ROPE_SCALE_NONE = 0
+PIFA_ROPE_SCALE_LINEAR = 1
+PIFA_ROPE_SCALE_BASE = 2
+PIFA_ROPE_SCALE_BANDS = 3
+
 # every symbol include/pifa.h declares
 EXPORTS = (
     "pifa_forward", "pifa_forward_variant", "pifa_workspace_size", "pifa_select_variant",
@@ -51,6 +61,8 @@ EXPORTS = (
     "pifa_workspace_size_grouped", "pifa_compress_device", "pifa_compress_device_workspace_size",
     "pifa_backward", "pifa_backward_workspace_size", "pifa_m_accumulate", "pifa_m_accumulate_workspace_size",
     "pifa_m_reconstruct", "pifa_m_reconstruct_workspace_size",
+    "pifa_page_tables", "pifa_rope_frequencies", "pifa_rope", "pifa_rope_cache",
+    "pifa_paged_attention", "pifa_paged_attention_workspace_size",
 )
 
 
@@ -123,6 +135,25 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.pifa_m_reconstruct.restype = ctypes.c_int
         lib.pifa_m_reconstruct_workspace_size.argtypes = [_I64, _I64, _I64]
         lib.pifa_m_reconstruct_workspace_size.restype = _I64
+        lib.pifa_page_tables.argtypes = [_VP, _VP, _I64, _I64, _VP, _I64, _VP, _VP, _I64, _I64, _VP, _VP, _VP, _VP,
+                                         _I64, _VP, _VP]
+        lib.pifa_page_tables.restype = ctypes.c_int
+        lib.pifa_rope_frequencies.argtypes = [_I64, ctypes.c_double, ctypes.c_int, ctypes.c_double, ctypes.c_double,
+                                              ctypes.c_double, ctypes.c_double, _VP]
+        lib.pifa_rope_frequencies.restype = ctypes.c_int
+        lib.pifa_rope.argtypes = [_VP, _I64, _I64, _I64, _I64, ctypes.c_int, _VP, _VP, _I64, ctypes.c_int,
+                                  ctypes.c_float, ctypes.c_int, _VP, _I64, _VP]
+        lib.pifa_rope.restype = ctypes.c_int
+        lib.pifa_rope_cache.argtypes = [_VP, _I64, _VP, _I64, _VP, _I64, _I64, _I64, _I64, _I64, ctypes.c_int, _VP,
+                                        _VP, _VP, _I64, ctypes.c_int, ctypes.c_float, _VP, _I64, _VP, _VP, _I64, _I64,
+                                        _I64, _I64, _I64, _VP]
+        lib.pifa_rope_cache.restype = ctypes.c_int
+        lib.pifa_paged_attention.argtypes = [_VP, _I64, _I64, _I64, _I64, _I64, ctypes.c_int, _VP, _VP, _I64, _I64,
+                                             _I64, _I64, _I64, _VP, _I64, _I64, _VP, _VP, _I64, _I64, ctypes.c_float,
+                                             _VP, _I64, _VP, _I64, _VP]
+        lib.pifa_paged_attention.restype = ctypes.c_int
+        lib.pifa_paged_attention_workspace_size.argtypes = [_I64] * 6
+        lib.pifa_paged_attention_workspace_size.restype = _I64
         lib.pifa_validate_indices.argtypes = [_VP, _VP, _I64, _I64]
         lib.pifa_validate_indices.restype = ctypes.c_int
         lib.pifa_device_status.argtypes = [_VP]
@@ -616,3 +647,214 @@ def pifa_m_reconstruct(XXt, YtXt, V, W=None, alpha=0.0, stream=None):
                                    _stream_ptr(stream))
     _check(st, "pifa_m_reconstruct")
     return U_r, V_r
+
+
+# ---- between the projections: page tables, rotary positions, attention over a paged cache ----------
+def _refuse(msg):
+    raise ValueError(f"pifa: {msg}")
+
+
+def _on(stream):
+    """A context in which torch allocates and fills on `stream`, where the call's kernels will run."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
+def _vector(name, t, n, dtype, device):
+    """`t`, a contiguous 1-D tensor of n elements of `dtype` on `device` (n None: any number)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous() \
+            or (n is not None and t.shape[0] != n):
+        _refuse(f"{name} must be a contiguous 1-D {dtype} tensor" + ("" if n is None else f" of {n} elements"))
+    if t.device != device:
+        _refuse(f"{name} is on {t.device}, not on {device}")
+    return t.data_ptr()
+
+
+def _rows_of_heads(name, t, dtype=None, device=None):
+    """(T, heads, head_dim, row pitch) of a T x heads x head_dim bf16 or fp16 tensor whose heads are dense."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != 3 or (t.dtype is not torch.bfloat16 and t.dtype is not torch.float16):
+        _refuse(f"{name} must be a tokens x heads x head_dim tensor, bfloat16 or float16")
+    T, h, d = t.shape
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 and d != 1) or (s1 != d and h != 1):
+        _refuse(f"{name}: the heads of a token must lie one after another (strides {t.stride()})")
+    if dtype is not None and t.dtype is not dtype:
+        _refuse(f"{name} is {t.dtype}, not {dtype}")
+    if device is None:
+        if t.device.type != "cuda":
+            _refuse(f"{name} must be a CUDA tensor (it is on {t.device})")
+    elif t.device != device:
+        _refuse(f"{name} is on {t.device}, not on {device}")
+    return T, h, d, (s0 if T > 1 else h * d)  # one row has no pitch, whatever its stride says
+
+
+def _cache_strides(k_cache, v_cache, d, dtype, device):
+    """(pages, page_size, kv_heads, page stride, token stride, head stride) of two pages x page_size x
+    kv_heads x head_dim tensors of one set of strides."""
+    import torch
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 4 or t.dtype is not dtype or t.shape[3] != d:
+            _refuse(f"{name} must be a pages x page_size x kv_heads x {d} tensor, {dtype}")
+        if t.device != device:
+            _refuse(f"{name} is on {t.device}, not on {device}")
+    pages, size, heads, _ = k_cache.shape
+    st = k_cache.stride()
+    if v_cache.shape != k_cache.shape or v_cache.stride() != st or st[3] != 1:
+        _refuse("k_cache and v_cache must have one shape and one set of strides, the last stride 1")
+    return pages, size, heads, st[0], st[1], st[2]
+
+
+def _table_ld(table, B, device):
+    import torch
+    if not isinstance(table, torch.Tensor) or table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != B \
+            or (table.shape[1] > 1 and table.stride(1) != 1):
+        _refuse(f"table must be an int32 tensor of {B} rows with unit column stride")
+    if table.device != device:
+        _refuse(f"table is on {table.device}, not on {device}")
+    return max(table.stride(0), table.shape[1]) if B > 1 else table.shape[1]
+
+
+def pifa_page_tables(cached_len, new_len, page_size: int, free_pages, free_first, table, tokens: int, out=None, stream=None):
+    """Page tables of one step (pifa_page_tables): cached_len, new_len int32 (B), free_pages int32, free_first
+    int32 (1), table int32 (B x columns, updated in place), `tokens` rows of room for the new tokens. Returns
+    (q_start, kv_len, positions, slots, free_next); `out` gives those tensors."""
+    import torch
+    i32 = torch.int32
+    if not isinstance(cached_len, torch.Tensor) or cached_len.device.type != "cuda":
+        _refuse("cached_len must be a CUDA tensor")
+    dev = cached_len.device
+    c = _vector("cached_len", cached_len, None, i32, dev)
+    B = cached_len.shape[0]
+    n = _vector("new_len", new_len, B, i32, dev)
+    f = _vector("free_pages", free_pages, None, i32, dev)
+    ff = _vector("free_first", free_first, 1, i32, dev)
+    ldt = _table_ld(table, B, dev)
+    T = int(tokens)
+    if T < 0:
+        _refuse("tokens must be >= 0")
+    if out is None:
+        with _on(stream):
+            out = (torch.empty(B + 1, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev),
+                   torch.empty(T, dtype=i32, device=dev), torch.empty(T, dtype=torch.int64, device=dev),
+                   torch.empty(1, dtype=i32, device=dev))
+    q_start, kv_len, positions, slots, free_next = out
+    st = _lib().pifa_page_tables(
+        c, n, B, int(page_size), f, free_pages.shape[0], ff, table.data_ptr(), table.shape[1], ldt,
+        _vector("q_start", q_start, B + 1, i32, dev), _vector("kv_len", kv_len, B, i32, dev),
+        _vector("positions", positions, T, i32, dev), _vector("slots", slots, T, torch.int64, dev), T,
+        _vector("free_next", free_next, 1, i32, dev), _stream_ptr(stream))
+    _check(st, "pifa_page_tables")
+    return q_start, kv_len, positions, slots, free_next
+
+
+def pifa_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = PIFA_ROPE_SCALE_NONE, factor: float = 1.0,
+                          original: float = 0.0, low: float = 1.0, high: float = 4.0, device=None):
+    """Frequencies of rot_dim / 2 pairs as whole multiples of 2^-64 turn a position (pifa_rope_frequencies, host
+    arithmetic): an int64 tensor on `device` (default: the host)."""
+    import torch
+    freq = torch.empty(max(int(rot_dim) // 2, 0), dtype=torch.int64)
+    _check(_lib().pifa_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor), float(original),
+                                        float(low), float(high), freq.data_ptr() or None), "pifa_rope_frequencies")
+    return freq if device is None else freq.to(device)
+
+
+def pifa_rope(X, positions, freq, layout: int = PIFA_ROPE_HALF, scale: float = 1.0, inverse: bool = False, Y=None,
+              stream=None):
+    """Rotary positions (pifa_rope) of X (T x heads x head_dim, bf16 or fp16); positions int32 (T), freq int64
+    (rot_dim / 2). inverse: the gradient, dX from dY. Y may be X; allocated if not given."""
+    import torch
+    T, h, d, ldx = _rows_of_heads("X", X)
+    dev = X.device
+    p = _vector("positions", positions, T, torch.int32, dev)
+    f = _vector("freq", freq, None, torch.int64, dev)
+    if Y is None:
+        with _on(stream):
+            Y = torch.empty((T, h, d), dtype=X.dtype, device=dev)
+    ys = _rows_of_heads("Y", Y, X.dtype, dev)
+    if ys[:3] != (T, h, d):
+        _refuse(f"Y must be a tensor of shape {(T, h, d)}")
+    st = _lib().pifa_rope(X.data_ptr(), T, h, ldx, d, c_dtype_of(X), p, f, 2 * freq.shape[0], int(layout), float(scale),
+                          int(bool(inverse)), Y.data_ptr(), ys[3], _stream_ptr(stream))
+    _check(st, "pifa_rope")
+    return Y
+
+
+def pifa_rope_cache(Q, K, V, positions, slots, freq, k_cache, v_cache, layout: int = PIFA_ROPE_HALF, scale: float = 1.0,
+                    Qr=None, stream=None):
+    """Q (T x heads x head_dim) turned into Qr, K (T x kv_heads x head_dim) turned into k_cache and V into v_cache
+    (pages x page_size x kv_heads x head_dim, updated in place) at `slots` int64 (T): pifa_rope_cache. Qr may be
+    Q; allocated if not given."""
+    import torch
+    T, h, d, ldq = _rows_of_heads("Q", Q)
+    dev, dt = Q.device, Q.dtype
+    ks, vs = _rows_of_heads("K", K, dt, dev), _rows_of_heads("V", V, dt, dev)
+    pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, dt, dev)
+    if ks[:3] != (T, hk, d) or vs[:3] != (T, hk, d):
+        _refuse(f"K and V must be tensors of shape {(T, hk, d)}")
+    p = _vector("positions", positions, T, torch.int32, dev)
+    s = _vector("slots", slots, T, torch.int64, dev)
+    f = _vector("freq", freq, None, torch.int64, dev)
+    if Qr is None:
+        with _on(stream):
+            Qr = torch.empty((T, h, d), dtype=dt, device=dev)
+    qs = _rows_of_heads("Qr", Qr, dt, dev)
+    if qs[:3] != (T, h, d):
+        _refuse(f"Qr must be a tensor of shape {(T, h, d)}")
+    st = _lib().pifa_rope_cache(Q.data_ptr(), ldq, K.data_ptr(), ks[3], V.data_ptr(), vs[3], T, h, hk, d, c_dtype_of(Q),
+                                p, s, f, 2 * freq.shape[0], int(layout), float(scale), Qr.data_ptr(), qs[3],
+                                k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh, _stream_ptr(stream))
+    _check(st, "pifa_rope_cache")
+    return Qr
+
+
+@functools.lru_cache(maxsize=1024)  # host arithmetic on plain ints
+def _attention_workspace_size(T, q_heads, kv_heads, head_dim, B, max_q) -> int:
+    v = int(_lib().pifa_paged_attention_workspace_size(T, q_heads, kv_heads, head_dim, B, max_q))
+    if v < 0:
+        _check(v, "pifa_paged_attention_workspace_size")
+    return v
+
+
+def pifa_paged_attention_workspace_size(T: int, q_heads: int, kv_heads: int, head_dim: int, B: int, max_q: int) -> int:
+    return _attention_workspace_size(int(T), int(q_heads), int(kv_heads), int(head_dim), int(B), int(max_q))
+
+
+def pifa_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, max_q: int, scale=None, O=None,
+                         workspace_tensor=None, stream=None):
+    """Causal attention of each request's new tokens over its pages (pifa_paged_attention): Q (T x heads x
+    head_dim), caches as pifa_rope_cache, table int32 (B x columns), q_start int32 (B + 1), kv_len int32 (B),
+    max_q at least every request's number of new tokens. scale: 1 / sqrt(head_dim) if not given. Returns O,
+    shaped like Q (allocated as zeros if not given: rows of no request are not written)."""
+    import torch
+    T, h, d, ldq = _rows_of_heads("Q", Q)
+    dev, dt = Q.device, Q.dtype
+    pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, dt, dev)
+    kl = _vector("kv_len", kv_len, None, torch.int32, dev)
+    B = kv_len.shape[0]
+    qs = _vector("q_start", q_start, B + 1, torch.int32, dev)
+    ldt = _table_ld(table, B, dev)
+    if O is None:
+        with _on(stream):
+            O = torch.zeros((T, h, d), dtype=dt, device=dev)
+    os_ = _rows_of_heads("O", O, dt, dev)
+    if os_[:3] != (T, h, d):
+        _refuse(f"O must be a tensor of shape {(T, h, d)}")
+    need = _attention_workspace_size(T, h, hk, d, B, int(max_q))
+    ws = workspace_tensor
+    if ws is None:
+        with _on(stream):  # one for each stream that calls run on, the current one among them
+            ws = workspace(need, dev, _stream_ptr(None), tag="attention")
+    elif not isinstance(ws, torch.Tensor) or ws.device != dev:
+        _refuse("workspace_tensor must be a tensor on Q's device")
+    ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
+    ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
+    st = _lib().pifa_paged_attention(
+        Q.data_ptr(), ldq, T, h, hk, d, c_dtype_of(Q), k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh,
+        table.data_ptr(), table.shape[1], ldt, qs, kl, B, int(max_q), d ** -0.5 if scale is None else float(scale),
+        O.data_ptr(), os_[3], ws_ptr, ws_bytes, _stream_ptr(stream))
+    _check(st, "pifa_paged_attention")
+    return O
