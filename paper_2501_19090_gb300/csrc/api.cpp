@@ -106,6 +106,41 @@ int make_tmap_2d(CUtensorMap* map, int dtype, const void* base, int64_t rows, in
   return PIFA_OK;
 }
 
+int make_tmap_cache(CUtensorMap* map, int dtype, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return pifa_fail(PIFA_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  struct { int64_t n, stride; uint32_t box; int is; } d[3] = {
+      {c.page_size, c.token_stride, rows, 0}, {c.heads, c.head_stride, 1, 1}, {c.pages, c.page_stride, 1, 2}};
+  // a dimension of one element is never stepped over: whatever its stride says, it takes the largest one
+  int64_t most = 8;
+  for (const auto& x : d)
+    if (x.n > 1 && x.stride > most) most = x.stride;
+  for (auto& x : d)
+    if (x.n == 1) x.stride = most;
+  for (int i = 0; i < 3; ++i)
+    for (int j = 0; j < i; ++j)
+      if (d[i].stride < d[j].stride) std::swap(d[i], d[j]);
+  cuuint64_t dims[4] = {(cuuint64_t)c.dim}, strides[3];
+  cuuint32_t box[4] = {64}, estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) {
+    if (d[i].stride * 2 >= ((int64_t)1 << 40)) return pifa_fail(PIFA_ERR_UNSUPPORTED, "cache: a stride of 2^40 bytes or more");
+    dims[i + 1] = (cuuint64_t)d[i].n;
+    strides[i] = (cuuint64_t)(d[i].stride * 2);
+    box[i + 1] = d[i].box;
+    order[d[i].is] = i;
+  }
+  const CUtensorMapDataType dt =
+      dtype == PIFA_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  CUresult r = fn(map, dt, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    char buf[120];
+    std::snprintf(buf, sizeof buf, "cuTensorMapEncodeTiled failed (CUresult %d) for a paged cache", (int)r);
+    return pifa_fail(PIFA_ERR_CUDA, buf);
+  }
+  return PIFA_OK;
+}
+
 int pifa_check_cache(const PifaCacheShape& c, int64_t least, int64_t most) {
   const int64_t lim = (int64_t)1 << 31, far = (int64_t)1 << 46;
   if (c.heads < 1 || c.heads > 65536 || c.dim < 1 || c.pages < 1 || c.pages >= lim || c.page_size < 1)

@@ -119,6 +119,9 @@ int check_sizes(int64_t T, int64_t hq, int64_t hk, int64_t dim, int64_t B, int64
   return PIFA_OK;
 }
 
+// Whether a request's rows for one key / value head may be more than one 16-row product.
+bool takes_tc(int64_t group, int64_t max_q) { return max_q > 16 || group * max_q > 16; }
+
 }  // namespace
 
 extern "C" {
@@ -128,7 +131,8 @@ int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t 
   pifa_clear_error();
   const int st = check_sizes(T, q_heads, kv_heads, head_dim, B, max_q);
   if (st != PIFA_OK) return st;
-  return T == 0 || B == 0 ? 0 : kWorkspaceReserve;
+  if (T == 0 || B == 0) return 0;
+  return kWorkspaceReserve + (takes_tc(q_heads / kv_heads, max_q) ? attention_tc_workspace_bytes(T, q_heads, kv_heads, head_dim, B) : 0);
 }
 
 int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
@@ -169,6 +173,11 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   cudaError_t e = cudaSuccess;
   int* status = pifa_status_word(&e);
   if (!status) return pifa_fail_cuda("device status word", e);
+  if (takes_tc(q_heads / kv_heads, max_q)) {
+    PifaAttention a = {Q, k_cache, v_cache, O, table, q_start, kv_len, T, ldq, ldo, ldt, cols, B, max_q, q_heads, c, dtype,
+                       scale * 1.4426950408889634f, static_cast<uint8_t*>(workspace) + kWorkspaceReserve};
+    return launch_attention_tc(a, status, pifa_wait_timeout_ns(), reinterpret_cast<cudaStream_t>(cuda_stream));
+  }
   AttnArgs g = {};
   g.q = static_cast<const uint16_t*>(Q);
   g.k = static_cast<const uint16_t*>(k_cache);

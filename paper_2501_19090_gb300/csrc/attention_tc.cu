@@ -1,0 +1,832 @@
+// attention_tc.cu -- attention of chunks of new tokens over a paged cache, on the 5th-generation tensor cores.
+//
+//   o = sum_j softmax_j(scale q . k_j) v_j over the keys j < L - n + i + 1 of new token i (L keys, n new tokens).
+//
+// Rows: the query heads of a key / value head share its keys, so the n new tokens of a request and the G heads
+// of a group make n G rows, token-major. A work item is 256 of them (two tiles of 128) of one request and one
+// key / value head; it walks the keys in tiles of 128 and reads K and V once for both tiles.
+// One pass with a running maximum: S = Q K^T (128 x 128, fp32, tensor memory); a thread owns a row, so maximum
+// and sum need no exchange; p = exp2(c s - c m) goes back to tensor memory as bf16 or fp16 over S's columns
+// and is the first operand of O += P V. m is only raised, and O and l rescaled, when the row's maximum
+// has grown by more than 8 in the exponent (then O's columns are read and written by the row's warp);
+// until then weights reach 2^8 at most, which costs neither format precision.
+//
+// CTA of 384 threads, one per SM, persistent:
+//   warps 0-3, 4-7   softmax and epilogue of tile 0 and 1 (tensor memory quarter = warp % 4)
+//   warp 8           takes work items from a queue and loads K and V tiles by TMA into a ring of slots, a page (or a
+//                    128-token part of one) and 64 columns a copy, a lane for each
+//   warp 9           issues the MMAs: PV of tile 0 and its next S, then the same of tile 1, so that one tile's
+//                    softmax runs under the other tile's MMAs
+//   warps 10, 11     load the next item's rows of Q, as soon as its last S has been computed
+// P lies over S, and S of the next keys is written over both: the MMAs of one thread run in issue
+// order, PV(j) before S(j + 1), and S(j)'s values were read before P was announced.
+// Keys past L: their scores are masked, and their rows of V, which may hold anything, are set to zero in shared
+// memory, since 0 times NaN is NaN.
+//
+// Work: a first kernel (one CTA) reads the lengths, lists the items (later rows of a request first: they have
+// more keys) and cuts the last ones along the keys where whole items would leave SMs idle in the
+// last round: a piece writes its unnormalised sums, and the warp that comes last (a counter per 32 rows) adds up the
+// pieces in their order. Every wait is bounded; on timeout PIFA_ERR_TIMEOUT is latched and the CTA drains.
+#include <cmath>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "pifa.h"
+#include "pifa_internal.h"
+#include "ptx.cuh"
+
+namespace {
+
+using namespace pifa;
+
+constexpr int BM = 128;             // rows of a tile
+constexpr int ROWS = 2 * BM;        // rows of an item
+constexpr int BN = 128;             // keys of a tile
+constexpr int THREADS = 384;
+constexpr int PLAN_THREADS = 1024;
+constexpr int MAX_PARTS = 456;      // pieces (times heads) that may leave partial sums: three for each SM
+constexpr uint32_t HALF = BN * 128;  // 128 rows of 64 columns: 16 KB
+
+template <int D>
+struct Cfg {
+  static constexpr uint32_t TILE = D / 64 * HALF;
+  static constexpr int SLOTS = D == 128 ? 5 : 8;
+  static constexpr uint32_t SMEM = 1024 + (2 + SLOTS) * TILE + 1024;
+  static constexpr int64_t PART_FLOATS = ROWS * D + 2 * ROWS;  // O, then (m, l) of each row
+};
+
+// One work item, as the plan lists it; each stands for `heads` items, one for each key / value head.
+struct Entry {
+  int b, row0;       // request, first row
+  int j0, j1;        // key tiles
+  int part, parts;   // which piece of how many
+  int slot, counter; // first partial-sum slot / counter (of head 0; times heads)
+};
+
+struct Plan {
+  int next;          // queue head: items beyond the grid's first ones taken so far
+  int entries;
+  int pad[6];
+};
+
+struct TcArgs {
+  const uint16_t* q;
+  uint16_t* o;
+  const int32_t *table, *q_start, *kv_len;
+  Plan* plan;
+  int* counters;
+  Entry* list;
+  float* partial;
+  int64_t ldq, ldo, ldt, pages;
+  int T, heads, group, B, max_q, cols, page_size, page_shift;
+  int token_at, head_at, page_at;    // their places among the tensor maps' coordinates 1 to 3
+  float c;                           // |scale| log2(e)
+  int negate;                        // scale < 0
+  int* status;
+  uint64_t timeout_ns;
+};
+
+struct Item {
+  int b, head, row0, rows;           // rows: of the request
+  int n, L, q0;
+  int j0, j1, e0, e1;                // e: end of the key tiles that a tile's rows see
+  int part, parts, slot, counter, end;
+};
+
+struct Lengths {
+  int q0, n, L;
+};
+
+// Lengths of request b, kept within the buffers whatever the arrays hold.
+__device__ __forceinline__ Lengths lengths_of(const TcArgs& g, int b) {
+  Lengths x;
+  x.q0 = min(max(g.q_start[b], 0), g.T);
+  x.n = min(min(max(g.q_start[b + 1], x.q0), g.T) - x.q0, g.max_q);
+  x.L = min(max(g.kv_len[b], 0), g.cols << g.page_shift);
+  return x;
+}
+
+// Key tiles that rows [row, row + 128) of a request see: up to its last row's last key.
+__device__ __forceinline__ int tile_end(const Lengths& x, int group, int row) {
+  const int rows = x.n * group;
+  if (row >= rows) return 0;
+  const int last = (min(row + BM, rows) - 1) / group;  // token
+  return (max(x.L - x.n + last + 1, 0) + BN - 1) / BN;
+}
+__device__ __forceinline__ int item_end(const Lengths& x, int group, int row0) {
+  return max(tile_end(x, group, row0), tile_end(x, group, row0 + BM));
+}
+
+// ---- plan ---------------------------------------------------------------------------------------
+__device__ __forceinline__ int block_sum_scan(int v, int* part, int& total) {  // exclusive sum, and the total
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int a = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, a, o);
+    if (lane >= o) a += x;
+  }
+  __syncthreads();  // part is free
+  if (lane == 31) part[warp] = a;
+  __syncthreads();
+  if (warp == 0) {
+    int p = part[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, p, o);
+      if (lane >= o) p += x;
+    }
+    part[lane] = p;
+  }
+  __syncthreads();
+  total = part[31];
+  return a - v + (warp ? part[warp - 1] : 0);
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g, int grid) {
+  extern __shared__ int first[];  // B + 1: first row tile of each request
+  __shared__ int part[32];
+  __shared__ int red[4];          // largest and smallest item, largest and sum of those that may be cut
+  __shared__ int cut;             // key tiles of a piece
+  pdl_launch_dependents();
+  pdl_wait_primary();
+  const int tid = threadIdx.x;
+  if (tid == 0) {
+    red[0] = red[2] = red[3] = 0;
+    red[1] = 0x7fffffff;
+  }
+  for (int i = tid; i < MAX_PARTS / 2 * 8; i += PLAN_THREADS) g.counters[i] = 0;
+  bool over = false;
+  int items = 0;
+  for (int b0 = 0; b0 < g.B; b0 += PLAN_THREADS) {
+    const int b = b0 + tid;
+    int n = 0;
+    if (b < g.B) {
+      const Lengths x = lengths_of(g, b);
+      over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
+      n = (x.n * g.group + ROWS - 1) / ROWS;
+    }
+    int total;
+    const int at = block_sum_scan(n, part, total);
+    if (b < g.B) first[b] = items + at;
+    items += total;
+  }
+  if (tid == 0) first[g.B] = items;
+  if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
+  __syncthreads();
+
+  // the item at place k of the list: later rows of a request first
+  auto item_at = [&](int k, Lengths& x, int& b, int& row0) {
+    int lo = 0, hi = g.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= k) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    x = lengths_of(g, b);
+    row0 = (first[b + 1] - 1 - k) * ROWS;
+    return item_end(x, g.group, row0);
+  };
+  // Whole rounds of the grid stay whole; the items of the last, unfilled round may be cut.
+  const int whole = (int)((int64_t)items * g.heads / grid * grid / g.heads);
+  int most = 0, least = 0x7fffffff, most_cut = 0, sum_cut = 0;
+  for (int k = tid; k < items; k += PLAN_THREADS) {
+    Lengths x;
+    int b, row0;
+    const int cost = item_at(k, x, b, row0);
+    most = max(most, cost);
+    least = min(least, cost);
+    if (k >= whole) {
+      most_cut = max(most_cut, cost);
+      sum_cut += cost;
+    }
+  }
+  atomicMax(&red[0], most);
+  atomicMin(&red[1], least);
+  atomicMax(&red[2], most_cut);
+  atomicAdd(&red[3], sum_cut);
+  __syncthreads();
+  if (tid < 32) {
+    // The time of the last round, in key tiles, if its items are cut into pieces of `size`: an even share for each
+    // CTA, and where items are alike, the wait for a last round of pieces that does not fill the grid. A piece
+    // costs about two tiles on top (rows of Q, first and last products), with partial sums about three.
+    const int rest = items - whole;
+    const int size = max((red[2] + tid) / (tid + 1), 1);
+    const float alike = red[0] > 0 ? (float)red[1] / (float)red[0] : 0.0f;
+    const float pieces = tid == 0 ? (float)rest : (float)rest * 0.5f + (float)red[3] / (float)size;
+    const float extra = tid == 0 ? 2.0f : 3.0f;
+    const float rounds = pieces * (float)g.heads / (float)grid;
+    float t = rounds * extra + (float)red[3] * (float)g.heads / (float)grid +
+              alike * (ceilf(rounds) - rounds) * ((float)size + extra);
+    t = fmaxf(t, (float)size + extra);
+    const bool fits = tid == 0 || (int64_t)(rest + red[3] / size) * g.heads <= MAX_PARTS;
+    if (!fits) t = 3e38f;
+    int who = tid;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      const float ot = __shfl_xor_sync(0xffffffffu, t, o);
+      const int ow = __shfl_xor_sync(0xffffffffu, who, o);
+      if (ot < t || (ot == t && ow < who)) {
+        t = ot;
+        who = ow;
+      }
+    }
+    if (tid == who) cut = who == 0 ? 0x3fffffff : size;
+  }
+  __syncthreads();
+  const int size = cut;
+  int entries = 0, slots = 0, counters = 0;
+  for (int k0 = 0; k0 < items; k0 += PLAN_THREADS) {
+    const int k = k0 + tid;
+    Lengths x;
+    int b = 0, row0 = 0, cost = 0, pieces = 0;
+    if (k < items) {
+      cost = item_at(k, x, b, row0);
+      pieces = k < whole ? 1 : max((cost + size - 1) / size, 1);
+    }
+    int total, s_total, c_total;
+    const int at = entries + block_sum_scan(pieces, part, total);
+    const int slot = slots + block_sum_scan(pieces > 1 ? pieces : 0, part, s_total);
+    const int counter = counters + block_sum_scan(pieces > 1 ? 1 : 0, part, c_total);
+    for (int p = 0; p < pieces; ++p) {  // even pieces
+      Entry e;
+      e.b = b;
+      e.row0 = row0;
+      e.j0 = (int)((int64_t)cost * p / pieces);
+      e.j1 = (int)((int64_t)cost * (p + 1) / pieces);
+      e.part = p;
+      e.parts = pieces;
+      e.slot = slot;
+      e.counter = counter;
+      g.list[at + p] = e;
+    }
+    entries += total;
+    slots += s_total;
+    counters += c_total;
+  }
+  if (tid == 0) {
+    g.plan->next = 0;
+    g.plan->entries = entries;
+  }
+}
+
+// ---- attention -------------------------------------------------------------------------------------
+// Descriptor of V's tile as the MN-major second operand: rows of 64 columns (128 bytes, swizzled), one for each
+// key, 8-key groups 1024 bytes apart, 64-column blocks HALF bytes apart.
+__device__ __forceinline__ uint64_t sw128_mn_desc(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)((HALF >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+  if constexpr (F16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+}
+
+template <bool F16, int D>
+__global__ void __launch_bounds__(THREADS, 1)
+    attention_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const TcArgs g) {
+  using C = Cfg<D>;
+  constexpr int SLOTS = C::SLOTS;
+  constexpr uint32_t TILE = C::TILE;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = smem + 2 * TILE;
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + SLOTS * TILE);
+  uint64_t* empty = full + SLOTS;
+  uint64_t* s_full = empty + SLOTS;   // S of a tile is in tensor memory
+  uint64_t* p_full = s_full + 2;      // its P is, and its O may be added to
+  uint64_t* o_full = p_full + 2;      // the item's last PV is done
+  uint64_t* q_full = o_full + 2;
+  uint64_t* q_free = q_full + 2;
+  uint64_t* item_full = q_free + 2;
+  uint64_t* item_free = item_full + 2;
+  uint64_t* drain = item_free + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  Item* items = reinterpret_cast<Item*>(tmem_slot + 2);
+
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < SLOTS; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&s_full[t], 1);
+      mbar_init(&p_full[t], 4);
+      mbar_init(&o_full[t], 1);
+      mbar_init(&q_full[t], 1);
+      mbar_init(&q_free[t], 1);
+      mbar_init(&item_full[t], 1);
+      mbar_init(&item_free[t], 11);
+    }
+    mbar_init(drain, 1);
+    fence_mbar_init();
+    prefetch_tmap(&kmap);
+    prefetch_tmap(&vmap);
+  }
+  if (warp == 9) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_wait_primary();
+  bool dead = false;
+  // all lanes of the warp wait; false (and the status latched) if the wait ran out
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, g.timeout_ns));
+    if (!ok) {
+      latch_status(g.status, PIFA_ERR_TIMEOUT);
+      dead = true;
+    }
+    return ok;
+  };
+
+  if (warp == 8) {
+    // ---------------- queue, K and V ----------------
+    const int total = g.plan->entries * g.heads;
+    int s = 0, fills = 0;
+    uint32_t ph = 1;
+    const int per_tile = g.page_size >= BN ? 1 : BN / g.page_size;
+    const int box_rows = min(g.page_size, BN);
+    const int mine = lane / (D / 64), half = lane % (D / 64);
+    for (int n = 0; !dead; ++n) {
+      if (!wait(&item_free[n & 1], (((uint32_t)n >> 1) & 1u) ^ 1u)) break;
+      int k = (int)blockIdx.x;
+      if (n > 0) {
+        if (lane == 0) k = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
+        k = __shfl_sync(0xffffffffu, k, 0);
+      }
+      Item it = {};
+      it.end = k >= total;
+      if (!it.end) {
+        const Entry e = g.list[k / g.heads];
+        const Lengths x = lengths_of(g, e.b);
+        it.b = e.b;
+        it.head = k % g.heads;
+        it.row0 = e.row0;
+        it.rows = x.n * g.group;
+        it.n = x.n;
+        it.L = x.L;
+        it.q0 = x.q0;
+        it.j0 = e.j0;
+        it.j1 = e.j1;
+        it.e0 = min(e.j1, tile_end(x, g.group, e.row0));
+        it.e1 = min(e.j1, tile_end(x, g.group, e.row0 + BM));
+        it.part = e.part;
+        it.parts = e.parts;
+        it.slot = (e.slot + e.part) * g.heads + it.head;
+        it.counter = (e.counter * g.heads + it.head) * 8;
+      }
+      if (lane == 0) {
+        items[n & 1] = it;
+        mbar_arrive(&item_full[n & 1]);
+      }
+      if (it.end) break;
+      const int n_pages = (it.L + g.page_size - 1) >> g.page_shift;
+      const int32_t* row = g.table + it.b * g.ldt;
+      auto page_of = [&](int j) {
+        const int p = ((j * BN) >> g.page_shift) + mine;
+        return mine < per_tile && j < it.j1 && p < n_pages ? row[p] : -2;  // -2: no page
+      };
+      int id = page_of(it.j0);
+      for (int j = it.j0; j < it.j1 && !dead; ++j) {
+        const int next = page_of(j + 1);
+        const bool has = id != -2 || (mine < per_tile && ((j * BN) >> g.page_shift) + mine < n_pages);
+        if (has && (id < 0 || id >= g.pages)) {
+          latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+          id = (int)g.pages;  // outside the tensor map: zeros
+        }
+        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, has)) * (uint32_t)box_rows * 128u;
+        const int token = (j * BN) & (g.page_size - 1);
+        const uint32_t at = (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u;
+        const int y = g.token_at == 0 ? token : g.head_at == 0 ? it.head : id;
+        const int z = g.token_at == 1 ? token : g.head_at == 1 ? it.head : id;
+        const int w = g.token_at == 2 ? token : g.head_at == 2 ? it.head : id;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          if (!wait(&empty[s], ph)) break;
+          if (lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
+          __syncwarp();
+          if (has) tma_load_4d(smem_u32(ring) + (uint32_t)s * TILE + at, kv ? &vmap : &kmap, half * 64, y, z, w, &full[s]);
+          ++fills;
+          if (++s == SLOTS) {
+            s = 0;
+            ph ^= 1u;
+          }
+        }
+        id = next;
+      }
+    }
+    // nothing may land in shared memory after the CTA has left
+    for (int i = fills > SLOTS ? fills - SLOTS : 0; i < fills; ++i)
+      if (!mbar_wait(&full[i % SLOTS], (uint32_t)(i / SLOTS) & 1u, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
+  } else if (warp == 9) {
+    // ---------------- MMAs ----------------
+    const uint32_t kind = F16 ? idesc_f16_f32(BM, BN) : idesc_bf16_f32(BM, BN);
+    const uint32_t qk_desc = kind | (g.negate ? 1u << 13 : 0u);
+    const uint32_t pv_desc = (F16 ? idesc_f16_f32(BM, D) : idesc_bf16_f32(BM, D)) | (1u << 16);
+    const uint64_t q_desc = sw128_desc(smem_u32(smem)), k_desc = sw128_desc(smem_u32(ring)), v_desc = sw128_mn_desc(smem_u32(ring));
+    int s = 0;
+    uint32_t ph = 0, q_ph = 0, p_ph = 0;  // a bit for each tile
+    auto score = [&](int t, int slot) {
+      if (lane == 0) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t at = (uint32_t)(kk / 4) * (HALF / 16) + (uint32_t)(kk % 4) * 2;
+          mma_bf16_ss(tmem + t * BN, q_desc + t * (TILE / 16) + at, k_desc + slot * (TILE / 16) + at, qk_desc, kk > 0);
+        }
+        mma_commit(&s_full[t]);
+      }
+    };
+    for (int n = 0; !dead; ++n) {
+      if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
+      const int end = items[n & 1].end, j0 = items[n & 1].j0, j1 = items[n & 1].j1, L = items[n & 1].L;
+      const int e[2] = {items[n & 1].e0, items[n & 1].e1};
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_free[n & 1]);
+      if (end) break;
+      if (j0 >= j1) continue;
+      if (!wait(&full[s], ph)) break;
+      tc_fence_after();
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (j0 < e[t]) {
+          if (!wait(&q_full[t], (q_ph >> t) & 1u)) break;
+          q_ph ^= 1u << t;
+          tc_fence_after();
+          score(t, s);
+          if (j0 + 1 >= e[t] && lane == 0) mma_commit(&q_free[t]);
+        }
+      }
+      if (dead) break;
+      if (lane == 0) mma_commit(&empty[s]);
+      if (++s == SLOTS) {
+        s = 0;
+        ph ^= 1u;
+      }
+      for (int j = j0; j < j1 && !dead; ++j) {
+        if (!wait(&full[s], ph)) break;
+        const int vs = s;
+        if (++s == SLOTS) {
+          s = 0;
+          ph ^= 1u;
+        }
+        const int tail = L - j * BN;  // keys of this tile
+        if (tail < BN) {
+          uint8_t* v = ring + vs * TILE;
+          for (int i = max(tail, 0) * 8 + lane; i < BN * 8; i += 32)
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(v + h * HALF + i * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        int ks = -1;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (dead || j >= e[t]) continue;
+          if (!wait(&p_full[t], (p_ph >> t) & 1u)) continue;
+          p_ph ^= 1u << t;
+          tc_fence_after();
+          if (lane == 0) {
+#pragma unroll
+            for (int kk = 0; kk < BN / 16; ++kk)
+              mma_bf16_ts(tmem + 2 * BN + t * D, tmem + t * BN + kk * 8, v_desc + vs * (TILE / 16) + kk * 128, pv_desc,
+                          j > j0 || kk > 0);
+            if (j + 1 >= e[t]) mma_commit(&o_full[t]);
+            if (t == 1 || j >= e[1]) mma_commit(&empty[vs]);
+          }
+          if (j + 1 < e[t]) {
+            if (ks < 0) {
+              if (!wait(&full[s], ph)) continue;
+              tc_fence_after();
+              ks = s;
+              if (++s == SLOTS) {
+                s = 0;
+                ph ^= 1u;
+              }
+            }
+            score(t, ks);
+            if (j + 2 >= e[t] && lane == 0) mma_commit(&q_free[t]);
+          }
+        }
+        if (ks >= 0 && lane == 0) mma_commit(&empty[ks]);
+      }
+    }
+    __syncwarp();
+    if (lane == 0) {
+      mma_commit(drain);  // every MMA has completed before the tensor memory is freed
+      if (!mbar_wait(drain, 0, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
+    }
+  } else if (warp >= 10) {
+    // ---------------- rows of Q ----------------
+    const int t = warp - 10;
+    uint32_t ph = 1;
+    constexpr int CH = D / 8;  // 16-byte pieces of a row
+    for (int n = 0; !dead; ++n) {
+      if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
+      const Item it = items[n & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_free[n & 1]);
+      if (it.end) break;
+      if (it.j0 >= (t ? it.e1 : it.e0)) continue;
+      if (!wait(&q_free[t], ph)) break;
+      ph ^= 1u;
+      const int row0 = it.row0 + t * BM, rows = min(it.rows - row0, BM);
+      const uint32_t base = smem_u32(smem) + (uint32_t)t * TILE;
+      for (int i = lane; i < rows * CH; i += 32) {
+        const int r = i / CH, c = i % CH, token = (row0 + r) / g.group, h = row0 + r - token * g.group;
+        const uint16_t* src = g.q + (int64_t)(it.q0 + token) * g.ldq + (int64_t)(it.head * g.group + h) * D + c * 8;
+        cp_async16(base + (uint32_t)(c / 8) * HALF + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4), src, 16);
+      }
+      cp_async_wait_all();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[t]);
+    }
+  } else {
+    // ---------------- softmax and epilogue: a row per thread ----------------
+    const int t = warp >> 2, quarter = warp & 3;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t s_at = tmem + lanes + t * BN, o_at = tmem + lanes + 2 * BN + t * D;
+    const float c = g.c;
+    uint32_t s_ph = 0, o_ph = 0;
+    for (int n = 0; !dead; ++n) {
+      if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
+      const Item it = items[n & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_free[n & 1]);
+      if (it.end) break;
+      const int end = t ? it.e1 : it.e0;
+      const int row = it.row0 + t * BM + quarter * 32 + lane;       // of the request
+      const int token = row / g.group, h = row - token * g.group;
+      const int seen = row < it.rows ? max(it.L - it.n + token + 1, 0) : 0;
+      const bool idle = it.row0 + t * BM + quarter * 32 >= it.rows;  // no row of this warp exists
+      float m = -INFINITY, l = 0.0f;
+      for (int j = it.j0; j < end; ++j) {
+        if (!wait(&s_full[t], s_ph)) break;
+        s_ph ^= 1u;
+        if (!idle) {
+          tc_fence_after();
+          uint32_t v[4][32];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
+          tmem_ld_wait();
+          const int lim = seen - j * BN;  // keys of this tile that the row sees
+          if (__any_sync(0xffffffffu, lim < BN)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
+          }
+          float mx[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            mx[i] = __uint_as_float(v[i][0]);
+#pragma unroll
+            for (int k = 1; k < 32; ++k) mx[i] = fmaxf(mx[i], __uint_as_float(v[i][k]));
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          // S(j) is in: so is PV(j - 1), issued before it, and O may be touched
+          const bool grows = (top - m) * c > 8.0f && m > -INFINITY;
+          if (__any_sync(0xffffffffu, grows)) {
+            const float up = m > -INFINITY ? fmaxf(m, top) : m;
+            const float f = up > m ? fast_exp2((m - up) * c) : 1.0f;
+            m = up;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+              uint32_t o[32];
+              tmem_ld_32x32b_x32(o_at + i * 32, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              tmem_st_32x32b_x32(o_at + i * 32, o);
+            }
+          }
+          if (m == -INFINITY) m = top;
+          const float mc = m > -INFINITY ? m * c : 0.0f;
+          float sum[4] = {};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t w[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const uint32_t* u = v[2 * i + k / 16];
+              const float p0 = fast_exp2(fmaf(__uint_as_float(u[2 * k % 32]), c, -mc));
+              const float p1 = fast_exp2(fmaf(__uint_as_float(u[2 * k % 32 + 1]), c, -mc));
+              sum[2 * i] += p0;
+              sum[2 * i + 1] += p1;
+              w[k] = pack<F16>(p0, p1);
+            }
+            tmem_st_32x32b_x32(s_at + i * 32, w);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tmem_st_wait();
+          tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[t]);
+      }
+      if (dead) break;
+      const bool any = it.j0 < end;
+      if (any) {
+        if (!wait(&o_full[t], o_ph)) break;
+        o_ph ^= 1u;
+        tc_fence_after();
+      }
+      if (idle) continue;
+      uint16_t* out = g.o + (int64_t)(it.q0 + token) * g.ldo + (int64_t)(it.head * g.group + h) * D;
+      auto store = [&](int i, const float* x) {  // 32 columns
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          *reinterpret_cast<uint4*>(out + i * 32 + k * 8) =
+              make_uint4(pack<F16>(x[8 * k], x[8 * k + 1]), pack<F16>(x[8 * k + 2], x[8 * k + 3]),
+                         pack<F16>(x[8 * k + 4], x[8 * k + 5]), pack<F16>(x[8 * k + 6], x[8 * k + 7]));
+      };
+      if (it.parts == 1) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          if (any) {
+            tmem_ld_32x32b_x32(o_at + i * 32, o);
+            tmem_ld_wait();
+          }
+          float x[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) x[k] = any && seen > 0 ? __uint_as_float(o[k]) * inv : 0.0f;
+          if (row < it.rows) store(i, x);
+        }
+      } else {
+        // This piece's sums: for each 32 rows, four columns of them at a time, so that a warp's accesses are whole.
+        const int w8 = t * 4 + quarter;
+        auto slot_of = [&](int p) { return g.partial + (int64_t)(it.slot + (p - it.part) * g.heads) * C::PART_FLOATS; };
+        float* mine = slot_of(it.part);
+        if (any) {
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tmem_ld_32x32b_x32(o_at + i * 32, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              __stcg(reinterpret_cast<uint4*>(mine) + (w8 * (D / 4) + i * 8 + k) * 32 + lane,
+                     make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
+          }
+        }
+        __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, make_float2(m * c, l));
+        __threadfence();
+        __syncwarp();
+        int before = 0;
+        if (lane == 0) before = atomicAdd(&g.counters[it.counter + w8], 1);
+        before = __shfl_sync(0xffffffffu, before, 0);
+        if (before == it.parts - 1) {  // the last piece of these 32 rows: add up all in their order
+          __threadfence();
+          float top = -INFINITY;
+          for (int p = 0; p < it.parts; ++p) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(p) + ROWS * D) + w8 * 32 + lane);
+            if (ml.y != 0.0f) top = fmaxf(top, ml.x);
+          }
+          if (top == -INFINITY) top = 0.0f;
+          float all = 0.0f;
+          for (int p = 0; p < it.parts; ++p) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(p) + ROWS * D) + w8 * 32 + lane);
+            if (ml.y != 0.0f) all += ml.y * fast_exp2(ml.x - top);
+          }
+          const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+#pragma unroll 1
+          for (int i = 0; i < D / 32; ++i) {
+            float x[32] = {};
+            for (int p = 0; p < it.parts; ++p) {
+              const float* from = slot_of(p);
+              const float2 ml = __ldcg(reinterpret_cast<const float2*>(from + ROWS * D) + w8 * 32 + lane);
+              if (ml.y == 0.0f) continue;  // nothing seen: the columns may not even be written
+              const float f = fast_exp2(ml.x - top) * inv;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float4 o = __ldcg(reinterpret_cast<const float4*>(from) + (w8 * (D / 4) + i * 8 + k) * 32 + lane);
+                x[4 * k] += f * o.x;
+                x[4 * k + 1] += f * o.y;
+                x[4 * k + 2] += f * o.z;
+                x[4 * k + 3] += f * o.w;
+              }
+            }
+            if (row < it.rows) store(i, x);
+          }
+          __syncwarp();
+        }
+      }
+    }
+  }
+
+  // Every wait above is bounded, so every thread gets here: the tensor memory is freed after its last use.
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
+
+int64_t list_bytes(int64_t T, int64_t group, int64_t B) {
+  return round256(((T * group + ROWS - 1) / ROWS + B + MAX_PARTS) * (int64_t)sizeof(Entry));
+}
+constexpr int64_t kCounterBytes = MAX_PARTS / 2 * 8 * 4 + 256;  // the plan's head, then the counters
+
+}  // namespace
+
+int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B) {
+  const int64_t part = (dim == 64 ? Cfg<64>::PART_FLOATS : Cfg<128>::PART_FLOATS) * 4;
+  return round256(kCounterBytes) + list_bytes(T, q_heads / kv_heads, B) + MAX_PARTS * part;
+}
+
+int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream) {
+  TcArgs g = {};
+  uint8_t* ws = static_cast<uint8_t*>(a.ws);
+  const int64_t group = a.q_heads / a.cache.heads;
+  g.q = static_cast<const uint16_t*>(a.q);
+  g.o = static_cast<uint16_t*>(a.o);
+  g.table = a.table;
+  g.q_start = a.q_start;
+  g.kv_len = a.kv_len;
+  g.plan = reinterpret_cast<Plan*>(ws);
+  g.counters = reinterpret_cast<int*>(ws + 256);
+  g.list = reinterpret_cast<Entry*>(ws + round256(kCounterBytes));
+  g.partial = reinterpret_cast<float*>(ws + round256(kCounterBytes) + list_bytes(a.T, group, a.B));
+  g.ldq = a.ldq;
+  g.ldo = a.ldo;
+  g.ldt = a.ldt;
+  g.pages = a.cache.pages;
+  g.T = (int)a.T;
+  g.heads = (int)a.cache.heads;
+  g.group = (int)group;
+  g.B = (int)a.B;
+  g.max_q = (int)(a.max_q < a.T ? a.max_q : a.T);
+  g.cols = (int)a.cols;
+  g.page_size = (int)a.cache.page_size;
+  while ((1 << g.page_shift) < g.page_size) ++g.page_shift;
+  g.negate = a.scale_log2 < 0.0f;
+  // equal weights for a scale of zero: the masked scores, -inf, still have to vanish
+  g.c = a.scale_log2 == 0.0f ? 1e-30f : std::fabs(a.scale_log2);
+  g.status = status;
+  g.timeout_ns = timeout_ns;
+  CUtensorMap kmap, vmap;
+  int order[3], st;
+  const uint32_t rows = (uint32_t)(a.cache.page_size < BN ? a.cache.page_size : BN);
+  if ((st = make_tmap_cache(&kmap, a.dtype, a.k, a.cache, rows, order)) != PIFA_OK) return st;
+  if ((st = make_tmap_cache(&vmap, a.dtype, a.v, a.cache, rows, order)) != PIFA_OK) return st;
+  g.token_at = order[0];
+  g.head_at = order[1];
+  g.page_at = order[2];
+  const int grid = pifa_sm_count();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(1);
+  cfg.blockDim = dim3(PLAN_THREADS);
+  cfg.dynamicSmemBytes = (size_t)(a.B + 1) * 4;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = pifa_launch_ex(&cfg, attention_plan, g, grid);
+  if (e != cudaSuccess) return pifa_fail_cuda("attention_plan launch", e);
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(THREADS);
+  auto go = [&](auto kernel, uint32_t smem) {
+    cfg.dynamicSmemBytes = smem;
+    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return err != cudaSuccess ? err : pifa_launch_ex(&cfg, kernel, kmap, vmap, g);
+  };
+  const bool f16 = a.dtype == PIFA_DTYPE_FP16;
+  if (a.cache.dim == 64) e = f16 ? go(attention_tc<true, 64>, Cfg<64>::SMEM) : go(attention_tc<false, 64>, Cfg<64>::SMEM);
+  else e = f16 ? go(attention_tc<true, 128>, Cfg<128>::SMEM) : go(attention_tc<false, 128>, Cfg<128>::SMEM);
+  if (e != cudaSuccess) return pifa_fail_cuda("attention_tc launch", e);
+  return PIFA_OK;
+}

@@ -91,6 +91,21 @@ int pifa_check_cache(const PifaCacheShape& c, int64_t least, int64_t most);
 // The bytes from the first to the last element of one buffer.
 PifaSpan pifa_cache_span(const void* base, const PifaCacheShape& c);
 
+// ---- attention over a paged cache (attention.cu, attention_tc.cu) --------------------------------
+struct PifaAttention {
+  const void *q, *k, *v;
+  void* o;
+  const int32_t *table, *q_start, *kv_len;
+  int64_t T, ldq, ldo, ldt, cols, B, max_q, q_heads;
+  PifaCacheShape cache;
+  int dtype;          // PIFA_DTYPE_*
+  float scale_log2;   // scale log2(e)
+  void* ws;           // after the reserve
+};
+// Chunks of new tokens on the tensor cores.
+int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B);
+int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream);
+
 // ---- decode (decode.cu) ----------------------------------------------------------------------
 int64_t decode_workspace_bytes(const PifaShape& s);
 int launch_decode(const PifaShape& s, const PifaPointers& p, int* status, cudaStream_t stream);
@@ -202,5 +217,9 @@ int launch_prefill_split(const PifaShape& s, const PifaPointers& p, int* status,
 // swizzle, zero fill outside the matrix.
 int make_tmap_2d(CUtensorMap* map, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld,
                  uint32_t box_cols, uint32_t box_rows);
+// 4-D tensor map over one buffer of a paged cache, innermost the head's elements, then tokens, heads and pages by
+// rising stride; box of 64 elements x `rows` tokens, 128-byte swizzle, zero fill outside. order[0..2]: which of
+// the map's coordinates 1 to 3 the token, the head and the page are.
+int make_tmap_cache(CUtensorMap* map, int dtype, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]);
 
 #endif  // PIFA_INTERNAL_H_
