@@ -1,9 +1,23 @@
-// attention.cu -- pifa_paged_attention: argument checks and a kernel of one warp per (token, query head).
+// attention.cu -- pifa_paged_attention: argument checks, and the kernels for requests with few rows.
 //
 //   o = sum_j softmax_j(scale q . k_j) v_j over the keys j < L - n + i + 1 of new token i (L keys, n new tokens).
 //
-// One pass over the keys with a running maximum m and sum l in fp32: a key's weight is exp2(s - m) with
-// s = scale log2(e) q . k, and sums and outputs are rescaled when m grows.
+// Rows: the query heads of a key / value head share its keys, so the n new tokens of a request and the G heads
+// of a group make n G rows, token-major. Up to 16 rows (decode and its neighbours) are one operand of
+// mma.sync, which is enough here: the work is bound by the cache's bytes, of which each feeds at most
+// 16 rows. More rows go to attention_tc.cu.
+//
+// Work is cut into steps of 16 keys of one request and one key / value head; all steps, in the order (request,
+// head, step), are dealt to warps in equal runs, whatever the requests' lengths: no CTA waits for the
+// longest. Each warp streams its steps on its own, without barriers: a lane copies the 16-byte pieces that it
+// will need itself (cp.async, three stages of 8 KB a warp, eight warps an SM: up to 128 KB in flight), so
+// shared memory is a longer register file. The d elements of q . k may be added in any order and the
+// columns of V assigned to any column of the product, which lets every piece be a 16-byte vector: a lane's K
+// pieces hold both halves of two steps of the contraction, and pairs of V's rows are interleaved in registers.
+// One pass with a running maximum m: p = exp2(c s - c m); m is raised, and O and l rescaled, only when a
+// score passes it by 8 in the exponent (weights reach 2^8 at most), so most steps exchange nothing between lanes.
+// A head whose steps fall to one warp is finished by it; else the warps write (m, l, O) and a second kernel
+// adds them up in the order of the keys.
 #include <cmath>
 
 #include <cuda_bf16.h>
@@ -17,91 +31,383 @@ namespace {
 
 using namespace pifa;
 
-struct AttnArgs {
+constexpr int WARPS = 8;
+constexpr int THREADS = 32 * WARPS;
+template <int D>
+constexpr int kStages = 384 / D;     // of 16 keys: 8 KB (D = 128) or 4 KB
+constexpr int STEP = 16;             // keys
+constexpr int MIN_STEPS = 4;         // of a warp: fewer cost more in partial sums than they save
+constexpr int MAX_ROWS = 16;
+constexpr int MAX_CTAS = 160;        // of the streaming kernel (one for each SM), which the workspace is sized for
+
+struct RowArgs {
   const uint16_t *q, *k, *v;
   uint16_t* o;
   const int32_t *table, *q_start, *kv_len;
+  int* sums;          // B + 1: first step of each request (times heads), then the steps of one warp
+  float* partial;     // for each warp two of max_rows x (D + 2): O, m, l
   int64_t ldq, ldo, ldt, page_stride, token_stride, head_stride, pages;
-  int T, hq, group, page_size, cols, B, max_q;
-  float scale_log2;
+  int T, heads, group, page_size, page_shift, cols, B, max_q, max_rows;
+  float c;            // |scale| log2(e), with scale's sign in `flip`
+  uint32_t flip;
   int* status;
 };
 
+struct Lengths {
+  int q0, n, L;
+};
+// Lengths of request b, kept within the buffers whatever the arrays hold.
+__device__ __forceinline__ Lengths lengths_of(const RowArgs& g, int b) {
+  Lengths x;
+  x.q0 = min(max(g.q_start[b], 0), g.T);
+  x.n = min(min(max(g.q_start[b + 1], x.q0), g.T) - x.q0, g.max_q);
+  x.L = min(max(g.kv_len[b], 0), g.cols << g.page_shift);
+  return x;
+}
+// Steps of a request: those of its keys; a request with rows but no keys has one, to write zeros.
+__device__ __forceinline__ int steps_of(const Lengths& x) { return x.n == 0 ? 0 : max((x.L + STEP - 1) / STEP, 1); }
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 template <bool F16>
-__device__ __forceinline__ float2 unpack(uint32_t w) {
-  if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
-  else return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+  if constexpr (F16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+}
+template <bool F16>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (F16) mma_m16n8k16_f16(d, a0, a1, a2, a3, b0, b1);
+  else mma_m16n8k16_bf16(d, a0, a1, a2, a3, b0, b1);
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The last index i in [0, n) with first[i] <= v (ascending, first[0] = 0 <= v).
+__device__ __forceinline__ int find(const int* first, int n, int v) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
 }
 
 template <bool F16, int D>
-__global__ void __launch_bounds__(128) attention_rows(const AttnArgs g) {
-  constexpr int W = D / 64;  // words of two elements a lane holds
+__global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
+  constexpr int KC = D / 32, VC = D / 64;            // 16-byte pieces of a lane: of one key, of one key of V
+  constexpr int PIECES = 2 * KC + 4 * VC;            // of one step
+  constexpr int STAGES = kStages<D>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  int* first = reinterpret_cast<int*>(smem + WARPS * STAGES * PIECES * 512);  // B + 1
+  __shared__ int part[32];
   pdl_launch_dependents();
   pdl_wait_primary();
-  const int lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int t = (int)(unit / g.hq), h = (int)(unit % g.hq);
-  if (t >= g.T || t >= g.q_start[g.B]) return;
-  int lo = 0, hi = g.B;  // the last request with q_start <= t
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (g.q_start[mid] <= t) lo = mid;
-    else hi = mid;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // ---- the requests' first steps ----
+  int total = 0;
+  bool over = false;
+  for (int b0 = 0; b0 < g.B; b0 += THREADS) {
+    const int b = b0 + tid;
+    int v = 0;
+    if (b < g.B) {
+      const Lengths x = lengths_of(g, b);
+      over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
+      v = steps_of(x) * g.heads;
+    }
+    int a = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, a, o);
+      if (lane >= o) a += x;
+    }
+    __syncthreads();
+    if (lane == 31) part[warp] = a;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      before += w < warp ? part[w] : 0;
+      all += part[w];
+    }
+    if (b < g.B) first[b] = total + before + a - v;
+    total += all;
   }
-  const int i = t - g.q_start[lo], n = g.q_start[lo + 1] - g.q_start[lo];
-  int L = g.kv_len[lo];
-  if (i >= g.max_q) {
-    latch_status(g.status, PIFA_ERR_CAPACITY);
-    return;
+  if (tid == 0) first[g.B] = total;
+  __syncthreads();
+  const int workers = (int)gridDim.x * WARPS;
+  const int run = max((total + workers - 1) / workers, MIN_STEPS);
+  if (blockIdx.x == 0) {
+    for (int b = tid; b <= g.B; b += THREADS) g.sums[b] = first[b];
+    if (tid == 0) g.sums[g.B + 1] = run;
+    if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
   }
-  if ((int64_t)L > (int64_t)g.cols * g.page_size) {
-    latch_status(g.status, PIFA_ERR_CAPACITY);
-    L = g.cols * g.page_size;
-  }
-  const int seen = L - n + i + 1;
-  float q[2 * W], o[2 * W] = {};
-  const uint32_t* qw = reinterpret_cast<const uint32_t*>(g.q + t * g.ldq + (int64_t)h * D) + lane * W;
-  for (int w = 0; w < W; ++w) {
-    const float2 x = unpack<F16>(qw[w]);
-    q[2 * w] = x.x * g.scale_log2;
-    q[2 * w + 1] = x.y * g.scale_log2;
-  }
-  float m = -INFINITY, l = 0.0f;
-  for (int j = 0; j < seen; ++j) {
-    const int page = g.table[lo * g.ldt + j / g.page_size];
-    float kf[2 * W] = {}, vf[2 * W] = {};
-    if (page >= 0 && page < g.pages) {
-      const int64_t at = page * g.page_stride + (j % g.page_size) * g.token_stride + (h / g.group) * g.head_stride;
-      for (int w = 0; w < W; ++w) {
-        const float2 x = unpack<F16>(reinterpret_cast<const uint32_t*>(g.k + at)[lane * W + w]);
-        const float2 y = unpack<F16>(reinterpret_cast<const uint32_t*>(g.v + at)[lane * W + w]);
-        kf[2 * w] = x.x;
-        kf[2 * w + 1] = x.y;
-        vf[2 * w] = y.x;
-        vf[2 * w + 1] = y.y;
+
+  // ---- this warp's run of steps: segments of one request and head each ----
+  const int worker = warp * (int)gridDim.x + (int)blockIdx.x;  // neighbours on different SMs
+  const int64_t at64 = (int64_t)worker * run;
+  int at = (int)min(at64, (int64_t)total);
+  const int stop = (int)min(at64 + run, (int64_t)total);
+  const int gr = lane >> 2, c4 = lane & 3;
+  uint8_t* mine = smem + (warp * STAGES * PIECES * 32 + lane) * 16;
+  const uint32_t mine_at = smem_u32(mine);
+  while (at < stop) {
+    const int b = find(first, g.B, at);
+    const Lengths x = lengths_of(g, b);
+    const int steps = steps_of(x), head = (at - first[b]) / steps, s0 = at - first[b] - head * steps;
+    const int s1 = min(steps, s0 + stop - at);
+    const int rows = x.n * g.group;
+    // the rows of Q: this lane's are gr and gr + 8
+    uint4 q[2][KC];
+    int seen[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int row = gr + 8 * r, token = row / g.group;
+      seen[r] = row < rows ? max(x.L - x.n + token + 1, 0) : 0;
+#pragma unroll
+      for (int i = 0; i < KC; ++i) {
+        q[r][i] = make_uint4(0, 0, 0, 0);
+        if (row < rows) {
+          q[r][i] = *reinterpret_cast<const uint4*>(g.q + (int64_t)(x.q0 + token) * g.ldq +
+                                                    (int64_t)(head * g.group + row - token * g.group) * D + c4 * 8 + 32 * i);
+          q[r][i].x ^= g.flip;
+          q[r][i].y ^= g.flip;
+          q[r][i].z ^= g.flip;
+          q[r][i].w ^= g.flip;
+        }
       }
-    } else {
-      latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
     }
-    float s = 0.0f;
-    for (int w = 0; w < 2 * W; ++w) s += q[w] * kf[w];
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    const float nm = fmaxf(m, s), up = nm == -INFINITY ? 0.0f : nm;
-    const float c = exp2f(m - up), p = exp2f(s - up);
-    l = l * c + p;
-    for (int w = 0; w < 2 * W; ++w) o[w] = o[w] * c + p * vf[w];
-    m = nm;
+    const int32_t* pages = g.table + b * g.ldt;
+    const int n_pages = (x.L + g.page_size - 1) >> g.page_shift;
+    int known = -1, ids = 0;  // ids: lane i holds the page of step known + i
+    auto load = [&](int s, int stage) {  // K, then V, as two groups; nothing past s1
+      if (s < s1) {
+        if (known < 0 || s >= known + 32) {
+          known = s;
+          const int p = ((s + lane) * STEP) >> g.page_shift;
+          ids = s + lane < s1 && p < n_pages ? pages[p] : 0;
+        }
+        const int id = __shfl_sync(0xffffffffu, ids, s - known);
+        const bool bad = id < 0 || id >= g.pages;
+        if (bad && x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+        const int64_t page = (bad ? 0 : (int64_t)id) * g.page_stride + head * g.head_stride +
+                             ((s * STEP) & (g.page_size - 1)) * g.token_stride;
+        const int left = bad ? 0 : x.L - s * STEP;  // keys from here on
+        const uint32_t dst = mine_at + stage * PIECES * 512;
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+          const int key = gr + 8 * nb;
+          const uint16_t* src = g.k + page + (key < left ? key : 0) * g.token_stride + c4 * 8;
+#pragma unroll
+          for (int i = 0; i < KC; ++i) cp_async16(dst + (nb * KC + i) * 512, src + 32 * i, key < left ? 16 : 0);
+        }
+        cp_commit();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int key = c4 * 2 + (k & 1) + 8 * (k >> 1);
+          const uint16_t* src = g.v + page + (key < left ? key : 0) * g.token_stride + gr * 8;
+#pragma unroll
+          for (int h = 0; h < VC; ++h) cp_async16(dst + (2 * KC + k * VC + h) * 512, src + 64 * h, key < left ? 16 : 0);
+        }
+      } else {
+        cp_commit();
+      }
+      cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) load(s0 + i, i);
+    float o[VC * 8][4] = {};
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
+    int stage = 0;
+    for (int s = s0; s < s1; ++s) {
+      load(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+      const uint4* buf = reinterpret_cast<const uint4*>(mine + stage * PIECES * 512);
+      cp_wait<2 * STAGES - 1>();
+      float sc[2][4] = {};
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+          const uint4 k = buf[(nb * KC + i) * 32];
+          mma<F16>(sc[nb], q[0][i].x, q[1][i].x, q[0][i].y, q[1][i].y, k.x, k.y);
+          mma<F16>(sc[nb], q[0][i].z, q[1][i].z, q[0][i].w, q[1][i].w, k.z, k.w);
+        }
+      // keys that a row does not see; scores relative to m
+      float v[2][4];
+      bool grows = false;
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int key = s * STEP + 8 * (k >> 1) + c4 * 2 + (k & 1);
+          v[r][k] = key < seen[r] ? sc[k >> 1][2 * r + (k & 1)] * g.c : -INFINITY;
+          grows |= v[r][k] > m[r] + 8.0f;
+        }
+      if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float top = fmaxf(fmaxf(v[r][0], v[r][1]), fmaxf(v[r][2], v[r][3]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          top = fmaxf(top, m[r]);
+          const float f = top > m[r] ? fast_exp2(m[r] - top) : 1.0f;  // 0 where nothing was seen before
+          m[r] = top;
+          l[r] *= f;
+#pragma unroll
+          for (int i = 0; i < VC * 8; ++i) {
+            o[i][2 * r] *= f;
+            o[i][2 * r + 1] *= f;
+          }
+        }
+      }
+      uint32_t p[2][2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float base = m[r] > -INFINITY ? m[r] : 0.0f;
+        float e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] = fast_exp2(v[r][k] - base);
+        l[r] += (e[0] + e[1]) + (e[2] + e[3]);
+        p[r][0] = pack<F16>(e[0], e[1]);
+        p[r][1] = pack<F16>(e[2], e[3]);
+      }
+      cp_wait<2 * STAGES - 2>();
+#pragma unroll
+      for (int h = 0; h < VC; ++h) {
+        uint4 w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = buf[(2 * KC + k * VC + h) * 32];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // columns 2 i and 2 i + 1 of the lane's eight
+          const uint32_t a = (&w[0].x)[i], bb = (&w[1].x)[i], cc = (&w[2].x)[i], dd = (&w[3].x)[i];
+          mma<F16>(o[h * 8 + 2 * i], p[0][0], p[1][0], p[0][1], p[1][1], __byte_perm(a, bb, 0x5410), __byte_perm(cc, dd, 0x5410));
+          mma<F16>(o[h * 8 + 2 * i + 1], p[0][0], p[1][0], p[0][1], p[1][1], __byte_perm(a, bb, 0x7632), __byte_perm(cc, dd, 0x7632));
+        }
+      }
+      stage = stage == STAGES - 1 ? 0 : stage + 1;
+    }
+    cp_wait<0>();
+    // o[h 8 + i][2 r + e]: row gr + 8 r, column 64 h + 16 c4 + 8 e + i
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      const int row = gr + 8 * r, token = row / g.group;
+      if (row >= rows) continue;
+      if (s0 == 0 && s1 == steps) {
+        const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+        uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + c4 * 16;
+#pragma unroll
+        for (int h = 0; h < VC; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack<F16>(o[h * 8 + 2 * i][2 * r + e] * inv, o[h * 8 + 2 * i + 1][2 * r + e] * inv);
+            *reinterpret_cast<uint4*>(out + 64 * h + 8 * e) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+      } else {  // a head that began before this run: the first of the warp's two places, else the second
+        float* to = g.partial + (((int64_t)worker * 2 + (s0 > 0 ? 0 : 1)) * g.max_rows + row) * (D + 2);
+        float2* ml = reinterpret_cast<float2*>(to + D);
+        if (c4 == 0) *ml = make_float2(m[r], l[r]);
+#pragma unroll
+        for (int h = 0; h < VC; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<float2*>(to + 64 * h + 16 * c4 + 8 * e + 2 * i) =
+                  make_float2(o[h * 8 + 2 * i][2 * r + e], o[h * 8 + 2 * i + 1][2 * r + e]);
+      }
+    }
+    at += s1 - s0;
   }
-  const float inv = l > 0.0f ? 1.0f / l : (l == l ? 0.0f : l);
-  uint32_t* ow = reinterpret_cast<uint32_t*>(g.o + t * g.ldo + (int64_t)h * D) + lane * W;
-  for (int w = 0; w < W; ++w) {
-    if constexpr (F16) {
-      const __half2 x = __floats2half2_rn(o[2 * w] * inv, o[2 * w + 1] * inv);
-      ow[w] = *reinterpret_cast<const uint32_t*>(&x);
-    } else {
-      const __nv_bfloat162 x = __floats2bfloat162_rn(o[2 * w] * inv, o[2 * w + 1] * inv);
-      ow[w] = *reinterpret_cast<const uint32_t*>(&x);
+}
+
+// Adds up the pieces of heads whose steps fell to several warps, in the order of the keys: WPR warps for each
+// row, each with every WPR-th piece.
+template <bool F16, int D, int WPR>
+__global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g) {
+  constexpr int E = D / 32;  // columns of a lane
+  __shared__ float2 sh_ml[WARPS];
+  __shared__ float sh_o[WARPS][D];
+  pdl_launch_dependents();
+  pdl_wait_primary();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t unit = (int64_t)blockIdx.x * (WARPS / WPR) + warp / WPR, item = unit / g.max_rows;
+  const int row = (int)(unit - item * g.max_rows), b = (int)(item / g.heads), head = (int)(item - (int64_t)b * g.heads);
+  bool here = b < g.B;
+  Lengths x = {};
+  int w0 = 0, w1 = 0;
+  if (here) {
+    x = lengths_of(g, b);
+    const int steps = steps_of(x), run = g.sums[g.B + 1], from = g.sums[b] + head * steps;
+    w0 = from / run;
+    w1 = (from + steps - 1) / run;
+    here = row < x.n * g.group && w1 > w0;
+  }
+  float top = -INFINITY, all = 0.0f, acc[E] = {};
+  if (here) {
+    const float* base = g.partial + row * (D + 2);
+    const int place = g.max_rows * (D + 2);  // a warp has two: the head that began before its run, and the last one
+    auto piece = [&](int w) { return base + ((int64_t)w * 2 + (w == w0 ? 1 : 0)) * place; };
+    const int k = w0 + warp % WPR;
+    for (int w = k + lane * WPR; w <= w1; w += 32 * WPR) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(w) + D));
+      if (ml.y != 0.0f) top = fmaxf(top, ml.x);
     }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float base_m = top > -INFINITY ? top : 0.0f;
+#pragma unroll 4
+    for (int w = k; w <= w1; w += WPR) {
+      const float* p = piece(w);
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + D));
+      const float f = ml.y != 0.0f ? fast_exp2(ml.x - base_m) : 0.0f;
+      all += ml.y * f;
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 y = __ldcg(reinterpret_cast<const float2*>(p + lane * E + e));
+        acc[e] += y.x * f;
+        acc[e + 1] += y.y * f;
+      }
+    }
+  }
+  if constexpr (WPR > 1) {
+    if (lane == 0) sh_ml[warp] = make_float2(top, all);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sh_o[warp][lane * E + e] = acc[e];
+    __syncthreads();
+    if (warp % WPR) return;
+#pragma unroll
+    for (int k = 0; k < WPR; ++k) top = fmaxf(top, sh_ml[warp + k].x);
+    all = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < WPR; ++k) {
+      const float2 ml = sh_ml[warp + k];
+      const float f = ml.y != 0.0f ? fast_exp2(ml.x - top) : 0.0f;
+      all += ml.y * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += sh_o[warp + k][lane * E + e] * f;
+    }
+  }
+  if (here) {
+    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+    const int token = row / g.group;
+    uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(out + e) = pack<F16>(acc[e] * inv, acc[e + 1] * inv);
   }
 }
 
@@ -120,7 +426,39 @@ int check_sizes(int64_t T, int64_t hq, int64_t hk, int64_t dim, int64_t B, int64
 }
 
 // Whether a request's rows for one key / value head may be more than one 16-row product.
-bool takes_tc(int64_t group, int64_t max_q) { return max_q > 16 || group * max_q > 16; }
+bool takes_tc(int64_t group, int64_t max_q) { return max_q > MAX_ROWS || group * max_q > MAX_ROWS; }
+
+int64_t sums_bytes(int64_t B) { return ((B + 2) * 4 + 255) / 256 * 256; }
+int64_t rows_workspace_bytes(int64_t max_rows, int64_t dim, int64_t B) {
+  return sums_bytes(B) + (int64_t)MAX_CTAS * WARPS * 2 * max_rows * (dim + 2) * 4;
+}
+
+template <bool F16, int D>
+cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
+  const int sms = pifa_sm_count(), grid = sms < MAX_CTAS ? sms : MAX_CTAS;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = (size_t)WARPS * kStages<D> * (D / 8) * 512 + (size_t)(g.B + 1) * 4;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaFuncSetAttribute(attention_rows<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 256);
+  if (e == cudaSuccess) e = pifa_launch_ex(&cfg, attention_rows<F16, D>, g);
+  if (e != cudaSuccess) return e;
+  // a warp for each row; few rows, of which each may have pieces from all over the grid: eight
+  const int64_t units = (int64_t)g.B * g.heads * g.max_rows;
+  cfg.dynamicSmemBytes = 0;
+  if (units <= 1024) {
+    cfg.gridDim = dim3((unsigned)units);
+    return pifa_launch_ex(&cfg, attention_join<F16, D, WARPS>, g);
+  }
+  cfg.gridDim = dim3((unsigned)((units + WARPS - 1) / WARPS));
+  return pifa_launch_ex(&cfg, attention_join<F16, D, 1>, g);
+}
 
 }  // namespace
 
@@ -132,7 +470,9 @@ int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t 
   const int st = check_sizes(T, q_heads, kv_heads, head_dim, B, max_q);
   if (st != PIFA_OK) return st;
   if (T == 0 || B == 0) return 0;
-  return kWorkspaceReserve + (takes_tc(q_heads / kv_heads, max_q) ? attention_tc_workspace_bytes(T, q_heads, kv_heads, head_dim, B) : 0);
+  const int64_t group = q_heads / kv_heads;
+  return kWorkspaceReserve + (takes_tc(group, max_q) ? attention_tc_workspace_bytes(T, q_heads, kv_heads, head_dim, B)
+                                                     : rows_workspace_bytes(group * max_q, head_dim, B));
 }
 
 int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
@@ -149,9 +489,11 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   int st = pifa_check_cache(c, 16, 256);
   if (st != PIFA_OK) return st;
   if (page_size & (page_size - 1)) return pifa_fail(PIFA_ERR_UNSUPPORTED, "attention takes a page_size that is a power of two");
-  const int64_t lim = (int64_t)1 << 31;
-  if (cols < 0 || cols * page_size >= lim || ldt < cols || !std::isfinite(scale))
+  const int64_t lim = (int64_t)1 << 30;
+  if (cols < 0 || cols >= lim || cols * page_size > lim || ldt < cols || !(std::fabs(scale) <= 1e30f))
     return pifa_fail(PIFA_ERR_INVALID_ARG, "cols, ldt or scale out of range");
+  if (B * kv_heads * (cols * page_size / STEP + 1) >= 2 * lim)
+    return pifa_fail(PIFA_ERR_UNSUPPORTED, "attention takes at most 2^35 keys, over all requests and heads, in the tables");
   if (T == 0 || B == 0) return PIFA_OK;
   if (!Q || !k_cache || !v_cache || !O || !q_start || !kv_len || (cols && !table))
     return pifa_fail(PIFA_ERR_INVALID_ARG, "null argument");
@@ -173,12 +515,11 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   cudaError_t e = cudaSuccess;
   int* status = pifa_status_word(&e);
   if (!status) return pifa_fail_cuda("device status word", e);
-  if (takes_tc(q_heads / kv_heads, max_q)) {
-    PifaAttention a = {Q, k_cache, v_cache, O, table, q_start, kv_len, T, ldq, ldo, ldt, cols, B, max_q, q_heads, c, dtype,
-                       scale * 1.4426950408889634f, static_cast<uint8_t*>(workspace) + kWorkspaceReserve};
+  const PifaAttention a = {Q, k_cache, v_cache, O, table, q_start, kv_len, T, ldq, ldo, ldt, cols, B, max_q, q_heads, c, dtype,
+                           scale * 1.4426950408889634f, static_cast<uint8_t*>(workspace) + kWorkspaceReserve};
+  if (takes_tc(q_heads / kv_heads, max_q))
     return launch_attention_tc(a, status, pifa_wait_timeout_ns(), reinterpret_cast<cudaStream_t>(cuda_stream));
-  }
-  AttnArgs g = {};
+  RowArgs g = {};
   g.q = static_cast<const uint16_t*>(Q);
   g.k = static_cast<const uint16_t*>(k_cache);
   g.v = static_cast<const uint16_t*>(v_cache);
@@ -186,6 +527,8 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   g.table = table;
   g.q_start = q_start;
   g.kv_len = kv_len;
+  g.sums = reinterpret_cast<int*>(a.ws);
+  g.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + sums_bytes(B));
   g.ldq = ldq;
   g.ldo = ldo;
   g.ldt = ldt;
@@ -194,26 +537,22 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   g.head_stride = head_stride;
   g.pages = pages;
   g.T = (int)T;
-  g.hq = (int)q_heads;
+  g.heads = (int)kv_heads;
   g.group = (int)(q_heads / kv_heads);
   g.page_size = (int)page_size;
+  while ((1 << g.page_shift) < g.page_size) ++g.page_shift;
   g.cols = (int)cols;
   g.B = (int)B;
-  g.max_q = (int)(max_q < lim ? max_q : lim - 1);
-  g.scale_log2 = scale * 1.4426950408889634f;
+  g.max_q = (int)max_q;
+  g.max_rows = g.max_q * g.group;
+  g.flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+  // equal weights for a scale of zero: the masked scores, -inf, still have to vanish
+  g.c = a.scale_log2 == 0.0f ? 1e-30f : std::fabs(a.scale_log2);
   g.status = status;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((T * q_heads + 3) / 4));
-  cfg.blockDim = dim3(128);
-  cfg.stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
   const bool f16 = dtype == PIFA_DTYPE_FP16;
-  if (head_dim == 64) e = f16 ? pifa_launch_ex(&cfg, attention_rows<true, 64>, g) : pifa_launch_ex(&cfg, attention_rows<false, 64>, g);
-  else e = f16 ? pifa_launch_ex(&cfg, attention_rows<true, 128>, g) : pifa_launch_ex(&cfg, attention_rows<false, 128>, g);
+  cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (head_dim == 64) e = f16 ? launch_rows<true, 64>(g, stream) : launch_rows<false, 64>(g, stream);
+  else e = f16 ? launch_rows<true, 128>(g, stream) : launch_rows<false, 128>(g, stream);
   if (e != cudaSuccess) return pifa_fail_cuda("attention launch", e);
   return PIFA_OK;
 }

@@ -435,7 +435,7 @@ def test_attention_reports_bad_tables_and_bounds():
         b = dict(a, kv_len=i32([10 ** 6, 90]))
         O = attend(b)
         assert P.pifa_device_status() in (P.PIFA_ERR_CAPACITY, P.PIFA_ERR_DEVICE_INDEX)
-        assert torch.equal(O[new:], good[new:])
+        check_attention(a, torch.cat([good[:new], O[new:]]), 128 ** -0.5)   # other lengths, other cuts of the work
     O = torch.full_like(a["Q"], 5.0)
     attend(a, max_q=3, O=O)
     assert P.pifa_device_status() == P.PIFA_ERR_CAPACITY
