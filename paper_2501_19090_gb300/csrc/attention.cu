@@ -54,7 +54,8 @@ struct RowArgs {
 };
 
 struct Lengths {
-  int q0, n, L;
+  int q0, n, L;   // first row of Q, new tokens that are computed, keys
+  int ahead;      // token i sees ahead + i keys
 };
 // Lengths of request b, kept within the buffers whatever the arrays hold.
 __device__ __forceinline__ Lengths lengths_of(const RowArgs& g, int b) {
@@ -62,6 +63,7 @@ __device__ __forceinline__ Lengths lengths_of(const RowArgs& g, int b) {
   x.q0 = min(max(g.q_start[b], 0), g.T);
   x.n = min(min(max(g.q_start[b + 1], x.q0), g.T) - x.q0, g.max_q);
   x.L = min(max(g.kv_len[b], 0), g.cols << g.page_shift);
+  x.ahead = x.L - (max(g.q_start[b + 1], x.q0) - x.q0) + 1;
   return x;
 }
 // Steps of a request: those of its keys; a request with rows but no keys has one, to write zeros.
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int row = gr + 8 * r, token = row / g.group;
-      seen[r] = row < rows ? max(x.L - x.n + token + 1, 0) : 0;
+      seen[r] = row < rows ? max(x.ahead + token, 0) : 0;
 #pragma unroll
       for (int i = 0; i < KC; ++i) {
         q[r][i] = make_uint4(0, 0, 0, 0);

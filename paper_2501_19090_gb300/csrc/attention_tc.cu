@@ -89,13 +89,14 @@ struct TcArgs {
 
 struct Item {
   int b, head, row0, rows;           // rows: of the request
-  int n, L, q0;
+  int L, q0, ahead;
   int j0, j1, e0, e1;                // e: end of the key tiles that a tile's rows see
   int part, parts, slot, counter, end;
 };
 
 struct Lengths {
-  int q0, n, L;
+  int q0, n, L;   // first row of Q, new tokens that are computed, keys
+  int ahead;      // token i sees ahead + i keys
 };
 
 // Lengths of request b, kept within the buffers whatever the arrays hold.
@@ -104,6 +105,7 @@ __device__ __forceinline__ Lengths lengths_of(const TcArgs& g, int b) {
   x.q0 = min(max(g.q_start[b], 0), g.T);
   x.n = min(min(max(g.q_start[b + 1], x.q0), g.T) - x.q0, g.max_q);
   x.L = min(max(g.kv_len[b], 0), g.cols << g.page_shift);
+  x.ahead = x.L - (max(g.q_start[b + 1], x.q0) - x.q0) + 1;
   return x;
 }
 
@@ -112,7 +114,7 @@ __device__ __forceinline__ int tile_end(const Lengths& x, int group, int row) {
   const int rows = x.n * group;
   if (row >= rows) return 0;
   const int last = (min(row + BM, rows) - 1) / group;  // token
-  return (max(x.L - x.n + last + 1, 0) + BN - 1) / BN;
+  return (max(x.ahead + last, 0) + BN - 1) / BN;
 }
 __device__ __forceinline__ int item_end(const Lengths& x, int group, int row0) {
   return max(tile_end(x, group, row0), tile_end(x, group, row0 + BM));
@@ -147,7 +149,8 @@ __device__ __forceinline__ int block_sum_scan(int v, int* part, int& total) {  /
 __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g, int grid) {
   extern __shared__ int first[];  // B + 1: first row tile of each request
   __shared__ int part[32];
-  __shared__ int red[4];          // largest and smallest item, largest and sum of those that may be cut
+  __shared__ int red[4];          // largest and smallest item; of those that may be cut, the largest and the sum
+  __shared__ unsigned long long sum_all;  // of all items
   __shared__ int cut;             // key tiles of a piece
   pdl_launch_dependents();
   pdl_wait_primary();
@@ -155,6 +158,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   if (tid == 0) {
     red[0] = red[2] = red[3] = 0;
     red[1] = 0x7fffffff;
+    sum_all = 0;
   }
   for (int i = tid; i < MAX_PARTS / 2 * 8; i += PLAN_THREADS) g.counters[i] = 0;
   bool over = false;
@@ -192,6 +196,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   // Whole rounds of the grid stay whole; the items of the last, unfilled round may be cut.
   const int whole = (int)((int64_t)items * g.heads / grid * grid / g.heads);
   int most = 0, least = 0x7fffffff, most_cut = 0, sum_cut = 0;
+  unsigned long long sum = 0;
   for (int k = tid; k < items; k += PLAN_THREADS) {
     Lengths x;
     int b, row0;
@@ -202,27 +207,28 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
       most_cut = max(most_cut, cost);
       sum_cut += cost;
     }
+    sum += cost;
   }
+  atomicAdd(&sum_all, sum);
   atomicMax(&red[0], most);
   atomicMin(&red[1], least);
   atomicMax(&red[2], most_cut);
   atomicAdd(&red[3], sum_cut);
   __syncthreads();
   if (tid < 32) {
-    // The time of the last round, in key tiles, if its items are cut into pieces of `size`: an even share for each
-    // CTA, and where items are alike, the wait for a last round of pieces that does not fill the grid. A piece
-    // costs about two tiles on top (rows of Q, first and last products), with partial sums about three.
+    // The time of all, in key tiles, if those items are cut into pieces of `size`: an even share for each CTA,
+    // and, where items are alike, the wait for a last round of pieces that does not fill the grid. An item or
+    // piece costs about two tiles on top (rows of Q, first and last products), one with partial sums three.
     const int rest = items - whole;
     const int size = max((red[2] + tid) / (tid + 1), 1);
     const float alike = red[0] > 0 ? (float)red[1] / (float)red[0] : 0.0f;
     const float pieces = tid == 0 ? (float)rest : (float)rest * 0.5f + (float)red[3] / (float)size;
-    const float extra = tid == 0 ? 2.0f : 3.0f;
-    const float rounds = pieces * (float)g.heads / (float)grid;
-    float t = rounds * extra + (float)red[3] * (float)g.heads / (float)grid +
+    const float extra = tid == 0 ? 2.0f : 3.0f, per_cta = (float)g.heads / (float)grid;
+    const float rounds = pieces * per_cta;
+    float t = ((float)sum_all + 2.0f * (float)whole + extra * pieces) * per_cta +
               alike * (ceilf(rounds) - rounds) * ((float)size + extra);
     t = fmaxf(t, (float)size + extra);
-    const bool fits = tid == 0 || (int64_t)(rest + red[3] / size) * g.heads <= MAX_PARTS;
-    if (!fits) t = 3e38f;
+    if (tid > 0 && (int64_t)(rest + red[3] / size) * g.heads > MAX_PARTS) t = 3e38f;  // more than there is room for
     int who = tid;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -364,6 +370,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     return ok;
   };
 
+  // Registers: a softmax thread holds a row of S. 2 x 128 x 208 + 128 x 88 = 384 x 168, as launched.
+  if (warp >= 8) {
+  regs_lower<88>();
   if (warp == 8) {
     // ---------------- queue, K and V ----------------
     const int total = g.plan->entries * g.heads;
@@ -388,7 +397,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         it.head = k % g.heads;
         it.row0 = e.row0;
         it.rows = x.n * g.group;
-        it.n = x.n;
+        it.ahead = x.ahead;
         it.L = x.L;
         it.q0 = x.q0;
         it.j0 = e.j0;
@@ -541,7 +550,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mma_commit(drain);  // every MMA has completed before the tensor memory is freed
       if (!mbar_wait(drain, 0, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
     }
-  } else if (warp >= 10) {
+  } else {
     // ---------------- rows of Q ----------------
     const int t = warp - 10;
     uint32_t ph = 1;
@@ -567,7 +576,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&q_full[t]);
     }
+  }
   } else {
+    regs_raise<208>();
     // ---------------- softmax and epilogue: a row per thread ----------------
     const int t = warp >> 2, quarter = warp & 3;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
@@ -583,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int end = t ? it.e1 : it.e0;
       const int row = it.row0 + t * BM + quarter * 32 + lane;       // of the request
       const int token = row / g.group, h = row - token * g.group;
-      const int seen = row < it.rows ? max(it.L - it.n + token + 1, 0) : 0;
+      const int seen = row < it.rows ? max(it.ahead + token, 0) : 0;
       const bool idle = it.row0 + t * BM + quarter * 32 >= it.rows;  // no row of this warp exists
       float m = -INFINITY, l = 0.0f;
       for (int j = it.j0; j < end; ++j) {
@@ -617,34 +628,35 @@ __global__ void __launch_bounds__(THREADS, 1)
             const float f = up > m ? fast_exp2((m - up) * c) : 1.0f;
             m = up;
             l *= f;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-              uint32_t o[32];
-              tmem_ld_32x32b_x32(o_at + i * 32, o);
+#pragma unroll 1
+            for (int i = 0; i < D / 16; ++i) {  // a few registers at a time: the row of S is held meanwhile
+              uint32_t o[16];
+              tmem_ld_32x32b_x16(o_at + i * 16, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-              tmem_st_32x32b_x32(o_at + i * 32, o);
+              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              tmem_st_32x32b_x16(o_at + i * 16, o);
             }
           }
           if (m == -INFINITY) m = top;
           const float mc = m > -INFINITY ? m * c : 0.0f;
-          float sum[4] = {};
+          const uint64_t c2 = f32x2(c, c), mc2 = f32x2(-mc, -mc);
+          uint64_t sum[2] = {0, 0};
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             uint32_t w[32];
 #pragma unroll
             for (int k = 0; k < 32; ++k) {
-              const uint32_t* u = v[2 * i + k / 16];
-              const float p0 = fast_exp2(fmaf(__uint_as_float(u[2 * k % 32]), c, -mc));
-              const float p1 = fast_exp2(fmaf(__uint_as_float(u[2 * k % 32 + 1]), c, -mc));
-              sum[2 * i] += p0;
-              sum[2 * i + 1] += p1;
+              const float2 x = f32x2_parts(fma_f32x2(
+                  f32x2(__uint_as_float(v[2 * i + k / 16][2 * k % 32]), __uint_as_float(v[2 * i + k / 16][2 * k % 32 + 1])), c2, mc2));
+              const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+              sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
               w[k] = pack<F16>(p0, p1);
             }
             tmem_st_32x32b_x32(s_at + i * 32, w);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
+          l += both.x + both.y;
           tmem_st_wait();
           tc_fence_before();
         }
