@@ -15,10 +15,10 @@
 //   warps 0-3, 4-7   softmax and epilogue of tile 0 and 1 (tensor memory quarter = warp % 4)
 //   warp 8           takes work items from a queue and loads K and V tiles by TMA into a ring of slots, a page (or a
 //                    128-token part of one) and 64 columns a copy, a lane for each
-//   warp 9           issues the MMAs: PV of tile 0 and its next S, then the same of tile 1, so that one tile's
-//                    softmax runs under the other tile's MMAs
-//   warps 10, 11     load the next item's rows of Q, as soon as its last S has been computed
-// P lies over S, and S of the next keys is written over both: the MMAs of one thread run in issue
+//   warps 9, 10      issue the MMAs of tile 0 and 1: PV, in two halves of the keys as P arrives, and the next S; one
+//                    tile's softmax runs under the other tile's MMAs. (One warp for both was the bound.)
+//   warp 11          loads the next item's rows of Q, as soon as the last S of a tile has been computed
+// P lies over S, and S of the next keys is written over both: the MMAs of one warp run in issue
 // order, PV(j) before S(j + 1), and S(j)'s values were read before P was announced.
 // Keys past L: their scores are masked, and their rows of V, which may hold anything, are set to zero in shared
 // memory, since 0 times NaN is NaN.
@@ -319,33 +319,36 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* full = reinterpret_cast<uint64_t*>(ring + SLOTS * TILE);
   uint64_t* empty = full + SLOTS;
   uint64_t* s_full = empty + SLOTS;   // S of a tile is in tensor memory
-  uint64_t* p_full = s_full + 2;      // its P is, and its O may be added to
-  uint64_t* o_full = p_full + 2;      // the item's last PV is done
+  uint64_t* p_full = s_full + 2;      // half of its P is, and its O may be added to: two for each tile
+  uint64_t* o_full = p_full + 4;      // the item's last PV is done
   uint64_t* q_full = o_full + 2;
   uint64_t* q_free = q_full + 2;
   uint64_t* item_full = q_free + 2;
   uint64_t* item_free = item_full + 2;
-  uint64_t* drain = item_free + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t* v_clean = item_free + 2;  // of a slot: rows of V past the last key are zero
+  uint64_t* drain = v_clean + SLOTS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 2);
   Item* items = reinterpret_cast<Item*>(tmem_slot + 2);
 
   pdl_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < SLOTS; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
+      mbar_init(&empty[s], 2);
+      mbar_init(&v_clean[s], 1);
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(&s_full[t], 1);
-      mbar_init(&p_full[t], 4);
+      mbar_init(&p_full[2 * t], 4);
+      mbar_init(&p_full[2 * t + 1], 4);
+      mbar_init(&drain[t], 1);
       mbar_init(&o_full[t], 1);
       mbar_init(&q_full[t], 1);
       mbar_init(&q_free[t], 1);
       mbar_init(&item_full[t], 1);
       mbar_init(&item_free[t], 11);
     }
-    mbar_init(drain, 1);
     fence_mbar_init();
     prefetch_tmap(&kmap);
     prefetch_tmap(&vmap);
@@ -357,7 +360,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
   pdl_wait_primary();
   bool dead = false;
   // all lanes of the warp wait; false (and the status latched) if the wait ran out
@@ -452,129 +455,149 @@ __global__ void __launch_bounds__(THREADS, 1)
     // nothing may land in shared memory after the CTA has left
     for (int i = fills > SLOTS ? fills - SLOTS : 0; i < fills; ++i)
       if (!mbar_wait(&full[i % SLOTS], (uint32_t)(i / SLOTS) & 1u, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
-  } else if (warp == 9) {
-    // ---------------- MMAs ----------------
+  } else if (warp < 11) {
+    // ---------------- MMAs of a tile ----------------
+    const int t = warp - 9;
     const uint32_t kind = F16 ? idesc_f16_f32(BM, BN) : idesc_bf16_f32(BM, BN);
     const uint32_t qk_desc = kind | (g.negate ? 1u << 13 : 0u);
     const uint32_t pv_desc = (F16 ? idesc_f16_f32(BM, D) : idesc_bf16_f32(BM, D)) | (1u << 16);
-    const uint64_t q_desc = sw128_desc(smem_u32(smem)), k_desc = sw128_desc(smem_u32(ring)), v_desc = sw128_mn_desc(smem_u32(ring));
+    const uint64_t q_desc = sw128_desc(smem_u32(smem) + (uint32_t)t * TILE);
+    const uint64_t k_desc = sw128_desc(smem_u32(ring)), v_desc = sw128_mn_desc(smem_u32(ring));
+    const uint32_t s_at = tmem + t * BN, o_at = tmem + 2 * BN + t * D;
     int s = 0;
-    uint32_t ph = 0, q_ph = 0, p_ph = 0;  // a bit for each tile
-    auto score = [&](int t, int slot) {
-      if (lane == 0) {
+    uint32_t ph = 0, q_ph = 0, p_ph = 0, tail_ph = 0;
+    auto advance = [&] {
+      if (++s == SLOTS) {
+        s = 0;
+        ph ^= 1u;
+      }
+    };
+    // S = Q K^T; then K's slot is given back, and Q after the item's last S
+    auto score = [&](int slot, bool last) {
+      if (elect_one()) {
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
           const uint32_t at = (uint32_t)(kk / 4) * (HALF / 16) + (uint32_t)(kk % 4) * 2;
-          mma_bf16_ss(tmem + t * BN, q_desc + t * (TILE / 16) + at, k_desc + slot * (TILE / 16) + at, qk_desc, kk > 0);
+          mma_bf16_ss(s_at, q_desc + at, k_desc + slot * (TILE / 16) + at, qk_desc, kk > 0);
         }
         mma_commit(&s_full[t]);
+        mma_commit(&empty[slot]);
+        if (last) mma_commit(&q_free[t]);
       }
+    };
+    auto skip = [&](int slot) {  // a slot that this tile does not read
+      if (lane == 0) mbar_arrive(&empty[slot]);
     };
     for (int n = 0; !dead; ++n) {
       if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
-      const int end = items[n & 1].end, j0 = items[n & 1].j0, j1 = items[n & 1].j1, L = items[n & 1].L;
-      const int e[2] = {items[n & 1].e0, items[n & 1].e1};
+      const int end = uniform(items[n & 1].end), j0 = uniform(items[n & 1].j0), j1 = uniform(items[n & 1].j1);
+      const int L = uniform(items[n & 1].L), e = uniform(t ? items[n & 1].e1 : items[n & 1].e0);
       __syncwarp();
       if (lane == 0) mbar_arrive(&item_free[n & 1]);
       if (end) break;
       if (j0 >= j1) continue;
       if (!wait(&full[s], ph)) break;
-      tc_fence_after();
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (j0 < e[t]) {
-          if (!wait(&q_full[t], (q_ph >> t) & 1u)) break;
-          q_ph ^= 1u << t;
-          tc_fence_after();
-          score(t, s);
-          if (j0 + 1 >= e[t] && lane == 0) mma_commit(&q_free[t]);
-        }
+      if (j0 < e) {
+        if (!wait(&q_full[t], q_ph)) break;
+        q_ph ^= 1u;
+        tc_fence_after();
+        score(s, j0 + 1 >= e);
+      } else {
+        skip(s);
       }
-      if (dead) break;
-      if (lane == 0) mma_commit(&empty[s]);
-      if (++s == SLOTS) {
-        s = 0;
-        ph ^= 1u;
-      }
-      for (int j = j0; j < j1 && !dead; ++j) {
-        if (!wait(&full[s], ph)) break;
+      advance();
+      for (int j = j0; j < j1; ++j) {
         const int vs = s;
-        if (++s == SLOTS) {
-          s = 0;
-          ph ^= 1u;
+        if (!wait(&full[vs], ph)) break;
+        advance();
+        const int ks = s;
+        if (j + 1 < j1) {
+          if (!wait(&full[ks], ph)) break;
+          advance();
         }
         const int tail = L - j * BN;  // keys of this tile
         if (tail < BN) {
-          uint8_t* v = ring + vs * TILE;
-          for (int i = max(tail, 0) * 8 + lane; i < BN * 8; i += 32)
+          if (t == 0) {
+            uint8_t* v = ring + vs * TILE;
+            for (int i = max(tail, 0) * 8 + lane; i < BN * 8; i += 32)
 #pragma unroll
-            for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(v + h * HALF + i * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        tc_fence_after();
-        int ks = -1;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (dead || j >= e[t]) continue;
-          if (!wait(&p_full[t], (p_ph >> t) & 1u)) continue;
-          p_ph ^= 1u << t;
-          tc_fence_after();
-          if (lane == 0) {
-#pragma unroll
-            for (int kk = 0; kk < BN / 16; ++kk)
-              mma_bf16_ts(tmem + 2 * BN + t * D, tmem + t * BN + kk * 8, v_desc + vs * (TILE / 16) + kk * 128, pv_desc,
-                          j > j0 || kk > 0);
-            if (j + 1 >= e[t]) mma_commit(&o_full[t]);
-            if (t == 1 || j >= e[1]) mma_commit(&empty[vs]);
+              for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(v + h * HALF + i * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&v_clean[vs]);
+          } else {
+            if (!wait(&v_clean[vs], (tail_ph >> vs) & 1u)) break;
+            tail_ph ^= 1u << vs;
           }
-          if (j + 1 < e[t]) {
-            if (ks < 0) {
-              if (!wait(&full[s], ph)) continue;
-              tc_fence_after();
-              ks = s;
-              if (++s == SLOTS) {
-                s = 0;
-                ph ^= 1u;
+        }
+        if (j < e) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (!wait(&p_full[2 * t + h], p_ph)) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int kk = 0; kk < BN / 32; ++kk) {
+                const int k = h * (BN / 32) + kk;
+                mma_bf16_ts(o_at, s_at + k * 8, v_desc + vs * (TILE / 16) + k * 128, pv_desc, j > j0 || k > 0);
+              }
+              if (h == 1) {
+                if (j + 1 >= e) mma_commit(&o_full[t]);
+                mma_commit(&empty[vs]);
               }
             }
-            score(t, ks);
-            if (j + 2 >= e[t] && lane == 0) mma_commit(&q_free[t]);
           }
+          if (dead) break;
+          p_ph ^= 1u;
+        } else {
+          skip(vs);
         }
-        if (ks >= 0 && lane == 0) mma_commit(&empty[ks]);
+        if (j + 1 < j1) {
+          if (j + 1 < e) score(ks, j + 2 >= e);
+          else skip(ks);
+        }
       }
     }
     __syncwarp();
-    if (lane == 0) {
-      mma_commit(drain);  // every MMA has completed before the tensor memory is freed
-      if (!mbar_wait(drain, 0, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
+    if (elect_one()) {
+      mma_commit(&drain[t]);  // every MMA has completed before the tensor memory is freed
+      if (!mbar_wait(&drain[t], 0, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
     }
   } else {
     // ---------------- rows of Q ----------------
-    const int t = warp - 10;
-    uint32_t ph = 1;
-    constexpr int CH = D / 8;  // 16-byte pieces of a row
+    uint32_t ph[2] = {1, 1};
+    constexpr int CH = D / 8, STEP = 32 / CH;  // 16-byte pieces of a row; rows of one turn
+    const int c = lane % CH;
+    const int by_tokens = STEP / g.group, by_heads = STEP - by_tokens * g.group;
     for (int n = 0; !dead; ++n) {
       if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
       const Item it = items[n & 1];
       __syncwarp();
       if (lane == 0) mbar_arrive(&item_free[n & 1]);
       if (it.end) break;
-      if (it.j0 >= (t ? it.e1 : it.e0)) continue;
-      if (!wait(&q_free[t], ph)) break;
-      ph ^= 1u;
-      const int row0 = it.row0 + t * BM, rows = min(it.rows - row0, BM);
-      const uint32_t base = smem_u32(smem) + (uint32_t)t * TILE;
-      for (int i = lane; i < rows * CH; i += 32) {
-        const int r = i / CH, c = i % CH, token = (row0 + r) / g.group, h = row0 + r - token * g.group;
-        const uint16_t* src = g.q + (int64_t)(it.q0 + token) * g.ldq + (int64_t)(it.head * g.group + h) * D + c * 8;
-        cp_async16(base + (uint32_t)(c / 8) * HALF + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4), src, 16);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (dead || it.j0 >= (t ? it.e1 : it.e0)) continue;
+        if (!wait(&q_free[t], ph[t])) continue;
+        ph[t] ^= 1u;
+        const int row0 = it.row0 + t * BM, rows = min(it.rows - row0, BM);
+        const uint32_t base = smem_u32(smem) + (uint32_t)t * TILE + (uint32_t)(c / 8) * HALF;
+        int token = (row0 + lane / CH) / g.group, h = row0 + lane / CH - token * g.group;
+        const uint16_t* q = g.q + (int64_t)it.q0 * g.ldq + (int64_t)it.head * g.group * D + c * 8;
+        for (int r = lane / CH; r < rows; r += STEP) {
+          cp_async16(base + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4), q + token * g.ldq + h * D, 16);
+          token += by_tokens;
+          h += by_heads;
+          if (h >= g.group) {
+            h -= g.group;
+            ++token;
+          }
+        }
+        cp_async_wait_all();
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full[t]);
       }
-      cp_async_wait_all();
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&q_full[t]);
     }
   }
   } else {
@@ -654,14 +677,17 @@ __global__ void __launch_bounds__(THREADS, 1)
               w[k] = pack<F16>(p0, p1);
             }
             tmem_st_32x32b_x32(s_at + i * 32, w);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[2 * t + i]);
           }
           const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
           l += both.x + both.y;
-          tmem_st_wait();
-          tc_fence_before();
+        } else if (lane == 0) {
+          mbar_arrive(&p_full[2 * t]);
+          mbar_arrive(&p_full[2 * t + 1]);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[t]);
       }
       if (dead) break;
       const bool any = it.j0 < end;
