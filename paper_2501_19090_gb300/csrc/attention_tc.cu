@@ -326,7 +326,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* item_full = q_free + 2;
   uint64_t* item_free = item_full + 2;
   uint64_t* v_clean = item_free + 2;  // of a slot: rows of V past the last key are zero
-  uint64_t* drain = v_clean + SLOTS;
+  uint64_t* turn = v_clean + SLOTS;   // the tiles' MMAs alternate
+  uint64_t* drain = turn + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 2);
   Item* items = reinterpret_cast<Item*>(tmem_slot + 2);
 
@@ -342,6 +343,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&s_full[t], 1);
       mbar_init(&p_full[2 * t], 4);
       mbar_init(&p_full[2 * t + 1], 4);
+      mbar_init(&turn[t], 1);
       mbar_init(&drain[t], 1);
       mbar_init(&o_full[t], 1);
       mbar_init(&q_full[t], 1);
@@ -461,11 +463,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t kind = F16 ? idesc_f16_f32(BM, BN) : idesc_bf16_f32(BM, BN);
     const uint32_t qk_desc = kind | (g.negate ? 1u << 13 : 0u);
     const uint32_t pv_desc = (F16 ? idesc_f16_f32(BM, D) : idesc_bf16_f32(BM, D)) | (1u << 16);
-    const uint64_t q_desc = sw128_desc(smem_u32(smem) + (uint32_t)t * TILE);
-    const uint64_t k_desc = sw128_desc(smem_u32(ring)), v_desc = sw128_mn_desc(smem_u32(ring));
+    // descriptors: the low word holds the address, which alone changes
+    const uint32_t q_desc = (uint32_t)sw128_desc(smem_u32(smem) + (uint32_t)t * TILE);
+    const uint32_t k_desc = (uint32_t)sw128_desc(smem_u32(ring)), v_desc = (uint32_t)sw128_mn_desc(smem_u32(ring));
+    constexpr uint32_t hi = (1024 >> 4) | (1u << 14) | (2u << 29);
     const uint32_t s_at = tmem + t * BN, o_at = tmem + 2 * BN + t * D;
     int s = 0;
-    uint32_t ph = 0, q_ph = 0, p_ph = 0, tail_ph = 0;
+    uint32_t ph = 0, q_ph = 0, p_ph = 0, tail_ph = 0, turn_ph = t ? 0u : 1u;  // tile 0 begins
     auto advance = [&] {
       if (++s == SLOTS) {
         s = 0;
@@ -473,12 +477,13 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     };
     // S = Q K^T; then K's slot is given back, and Q after the item's last S
-    auto score = [&](int slot, bool last) {
+    auto score = [&](int slot, bool last, bool pass) {
       if (elect_one()) {
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
+          if (kk == D / 32 && pass) mbar_arrive(&turn[1 - t]);
           const uint32_t at = (uint32_t)(kk / 4) * (HALF / 16) + (uint32_t)(kk % 4) * 2;
-          mma_bf16_ss(s_at, q_desc + at, k_desc + slot * (TILE / 16) + at, qk_desc, kk > 0);
+          mma_ss_words(s_at, q_desc + at, k_desc + slot * (TILE / 16) + at, hi, qk_desc, kk > 0);
         }
         mma_commit(&s_full[t]);
         mma_commit(&empty[slot]);
@@ -501,7 +506,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!wait(&q_full[t], q_ph)) break;
         q_ph ^= 1u;
         tc_fence_after();
-        score(s, j0 + 1 >= e);
+        score(s, j0 + 1 >= e, false);
       } else {
         skip(s);
       }
@@ -534,12 +539,13 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (!wait(&p_full[2 * t + h], p_ph)) break;
+            if (h == 0 && !wait(&turn[t], turn_ph)) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
               for (int kk = 0; kk < BN / 32; ++kk) {
                 const int k = h * (BN / 32) + kk;
-                mma_bf16_ts(o_at, s_at + k * 8, v_desc + vs * (TILE / 16) + k * 128, pv_desc, j > j0 || k > 0);
+                mma_ts_words(o_at, s_at + k * 8, v_desc + vs * (TILE / 16) + k * 128, hi, pv_desc, j > j0 || k > 0);
               }
               if (h == 1) {
                 if (j + 1 >= e) mma_commit(&o_full[t]);
@@ -550,11 +556,15 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (dead) break;
           p_ph ^= 1u;
         } else {
+          if (!wait(&turn[t], turn_ph)) break;
           skip(vs);
         }
-        if (j + 1 < j1) {
-          if (j + 1 < e) score(ks, j + 2 >= e);
-          else skip(ks);
+        turn_ph ^= 1u;
+        if (j + 1 < e) {
+          score(ks, j + 2 >= e, true);
+        } else {
+          if (lane == 0) mbar_arrive(&turn[1 - t]);
+          if (j + 1 < j1) skip(ks);
         }
       }
     }
@@ -626,48 +636,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!idle) {
           tc_fence_after();
           uint32_t v[4][32];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
-          tmem_ld_wait();
-          const int lim = seen - j * BN;  // keys of this tile that the row sees
-          if (__any_sync(0xffffffffu, lim < BN)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
-          }
-          float mx[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            mx[i] = __uint_as_float(v[i][0]);
-#pragma unroll
-            for (int k = 1; k < 32; ++k) mx[i] = fmaxf(mx[i], __uint_as_float(v[i][k]));
-          }
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-          // S(j) is in: so is PV(j - 1), issued before it, and O may be touched
-          const bool grows = (top - m) * c > 8.0f && m > -INFINITY;
-          if (__any_sync(0xffffffffu, grows)) {
-            const float up = m > -INFINITY ? fmaxf(m, top) : m;
-            const float f = up > m ? fast_exp2((m - up) * c) : 1.0f;
-            m = up;
-            l *= f;
-#pragma unroll 1
-            for (int i = 0; i < D / 16; ++i) {  // a few registers at a time: the row of S is held meanwhile
-              uint32_t o[16];
-              tmem_ld_32x32b_x16(o_at + i * 16, o);
-              tmem_ld_wait();
-#pragma unroll
-              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-              tmem_st_32x32b_x16(o_at + i * 16, o);
-            }
-          }
-          if (m == -INFINITY) m = top;
-          const float mc = m > -INFINITY ? m * c : 0.0f;
-          const uint64_t c2 = f32x2(c, c), mc2 = f32x2(-mc, -mc);
-          uint64_t sum[2] = {0, 0};
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            uint32_t w[32];
+          // The weights of the first 64 keys with the maximum as it was, beside the search for the new one; they
+          // are computed again, from S, if that has grown too far, as it does for the first keys and seldom later.
+          uint64_t sum[2];
+          uint32_t w[32];
+          const uint64_t c2 = f32x2(c, c);
+          auto weights = [&](int i) {  // keys 64 i to 64 i + 63
+            const float mc = m > -INFINITY ? -m * c : 0.0f;
+            const uint64_t mc2 = f32x2(mc, mc);
 #pragma unroll
             for (int k = 0; k < 32; ++k) {
               const float2 x = f32x2_parts(fma_f32x2(
@@ -676,12 +652,56 @@ __global__ void __launch_bounds__(THREADS, 1)
               sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
               w[k] = pack<F16>(p0, p1);
             }
+          };
+          auto hand_over = [&](int i) {
             tmem_st_32x32b_x32(s_at + i * 32, w);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&p_full[2 * t + i]);
+          };
+#pragma unroll 1
+          while (true) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
+            tmem_ld_wait();
+            const int lim = seen - j * BN;  // keys of this tile that the row sees
+            if (__any_sync(0xffffffffu, lim < BN)) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
+            }
+            float mx[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              mx[i] = __uint_as_float(v[i][0]);
+#pragma unroll
+              for (int k = 1; k < 32; ++k) mx[i] = fmaxf(mx[i], __uint_as_float(v[i][k]));
+            }
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            sum[0] = sum[1] = 0;
+            weights(0);
+            if (!__any_sync(0xffffffffu, (top - m) * c > 8.0f)) break;
+            const float up = fmaxf(m, top);
+            const float f = m > -INFINITY ? fast_exp2((m - up) * c) : 1.0f;  // (nothing was seen before: zeros)
+            m = up;
+            l *= f;
+            if (j > it.j0) {  // S(j) is in: so is PV(j - 1), issued before it, and O may be touched
+#pragma unroll 1
+              for (int i = 0; i < D / 16; ++i) {
+                uint32_t o[16];
+                tmem_ld_32x32b_x16(o_at + i * 16, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                tmem_st_32x32b_x16(o_at + i * 16, o);
+              }
+            }
           }
+          hand_over(0);
+          weights(1);
+          hand_over(1);
           const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
           l += both.x + both.y;
         } else if (lane == 0) {
