@@ -44,8 +44,9 @@ constexpr int BM = 128;             // rows of a tile
 constexpr int ROWS = 2 * BM;        // rows of an item
 constexpr int BN = 128;             // keys of a tile
 constexpr int THREADS = 384;
-constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_THREADS = 256;
 constexpr int MAX_PARTS = 456;      // pieces (times heads) that may leave partial sums: three for each SM
+constexpr int EARLY = 3;            // of four times 32 keys: those whose weights are handed to the MMAs first
 constexpr uint32_t HALF = BN * 128;  // 128 rows of 64 columns: 16 KB
 
 template <int D>
@@ -56,16 +57,19 @@ struct Cfg {
   static constexpr int64_t PART_FLOATS = ROWS * D + 2 * ROWS;  // O, then (m, l) of each row
 };
 
-// One work item, as the plan lists it; each stands for `heads` items, one for each key / value head.
-struct Entry {
-  int b, row0;       // request, first row
-  int j0, j1;        // key tiles
-  int part, parts;   // which piece of how many
-  int slot, counter; // first partial-sum slot / counter (of head 0; times heads)
+// A work item: 16 words. The plan lists those of head 0 with everything that a CTA has to know; a CTA takes one
+// for a head by filling in the last four.
+struct Item {
+  int b, row0, rows;       // request, first row, rows of the request
+  int L, q0, ahead;        // as Lengths
+  int j0, j1, e0, e1;      // key tiles; the end of those that the rows of tile 0 and 1 see
+  int part, parts;         // which piece of how many
+  int slot, counter;       // place of its partial sums, first of its counters (in the list: places of head 0, over heads)
+  int head, end;           // end: no item
 };
 
 struct Plan {
-  int next;          // queue head: items beyond the grid's first ones taken so far
+  int next;          // items taken beyond the grid's first ones
   int entries;
   int pad[6];
 };
@@ -76,7 +80,7 @@ struct TcArgs {
   const int32_t *table, *q_start, *kv_len;
   Plan* plan;
   int* counters;
-  Entry* list;
+  Item* list;
   float* partial;
   int64_t ldq, ldo, ldt, pages;
   int T, heads, group, B, max_q, cols, page_size, page_shift;
@@ -85,13 +89,6 @@ struct TcArgs {
   int negate;                        // scale < 0
   int* status;
   uint64_t timeout_ns;
-};
-
-struct Item {
-  int b, head, row0, rows;           // rows: of the request
-  int L, q0, ahead;
-  int j0, j1, e0, e1;                // e: end of the key tiles that a tile's rows see
-  int part, parts, slot, counter, end;
 };
 
 struct Lengths {
@@ -116,51 +113,47 @@ __device__ __forceinline__ int tile_end(const Lengths& x, int group, int row) {
   const int last = (min(row + BM, rows) - 1) / group;  // token
   return (max(x.ahead + last, 0) + BN - 1) / BN;
 }
-__device__ __forceinline__ int item_end(const Lengths& x, int group, int row0) {
-  return max(tile_end(x, group, row0), tile_end(x, group, row0 + BM));
-}
 
 // ---- plan ---------------------------------------------------------------------------------------
-__device__ __forceinline__ int block_sum_scan(int v, int* part, int& total) {  // exclusive sum, and the total
+// Exclusive sum over the block's threads, and the total; `part` holds a value for each warp.
+__device__ __forceinline__ unsigned long long block_scan(unsigned long long v, unsigned long long* part,
+                                                         unsigned long long& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int a = v;
+  unsigned long long a = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, a, o);
+    const unsigned long long x = __shfl_up_sync(0xffffffffu, a, o);
     if (lane >= o) a += x;
   }
   __syncthreads();  // part is free
   if (lane == 31) part[warp] = a;
   __syncthreads();
-  if (warp == 0) {
-    int p = part[lane];
+  unsigned long long before = 0;
+  total = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, p, o);
-      if (lane >= o) p += x;
-    }
-    part[lane] = p;
+  for (int w = 0; w < PLAN_THREADS / 32; ++w) {
+    before += w < warp ? part[w] : 0;
+    total += part[w];
   }
-  __syncthreads();
-  total = part[31];
-  return a - v + (warp ? part[warp - 1] : 0);
+  return a - v + before;
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g, int grid) {
-  extern __shared__ int first[];  // B + 1: first row tile of each request
-  __shared__ int part[32];
+  extern __shared__ __align__(16) uint8_t plan_smem[];
+  Lengths* len = reinterpret_cast<Lengths*>(plan_smem);          // B
+  int* first = reinterpret_cast<int*>(plan_smem + (size_t)g.B * sizeof(Lengths));  // B + 1: first row tile of each request
+  __shared__ unsigned long long part[PLAN_THREADS / 32];
   __shared__ int red[4];          // largest and smallest item; of those that may be cut, the largest and the sum
   __shared__ unsigned long long sum_all;  // of all items
   __shared__ int cut;             // key tiles of a piece
   pdl_launch_dependents();
-  pdl_wait_primary();
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
   if (tid == 0) {
     red[0] = red[2] = red[3] = 0;
     red[1] = 0x7fffffff;
     sum_all = 0;
   }
-  for (int i = tid; i < MAX_PARTS / 2 * 8; i += PLAN_THREADS) g.counters[i] = 0;
+  pdl_wait_primary();
   bool over = false;
   int items = 0;
   for (int b0 = 0; b0 < g.B; b0 += PLAN_THREADS) {
@@ -168,52 +161,61 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     int n = 0;
     if (b < g.B) {
       const Lengths x = lengths_of(g, b);
+      len[b] = x;
       over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
       n = (x.n * g.group + ROWS - 1) / ROWS;
     }
-    int total;
-    const int at = block_sum_scan(n, part, total);
+    unsigned long long total;
+    const int at = (int)block_scan(n, part, total);
     if (b < g.B) first[b] = items + at;
-    items += total;
+    items += (int)total;
   }
   if (tid == 0) first[g.B] = items;
   if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
+  for (int i = tid; i < MAX_PARTS / 2 * 8; i += PLAN_THREADS) g.counters[i] = 0;
   __syncthreads();
 
-  // the item at place k of the list: later rows of a request first
-  auto item_at = [&](int k, Lengths& x, int& b, int& row0) {
+  // the item at place k of the list, later rows of a request first, and its cost in key tiles
+  auto item_at = [&](int k, Item& x) {
     int lo = 0, hi = g.B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (first[mid] <= k) lo = mid;
       else hi = mid;
     }
-    b = lo;
-    x = lengths_of(g, b);
-    row0 = (first[b + 1] - 1 - k) * ROWS;
-    return item_end(x, g.group, row0);
+    const Lengths v = len[lo];
+    x.b = lo;
+    x.row0 = (first[lo + 1] - 1 - k) * ROWS;
+    x.rows = v.n * g.group;
+    x.L = v.L;
+    x.q0 = v.q0;
+    x.ahead = v.ahead;
+    x.e0 = tile_end(v, g.group, x.row0);
+    x.e1 = tile_end(v, g.group, x.row0 + BM);
+    return max(x.e0, x.e1);
   };
   // Whole rounds of the grid stay whole; the items of the last, unfilled round may be cut.
   const int whole = (int)((int64_t)items * g.heads / grid * grid / g.heads);
-  int most = 0, least = 0x7fffffff, most_cut = 0, sum_cut = 0;
-  unsigned long long sum = 0;
-  for (int k = tid; k < items; k += PLAN_THREADS) {
-    Lengths x;
-    int b, row0;
-    const int cost = item_at(k, x, b, row0);
-    most = max(most, cost);
-    least = min(least, cost);
-    if (k >= whole) {
-      most_cut = max(most_cut, cost);
-      sum_cut += cost;
+  Item x;
+  int cost = 0;
+  for (int k0 = 0; k0 < items; k0 += PLAN_THREADS) {
+    const int k = k0 + tid;
+    const bool here = k < items;
+    if (!__any_sync(0xffffffffu, here)) break;
+    if (here) cost = item_at(k, x);
+    const int most = __reduce_max_sync(0xffffffffu, here ? cost : 0);
+    const int least = __reduce_min_sync(0xffffffffu, here ? cost : 0x7fffffff);
+    const int most_cut = __reduce_max_sync(0xffffffffu, here && k >= whole ? cost : 0);
+    const int sum_cut = __reduce_add_sync(0xffffffffu, here && k >= whole ? cost : 0);
+    const int sum = __reduce_add_sync(0xffffffffu, here ? cost : 0);
+    if (lane == 0) {
+      atomicMax(&red[0], most);
+      atomicMin(&red[1], least);
+      atomicMax(&red[2], most_cut);
+      atomicAdd(&red[3], sum_cut);
+      atomicAdd(&sum_all, (unsigned long long)sum);
     }
-    sum += cost;
   }
-  atomicAdd(&sum_all, sum);
-  atomicMax(&red[0], most);
-  atomicMin(&red[1], least);
-  atomicMax(&red[2], most_cut);
-  atomicAdd(&red[3], sum_cut);
   __syncthreads();
   if (tid < 32) {
     // The time of all, in key tiles, if those items are cut into pieces of `size`: an even share for each CTA,
@@ -243,38 +245,38 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   }
   __syncthreads();
   const int size = cut;
-  int entries = 0, slots = 0, counters = 0;
+  unsigned long long done = 0;  // entries, from bit 32 on; partial-sum places, from bit 16 on; counters
   for (int k0 = 0; k0 < items; k0 += PLAN_THREADS) {
     const int k = k0 + tid;
-    Lengths x;
-    int b = 0, row0 = 0, cost = 0, pieces = 0;
+    int pieces = 0;
     if (k < items) {
-      cost = item_at(k, x, b, row0);
+      if (items > PLAN_THREADS) cost = item_at(k, x);
       pieces = k < whole ? 1 : max((cost + size - 1) / size, 1);
     }
-    int total, s_total, c_total;
-    const int at = entries + block_sum_scan(pieces, part, total);
-    const int slot = slots + block_sum_scan(pieces > 1 ? pieces : 0, part, s_total);
-    const int counter = counters + block_sum_scan(pieces > 1 ? 1 : 0, part, c_total);
+    unsigned long long total;
+    const unsigned long long at = done + block_scan(((unsigned long long)pieces << 32) |
+                                                        (pieces > 1 ? ((unsigned)pieces << 16) | 1u : 0u), part, total);
     for (int p = 0; p < pieces; ++p) {  // even pieces
-      Entry e;
-      e.b = b;
-      e.row0 = row0;
+      Item e = x;
       e.j0 = (int)((int64_t)cost * p / pieces);
       e.j1 = (int)((int64_t)cost * (p + 1) / pieces);
+      e.e0 = min(x.e0, e.j1);
+      e.e1 = min(x.e1, e.j1);
       e.part = p;
       e.parts = pieces;
-      e.slot = slot;
-      e.counter = counter;
-      g.list[at + p] = e;
+      e.slot = (int)(at >> 16 & 0xffffu) + p;
+      e.counter = (int)(at & 0xffffu);
+      e.head = e.end = 0;
+      int4* to = reinterpret_cast<int4*>(g.list + (at >> 32) + p);
+      const int4* from = reinterpret_cast<const int4*>(&e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[i] = from[i];
     }
-    entries += total;
-    slots += s_total;
-    counters += c_total;
+    done += total;
   }
   if (tid == 0) {
     g.plan->next = 0;
-    g.plan->entries = entries;
+    g.plan->entries = (int)(done >> 32);
   }
 }
 
@@ -380,54 +382,57 @@ __global__ void __launch_bounds__(THREADS, 1)
   regs_lower<88>();
   if (warp == 8) {
     // ---------------- queue, K and V ----------------
-    const int total = g.plan->entries * g.heads;
     int s = 0, fills = 0;
     uint32_t ph = 1;
     const int per_tile = g.page_size >= BN ? 1 : BN / g.page_size;
     const int box_rows = min(g.page_size, BN);
     const int mine = lane / (D / 64), half = lane % (D / 64);
-    for (int n = 0; !dead; ++n) {
-      if (!wait(&item_free[n & 1], (((uint32_t)n >> 1) & 1u) ^ 1u)) break;
-      int k = (int)blockIdx.x;
-      if (n > 0) {
-        if (lane == 0) k = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
-        k = __shfl_sync(0xffffffffu, k, 0);
-      }
-      Item it = {};
-      it.end = k >= total;
-      if (!it.end) {
-        const Entry e = g.list[k / g.heads];
-        const Lengths x = lengths_of(g, e.b);
-        it.b = e.b;
-        it.head = k % g.heads;
-        it.row0 = e.row0;
-        it.rows = x.n * g.group;
-        it.ahead = x.ahead;
-        it.L = x.L;
-        it.q0 = x.q0;
-        it.j0 = e.j0;
-        it.j1 = e.j1;
-        it.e0 = min(e.j1, tile_end(x, g.group, e.row0));
-        it.e1 = min(e.j1, tile_end(x, g.group, e.row0 + BM));
-        it.part = e.part;
-        it.parts = e.parts;
-        it.slot = (e.slot + e.part) * g.heads + it.head;
-        it.counter = (e.counter * g.heads + it.head) * 8;
-      }
-      if (lane == 0) {
-        items[n & 1] = it;
-        mbar_arrive(&item_full[n & 1]);
-      }
-      if (it.end) break;
-      const int n_pages = (it.L + g.page_size - 1) >> g.page_shift;
-      const int32_t* row = g.table + it.b * g.ldt;
+    // An entry's words, a lane each. The list has room for MAX_PARTS entries and more, so that the first can be read
+    // before it is known to be one.
+    auto fetch = [&](int k) { return lane < 16 ? __ldcg(reinterpret_cast<const int*>(g.list + k / g.heads) + lane) : 0; };
+    int k = (int)blockIdx.x, word = fetch(k);
+    const int total = __ldcg(&g.plan->entries) * g.heads;
+    // Item n for all: false after the last, or if the wait for its place ran out.
+    auto publish = [&](int n) {
+      if (!wait(&item_free[n & 1], (((uint32_t)n >> 1) & 1u) ^ 1u)) return false;
+      const int head = k % g.heads;
+      if (lane == 12) word = word * g.heads + head;
+      if (lane == 13) word = (word * g.heads + head) * 8;
+      if (lane == 14) word = head;
+      if (lane == 15) word = k >= total;
+      if (lane < 16) reinterpret_cast<int*>(&items[n & 1])[lane] = word;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_full[n & 1]);
+      return k < total;
+    };
+    int id = 0;
+    bool more = publish(0);
+    for (int n = 0; more; ++n) {
+      const int b = __shfl_sync(0xffffffffu, word, 0), L = __shfl_sync(0xffffffffu, word, 3);
+      const int j0 = __shfl_sync(0xffffffffu, word, 6), j1 = __shfl_sync(0xffffffffu, word, 7), head = k % g.heads;
+      const int n_pages = (L + g.page_size - 1) >> g.page_shift;
+      const int32_t* row = g.table + b * g.ldt;
       auto page_of = [&](int j) {
         const int p = ((j * BN) >> g.page_shift) + mine;
-        return mine < per_tile && j < it.j1 && p < n_pages ? row[p] : -2;  // -2: no page
+        return mine < per_tile && j < j1 && p < n_pages ? row[p] : -2;  // -2: no page
       };
-      int id = page_of(it.j0);
-      for (int j = it.j0; j < it.j1 && !dead; ++j) {
+      id = page_of(j0);
+      // The next item is taken towards the end of this one, each step a tile ahead of what needs it: late, so
+      // that the CTA that is done first takes it, and in time for its loads to follow on.
+      int step = 0, taken = 0;
+      for (int j = j0; j < j1 && !dead; ++j) {
         const int next = page_of(j + 1);
+        if (j >= j1 - 4 && step < 3) {
+          if (step == 0) {
+            if (lane == 0) taken = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
+          } else if (step == 1) {
+            k = __shfl_sync(0xffffffffu, taken, 0);
+            word = k < total ? fetch(k) : 0;
+          } else {
+            more = publish(n + 1);
+          }
+          ++step;
+        }
         const bool has = id != -2 || (mine < per_tile && ((j * BN) >> g.page_shift) + mine < n_pages);
         if (has && (id < 0 || id >= g.pages)) {
           latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
@@ -436,9 +441,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, has)) * (uint32_t)box_rows * 128u;
         const int token = (j * BN) & (g.page_size - 1);
         const uint32_t at = (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u;
-        const int y = g.token_at == 0 ? token : g.head_at == 0 ? it.head : id;
-        const int z = g.token_at == 1 ? token : g.head_at == 1 ? it.head : id;
-        const int w = g.token_at == 2 ? token : g.head_at == 2 ? it.head : id;
+        const int y = g.token_at == 0 ? token : g.head_at == 0 ? head : id;
+        const int z = g.token_at == 1 ? token : g.head_at == 1 ? head : id;
+        const int w = g.token_at == 2 ? token : g.head_at == 2 ? head : id;
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           if (!wait(&empty[s], ph)) break;
@@ -453,6 +458,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         id = next;
       }
+      if (dead) break;
+      if (step == 0 && lane == 0) taken = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
+      if (step <= 1) {
+        k = __shfl_sync(0xffffffffu, taken, 0);
+        word = k < total ? fetch(k) : 0;
+      }
+      if (step <= 2) more = publish(n + 1);
+      if (dead) break;
     }
     // nothing may land in shared memory after the CTA has left
     for (int i = fills > SLOTS ? fills - SLOTS : 0; i < fills; ++i)
@@ -543,8 +556,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-              for (int kk = 0; kk < BN / 32; ++kk) {
-                const int k = h * (BN / 32) + kk;
+              for (int k = h ? 2 * EARLY : 0; k < (h ? BN / 16 : 2 * EARLY); ++k) {
                 mma_ts_words(o_at, s_at + k * 8, v_desc + vs * (TILE / 16) + k * 128, hi, pv_desc, j > j0 || k > 0);
               }
               if (h == 1) {
@@ -639,22 +651,20 @@ __global__ void __launch_bounds__(THREADS, 1)
           // The weights of the first 64 keys with the maximum as it was, beside the search for the new one; they
           // are computed again, from S, if that has grown too far, as it does for the first keys and seldom later.
           uint64_t sum[2];
-          uint32_t w[32];
+          uint32_t w[4][16];
           const uint64_t c2 = f32x2(c, c);
-          auto weights = [&](int i) {  // keys 64 i to 64 i + 63
+          auto weights = [&](int i) {  // keys 32 i to 32 i + 31
             const float mc = m > -INFINITY ? -m * c : 0.0f;
             const uint64_t mc2 = f32x2(mc, mc);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const float2 x = f32x2_parts(fma_f32x2(
-                  f32x2(__uint_as_float(v[2 * i + k / 16][2 * k % 32]), __uint_as_float(v[2 * i + k / 16][2 * k % 32 + 1])), c2, mc2));
+            for (int k = 0; k < 16; ++k) {
+              const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), c2, mc2));
               const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
               sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
-              w[k] = pack<F16>(p0, p1);
+              w[i][k] = pack<F16>(p0, p1);
             }
           };
           auto hand_over = [&](int i) {
-            tmem_st_32x32b_x32(s_at + i * 32, w);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -675,13 +685,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             float mx[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              mx[i] = __uint_as_float(v[i][0]);
+              mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
 #pragma unroll
-              for (int k = 1; k < 32; ++k) mx[i] = fmaxf(mx[i], __uint_as_float(v[i][k]));
+              for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
             }
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
             sum[0] = sum[1] = 0;
-            weights(0);
+#pragma unroll
+            for (int i = 0; i < EARLY; ++i) weights(i);
             if (!__any_sync(0xffffffffu, (top - m) * c > 8.0f)) break;
             const float up = fmaxf(m, top);
             const float f = m > -INFINITY ? fast_exp2((m - up) * c) : 1.0f;  // (nothing was seen before: zeros)
@@ -699,8 +710,14 @@ __global__ void __launch_bounds__(THREADS, 1)
               }
             }
           }
+#pragma unroll
+          for (int i = 0; i < EARLY; ++i) tmem_st_32x32b_x16(s_at + i * 16, w[i]);
           hand_over(0);
-          weights(1);
+#pragma unroll
+          for (int i = EARLY; i < 4; ++i) {
+            weights(i);
+            tmem_st_32x32b_x16(s_at + i * 16, w[i]);
+          }
           hand_over(1);
           const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
           l += both.x + both.y;
@@ -744,17 +761,17 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int w8 = t * 4 + quarter;
         auto slot_of = [&](int p) { return g.partial + (int64_t)(it.slot + (p - it.part) * g.heads) * C::PART_FLOATS; };
         float* mine = slot_of(it.part);
-        if (any) {
 #pragma unroll
-          for (int i = 0; i < D / 32; ++i) {
-            uint32_t o[32];
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32] = {};
+          if (any) {
             tmem_ld_32x32b_x32(o_at + i * 32, o);
             tmem_ld_wait();
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              __stcg(reinterpret_cast<uint4*>(mine) + (w8 * (D / 4) + i * 8 + k) * 32 + lane,
-                     make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
           }
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            __stcg(reinterpret_cast<uint4*>(mine) + (w8 * (D / 4) + i * 8 + k) * 32 + lane,
+                   make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
         }
         __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, make_float2(m * c, l));
         __threadfence();
@@ -764,33 +781,37 @@ __global__ void __launch_bounds__(THREADS, 1)
         before = __shfl_sync(0xffffffffu, before, 0);
         if (before == it.parts - 1) {  // the last piece of these 32 rows: add up all in their order
           __threadfence();
-          float top = -INFINITY;
+          const float* from = slot_of(0);
+          const int64_t pitch = (int64_t)g.heads * C::PART_FLOATS;
+          auto ml_of = [&](int p) { return __ldcg(reinterpret_cast<const float2*>(from + p * pitch + ROWS * D) + w8 * 32 + lane); };
+          float top = -INFINITY, all = 0.0f;
+#pragma unroll 8
           for (int p = 0; p < it.parts; ++p) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(p) + ROWS * D) + w8 * 32 + lane);
-            if (ml.y != 0.0f) top = fmaxf(top, ml.x);
+            const float2 ml = ml_of(p);
+            top = fmaxf(top, ml.y != 0.0f ? ml.x : -INFINITY);
           }
           if (top == -INFINITY) top = 0.0f;
-          float all = 0.0f;
+          auto weight = [&](const float2& ml) { return ml.y != 0.0f ? fast_exp2(ml.x - top) : 0.0f; };  // nothing seen: O is zero
+#pragma unroll 8
           for (int p = 0; p < it.parts; ++p) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(slot_of(p) + ROWS * D) + w8 * 32 + lane);
-            if (ml.y != 0.0f) all += ml.y * fast_exp2(ml.x - top);
+            const float2 ml = ml_of(p);
+            all += ml.y * weight(ml);
           }
           const float inv = all == 0.0f ? 0.0f : 1.0f / all;
 #pragma unroll 1
           for (int i = 0; i < D / 32; ++i) {
             float x[32] = {};
+#pragma unroll 3
             for (int p = 0; p < it.parts; ++p) {
-              const float* from = slot_of(p);
-              const float2 ml = __ldcg(reinterpret_cast<const float2*>(from + ROWS * D) + w8 * 32 + lane);
-              if (ml.y == 0.0f) continue;  // nothing seen: the columns may not even be written
-              const float f = fast_exp2(ml.x - top) * inv;
+              const float f = weight(ml_of(p)) * inv;
+              const float4* o = reinterpret_cast<const float4*>(from + p * pitch) + (w8 * (D / 4) + i * 8) * 32 + lane;
 #pragma unroll
               for (int k = 0; k < 8; ++k) {
-                const float4 o = __ldcg(reinterpret_cast<const float4*>(from) + (w8 * (D / 4) + i * 8 + k) * 32 + lane);
-                x[4 * k] += f * o.x;
-                x[4 * k + 1] += f * o.y;
-                x[4 * k + 2] += f * o.z;
-                x[4 * k + 3] += f * o.w;
+                const float4 y = __ldcg(o + k * 32);
+                x[4 * k] += f * y.x;
+                x[4 * k + 1] += f * y.y;
+                x[4 * k + 2] += f * y.z;
+                x[4 * k + 3] += f * y.w;
               }
             }
             if (row < it.rows) store(i, x);
@@ -813,7 +834,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 
 int64_t list_bytes(int64_t T, int64_t group, int64_t B) {
-  return round256(((T * group + ROWS - 1) / ROWS + B + MAX_PARTS) * (int64_t)sizeof(Entry));
+  return round256(((T * group + ROWS - 1) / ROWS + B + MAX_PARTS) * (int64_t)sizeof(Item));
 }
 constexpr int64_t kCounterBytes = MAX_PARTS / 2 * 8 * 4 + 256;  // the plan's head, then the counters
 
@@ -835,7 +856,7 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   g.kv_len = a.kv_len;
   g.plan = reinterpret_cast<Plan*>(ws);
   g.counters = reinterpret_cast<int*>(ws + 256);
-  g.list = reinterpret_cast<Entry*>(ws + round256(kCounterBytes));
+  g.list = reinterpret_cast<Item*>(ws + round256(kCounterBytes));
   g.partial = reinterpret_cast<float*>(ws + round256(kCounterBytes) + list_bytes(a.T, group, a.B));
   g.ldq = a.ldq;
   g.ldo = a.ldo;
@@ -866,14 +887,16 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(1);
   cfg.blockDim = dim3(PLAN_THREADS);
-  cfg.dynamicSmemBytes = (size_t)(a.B + 1) * 4;
+  cfg.dynamicSmemBytes = (size_t)a.B * sizeof(Lengths) + (size_t)(a.B + 1) * 4;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cudaError_t e = pifa_launch_ex(&cfg, attention_plan, g, grid);
+  cudaError_t e = cudaFuncSetAttribute(attention_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(4096 * sizeof(Lengths) + 4097 * 4));
+  if (e != cudaSuccess) return pifa_fail_cuda("cudaFuncSetAttribute(attention_plan)", e);
+  e = pifa_launch_ex(&cfg, attention_plan, g, grid);
   if (e != cudaSuccess) return pifa_fail_cuda("attention_plan launch", e);
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);

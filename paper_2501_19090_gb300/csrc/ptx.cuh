@@ -248,6 +248,13 @@ __device__ __forceinline__ void regs_raise() { asm volatile("setmaxnreg.inc.sync
 template <int N>
 __device__ __forceinline__ void regs_lower() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// The largest of three; a NaN gives way to a number.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // Two fp32 operations at once, each rounded to nearest: a b + c, a + b.
 __device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
   uint64_t r;
