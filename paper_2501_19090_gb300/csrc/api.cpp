@@ -106,6 +106,26 @@ int make_tmap_2d(CUtensorMap* map, int dtype, const void* base, int64_t rows, in
   return PIFA_OK;
 }
 
+int make_tmap_heads(CUtensorMap* map, int dtype, const void* base, int64_t T, int64_t heads, int64_t dim, int64_t ld,
+                    uint32_t box_heads, uint32_t box_rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return pifa_fail(PIFA_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  if (ld * 2 >= ((int64_t)1 << 40)) return pifa_fail(PIFA_ERR_UNSUPPORTED, "a leading dimension of 2^40 bytes or more");
+  cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)T};
+  cuuint64_t strides[2] = {(cuuint64_t)(dim * 2), (cuuint64_t)(ld * 2)};
+  cuuint32_t box[3] = {64, box_heads, box_rows}, estr[3] = {1, 1, 1};
+  const CUtensorMapDataType dt =
+      dtype == PIFA_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  CUresult r = fn(map, dt, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    char buf[120];
+    std::snprintf(buf, sizeof buf, "cuTensorMapEncodeTiled failed (CUresult %d) for rows of heads", (int)r);
+    return pifa_fail(PIFA_ERR_CUDA, buf);
+  }
+  return PIFA_OK;
+}
+
 int make_tmap_cache(CUtensorMap* map, int dtype, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) return pifa_fail(PIFA_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");

@@ -3,8 +3,8 @@
 //   o = sum_j softmax_j(scale q . k_j) v_j over the keys j < L - n + i + 1 of new token i (L keys, n new tokens).
 //
 // Rows: the query heads of a key / value head share its keys, so the n new tokens of a request and the G heads
-// of a group make n G rows, token-major. A work item is 256 of them (two tiles of 128) of one request and one
-// key / value head; it walks the keys in tiles of 128 and reads K and V once for both tiles.
+// of a group make n G rows, token-major. A tile is the rows of floor(128 / G) tokens, 128 of them at most, a work
+// item two tiles of one request and one key / value head; it walks the keys in tiles of 128 and reads K and V once for both tiles.
 // One pass with a running maximum: S = Q K^T (128 x 128, fp32, tensor memory); a thread owns a row, so maximum
 // and sum need no exchange; p = exp2(c s - c m) goes back to tensor memory as bf16 or fp16 over S's columns
 // and is the first operand of O += P V. m is only raised, and O and l rescaled, when the row's maximum
@@ -17,7 +17,7 @@
 //                    128-token part of one) and 64 columns a copy, a lane for each
 //   warps 9, 10      issue the MMAs of tile 0 and 1: PV, in two halves of the keys as P arrives, and the next S; one
 //                    tile's softmax runs under the other tile's MMAs. (One warp for both was the bound.)
-//   warp 11          loads the next item's rows of Q, as soon as the last S of a tile has been computed
+//   warp 11          loads the next item's rows of Q by TMA, as soon as the last S of a tile has been computed
 // P lies over S, and S of the next keys is written over both: the MMAs of one warp run in issue
 // order, PV(j) before S(j + 1), and S(j)'s values were read before P was announced.
 // Keys past L: their scores are masked, and their rows of V, which may hold anything, are set to zero in shared
@@ -41,12 +41,12 @@ namespace {
 using namespace pifa;
 
 constexpr int BM = 128;             // rows of a tile
-constexpr int ROWS = 2 * BM;        // rows of an item
+constexpr int ROWS = 2 * BM;        // rows of an item (with those that a group's size leaves unused)
 constexpr int BN = 128;             // keys of a tile
 constexpr int THREADS = 384;
 constexpr int PLAN_THREADS = 256;
 constexpr int MAX_PARTS = 456;      // pieces (times heads) that may leave partial sums: three for each SM
-constexpr int EARLY = 3;            // of four times 32 keys: those whose weights are handed to the MMAs first
+constexpr int EARLY = 2;            // of four times 32 keys: those whose weights are handed to the MMAs first
 constexpr uint32_t HALF = BN * 128;  // 128 rows of 64 columns: 16 KB
 
 template <int D>
@@ -60,7 +60,7 @@ struct Cfg {
 // A work item: 16 words. The plan lists those of head 0 with everything that a CTA has to know; a CTA takes one
 // for a head by filling in the last four.
 struct Item {
-  int b, row0, rows;       // request, first row, rows of the request
+  int b, tok0, n;          // request, first token, tokens of the request
   int L, q0, ahead;        // as Lengths
   int j0, j1, e0, e1;      // key tiles; the end of those that the rows of tile 0 and 1 see
   int part, parts;         // which piece of how many
@@ -75,15 +75,15 @@ struct Plan {
 };
 
 struct TcArgs {
-  const uint16_t* q;
   uint16_t* o;
   const int32_t *table, *q_start, *kv_len;
   Plan* plan;
   int* counters;
   Item* list;
   float* partial;
-  int64_t ldq, ldo, ldt, pages;
-  int T, heads, group, B, max_q, cols, page_size, page_shift;
+  int64_t ldo, ldt, pages;
+  int T, heads, group, tpt, B, max_q,   // tpt: tokens of a tile
+       cols, page_size, page_shift;
   int token_at, head_at, page_at;    // their places among the tensor maps' coordinates 1 to 3
   float c;                           // |scale| log2(e)
   int negate;                        // scale < 0
@@ -106,12 +106,10 @@ __device__ __forceinline__ Lengths lengths_of(const TcArgs& g, int b) {
   return x;
 }
 
-// Key tiles that rows [row, row + 128) of a request see: up to its last row's last key.
-__device__ __forceinline__ int tile_end(const Lengths& x, int group, int row) {
-  const int rows = x.n * group;
-  if (row >= rows) return 0;
-  const int last = (min(row + BM, rows) - 1) / group;  // token
-  return (max(x.ahead + last, 0) + BN - 1) / BN;
+// Key tiles that the tile of tokens from `tok` on sees: up to its last token's last key.
+__device__ __forceinline__ int tile_end(const Lengths& x, int tpt, int tok) {
+  if (tok >= x.n) return 0;
+  return (max(x.ahead + min(tok + tpt, x.n) - 1, 0) + BN - 1) / BN;
 }
 
 // ---- plan ---------------------------------------------------------------------------------------
@@ -141,7 +139,7 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
 __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g, int grid) {
   extern __shared__ __align__(16) uint8_t plan_smem[];
   Lengths* len = reinterpret_cast<Lengths*>(plan_smem);          // B
-  int* first = reinterpret_cast<int*>(plan_smem + (size_t)g.B * sizeof(Lengths));  // B + 1: first row tile of each request
+  int* first = reinterpret_cast<int*>(plan_smem + (size_t)g.B * sizeof(Lengths));  // B + 1: first item of each request
   __shared__ unsigned long long part[PLAN_THREADS / 32];
   __shared__ int red[4];          // largest and smallest item; of those that may be cut, the largest and the sum
   __shared__ unsigned long long sum_all;  // of all items
@@ -163,7 +161,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
       const Lengths x = lengths_of(g, b);
       len[b] = x;
       over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
-      n = (x.n * g.group + ROWS - 1) / ROWS;
+      n = (x.n + 2 * g.tpt - 1) / (2 * g.tpt);
     }
     unsigned long long total;
     const int at = (int)block_scan(n, part, total);
@@ -185,13 +183,13 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     }
     const Lengths v = len[lo];
     x.b = lo;
-    x.row0 = (first[lo + 1] - 1 - k) * ROWS;
-    x.rows = v.n * g.group;
+    x.tok0 = (first[lo + 1] - 1 - k) * 2 * g.tpt;
+    x.n = v.n;
     x.L = v.L;
     x.q0 = v.q0;
     x.ahead = v.ahead;
-    x.e0 = tile_end(v, g.group, x.row0);
-    x.e1 = tile_end(v, g.group, x.row0 + BM);
+    x.e0 = tile_end(v, g.tpt, x.tok0);
+    x.e1 = tile_end(v, g.tpt, x.tok0 + g.tpt);
     return max(x.e0, x.e1);
   };
   // Whole rounds of the grid stay whole; the items of the last, unfilled round may be cut.
@@ -311,7 +309,8 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 
 template <bool F16, int D>
 __global__ void __launch_bounds__(THREADS, 1)
-    attention_tc(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const TcArgs g) {
+    attention_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                 const __grid_constant__ CUtensorMap vmap, const TcArgs g) {
   using C = Cfg<D>;
   constexpr int SLOTS = C::SLOTS;
   constexpr uint32_t TILE = C::TILE;
@@ -354,6 +353,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&item_free[t], 11);
     }
     fence_mbar_init();
+    prefetch_tmap(&qmap);
     prefetch_tmap(&kmap);
     prefetch_tmap(&vmap);
   }
@@ -492,9 +492,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     // S = Q K^T; then K's slot is given back, and Q after the item's last S
     auto score = [&](int slot, bool last, bool pass) {
       if (elect_one()) {
+        if (pass) mbar_arrive(&turn[1 - t]);  // the other tile's PV may follow on: after S it came too late by a wait
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          if (kk == D / 32 && pass) mbar_arrive(&turn[1 - t]);
           const uint32_t at = (uint32_t)(kk / 4) * (HALF / 16) + (uint32_t)(kk % 4) * 2;
           mma_ss_words(s_at, q_desc + at, k_desc + slot * (TILE / 16) + at, hi, qk_desc, kk > 0);
         }
@@ -587,10 +587,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   } else {
     // ---------------- rows of Q ----------------
-    uint32_t ph[2] = {1, 1};
-    constexpr int CH = D / 8, STEP = 32 / CH;  // 16-byte pieces of a row; rows of one turn
-    const int c = lane % CH;
-    const int by_tokens = STEP / g.group, by_heads = STEP - by_tokens * g.group;
+    int loads[2] = {0, 0};
     for (int n = 0; !dead; ++n) {
       if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
       const Item it = items[n & 1];
@@ -600,27 +597,19 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if (dead || it.j0 >= (t ? it.e1 : it.e0)) continue;
-        if (!wait(&q_free[t], ph[t])) continue;
-        ph[t] ^= 1u;
-        const int row0 = it.row0 + t * BM, rows = min(it.rows - row0, BM);
-        const uint32_t base = smem_u32(smem) + (uint32_t)t * TILE + (uint32_t)(c / 8) * HALF;
-        int token = (row0 + lane / CH) / g.group, h = row0 + lane / CH - token * g.group;
-        const uint16_t* q = g.q + (int64_t)it.q0 * g.ldq + (int64_t)it.head * g.group * D + c * 8;
-        for (int r = lane / CH; r < rows; r += STEP) {
-          cp_async16(base + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4), q + token * g.ldq + h * D, 16);
-          token += by_tokens;
-          h += by_heads;
-          if (h >= g.group) {
-            h -= g.group;
-            ++token;
-          }
+        if (!wait(&q_free[t], (uint32_t)(loads[t] & 1) ^ 1u)) continue;
+        ++loads[t];
+        if (lane == 0) {  // tokens of the next request or past T may come along: rows that nobody stores
+          mbar_arrive_expect_tx(&q_full[t], (uint32_t)(g.group * g.tpt) * D * 2);
+          for (int h = 0; h < D / 64; ++h)
+            tma_load_3d(smem_u32(smem) + (uint32_t)t * TILE + h * HALF, &qmap, h * 64, it.head * g.group, it.q0 + it.tok0 + t * g.tpt,
+                        &q_full[t]);
         }
-        cp_async_wait_all();
-        fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&q_full[t]);
       }
     }
+    for (int t = 0; t < 2; ++t)  // as for K and V
+      if (loads[t] && !mbar_wait(&q_full[t], (uint32_t)(loads[t] - 1) & 1u, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
   }
   } else {
     regs_raise<208>();
@@ -630,6 +619,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t s_at = tmem + lanes + t * BN, o_at = tmem + lanes + 2 * BN + t * D;
     const float c = g.c;
     uint32_t s_ph = 0, o_ph = 0;
+    const int my_tok = (quarter * 32 + lane) / g.group, h = quarter * 32 + lane - my_tok * g.group;
     for (int n = 0; !dead; ++n) {
       if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
       const Item it = items[n & 1];
@@ -637,10 +627,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (lane == 0) mbar_arrive(&item_free[n & 1]);
       if (it.end) break;
       const int end = t ? it.e1 : it.e0;
-      const int row = it.row0 + t * BM + quarter * 32 + lane;       // of the request
-      const int token = row / g.group, h = row - token * g.group;
-      const int seen = row < it.rows ? max(it.ahead + token, 0) : 0;
-      const bool idle = it.row0 + t * BM + quarter * 32 >= it.rows;  // no row of this warp exists
+      const int token = it.tok0 + t * g.tpt + my_tok;
+      const bool real = my_tok < g.tpt && token < it.n;
+      const int seen = real ? max(it.ahead + token, 0) : 0;
+      const bool idle = !__any_sync(0xffffffffu, real);
       float m = -INFINITY, l = 0.0f;
       for (int j = it.j0; j < end; ++j) {
         if (!wait(&s_full[t], s_ph)) break;
@@ -754,7 +744,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           float x[32];
 #pragma unroll
           for (int k = 0; k < 32; ++k) x[k] = any && seen > 0 ? __uint_as_float(o[k]) * inv : 0.0f;
-          if (row < it.rows) store(i, x);
+          if (real) store(i, x);
         }
       } else {
         // This piece's sums: for each 32 rows, four columns of them at a time, so that a warp's accesses are whole.
@@ -814,7 +804,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 x[4 * k + 3] += f * y.w;
               }
             }
-            if (row < it.rows) store(i, x);
+            if (real) store(i, x);
           }
           __syncwarp();
         }
@@ -834,7 +824,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 
 int64_t list_bytes(int64_t T, int64_t group, int64_t B) {
-  return round256(((T * group + ROWS - 1) / ROWS + B + MAX_PARTS) * (int64_t)sizeof(Item));
+  return round256((T / (2 * (BM / group)) + 1 + B + MAX_PARTS) * (int64_t)sizeof(Item));
 }
 constexpr int64_t kCounterBytes = MAX_PARTS / 2 * 8 * 4 + 256;  // the plan's head, then the counters
 
@@ -849,7 +839,6 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   TcArgs g = {};
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
   const int64_t group = a.q_heads / a.cache.heads;
-  g.q = static_cast<const uint16_t*>(a.q);
   g.o = static_cast<uint16_t*>(a.o);
   g.table = a.table;
   g.q_start = a.q_start;
@@ -858,13 +847,13 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   g.counters = reinterpret_cast<int*>(ws + 256);
   g.list = reinterpret_cast<Item*>(ws + round256(kCounterBytes));
   g.partial = reinterpret_cast<float*>(ws + round256(kCounterBytes) + list_bytes(a.T, group, a.B));
-  g.ldq = a.ldq;
   g.ldo = a.ldo;
   g.ldt = a.ldt;
   g.pages = a.cache.pages;
   g.T = (int)a.T;
   g.heads = (int)a.cache.heads;
   g.group = (int)group;
+  g.tpt = BM / g.group;
   g.B = (int)a.B;
   g.max_q = (int)(a.max_q < a.T ? a.max_q : a.T);
   g.cols = (int)a.cols;
@@ -875,9 +864,11 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   g.c = a.scale_log2 == 0.0f ? 1e-30f : std::fabs(a.scale_log2);
   g.status = status;
   g.timeout_ns = timeout_ns;
-  CUtensorMap kmap, vmap;
+  CUtensorMap qmap, kmap, vmap;
   int order[3], st;
   const uint32_t rows = (uint32_t)(a.cache.page_size < BN ? a.cache.page_size : BN);
+  if ((st = make_tmap_heads(&qmap, a.dtype, a.q, a.T, a.q_heads, a.cache.dim, a.ldq, (uint32_t)group, (uint32_t)g.tpt)) != PIFA_OK)
+    return st;
   if ((st = make_tmap_cache(&kmap, a.dtype, a.k, a.cache, rows, order)) != PIFA_OK) return st;
   if ((st = make_tmap_cache(&vmap, a.dtype, a.v, a.cache, rows, order)) != PIFA_OK) return st;
   g.token_at = order[0];
@@ -903,7 +894,7 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   auto go = [&](auto kernel, uint32_t smem) {
     cfg.dynamicSmemBytes = smem;
     cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    return err != cudaSuccess ? err : pifa_launch_ex(&cfg, kernel, kmap, vmap, g);
+    return err != cudaSuccess ? err : pifa_launch_ex(&cfg, kernel, qmap, kmap, vmap, g);
   };
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
   if (a.cache.dim == 64) e = f16 ? go(attention_tc<true, 64>, Cfg<64>::SMEM) : go(attention_tc<false, 64>, Cfg<64>::SMEM);

@@ -217,6 +217,9 @@ int launch_prefill_split(const PifaShape& s, const PifaPointers& p, int* status,
 // swizzle, zero fill outside the matrix.
 int make_tmap_2d(CUtensorMap* map, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld,
                  uint32_t box_cols, uint32_t box_rows);
+// 3-D tensor map over T rows of heads: box of 64 elements x `box_heads` heads x `box_rows` rows, 128-byte swizzle.
+int make_tmap_heads(CUtensorMap* map, int dtype, const void* base, int64_t T, int64_t heads, int64_t dim, int64_t ld,
+                    uint32_t box_heads, uint32_t box_rows);
 // 4-D tensor map over one buffer of a paged cache, innermost the head's elements, then tokens, heads and pages by
 // rising stride; box of 64 elements x `rows` tokens, 128-byte swizzle, zero fill outside. order[0..2]: which of
 // the map's coordinates 1 to 3 the token, the head and the page are.
