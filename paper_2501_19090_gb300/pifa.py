@@ -11,6 +11,7 @@ import contextlib
 import ctypes
 import functools
 import os
+import sys
 import threading
 
 import numpy as np
@@ -650,6 +651,9 @@ def pifa_m_reconstruct(XXt, YtXt, V, W=None, alpha=0.0, stream=None):
 
 
 # ---- between the projections: page tables, rotary positions, attention over a paged cache ----------
+# Calls of a decode step are short: their checks are made twice over, first as one chain of comparisons on each
+# tensor's plain attributes (a device by its index), then, where that chain does not hold, one by one with a
+# message for what is wrong. A tensor that only the second way accepts is accepted.
 def _refuse(msg):
     raise ValueError(f"pifa: {msg}")
 
@@ -722,31 +726,53 @@ def pifa_page_tables(cached_len, new_len, page_size: int, free_pages, free_first
     """Page tables of one step (pifa_page_tables): cached_len, new_len int32 (B), free_pages int32, free_first
     int32 (1), table int32 (B x columns, updated in place), `tokens` rows of room for the new tokens. Returns
     (q_start, kv_len, positions, slots, free_next); `out` gives those tensors."""
-    import torch
-    i32 = torch.int32
-    if not isinstance(cached_len, torch.Tensor) or cached_len.device.type != "cuda":
-        _refuse("cached_len must be a CUDA tensor")
-    dev = cached_len.device
-    c = _vector("cached_len", cached_len, None, i32, dev)
-    B = cached_len.shape[0]
-    n = _vector("new_len", new_len, B, i32, dev)
-    f = _vector("free_pages", free_pages, None, i32, dev)
-    ff = _vector("free_first", free_first, 1, i32, dev)
-    ldt = _table_ld(table, B, dev)
-    T = int(tokens)
-    if T < 0:
-        _refuse("tokens must be >= 0")
-    if out is None:
-        with _on(stream):
-            out = (torch.empty(B + 1, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev),
-                   torch.empty(T, dtype=i32, device=dev), torch.empty(T, dtype=torch.int64, device=dev),
-                   torch.empty(1, dtype=i32, device=dev))
-    q_start, kv_len, positions, slots, free_next = out
+    torch = sys.modules["torch"]
+    i32, T, sp = torch.int32, int(tokens), _stream_ptr(stream)
+    try:
+        q_start, kv_len, positions, slots, free_next = out
+        dev, (B,), (rows, cols) = cached_len.get_device(), cached_len.shape, table.shape
+        ldt, one = table.stride()
+        ldt = ldt if B > 1 else cols
+        fast = (dev >= 0 and rows == B and one == 1 and ldt >= cols
+                and cached_len.dtype is new_len.dtype is free_pages.dtype is free_first.dtype is table.dtype is i32
+                and q_start.dtype is kv_len.dtype is positions.dtype is free_next.dtype is i32 and slots.dtype is torch.int64
+                and dev == new_len.get_device() == free_pages.get_device() == free_first.get_device() == table.get_device()
+                and dev == q_start.get_device() == kv_len.get_device() == positions.get_device() == slots.get_device()
+                == free_next.get_device()
+                and new_len.shape == kv_len.shape == (B,) and free_first.shape == free_next.shape == (1,)
+                and q_start.shape == (B + 1,) and positions.shape == slots.shape == (T,) and free_pages.dim() == 1
+                and cached_len.is_contiguous() and new_len.is_contiguous() and free_pages.is_contiguous()
+                and q_start.is_contiguous() and kv_len.is_contiguous() and positions.is_contiguous() and slots.is_contiguous())
+    except (AttributeError, TypeError, ValueError):
+        fast = False
+    if not fast:
+        if not isinstance(cached_len, torch.Tensor) or cached_len.device.type != "cuda":
+            _refuse("cached_len must be a CUDA tensor")
+        dev = cached_len.device
+        _vector("cached_len", cached_len, None, i32, dev)
+        B = cached_len.shape[0]
+        _vector("new_len", new_len, B, i32, dev)
+        _vector("free_pages", free_pages, None, i32, dev)
+        _vector("free_first", free_first, 1, i32, dev)
+        ldt = _table_ld(table, B, dev)
+        cols = table.shape[1]
+        if T < 0:
+            _refuse("tokens must be >= 0")
+        if out is None:
+            with _on(stream):
+                out = (torch.empty(B + 1, dtype=i32, device=dev), torch.empty(B, dtype=i32, device=dev),
+                       torch.empty(T, dtype=i32, device=dev), torch.empty(T, dtype=torch.int64, device=dev),
+                       torch.empty(1, dtype=i32, device=dev))
+        q_start, kv_len, positions, slots, free_next = out
+        _vector("q_start", q_start, B + 1, i32, dev)
+        _vector("kv_len", kv_len, B, i32, dev)
+        _vector("positions", positions, T, i32, dev)
+        _vector("slots", slots, T, torch.int64, dev)
+        _vector("free_next", free_next, 1, i32, dev)
     st = _lib().pifa_page_tables(
-        c, n, B, int(page_size), f, free_pages.shape[0], ff, table.data_ptr(), table.shape[1], ldt,
-        _vector("q_start", q_start, B + 1, i32, dev), _vector("kv_len", kv_len, B, i32, dev),
-        _vector("positions", positions, T, i32, dev), _vector("slots", slots, T, torch.int64, dev), T,
-        _vector("free_next", free_next, 1, i32, dev), _stream_ptr(stream))
+        cached_len.data_ptr(), new_len.data_ptr(), B, int(page_size), free_pages.data_ptr(), free_pages.shape[0],
+        free_first.data_ptr(), table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), positions.data_ptr(),
+        slots.data_ptr(), T, free_next.data_ptr(), sp)
     _check(st, "pifa_page_tables")
     return q_start, kv_len, positions, slots, free_next
 
@@ -766,19 +792,34 @@ def pifa_rope(X, positions, freq, layout: int = PIFA_ROPE_HALF, scale: float = 1
               stream=None):
     """Rotary positions (pifa_rope) of X (T x heads x head_dim, bf16 or fp16); positions int32 (T), freq int64
     (rot_dim / 2). inverse: the gradient, dX from dY. Y may be X; allocated if not given."""
-    import torch
-    T, h, d, ldx = _rows_of_heads("X", X)
-    dev = X.device
-    p = _vector("positions", positions, T, torch.int32, dev)
-    f = _vector("freq", freq, None, torch.int64, dev)
-    if Y is None:
-        with _on(stream):
-            Y = torch.empty((T, h, d), dtype=X.dtype, device=dev)
-    ys = _rows_of_heads("Y", Y, X.dtype, dev)
-    if ys[:3] != (T, h, d):
-        _refuse(f"Y must be a tensor of shape {(T, h, d)}")
-    st = _lib().pifa_rope(X.data_ptr(), T, h, ldx, d, c_dtype_of(X), p, f, 2 * freq.shape[0], int(layout), float(scale),
-                          int(bool(inverse)), Y.data_ptr(), ys[3], _stream_ptr(stream))
+    torch = sys.modules["torch"]
+    try:
+        dev, dt, xs = X.get_device(), X.dtype, X.shape
+        (T, h, d), (ldx, xh, xe), (ldy, yh, ye), (pairs,) = xs, X.stride(), Y.stride(), freq.shape
+        if T == 1:  # one row has no pitch, whatever its stride says
+            ldx = ldy = h * d
+        fast = (dev >= 0 and xe == ye == 1 and xh == yh == d and Y.shape == xs
+                and (dt is torch.bfloat16 or dt is torch.float16) and Y.dtype is dt
+                and positions.dtype is torch.int32 and freq.dtype is torch.int64 and positions.shape == (T,)
+                and dev == Y.get_device() == positions.get_device() == freq.get_device()
+                and positions.is_contiguous() and freq.is_contiguous())
+    except (AttributeError, TypeError, ValueError):
+        fast = False
+    if not fast:
+        T, h, d, ldx = _rows_of_heads("X", X)
+        dev, dt = X.device, X.dtype
+        _vector("positions", positions, T, torch.int32, dev)
+        _vector("freq", freq, None, torch.int64, dev)
+        pairs = freq.shape[0]
+        if Y is None:
+            with _on(stream):
+                Y = torch.empty((T, h, d), dtype=dt, device=dev)
+        *ys, ldy = _rows_of_heads("Y", Y, dt, dev)
+        if ys != [T, h, d]:
+            _refuse(f"Y must be a tensor of shape {(T, h, d)}")
+    st = _lib().pifa_rope(X.data_ptr(), T, h, ldx, d, PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16,
+                          positions.data_ptr(), freq.data_ptr(), 2 * pairs, int(layout), float(scale), int(bool(inverse)),
+                          Y.data_ptr(), ldy, _stream_ptr(stream))
     _check(st, "pifa_rope")
     return Y
 
@@ -788,25 +829,46 @@ def pifa_rope_cache(Q, K, V, positions, slots, freq, k_cache, v_cache, layout: i
     """Q (T x heads x head_dim) turned into Qr, K (T x kv_heads x head_dim) turned into k_cache and V into v_cache
     (pages x page_size x kv_heads x head_dim, updated in place) at `slots` int64 (T): pifa_rope_cache. Qr may be
     Q; allocated if not given."""
-    import torch
-    T, h, d, ldq = _rows_of_heads("Q", Q)
-    dev, dt = Q.device, Q.dtype
-    ks, vs = _rows_of_heads("K", K, dt, dev), _rows_of_heads("V", V, dt, dev)
-    pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, dt, dev)
-    if ks[:3] != (T, hk, d) or vs[:3] != (T, hk, d):
-        _refuse(f"K and V must be tensors of shape {(T, hk, d)}")
-    p = _vector("positions", positions, T, torch.int32, dev)
-    s = _vector("slots", slots, T, torch.int64, dev)
-    f = _vector("freq", freq, None, torch.int64, dev)
-    if Qr is None:
-        with _on(stream):
-            Qr = torch.empty((T, h, d), dtype=dt, device=dev)
-    qs = _rows_of_heads("Qr", Qr, dt, dev)
-    if qs[:3] != (T, h, d):
-        _refuse(f"Qr must be a tensor of shape {(T, h, d)}")
-    st = _lib().pifa_rope_cache(Q.data_ptr(), ldq, K.data_ptr(), ks[3], V.data_ptr(), vs[3], T, h, hk, d, c_dtype_of(Q),
-                                p, s, f, 2 * freq.shape[0], int(layout), float(scale), Qr.data_ptr(), qs[3],
-                                k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh, _stream_ptr(stream))
+    torch = sys.modules["torch"]
+    try:
+        dev, dt, qs, ks, cs, strides = Q.get_device(), Q.dtype, Q.shape, K.shape, k_cache.shape, k_cache.stride()
+        (T, h, d), (_, hk, _), (pages, size, _, _), (sp, st_, sh, se) = qs, ks, cs, strides
+        (ldq, qh, qe), (ldk, kh, ke), (ldv, vh, ve), (ldqr, rh, re) = Q.stride(), K.stride(), V.stride(), Qr.stride()
+        if T == 1:
+            ldq, ldk, ldv, ldqr = h * d, hk * d, hk * d, h * d
+        fast = (dev >= 0 and se == qe == ke == ve == re == 1 and qh == kh == vh == rh == d
+                and ks == V.shape == (T, hk, d) and Qr.shape == qs and cs == v_cache.shape == (pages, size, hk, d)
+                and v_cache.stride() == strides and (dt is torch.bfloat16 or dt is torch.float16)
+                and dt is K.dtype is V.dtype is Qr.dtype is k_cache.dtype is v_cache.dtype
+                and positions.dtype is torch.int32 and slots.dtype is freq.dtype is torch.int64
+                and positions.shape == slots.shape == (T,) and freq.dim() == 1
+                and dev == K.get_device() == V.get_device() == Qr.get_device() == k_cache.get_device() == v_cache.get_device()
+                and dev == positions.get_device() == slots.get_device() == freq.get_device()
+                and positions.is_contiguous() and slots.is_contiguous() and freq.is_contiguous())
+    except (AttributeError, TypeError, ValueError):
+        fast = False
+    if not fast:
+        T, h, d, ldq = _rows_of_heads("Q", Q)
+        dev, dt = Q.device, Q.dtype
+        *ks, ldk = _rows_of_heads("K", K, dt, dev)
+        *vs, ldv = _rows_of_heads("V", V, dt, dev)
+        pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, dt, dev)
+        if ks != [T, hk, d] or vs != [T, hk, d]:
+            _refuse(f"K and V must be tensors of shape {(T, hk, d)}")
+        _vector("positions", positions, T, torch.int32, dev)
+        _vector("slots", slots, T, torch.int64, dev)
+        _vector("freq", freq, None, torch.int64, dev)
+        if Qr is None:
+            with _on(stream):
+                Qr = torch.empty((T, h, d), dtype=dt, device=dev)
+        *qs, ldqr = _rows_of_heads("Qr", Qr, dt, dev)
+        if qs != [T, h, d]:
+            _refuse(f"Qr must be a tensor of shape {(T, h, d)}")
+    st = _lib().pifa_rope_cache(
+        Q.data_ptr(), ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, T, h, hk, d,
+        PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16, positions.data_ptr(), slots.data_ptr(),
+        freq.data_ptr(), 2 * freq.shape[0], int(layout), float(scale), Qr.data_ptr(), ldqr,
+        k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh, _stream_ptr(stream))
     _check(st, "pifa_rope_cache")
     return Qr
 
@@ -823,38 +885,77 @@ def pifa_paged_attention_workspace_size(T: int, q_heads: int, kv_heads: int, hea
     return _attention_workspace_size(int(T), int(q_heads), int(kv_heads), int(head_dim), int(B), int(max_q))
 
 
+_attention_workspaces: dict = {}
+
+
+def _attention_workspace(need, dev, run_on, stream):
+    """(256-byte aligned address, bytes, tensor) of scratch kept for one device and one stream that calls run on."""
+    key = (dev, run_on if isinstance(run_on, int) else getattr(run_on, "value", None))
+    ws = _attention_workspaces.get(key)
+    if ws is None or ws[1] < need:
+        import torch
+        with _on(stream):
+            buf = torch.empty(need + 256, dtype=torch.uint8, device=f"cuda:{dev}")
+        pad = -buf.data_ptr() % 256
+        ws = _attention_workspaces[key] = (buf.data_ptr() + pad, need + 256 - pad, buf)
+    return ws
+
+
 def pifa_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, max_q: int, scale=None, O=None,
                          workspace_tensor=None, stream=None):
     """Causal attention of each request's new tokens over its pages (pifa_paged_attention): Q (T x heads x
     head_dim), caches as pifa_rope_cache, table int32 (B x columns), q_start int32 (B + 1), kv_len int32 (B),
     max_q at least every request's number of new tokens. scale: 1 / sqrt(head_dim) if not given. Returns O,
     shaped like Q (allocated as zeros if not given: rows of no request are not written)."""
-    import torch
-    T, h, d, ldq = _rows_of_heads("Q", Q)
-    dev, dt = Q.device, Q.dtype
-    pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, dt, dev)
-    kl = _vector("kv_len", kv_len, None, torch.int32, dev)
-    B = kv_len.shape[0]
-    qs = _vector("q_start", q_start, B + 1, torch.int32, dev)
-    ldt = _table_ld(table, B, dev)
-    if O is None:
-        with _on(stream):
-            O = torch.zeros((T, h, d), dtype=dt, device=dev)
-    os_ = _rows_of_heads("O", O, dt, dev)
-    if os_[:3] != (T, h, d):
-        _refuse(f"O must be a tensor of shape {(T, h, d)}")
+    torch = sys.modules["torch"]
+    run_on = _stream_ptr(stream)
+    try:
+        dev, dt, qs, cs, strides = Q.get_device(), Q.dtype, Q.shape, k_cache.shape, k_cache.stride()
+        (T, h, d), (pages, size, hk, _), (sp, st_, sh, se) = qs, cs, strides
+        (ldq, qh, qe), (ldo, oh, oe), (ldt, te), (B, cols) = Q.stride(), O.stride(), table.stride(), table.shape
+        if T == 1:
+            ldq = ldo = h * d
+        if B == 1:
+            ldt = cols
+        fast = (dev >= 0 and se == qe == oe == te == 1 and qh == oh == d and ldt >= cols and O.shape == qs
+                and cs == v_cache.shape == (pages, size, hk, d) and v_cache.stride() == strides
+                and (dt is torch.bfloat16 or dt is torch.float16) and dt is O.dtype is k_cache.dtype is v_cache.dtype
+                and table.dtype is q_start.dtype is kv_len.dtype is torch.int32
+                and q_start.shape == (B + 1,) and kv_len.shape == (B,)
+                and dev == O.get_device() == k_cache.get_device() == v_cache.get_device()
+                and dev == table.get_device() == q_start.get_device() == kv_len.get_device()
+                and q_start.is_contiguous() and kv_len.is_contiguous())
+    except (AttributeError, TypeError, ValueError):
+        fast = False
+    if not fast:
+        T, h, d, ldq = _rows_of_heads("Q", Q)
+        dt = Q.dtype
+        pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, dt, Q.device)
+        _vector("kv_len", kv_len, None, torch.int32, Q.device)
+        B = kv_len.shape[0]
+        _vector("q_start", q_start, B + 1, torch.int32, Q.device)
+        ldt = _table_ld(table, B, Q.device)
+        cols = table.shape[1]
+        if O is None:
+            with _on(stream):
+                O = torch.zeros((T, h, d), dtype=dt, device=Q.device)
+        *os_, ldo = _rows_of_heads("O", O, dt, Q.device)
+        if os_ != [T, h, d]:
+            _refuse(f"O must be a tensor of shape {(T, h, d)}")
+        dev = Q.get_device()
     need = _attention_workspace_size(T, h, hk, d, B, int(max_q))
-    ws = workspace_tensor
-    if ws is None:
-        with _on(stream):  # one for each stream that calls run on, the current one among them
-            ws = workspace(need, dev, _stream_ptr(None), tag="attention")
-    elif not isinstance(ws, torch.Tensor) or ws.device != dev:
-        _refuse("workspace_tensor must be a tensor on Q's device")
-    ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
-    ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
+    if workspace_tensor is None:
+        ws_ptr, ws_bytes, _ = _attention_workspace(need, dev, run_on, stream)
+    else:
+        ws = workspace_tensor
+        if not isinstance(ws, torch.Tensor) or ws.get_device() != dev:
+            _refuse("workspace_tensor must be a tensor on Q's device")
+        ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
+        ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
     st = _lib().pifa_paged_attention(
-        Q.data_ptr(), ldq, T, h, hk, d, c_dtype_of(Q), k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh,
-        table.data_ptr(), table.shape[1], ldt, qs, kl, B, int(max_q), d ** -0.5 if scale is None else float(scale),
-        O.data_ptr(), os_[3], ws_ptr, ws_bytes, _stream_ptr(stream))
+        Q.data_ptr(), ldq, T, h, hk, d, PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16,
+        k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh,
+        table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), B, int(max_q),
+        d ** -0.5 if scale is None else float(scale), O.data_ptr(), ldo, ws_ptr, ws_bytes, run_on)
     _check(st, "pifa_paged_attention")
     return O
