@@ -104,13 +104,20 @@ __device__ __forceinline__ int find(const int* first, int n, int v) {
   return lo;
 }
 
+// Where a 16-byte piece of a key's row lies in shared memory: its index xor this, so that the eight lanes of a
+// quarter warp, which read two keys' four neighbouring pieces of K, or two pieces of every other key of V, meet
+// eight different bank groups.
+__device__ __forceinline__ int k_swizzle(int key) { return (key & 1) << 2; }
+__device__ __forceinline__ int v_swizzle(int key) { return key & 6; }
+
 template <bool F16, int D>
 __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   constexpr int KC = D / 32, VC = D / 64;            // 16-byte pieces of a lane: of one key, of one key of V
-  constexpr int PIECES = 2 * KC + 4 * VC;            // of one step
+  constexpr int ROW = 2 * D, KEYS = 32 / (ROW / 16);   // bytes of a key's row; keys that a warp copies at once
+  constexpr int STAGE_BYTES = 2 * STEP * ROW;        // K and V of a step
   constexpr int STAGES = kStages<D>;
   extern __shared__ __align__(16) uint8_t smem[];
-  int* first = reinterpret_cast<int*>(smem + WARPS * STAGES * PIECES * 512);  // B + 1
+  int* first = reinterpret_cast<int*>(smem + WARPS * STAGES * STAGE_BYTES);  // B + 1
   __shared__ int part[32];
   pdl_launch_dependents();
   pdl_wait_primary();
@@ -160,8 +167,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   int at = (int)min(at64, (int64_t)total);
   const int stop = (int)min(at64 + run, (int64_t)total);
   const int gr = lane >> 2, c4 = lane & 3;
-  uint8_t* mine = smem + (warp * STAGES * PIECES * 32 + lane) * 16;
-  const uint32_t mine_at = smem_u32(mine);
+  const uint8_t* ring = smem + warp * STAGES * STAGE_BYTES;
+  const uint32_t ring_at = smem_u32(ring);
+  const int piece = lane % (ROW / 16), key0 = lane / (ROW / 16);
   while (at < stop) {
     const int b = find(first, g.B, at);
     const Lengths x = lengths_of(g, b);
@@ -201,24 +209,23 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
         const int id = __shfl_sync(0xffffffffu, ids, s - known);
         const bool bad = id < 0 || id >= g.pages;
         if (bad && x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-        const int64_t page = (bad ? 0 : (int64_t)id) * g.page_stride + head * g.head_stride +
-                             ((s * STEP) & (g.page_size - 1)) * g.token_stride;
-        const int left = bad ? 0 : x.L - s * STEP;  // keys from here on
-        const uint32_t dst = mine_at + stage * PIECES * 512;
+        // this lane's piece of every KEYS-th key: a warp's copy is whole rows
+        const int64_t at = (bad ? 0 : (int64_t)id) * g.page_stride + head * g.head_stride +
+                           (((s * STEP) & (g.page_size - 1)) + key0) * g.token_stride + piece * 8;
+        const int left = bad ? 0 : x.L - s * STEP - key0;  // keys from this lane's first on
+        const uint32_t dst = ring_at + stage * STAGE_BYTES + key0 * ROW;
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb) {
-          const int key = gr + 8 * nb;
-          const uint16_t* src = g.k + page + (key < left ? key : 0) * g.token_stride + c4 * 8;
-#pragma unroll
-          for (int i = 0; i < KC; ++i) cp_async16(dst + (nb * KC + i) * 512, src + 32 * i, key < left ? 16 : 0);
+        for (int i = 0; i < STEP / KEYS; ++i) {
+          const bool in = i * KEYS < left;
+          cp_async16(dst + i * KEYS * ROW + ((piece ^ k_swizzle(key0 + i * KEYS)) << 4),
+                     g.k + at + (in ? i * KEYS * g.token_stride : 0) - (left > 0 ? 0 : key0 * g.token_stride), in ? 16 : 0);
         }
         cp_commit();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int key = c4 * 2 + (k & 1) + 8 * (k >> 1);
-          const uint16_t* src = g.v + page + (key < left ? key : 0) * g.token_stride + gr * 8;
-#pragma unroll
-          for (int h = 0; h < VC; ++h) cp_async16(dst + (2 * KC + k * VC + h) * 512, src + 64 * h, key < left ? 16 : 0);
+        for (int i = 0; i < STEP / KEYS; ++i) {
+          const bool in = i * KEYS < left;
+          cp_async16(dst + STEP * ROW + i * KEYS * ROW + ((piece ^ v_swizzle(key0 + i * KEYS)) << 4),
+                     g.v + at + (in ? i * KEYS * g.token_stride : 0) - (left > 0 ? 0 : key0 * g.token_stride), in ? 16 : 0);
         }
       } else {
         cp_commit();
@@ -231,15 +238,17 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
     int stage = 0;
     for (int s = s0; s < s1; ++s) {
+      __syncwarp();  // all lanes have read the stage that is filled next
       load(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
-      const uint4* buf = reinterpret_cast<const uint4*>(mine + stage * PIECES * 512);
+      const uint8_t* buf = ring + stage * STAGE_BYTES;
       cp_wait<2 * STAGES - 1>();
+      __syncwarp();
       float sc[2][4] = {};
 #pragma unroll
       for (int i = 0; i < KC; ++i)
 #pragma unroll
         for (int nb = 0; nb < 2; ++nb) {
-          const uint4 k = buf[(nb * KC + i) * 32];
+          const uint4 k = *reinterpret_cast<const uint4*>(buf + (gr + 8 * nb) * ROW + (((c4 + 4 * i) ^ k_swizzle(gr)) << 4));
           mma<F16>(sc[nb], q[0][i].x, q[1][i].x, q[0][i].y, q[1][i].y, k.x, k.y);
           mma<F16>(sc[nb], q[0][i].z, q[1][i].z, q[0][i].w, q[1][i].w, k.z, k.w);
         }
@@ -283,11 +292,15 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
         p[r][1] = pack<F16>(e[2], e[3]);
       }
       cp_wait<2 * STAGES - 2>();
+      __syncwarp();
 #pragma unroll
       for (int h = 0; h < VC; ++h) {
         uint4 w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = buf[(2 * KC + k * VC + h) * 32];
+        for (int k = 0; k < 4; ++k) {
+          const int key = c4 * 2 + (k & 1) + 8 * (k >> 1);
+          w[k] = *reinterpret_cast<const uint4*>(buf + (STEP + key) * ROW + (((8 * h + gr) ^ v_swizzle(key)) << 4));
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // columns 2 i and 2 i + 1 of the lane's eight
           const uint32_t a = (&w[0].x)[i], bb = (&w[1].x)[i], cc = (&w[2].x)[i], dd = (&w[3].x)[i];
@@ -441,7 +454,7 @@ cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = (size_t)WARPS * kStages<D> * (D / 8) * 512 + (size_t)(g.B + 1) * 4;
+  cfg.dynamicSmemBytes = (size_t)WARPS * kStages<D> * 2 * STEP * 2 * D + (size_t)(g.B + 1) * 4;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
