@@ -348,81 +348,94 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   }
 }
 
-// Adds up the pieces of heads whose steps fell to several warps, in the order of the keys: WPR warps for each
-// row, each with every WPR-th piece.
-template <bool F16, int D, int WPR>
+// Adds up the pieces of a request's head whose steps fell to several warps, in the order of the keys: a CTA for
+// each, a thread for four columns of a row, or, where there are few rows, several threads with every so many-th
+// piece. Pieces and their weights are loaded together, four at a time: the kernel is two latencies long.
+template <bool F16, int D>
 __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g) {
-  constexpr int E = D / 32;  // columns of a lane
-  __shared__ float2 sh_ml[WARPS];
-  __shared__ float sh_o[WARPS][D];
+  __shared__ float2 sh_ml[THREADS];
+  __shared__ float4 sh_o[THREADS];
   pdl_launch_dependents();
+  const int b = (int)blockIdx.x / g.heads, head = (int)blockIdx.x - b * g.heads;
+  const int slots = g.max_rows * (D / 4), groups = max(THREADS / slots, 1);
   pdl_wait_primary();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t unit = (int64_t)blockIdx.x * (WARPS / WPR) + warp / WPR, item = unit / g.max_rows;
-  const int row = (int)(unit - item * g.max_rows), b = (int)(item / g.heads), head = (int)(item - (int64_t)b * g.heads);
-  bool here = b < g.B;
-  Lengths x = {};
-  int w0 = 0, w1 = 0;
-  if (here) {
-    x = lengths_of(g, b);
-    const int steps = steps_of(x), run = g.sums[g.B + 1], from = g.sums[b] + head * steps;
-    w0 = from / run;
-    w1 = (from + steps - 1) / run;
-    here = row < x.n * g.group && w1 > w0;
-  }
-  float top = -INFINITY, all = 0.0f, acc[E] = {};
-  if (here) {
-    const float* base = g.partial + row * (D + 2);
-    const int place = g.max_rows * (D + 2);  // a warp has two: the head that began before its run, and the last one
-    auto piece = [&](int w) { return base + ((int64_t)w * 2 + (w == w0 ? 1 : 0)) * place; };
-    const int k = w0 + warp % WPR;
-    for (int w = k + lane * WPR; w <= w1; w += 32 * WPR) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(w) + D));
-      if (ml.y != 0.0f) top = fmaxf(top, ml.x);
-    }
+  const Lengths x = lengths_of(g, b);
+  const int run = g.sums[g.B + 1], steps = steps_of(x), from = g.sums[b] + head * steps;
+  if (steps == 0) return;
+  const int w0 = from / run, w1 = (from + steps - 1) / run;
+  if (w0 == w1) return;  // the warp has finished it
+  const int place = g.max_rows * (D + 2);  // a warp has two: the head that began before its run, and the last one
+  for (int slot = (int)threadIdx.x % (slots * groups); slot < slots * groups; slot += THREADS) {
+    const int group = slot / slots, row = (slot - group * slots) / (D / 4), col = (slot - group * slots) % (D / 4) * 4;
+    const bool here = row < x.n * g.group && (int)threadIdx.x < slots * groups;
+    float top = -INFINITY, all = 0.0f;
+    float4 acc = make_float4(0, 0, 0, 0);
+    if (here) {
+      const float* base = g.partial + row * (D + 2);
+      for (int w = w0 + group; w <= w1; w += 4 * groups) {
+        float2 ml[4], lo[4], hi[4];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float base_m = top > -INFINITY ? top : 0.0f;
-#pragma unroll 4
-    for (int w = k; w <= w1; w += WPR) {
-      const float* p = piece(w);
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + D));
-      const float f = ml.y != 0.0f ? fast_exp2(ml.x - base_m) : 0.0f;
-      all += ml.y * f;
+        for (int i = 0; i < 4; ++i) {
+          const int v = min(w + i * groups, w1);
+          const float* p = base + ((int64_t)v * 2 + (v == w0 ? 1 : 0)) * place;
+          ml[i] = __ldcg(reinterpret_cast<const float2*>(p + D));
+          lo[i] = __ldcg(reinterpret_cast<const float2*>(p + col));
+          hi[i] = __ldcg(reinterpret_cast<const float2*>(p + col + 2));
+        }
+        float most = top;
 #pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float2 y = __ldcg(reinterpret_cast<const float2*>(p + lane * E + e));
-        acc[e] += y.x * f;
-        acc[e + 1] += y.y * f;
+        for (int i = 0; i < 4; ++i) {
+          if (w + i * groups > w1) ml[i].y = 0.0f;  // a piece that is not there
+          if (ml[i].y != 0.0f) most = fmaxf(most, ml[i].x);
+        }
+        const float f = top > -INFINITY ? fast_exp2(top - most) : 0.0f;
+        all *= f;
+        acc.x *= f;
+        acc.y *= f;
+        acc.z *= f;
+        acc.w *= f;
+        top = most;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = ml[i].y != 0.0f ? fast_exp2(ml[i].x - top) : 0.0f;
+          all += ml[i].y * e;
+          acc.x += lo[i].x * e;
+          acc.y += lo[i].y * e;
+          acc.z += hi[i].x * e;
+          acc.w += hi[i].y * e;
+        }
       }
     }
-  }
-  if constexpr (WPR > 1) {
-    if (lane == 0) sh_ml[warp] = make_float2(top, all);
-#pragma unroll
-    for (int e = 0; e < E; ++e) sh_o[warp][lane * E + e] = acc[e];
-    __syncthreads();
-    if (warp % WPR) return;
-#pragma unroll
-    for (int k = 0; k < WPR; ++k) top = fmaxf(top, sh_ml[warp + k].x);
-    all = 0.0f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < WPR; ++k) {
-      const float2 ml = sh_ml[warp + k];
-      const float f = ml.y != 0.0f ? fast_exp2(ml.x - top) : 0.0f;
-      all += ml.y * f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += sh_o[warp + k][lane * E + e] * f;
+    if (groups > 1) {  // (then every thread has one slot at most)
+      sh_ml[threadIdx.x] = make_float2(top, all);
+      sh_o[threadIdx.x] = acc;
+      __syncthreads();
+      if (group > 0) return;
+      float most = top;
+      for (int k = 1; k < groups; ++k) most = fmaxf(most, sh_ml[slot + k * slots].x);
+      const float f = top > -INFINITY ? fast_exp2(top - most) : 0.0f;
+      all *= f;
+      acc.x *= f;
+      acc.y *= f;
+      acc.z *= f;
+      acc.w *= f;
+      for (int k = 1; k < groups; ++k) {
+        const float2 ml = sh_ml[slot + k * slots];
+        const float4 o = sh_o[slot + k * slots];
+        const float e = ml.y != 0.0f ? fast_exp2(ml.x - most) : 0.0f;
+        all += ml.y * e;
+        acc.x += o.x * e;
+        acc.y += o.y * e;
+        acc.z += o.z * e;
+        acc.w += o.w * e;
+      }
     }
-  }
-  if (here) {
-    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-    const int token = row / g.group;
-    uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(out + e) = pack<F16>(acc[e] * inv, acc[e + 1] * inv);
+    if (here) {
+      const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+      const int token = row / g.group;
+      uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + col;
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack<F16>(acc.x * inv, acc.y * inv), pack<F16>(acc.z * inv, acc.w * inv));
+    }
   }
 }
 
@@ -464,15 +477,9 @@ cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(attention_rows<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 256);
   if (e == cudaSuccess) e = pifa_launch_ex(&cfg, attention_rows<F16, D>, g);
   if (e != cudaSuccess) return e;
-  // a warp for each row; few rows, of which each may have pieces from all over the grid: eight
-  const int64_t units = (int64_t)g.B * g.heads * g.max_rows;
   cfg.dynamicSmemBytes = 0;
-  if (units <= 1024) {
-    cfg.gridDim = dim3((unsigned)units);
-    return pifa_launch_ex(&cfg, attention_join<F16, D, WARPS>, g);
-  }
-  cfg.gridDim = dim3((unsigned)((units + WARPS - 1) / WARPS));
-  return pifa_launch_ex(&cfg, attention_join<F16, D, 1>, g);
+  cfg.gridDim = dim3((unsigned)(g.B * g.heads));
+  return pifa_launch_ex(&cfg, attention_join<F16, D>, g);
 }
 
 }  // namespace
