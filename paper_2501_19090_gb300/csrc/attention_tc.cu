@@ -13,11 +13,11 @@
 //
 // CTA of 384 threads, one per SM, persistent:
 //   warps 0-3, 4-7   softmax and epilogue of tile 0 and 1 (tensor memory quarter = warp % 4)
-//   warp 8           takes work items from a queue and loads K and V tiles by TMA into a ring of slots, a page (or a
-//                    128-token part of one) and 64 columns a copy, a lane for each
+//   warp 8           takes work items from a queue and loads K's tiles by TMA into a ring of slots that K and V take in
+//                    turn, a page (or a 128-token part of one) and 64 columns a copy, a lane for each
 //   warps 9, 10      issue the MMAs of tile 0 and 1: PV, in two halves of the keys as P arrives, and the next S; one
 //                    tile's softmax runs under the other tile's MMAs. (One warp for both was the bound.)
-//   warp 11          loads the next item's rows of Q by TMA, as soon as the last S of a tile has been computed
+//   warp 11          loads the next item's rows of Q, as soon as the last S of a tile has been computed, and V
 // P lies over S, and S of the next keys is written over both: the MMAs of one warp run in issue
 // order, PV(j) before S(j + 1), and S(j)'s values were read before P was announced.
 // Keys past L: their scores are masked, and their rows of V, which may hold anything, are set to zero in shared
@@ -380,13 +380,51 @@ __global__ void __launch_bounds__(THREADS, 1)
   // Registers: a softmax thread holds a row of S. 2 x 128 x 208 + 128 x 88 = 384 x 168, as launched.
   if (warp >= 8) {
   regs_lower<88>();
-  if (warp == 8) {
-    // ---------------- queue, K and V ----------------
-    int s = 0, fills = 0;
-    uint32_t ph = 1;
-    const int per_tile = g.page_size >= BN ? 1 : BN / g.page_size;
-    const int box_rows = min(g.page_size, BN);
+  // K (kv = 0) or V of an item's key tiles, fill after fill of the ring: K and V take its slots in turn. A lane
+  // copies 64 columns of a page's rows (or of 128 of them). One warp issuing both was the bound for pages of 16.
+  auto stream = [&](int kv, int& tiles, int b, int L, int head, int j0, int j1, auto&& every) {
+    const int per_tile = g.page_size >= BN ? 1 : BN / g.page_size, box_rows = min(g.page_size, BN);
     const int mine = lane / (D / 64), half = lane % (D / 64);
+    const int n_pages = (L + g.page_size - 1) >> g.page_shift;
+    const int32_t* row = g.table + b * g.ldt;
+    auto page_of = [&](int j) {
+      const int p = ((j * BN) >> g.page_shift) + mine;
+      return mine < per_tile && j < j1 && p < n_pages ? row[p] : -2;  // -2: no page
+    };
+    int id = page_of(j0);
+    for (int j = j0; j < j1 && !dead; ++j) {
+      const int next = page_of(j + 1);
+      every(j);
+      const bool has = id != -2 || (mine < per_tile && ((j * BN) >> g.page_shift) + mine < n_pages);
+      if (has && (id < 0 || id >= g.pages)) {
+        latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+        id = (int)g.pages;  // outside the tensor map: zeros
+      }
+      const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, has)) * (uint32_t)box_rows * 128u;
+      const int token = (j * BN) & (g.page_size - 1);
+      const int y = g.token_at == 0 ? token : g.head_at == 0 ? head : id;
+      const int z = g.token_at == 1 ? token : g.head_at == 1 ? head : id;
+      const int w = g.token_at == 2 ? token : g.head_at == 2 ? head : id;
+      const int fill = 2 * tiles + kv, s = fill % SLOTS;
+      if (!wait(&empty[s], ((uint32_t)(fill / SLOTS) & 1u) ^ 1u)) break;
+      if (lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
+      __syncwarp();
+      if (has)
+        tma_load_4d(smem_u32(ring) + (uint32_t)s * TILE + (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u,
+                    kv ? &vmap : &kmap, half * 64, y, z, w, &full[s]);
+      ++tiles;
+      id = next;
+    }
+  };
+  // nothing may land in shared memory after the CTA has left
+  auto landed = [&](int kv, int tiles) {
+    for (int i = max(2 * tiles - 2 * SLOTS, 0) + kv; i < 2 * tiles; i += 2)
+      if (i + SLOTS >= 2 * tiles && !mbar_wait(&full[i % SLOTS], (uint32_t)(i / SLOTS) & 1u, 100000000ull))
+        latch_status(g.status, PIFA_ERR_TIMEOUT);
+  };
+  if (warp == 8) {
+    // ---------------- queue and K ----------------
+    int tiles = 0;
     // An entry's words, a lane each. The list has room for MAX_PARTS entries and more, so that the first can be read
     // before it is known to be one.
     auto fetch = [&](int k) { return lane < 16 ? __ldcg(reinterpret_cast<const int*>(g.list + k / g.heads) + lane) : 0; };
@@ -405,71 +443,31 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (lane == 0) mbar_arrive(&item_full[n & 1]);
       return k < total;
     };
-    int id = 0;
     bool more = publish(0);
     for (int n = 0; more; ++n) {
       const int b = __shfl_sync(0xffffffffu, word, 0), L = __shfl_sync(0xffffffffu, word, 3);
-      const int j0 = __shfl_sync(0xffffffffu, word, 6), j1 = __shfl_sync(0xffffffffu, word, 7), head = k % g.heads;
-      const int n_pages = (L + g.page_size - 1) >> g.page_shift;
-      const int32_t* row = g.table + b * g.ldt;
-      auto page_of = [&](int j) {
-        const int p = ((j * BN) >> g.page_shift) + mine;
-        return mine < per_tile && j < j1 && p < n_pages ? row[p] : -2;  // -2: no page
-      };
-      id = page_of(j0);
+      const int j0 = __shfl_sync(0xffffffffu, word, 6), j1 = __shfl_sync(0xffffffffu, word, 7);
       // The next item is taken towards the end of this one, each step a tile ahead of what needs it: late, so
       // that the CTA that is done first takes it, and in time for its loads to follow on.
       int step = 0, taken = 0;
-      for (int j = j0; j < j1 && !dead; ++j) {
-        const int next = page_of(j + 1);
-        if (j >= j1 - 4 && step < 3) {
-          if (step == 0) {
-            if (lane == 0) taken = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
-          } else if (step == 1) {
-            k = __shfl_sync(0xffffffffu, taken, 0);
-            word = k < total ? fetch(k) : 0;
-          } else {
-            more = publish(n + 1);
-          }
-          ++step;
+      auto take = [&] {
+        if (step == 0) {
+          if (lane == 0) taken = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
+        } else if (step == 1) {
+          k = __shfl_sync(0xffffffffu, taken, 0);
+          word = k < total ? fetch(k) : 0;
+        } else {
+          more = publish(n + 1);
         }
-        const bool has = id != -2 || (mine < per_tile && ((j * BN) >> g.page_shift) + mine < n_pages);
-        if (has && (id < 0 || id >= g.pages)) {
-          latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-          id = (int)g.pages;  // outside the tensor map: zeros
-        }
-        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, has)) * (uint32_t)box_rows * 128u;
-        const int token = (j * BN) & (g.page_size - 1);
-        const uint32_t at = (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u;
-        const int y = g.token_at == 0 ? token : g.head_at == 0 ? head : id;
-        const int z = g.token_at == 1 ? token : g.head_at == 1 ? head : id;
-        const int w = g.token_at == 2 ? token : g.head_at == 2 ? head : id;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          if (!wait(&empty[s], ph)) break;
-          if (lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
-          __syncwarp();
-          if (has) tma_load_4d(smem_u32(ring) + (uint32_t)s * TILE + at, kv ? &vmap : &kmap, half * 64, y, z, w, &full[s]);
-          ++fills;
-          if (++s == SLOTS) {
-            s = 0;
-            ph ^= 1u;
-          }
-        }
-        id = next;
-      }
-      if (dead) break;
-      if (step == 0 && lane == 0) taken = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
-      if (step <= 1) {
-        k = __shfl_sync(0xffffffffu, taken, 0);
-        word = k < total ? fetch(k) : 0;
-      }
-      if (step <= 2) more = publish(n + 1);
+        ++step;
+      };
+      stream(0, tiles, b, L, k % g.heads, j0, j1, [&](int j) {
+        if (j >= j1 - 4 && step < 3) take();
+      });
+      while (!dead && step < 3) take();
       if (dead) break;
     }
-    // nothing may land in shared memory after the CTA has left
-    for (int i = fills > SLOTS ? fills - SLOTS : 0; i < fills; ++i)
-      if (!mbar_wait(&full[i % SLOTS], (uint32_t)(i / SLOTS) & 1u, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
+    landed(0, tiles);
   } else if (warp < 11) {
     // ---------------- MMAs of a tile ----------------
     const int t = warp - 9;
@@ -586,14 +584,17 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (!mbar_wait(&drain[t], 0, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
     }
   } else {
-    // ---------------- rows of Q ----------------
-    int loads[2] = {0, 0};
+    // ---------------- rows of Q, and V ----------------
+    int loads[2] = {0, 0}, tiles = 0;
     for (int n = 0; !dead; ++n) {
       if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
       const Item it = items[n & 1];
       __syncwarp();
       if (lane == 0) mbar_arrive(&item_free[n & 1]);
       if (it.end) break;
+      // Q waits for the last item's last S; the first V has room before
+      const int jv = n > 0 ? min(it.j0 + 1, it.j1) : it.j0;
+      stream(1, tiles, it.b, it.L, it.head, it.j0, jv, [](int) {});
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if (dead || it.j0 >= (t ? it.e1 : it.e0)) continue;
@@ -607,8 +608,10 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         __syncwarp();
       }
+      stream(1, tiles, it.b, it.L, it.head, jv, it.j1, [](int) {});
     }
-    for (int t = 0; t < 2; ++t)  // as for K and V
+    landed(1, tiles);
+    for (int t = 0; t < 2; ++t)
       if (loads[t] && !mbar_wait(&q_full[t], (uint32_t)(loads[t] - 1) & 1u, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
   }
   } else {
