@@ -25,8 +25,8 @@
 //
 // Work: a first kernel (one CTA) reads the lengths, lists the items (later rows of a request first: they have
 // more keys) and cuts the last ones along the keys where whole items would leave SMs idle in the
-// last round: a piece writes its unnormalised sums, and the warp that comes last (a counter per 32 rows) adds up the
-// pieces in their order. Every wait is bounded; on timeout PIFA_ERR_TIMEOUT is latched and the CTA drains.
+// last round: a piece writes its unnormalised sums, and when all have, all warps add them up, in the order of the
+// keys. Every wait is bounded; on timeout PIFA_ERR_TIMEOUT is latched and the CTA drains.
 #include <cmath>
 
 #include <cuda_bf16.h>
@@ -45,6 +45,7 @@ constexpr int ROWS = 2 * BM;        // rows of an item (with those that a group'
 constexpr int BN = 128;             // keys of a tile
 constexpr int THREADS = 384;
 constexpr int PLAN_THREADS = 256;
+constexpr int MAX_REST = 512;       // items that may be cut: fewer than a round's, and one more for each head
 constexpr int MAX_PARTS = 456;      // pieces (times heads) that may leave partial sums: three for each SM
 constexpr int EARLY = 2;            // of four times 32 keys: those whose weights are handed to the MMAs first
 constexpr uint32_t HALF = BN * 128;  // 128 rows of 64 columns: 16 KB
@@ -64,21 +65,23 @@ struct Item {
   int L, q0, ahead;        // as Lengths
   int j0, j1, e0, e1;      // key tiles; the end of those that the rows of tile 0 and 1 see
   int part, parts;         // which piece of how many
-  int slot, counter;       // place of its partial sums, first of its counters (in the list: places of head 0, over heads)
+  int slot, pad;           // place of its partial sums (in the list: of head 0, over heads)
   int head, end;           // end: no item
 };
 
 struct Plan {
-  int next;          // items taken beyond the grid's first ones
+  int next;          // items taken; beyond the grid's first ones if no item is cut
   int entries;
-  int pad[6];
+  int cuts, pieces;  // items that are cut (over heads), and their pieces
+  int done;          // warps that have written a piece's sums
+  int pad[3];
 };
 
 struct TcArgs {
   uint16_t* o;
   const int32_t *table, *q_start, *kv_len;
   Plan* plan;
-  int* counters;
+  int* splits;        // the first entry of each item that is cut
   Item* list;
   float* partial;
   int64_t ldo, ldt, pages;
@@ -141,15 +144,14 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   Lengths* len = reinterpret_cast<Lengths*>(plan_smem);          // B
   int* first = reinterpret_cast<int*>(plan_smem + (size_t)g.B * sizeof(Lengths));  // B + 1: first item of each request
   __shared__ unsigned long long part[PLAN_THREADS / 32];
-  __shared__ int red[4];          // largest and smallest item; of those that may be cut, the largest and the sum
-  __shared__ unsigned long long sum_all;  // of all items
+  __shared__ int rest_cost[MAX_REST], whole_most;
+  __shared__ unsigned long long whole_sum;
   __shared__ int cut;             // key tiles of a piece
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31;
   if (tid == 0) {
-    red[0] = red[2] = red[3] = 0;
-    red[1] = 0x7fffffff;
-    sum_all = 0;
+    whole_most = 0;
+    whole_sum = 0;
   }
   pdl_wait_primary();
   bool over = false;
@@ -170,7 +172,6 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   }
   if (tid == 0) first[g.B] = items;
   if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
-  for (int i = tid; i < MAX_PARTS / 2 * 8; i += PLAN_THREADS) g.counters[i] = 0;
   __syncthreads();
 
   // the item at place k of the list, later rows of a request first, and its cost in key tiles
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     return max(x.e0, x.e1);
   };
   // Whole rounds of the grid stay whole; the items of the last, unfilled round may be cut.
-  const int whole = (int)((int64_t)items * g.heads / grid * grid / g.heads);
+  const int whole = (int)((int64_t)items * g.heads / grid * grid / g.heads), rest = items - whole;
   Item x;
   int cost = 0;
   for (int k0 = 0; k0 < items; k0 += PLAN_THREADS) {
@@ -201,34 +202,41 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     const bool here = k < items;
     if (!__any_sync(0xffffffffu, here)) break;
     if (here) cost = item_at(k, x);
-    const int most = __reduce_max_sync(0xffffffffu, here ? cost : 0);
-    const int least = __reduce_min_sync(0xffffffffu, here ? cost : 0x7fffffff);
-    const int most_cut = __reduce_max_sync(0xffffffffu, here && k >= whole ? cost : 0);
-    const int sum_cut = __reduce_add_sync(0xffffffffu, here && k >= whole ? cost : 0);
-    const int sum = __reduce_add_sync(0xffffffffu, here ? cost : 0);
+    if (here && k >= whole && k - whole < MAX_REST) rest_cost[k - whole] = cost;
+    const int whole_cost = here && k < whole ? cost : 0;
+    const int most = __reduce_max_sync(0xffffffffu, whole_cost), sum = __reduce_add_sync(0xffffffffu, whole_cost);
     if (lane == 0) {
-      atomicMax(&red[0], most);
-      atomicMin(&red[1], least);
-      atomicMax(&red[2], most_cut);
-      atomicAdd(&red[3], sum_cut);
-      atomicAdd(&sum_all, (unsigned long long)sum);
+      atomicMax(&whole_most, most);
+      atomicAdd(&whole_sum, (unsigned long long)sum);
     }
   }
   __syncthreads();
   if (tid < 32) {
-    // The time of all, in key tiles, if those items are cut into pieces of `size`: an even share for each CTA,
-    // and, where items are alike, the wait for a last round of pieces that does not fill the grid. An item or
-    // piece costs about two tiles on top (rows of Q, first and last products), one with partial sums three.
-    const int rest = items - whole;
-    const int size = max((red[2] + tid) / (tid + 1), 1);
-    const float alike = red[0] > 0 ? (float)red[1] / (float)red[0] : 0.0f;
-    const float pieces = tid == 0 ? (float)rest : (float)rest * 0.5f + (float)red[3] / (float)size;
-    const float extra = tid == 0 ? 2.0f : 3.0f, per_cta = (float)g.heads / (float)grid;
-    const float rounds = pieces * per_cta;
-    float t = ((float)sum_all + 2.0f * (float)whole + extra * pieces) * per_cta +
-              alike * (ceilf(rounds) - rounds) * ((float)size + extra);
-    t = fmaxf(t, (float)size + extra);
-    if (tid > 0 && (int64_t)(rest + red[3] / size) * g.heads > MAX_PARTS) t = 3e38f;  // more than there is room for
+    // The time, in key tiles, if the longest of those items is cut into `want` pieces and the others into pieces
+    // no longer: one round if there is a CTA for each piece; else an even share for every CTA, and the wait for
+    // the last pieces: of alike ones, what is left of their last round, of unlike ones about half a piece. An item
+    // costs about two tiles on top (rows of Q, first and last products), a piece with partial sums six.
+    int longest = 0;
+    for (int i = 0; i < min(rest, MAX_REST); ++i) longest = max(longest, rest_cost[i]);
+    const int want = tid < 16 ? tid + 1 : (int)(16.0f * exp2f(0.21f * (float)(tid - 15)));
+    const int size = max((longest + want - 1) / want, 1);
+    int pieces = 0, most = 0;
+    float work = 0.0f;
+    for (int i = 0; i < min(rest, MAX_REST); ++i) {
+      const int c = rest_cost[i], n = max((c + size - 1) / size, 1);
+      const float extra = n > 1 ? 6.0f : 2.0f;
+      pieces += n;
+      most = max(most, (c + n - 1) / n + (int)extra);
+      work += (float)c + extra * (float)n;
+    }
+    const float jobs = (float)pieces * (float)g.heads, rounds = jobs / (float)grid;
+    const float alike = pieces ? work / ((float)pieces * (float)most) : 0.0f;
+    const float share = (work + (float)whole_sum + 2.0f * (float)whole) * (float)g.heads / (float)grid;
+    float t = whole == 0 && rounds <= 1.0f ? (float)most
+                                            : share + (float)most * (alike * (ceilf(rounds) - rounds) + (1.0f - alike) * 0.5f);
+    t = fmaxf(t, fmaxf((float)most, (float)(whole_most + 2)));
+    // more than there is room for
+    if (tid > 0 && ((int64_t)pieces * g.heads > MAX_PARTS || rest > MAX_REST || want > longest)) t = 3e38f;
     int who = tid;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   }
   __syncthreads();
   const int size = cut;
-  unsigned long long done = 0;  // entries, from bit 32 on; partial-sum places, from bit 16 on; counters
+  unsigned long long done = 0;  // entries, from bit 32 on; partial-sum places, from bit 16 on; cut items
   for (int k0 = 0; k0 < items; k0 += PLAN_THREADS) {
     const int k = k0 + tid;
     int pieces = 0;
@@ -263,18 +271,18 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
       e.part = p;
       e.parts = pieces;
       e.slot = (int)(at >> 16 & 0xffffu) + p;
-      e.counter = (int)(at & 0xffffu);
-      e.head = e.end = 0;
+      e.pad = e.head = e.end = 0;
       int4* to = reinterpret_cast<int4*>(g.list + (at >> 32) + p);
       const int4* from = reinterpret_cast<const int4*>(&e);
 #pragma unroll
       for (int i = 0; i < 4; ++i) to[i] = from[i];
     }
+    if (pieces > 1) g.splits[at & 0xffffu] = (int)(at >> 32);
     done += total;
   }
   if (tid == 0) {
-    g.plan->next = 0;
-    g.plan->entries = (int)(done >> 32);
+    const Plan p = {0, (int)(done >> 32), (int)(done & 0xffffu), (int)(done >> 16 & 0xffffu), 0, {0, 0, 0}};
+    *g.plan = p;
   }
 }
 
@@ -430,12 +438,19 @@ __global__ void __launch_bounds__(THREADS, 1)
     auto fetch = [&](int k) { return lane < 16 ? __ldcg(reinterpret_cast<const int*>(g.list + k / g.heads) + lane) : 0; };
     int k = (int)blockIdx.x, word = fetch(k);
     const int total = __ldcg(&g.plan->entries) * g.heads;
+    // With cut items the first one comes from the queue too: a CTA that does not run yet must hold no piece, since
+    // the others wait for all pieces at the end.
+    const int ahead = __ldcg(&g.plan->cuts) > 0 ? 0 : (int)gridDim.x;
+    if (ahead == 0) {
+      if (lane == 0) k = atomicAdd(&g.plan->next, 1);
+      k = __shfl_sync(0xffffffffu, k, 0);
+      word = k < total ? fetch(k) : 0;
+    }
     // Item n for all: false after the last, or if the wait for its place ran out.
     auto publish = [&](int n) {
       if (!wait(&item_free[n & 1], (((uint32_t)n >> 1) & 1u) ^ 1u)) return false;
       const int head = k % g.heads;
       if (lane == 12) word = word * g.heads + head;
-      if (lane == 13) word = (word * g.heads + head) * 8;
       if (lane == 14) word = head;
       if (lane == 15) word = k >= total;
       if (lane < 16) reinterpret_cast<int*>(&items[n & 1])[lane] = word;
@@ -452,7 +467,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       int step = 0, taken = 0;
       auto take = [&] {
         if (step == 0) {
-          if (lane == 0) taken = (int)gridDim.x + atomicAdd(&g.plan->next, 1);
+          if (lane == 0) taken = ahead + atomicAdd(&g.plan->next, 1);
         } else if (step == 1) {
           k = __shfl_sync(0xffffffffu, taken, 0);
           word = k < total ? fetch(k) : 0;
@@ -726,7 +741,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         o_ph ^= 1u;
         tc_fence_after();
       }
-      if (idle) continue;
+      if (idle && it.parts == 1) continue;
       uint16_t* out = g.o + (int64_t)(it.q0 + token) * g.ldo + (int64_t)(it.head * g.group + h) * D;
       auto store = [&](int i, const float* x) {  // 32 columns
 #pragma unroll
@@ -752,64 +767,102 @@ __global__ void __launch_bounds__(THREADS, 1)
       } else {
         // This piece's sums: for each 32 rows, four columns of them at a time, so that a warp's accesses are whole.
         const int w8 = t * 4 + quarter;
-        auto slot_of = [&](int p) { return g.partial + (int64_t)(it.slot + (p - it.part) * g.heads) * C::PART_FLOATS; };
-        float* mine = slot_of(it.part);
+        float* mine = g.partial + (int64_t)it.slot * C::PART_FLOATS;
+        if (!idle) {
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32] = {};
-          if (any) {
-            tmem_ld_32x32b_x32(o_at + i * 32, o);
-            tmem_ld_wait();
-          }
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            __stcg(reinterpret_cast<uint4*>(mine) + (w8 * (D / 4) + i * 8 + k) * 32 + lane,
-                   make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
-        }
-        __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, make_float2(m * c, l));
-        __threadfence();
-        __syncwarp();
-        int before = 0;
-        if (lane == 0) before = atomicAdd(&g.counters[it.counter + w8], 1);
-        before = __shfl_sync(0xffffffffu, before, 0);
-        if (before == it.parts - 1) {  // the last piece of these 32 rows: add up all in their order
-          __threadfence();
-          const float* from = slot_of(0);
-          const int64_t pitch = (int64_t)g.heads * C::PART_FLOATS;
-          auto ml_of = [&](int p) { return __ldcg(reinterpret_cast<const float2*>(from + p * pitch + ROWS * D) + w8 * 32 + lane); };
-          float top = -INFINITY, all = 0.0f;
-#pragma unroll 8
-          for (int p = 0; p < it.parts; ++p) {
-            const float2 ml = ml_of(p);
-            top = fmaxf(top, ml.y != 0.0f ? ml.x : -INFINITY);
-          }
-          if (top == -INFINITY) top = 0.0f;
-          auto weight = [&](const float2& ml) { return ml.y != 0.0f ? fast_exp2(ml.x - top) : 0.0f; };  // nothing seen: O is zero
-#pragma unroll 8
-          for (int p = 0; p < it.parts; ++p) {
-            const float2 ml = ml_of(p);
-            all += ml.y * weight(ml);
-          }
-          const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-#pragma unroll 1
           for (int i = 0; i < D / 32; ++i) {
-            float x[32] = {};
-#pragma unroll 3
-            for (int p = 0; p < it.parts; ++p) {
-              const float f = weight(ml_of(p)) * inv;
-              const float4* o = reinterpret_cast<const float4*>(from + p * pitch) + (w8 * (D / 4) + i * 8) * 32 + lane;
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float4 y = __ldcg(o + k * 32);
-                x[4 * k] += f * y.x;
-                x[4 * k + 1] += f * y.y;
-                x[4 * k + 2] += f * y.z;
-                x[4 * k + 3] += f * y.w;
-              }
+            uint32_t o[32] = {};
+            if (any) {
+              tmem_ld_32x32b_x32(o_at + i * 32, o);
+              tmem_ld_wait();
             }
-            if (real) store(i, x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              __stcg(reinterpret_cast<uint4*>(mine) + (w8 * (D / 4) + i * 8 + k) * 32 + lane,
+                     make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
           }
+          __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, make_float2(m * c, l));
+          __threadfence();
           __syncwarp();
+        }
+        if (lane == 0) atomicAdd(&g.plan->done, 1);
+      }
+    }
+    // ---------------- the pieces' sums ----------------
+    // Every piece has been taken by a CTA that runs, so this ends; then all warps share 32 rows x 32 columns at a time.
+    // (The last warp of an item doing it alone was bound by what one SM can read.)
+    const int cuts = dead ? 0 : __ldcg(&g.plan->cuts);
+    if (cuts > 0) {
+      const int all_done = __ldcg(&g.plan->pieces) * g.heads * 8;
+      const uint64_t t0 = globaltimer_ns();
+      int seen = 0;
+      while (true) {
+        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(&g.plan->done) : "memory");
+        if (seen >= all_done) break;
+        if (globaltimer_ns() - t0 > g.timeout_ns) {
+          latch_status(g.status, PIFA_ERR_TIMEOUT);
+          break;
+        }
+        __nanosleep(40);
+      }
+      const bool ready = __all_sync(0xffffffffu, seen >= all_done);
+      const int tasks = ready ? cuts * g.heads * 8 * (D / 32) : 0;
+      for (int k = warp * (int)gridDim.x + (int)blockIdx.x; k < tasks; k += 8 * (int)gridDim.x) {
+        const int i = k % (D / 32), w8 = k / (D / 32) % 8, which = k / (D / 32 * 8), head = which % g.heads;
+        const Item* at = g.list + g.splits[which / g.heads];
+        const int tok0 = __ldcg(&at->tok0), n_tok = __ldcg(&at->n), q0 = __ldcg(&at->q0), parts = __ldcg(&at->parts);
+        const int row = w8 % 4 * 32 + lane, tok = row / g.group, h = row - tok * g.group;
+        const int token = tok0 + w8 / 4 * g.tpt + tok;
+        const bool real = tok < g.tpt && token < n_tok;
+        if (!__any_sync(0xffffffffu, real)) continue;
+        const float* from = g.partial + ((int64_t)__ldcg(&at->slot) * g.heads + head) * C::PART_FLOATS;
+        const int64_t pitch = (int64_t)g.heads * C::PART_FLOATS;
+        constexpr int FLIGHT = 4;  // pieces and their weights in flight
+        float x[32] = {}, top = -INFINITY, all = 0.0f;
+#pragma unroll 1
+        for (int p0 = 0; p0 < parts; p0 += FLIGHT) {
+          float2 ml[FLIGHT];
+          float4 o[FLIGHT][8];
+#pragma unroll
+          for (int p = 0; p < FLIGHT; ++p) {
+            const float* piece = from + min(p0 + p, parts - 1) * pitch;
+            ml[p] = __ldcg(reinterpret_cast<const float2*>(piece + ROWS * D) + w8 * 32 + lane);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              o[p][q] = __ldcg(reinterpret_cast<const float4*>(piece) + (w8 * (D / 4) + i * 8 + q) * 32 + lane);
+          }
+          float most = top;
+#pragma unroll
+          for (int p = 0; p < FLIGHT; ++p) {
+            if (p0 + p >= parts) ml[p].y = 0.0f;  // a piece that is not there; nothing seen: O is zero
+            if (ml[p].y != 0.0f) most = fmaxf(most, ml[p].x);
+          }
+          const float old = top > -INFINITY ? fast_exp2(top - most) : 0.0f;
+          top = most;
+          all *= old;
+#pragma unroll
+          for (int q = 0; q < 32; ++q) x[q] *= old;
+#pragma unroll
+          for (int p = 0; p < FLIGHT; ++p) {
+            const float f = ml[p].y != 0.0f ? fast_exp2(ml[p].x - top) : 0.0f;
+            all += ml[p].y * f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              x[4 * q] += f * o[p][q].x;
+              x[4 * q + 1] += f * o[p][q].y;
+              x[4 * q + 2] += f * o[p][q].z;
+              x[4 * q + 3] += f * o[p][q].w;
+            }
+          }
+        }
+        const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+        uint16_t* out = g.o + (int64_t)(q0 + token) * g.ldo + (int64_t)(head * g.group + h) * D + i * 32;
+        if (real) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<uint4*>(out + q * 8) =
+                make_uint4(pack<F16>(x[8 * q] * inv, x[8 * q + 1] * inv), pack<F16>(x[8 * q + 2] * inv, x[8 * q + 3] * inv),
+                           pack<F16>(x[8 * q + 4] * inv, x[8 * q + 5] * inv), pack<F16>(x[8 * q + 6] * inv, x[8 * q + 7] * inv));
         }
       }
     }
@@ -829,13 +882,13 @@ int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t list_bytes(int64_t T, int64_t group, int64_t B) {
   return round256((T / (2 * (BM / group)) + 1 + B + MAX_PARTS) * (int64_t)sizeof(Item));
 }
-constexpr int64_t kCounterBytes = MAX_PARTS / 2 * 8 * 4 + 256;  // the plan's head, then the counters
+constexpr int64_t kPlanBytes = MAX_PARTS / 2 * 4 + 256;  // struct Plan, then the cut items
 
 }  // namespace
 
 int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B) {
   const int64_t part = (dim == 64 ? Cfg<64>::PART_FLOATS : Cfg<128>::PART_FLOATS) * 4;
-  return round256(kCounterBytes) + list_bytes(T, q_heads / kv_heads, B) + MAX_PARTS * part;
+  return round256(kPlanBytes) + list_bytes(T, q_heads / kv_heads, B) + MAX_PARTS * part;
 }
 
 int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream) {
@@ -847,9 +900,9 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   g.q_start = a.q_start;
   g.kv_len = a.kv_len;
   g.plan = reinterpret_cast<Plan*>(ws);
-  g.counters = reinterpret_cast<int*>(ws + 256);
-  g.list = reinterpret_cast<Item*>(ws + round256(kCounterBytes));
-  g.partial = reinterpret_cast<float*>(ws + round256(kCounterBytes) + list_bytes(a.T, group, a.B));
+  g.splits = reinterpret_cast<int*>(ws + 256);
+  g.list = reinterpret_cast<Item*>(ws + round256(kPlanBytes));
+  g.partial = reinterpret_cast<float*>(ws + round256(kPlanBytes) + list_bytes(a.T, group, a.B));
   g.ldo = a.ldo;
   g.ldt = a.ldt;
   g.pages = a.cache.pages;
