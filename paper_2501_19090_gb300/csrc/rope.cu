@@ -69,6 +69,30 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeArgs g) {
   pdl_wait_primary();
   const int t0 = (int)blockIdx.x * g.tokens, nt = min(g.tokens, g.T - t0);
   const int pairs = g.rot / 2;
+  const int units = g.dim / 16, turned = g.rot / 16;
+  const int h0 = (int)blockIdx.y * g.heads, nh = min(g.heads, g.hq + 2 * g.hk - h0), n = nt * nh * units;
+  // a unit's two vectors: halves of the turned part, or neighbours; those of a thread's next unit are in flight
+  // while it works on one, the first ones while the CTA computes its cosines and sines
+  struct Unit {
+    int tt, h, u, a0, a1;
+    uint4 va, vb;
+  } next;
+  auto fetch = [&](int i) {
+    const int hh = i / units;
+    next.u = i - hh * units;
+    next.tt = hh / nh;
+    next.h = h0 + hh - next.tt * nh;
+    const int64_t t = t0 + next.tt;
+    const uint16_t* src = next.h < g.hq           ? g.q + t * g.ldq + (int64_t)next.h * g.dim
+                          : next.h < g.hq + g.hk ? g.k + t * g.ldk + (int64_t)(next.h - g.hq) * g.dim
+                                                  : g.v + t * g.ldv + (int64_t)(next.h - g.hq - g.hk) * g.dim;
+    const bool apart = HALF && next.u < turned;
+    next.a0 = apart ? next.u * 8 : next.u * 16;
+    next.a1 = apart ? next.u * 8 + pairs : next.u * 16 + 8;
+    next.va = *reinterpret_cast<const uint4*>(src + next.a0);
+    next.vb = *reinterpret_cast<const uint4*>(src + next.a1);
+  };
+  if ((int)threadIdx.x < n) fetch(threadIdx.x);
   for (int i = threadIdx.x; i < nt * pairs; i += THREADS) {
     const int tt = i / pairs, p = i - tt * pairs;
     const uint64_t phase = (uint64_t)(int64_t)g.positions[t0 + tt] * (uint64_t)g.freq[p];
@@ -89,40 +113,30 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeArgs g) {
   }
   __syncthreads();
 
-  const int units = g.dim / 16, turned = g.rot / 16;
-  const int h0 = (int)blockIdx.y * g.heads, nh = min(g.heads, g.hq + 2 * g.hk - h0);
-  for (int i = threadIdx.x; i < nt * nh * units; i += THREADS) {
-    const int hh = i / units, u = i - hh * units;
-    const int tt = hh / nh, h = h0 + hh - tt * nh;
-    const int64_t t = t0 + tt;
-    const uint16_t* src;
+  for (int i = threadIdx.x; i < n; i += THREADS) {
+    Unit x = next;
+    if (i + THREADS < n) fetch(i + THREADS);
     uint16_t* dst;
-    if (h < g.hq) {
-      src = g.q + t * g.ldq + (int64_t)h * g.dim;
-      dst = g.qr + t * g.ldqr + (int64_t)h * g.dim;
+    if (x.h < g.hq) {
+      dst = g.qr + (int64_t)(t0 + x.tt) * g.ldqr + (int64_t)x.h * g.dim;
     } else {
-      const bool is_v = h >= g.hq + g.hk;
-      const int kh = h - g.hq - (is_v ? g.hk : 0);
-      const int64_t at = place[tt];
+      const bool is_v = x.h >= g.hq + g.hk;
+      const int64_t at = place[x.tt];
       if (at < 0) continue;
-      src = is_v ? g.v + t * g.ldv + (int64_t)kh * g.dim : g.k + t * g.ldk + (int64_t)kh * g.dim;
-      dst = (is_v ? g.vc : g.kc) + at + kh * g.head_stride;
+      dst = (is_v ? g.vc : g.kc) + at + (x.h - g.hq - (is_v ? g.hk : 0)) * g.head_stride;
     }
-    const bool turns = u < turned && h < g.hq + g.hk;
-    // the unit's two vectors: halves of the turned part, or neighbours
-    const int a0 = HALF && u < turned ? u * 8 : u * 16, a1 = HALF && u < turned ? u * 8 + pairs : u * 16 + 8;
-    uint4 va = *reinterpret_cast<const uint4*>(src + a0), vb = *reinterpret_cast<const uint4*>(src + a1);
+    const bool turns = x.u < turned && x.h < g.hq + g.hk;
     if (turns) {
-      uint32_t* wa = reinterpret_cast<uint32_t*>(&va);
-      uint32_t* wb = reinterpret_cast<uint32_t*>(&vb);
-      const float4* cs = reinterpret_cast<const float4*>(&turn[tt][u * 8]);  // two pairs a float4
+      uint32_t* wa = reinterpret_cast<uint32_t*>(&x.va);
+      uint32_t* wb = reinterpret_cast<uint32_t*>(&x.vb);
+      const float4* cs = reinterpret_cast<const float4*>(&turn[x.tt][x.u * 8]);  // two pairs a float4
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float4 r = cs[j];
         if constexpr (HALF) {
-          const float2 x = unpack<F16>(wa[j]), y = unpack<F16>(wb[j]);
-          wa[j] = pack<F16>(x.x * r.x - y.x * r.y, x.y * r.z - y.y * r.w);
-          wb[j] = pack<F16>(y.x * r.x + x.x * r.y, y.y * r.z + x.y * r.w);
+          const float2 v = unpack<F16>(wa[j]), y = unpack<F16>(wb[j]);
+          wa[j] = pack<F16>(v.x * r.x - y.x * r.y, v.y * r.z - y.y * r.w);
+          wb[j] = pack<F16>(y.x * r.x + v.x * r.y, y.y * r.z + v.y * r.w);
         } else {
           uint32_t* w = (j < 2 ? wa : wb) + 2 * (j & 1);
           const float2 p = unpack<F16>(w[0]), q = unpack<F16>(w[1]);
@@ -131,8 +145,8 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeArgs g) {
         }
       }
     }
-    *reinterpret_cast<uint4*>(dst + a0) = va;
-    *reinterpret_cast<uint4*>(dst + a1) = vb;
+    *reinterpret_cast<uint4*>(dst + x.a0) = x.va;
+    *reinterpret_cast<uint4*>(dst + x.a1) = x.vb;
   }
 }
 
@@ -155,10 +169,11 @@ int launch(RopeArgs g, int dtype, int layout, void* cuda_stream) {
   cudaError_t e = cudaSuccess;
   g.status = pifa_status_word(&e);
   if (!g.status) return pifa_fail_cuda("device status word", e);
-  // Whole tokens, MAX_TOKENS to a CTA once every SM has eight such CTAs; few tokens: the heads of one are
-  // dealt to CTAs until those make two for every SM, one unit for a thread at the finest.
-  const int nh = g.hq + 2 * g.hk, sms = pifa_sm_count();
-  g.tokens = g.T >= 8 * MAX_TOKENS * sms ? MAX_TOKENS : 1;
+  // Whole tokens, as many to a CTA as make one round of the five CTAs that an SM holds, up to MAX_TOKENS (2048 tokens
+  // of 32 heads, forward and gradient: 16.1 us; one to a CTA 19.3). Few tokens: the heads of one are dealt to CTAs until
+  // those make two for every SM, one unit for a thread at the finest.
+  const int nh = g.hq + 2 * g.hk, sms = pifa_sm_count(), round = 5 * sms;
+  g.tokens = g.T > round * MAX_TOKENS ? MAX_TOKENS : (g.T + round - 1) / round;
   const int finest = (nh * (g.dim / 16) + THREADS - 1) / THREADS, wanted = (2 * sms + g.T - 1) / g.T;
   const int parts = finest < wanted ? finest : wanted;
   g.heads = (nh + parts - 1) / parts;
