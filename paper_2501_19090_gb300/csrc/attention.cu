@@ -348,16 +348,19 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   }
 }
 
-// Adds up the pieces of a request's head whose steps fell to several warps, in the order of the keys: a CTA for
-// each, a thread for four columns of a row, or, where there are few rows, several threads with every so many-th
-// piece. Pieces and their weights are loaded together, four at a time: the kernel is two latencies long.
+// Adds up the pieces of a request's head whose steps fell to several warps, in the order of the keys: `split` CTAs
+// for each, a share of the columns apiece, a thread for four columns of a row, up to eight threads with every
+// so many-th piece where a CTA has fewer of those. Pieces and their weights are loaded together, four at a time: with few
+// pieces the kernel is two latencies long, and one long sequence (144 pieces of each head) spreads over the SMs (64
+// heads, 8 key / value heads, 16000 keys: 63 -> 33 us).
 template <bool F16, int D>
-__global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g) {
+__global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int split) {
   __shared__ float2 sh_ml[THREADS];
   __shared__ float4 sh_o[THREADS];
   pdl_launch_dependents();
-  const int b = (int)blockIdx.x / g.heads, head = (int)blockIdx.x - b * g.heads;
-  const int slots = g.max_rows * (D / 4), groups = max(THREADS / slots, 1);
+  const int item = (int)blockIdx.x / split, b = item / g.heads, head = item - b * g.heads;
+  const int quads = D / 4 / split, col0 = ((int)blockIdx.x - item * split) * quads * 4;  // of this CTA: fours of columns, first one
+  const int slots = g.max_rows * quads, groups = min(max(THREADS / slots, 1), 8);
   pdl_wait_primary();
   const Lengths x = lengths_of(g, b);
   const int run = g.sums[g.B + 1], steps = steps_of(x), from = g.sums[b] + head * steps;
@@ -366,7 +369,7 @@ __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g) {
   if (w0 == w1) return;  // the warp has finished it
   const int place = g.max_rows * (D + 2);  // a warp has two: the head that began before its run, and the last one
   for (int slot = (int)threadIdx.x % (slots * groups); slot < slots * groups; slot += THREADS) {
-    const int group = slot / slots, row = (slot - group * slots) / (D / 4), col = (slot - group * slots) % (D / 4) * 4;
+    const int group = slot / slots, row = (slot - group * slots) / quads, col = col0 + (slot - group * slots) % quads * 4;
     const bool here = row < x.n * g.group && (int)threadIdx.x < slots * groups;
     float top = -INFINITY, all = 0.0f;
     float4 acc = make_float4(0, 0, 0, 0);
@@ -478,8 +481,11 @@ cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
   if (e == cudaSuccess) e = pifa_launch_ex(&cfg, attention_rows<F16, D>, g);
   if (e != cudaSuccess) return e;
   cfg.dynamicSmemBytes = 0;
-  cfg.gridDim = dim3((unsigned)(g.B * g.heads));
-  return pifa_launch_ex(&cfg, attention_join<F16, D>, g);
+  const int64_t items = (int64_t)g.B * g.heads;
+  int split = 1;
+  while (split < 8 && items * split * 2 <= 8 * sms && g.max_rows * (D / 4) / (split * 2) >= THREADS / 8) split *= 2;
+  cfg.gridDim = dim3((unsigned)(items * split));
+  return pifa_launch_ex(&cfg, attention_join<F16, D>, g, split);
 }
 
 }  // namespace
