@@ -472,3 +472,18 @@ def test_attention_in_a_graph_and_on_a_stream():
         O2 = attend(b)
     stream.synchronize()
     assert torch.equal(O, O2)
+
+
+@pytest.mark.parametrize("width,heads", [(512, 4), (1024, 16)])
+def test_the_example_serves_prompts_and_decode_steps(width, heads):
+    """PIFA projections, page tables, rotation with the cache write and attention together, the decode step as a replayed
+    graph. The bf16 values between the calls (x, q, k, v, o) carry relative errors of 2^-9 rms each: within 4%
+    of the outputs' rms at the largest of some thousands of elements (4.5 sigma of about 2^-7)."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "attention_block.py")
+    spec = importlib.util.spec_from_file_location("attention_block", path)
+    block = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(block)
+    error, _, _ = block.serve(width=width, heads=heads, requests=5, prompt=83, steps=20)
+    assert error < 0.04
