@@ -464,15 +464,21 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
  *                PIFA_ERR_CAPACITY; keys of a page outside [0, pages) read as zeros and latch
  *                PIFA_ERR_DEVICE_INDEX.
  *   q_start      DEVICE, int32[B + 1], ascending from 0; kv_len DEVICE, int32[B].
- *   max_q        at least every request's number of new tokens, at least 1 (host): picks the kernel. A request with more
+ *   max_q        at least every request's number of new tokens, at least 1 (host): picks the kernel (group max_q <= 16
+ *                rows: streamed by warps; more: on the tensor cores). A request with more
  *                latches PIFA_ERR_CAPACITY and its further rows are not written.
  *   workspace    DEVICE scratch of pifa_paged_attention_workspace_size() bytes, 256-byte aligned, no
  *                initialisation needed.
  *   head_dim 64 or 128; page_size a power of two from 16 to 256; q_heads a multiple of kv_heads, at most 64 query heads to a
  *   key / value head; B <= 4096 (PIFA_ERR_UNSUPPORTED).
- *   What the cache holds past a request's kv_len, or in pages of no request, is not used, whatever its bits.
- *   Numerics: fp32 scores, running maximum and sums; the weights enter the second product in dtype, scaled to at
- *   most 1, O is rounded once. Results do not depend on the order in which blocks run.
+ *   What the cache holds past a request's kv_len, or in pages of no request, is not used, whatever its bits. A key
+ *   that some new token of its request sees is part of that request's products: an infinity or NaN in its V
+ *   may reach the request's other new tokens too (0 times infinity). A K that is not finite stays with the tokens
+ *   that see it.
+ *   Numerics: fp32 scores, running maximum and sums; the weights enter the second product in dtype, at most 2^8 (the
+ *   maximum that they refer to is raised when a score passes it by 8 in the exponent), O is rounded once. Results
+ *   do not depend on the order in which blocks run; where the keys are cut, and with it the last bits, follows
+ *   from the lengths of all requests of the call.
  */
 int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                          int dtype, const void* k_cache, const void* v_cache, int64_t pages, int64_t page_size,
@@ -481,8 +487,9 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
                          const int32_t* q_start, const int32_t* kv_len, int64_t B, int64_t max_q, float scale,
                          void* O, int64_t ldo, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
-/* pifa_paged_attention_workspace_size -- bytes of device scratch pifa_paged_attention needs; negative
- * pifa_status on bad arguments. */
+/* pifa_paged_attention_workspace_size -- bytes of device scratch pifa_paged_attention needs: with max_q and group =
+ * q_heads / kv_heads, 1.3 MB for each of group max_q <= 16 rows, else about 60 MB (head_dim 64: half). Negative pifa_status
+ * on bad arguments. Pure host arithmetic. */
 int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
                                             int64_t max_q);
 

@@ -98,7 +98,8 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeArgs g) {
     const uint64_t phase = (uint64_t)(int64_t)g.positions[t0 + tt] * (uint64_t)g.freq[p];
     float s, c;
     sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);
-    turn[tt][p] = make_float2(c * g.scale, (g.inverse ? -s : s) * g.scale);
+    // two pairs make a float4; those that a unit's lanes read together lie together
+    turn[tt][2 * ((p & 7) / 2 * turned + p / 8) + (p & 1)] = make_float2(c * g.scale, (g.inverse ? -s : s) * g.scale);
   }
   if (g.hk && threadIdx.x < nt) {
     const int64_t slot = g.slots[t0 + threadIdx.x];
@@ -129,10 +130,10 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeArgs g) {
     if (turns) {
       uint32_t* wa = reinterpret_cast<uint32_t*>(&x.va);
       uint32_t* wb = reinterpret_cast<uint32_t*>(&x.vb);
-      const float4* cs = reinterpret_cast<const float4*>(&turn[x.tt][x.u * 8]);  // two pairs a float4
+      const float4* cs = reinterpret_cast<const float4*>(turn[x.tt]) + x.u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float4 r = cs[j];
+        const float4 r = cs[j * turned];
         if constexpr (HALF) {
           const float2 v = unpack<F16>(wa[j]), y = unpack<F16>(wb[j]);
           wa[j] = pack<F16>(v.x * r.x - y.x * r.y, v.y * r.z - y.y * r.w);
