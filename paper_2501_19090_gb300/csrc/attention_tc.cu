@@ -90,6 +90,7 @@ struct TcArgs {
   int token_at, head_at, page_at;    // their places among the tensor maps' coordinates 1 to 3
   float c;                           // |scale| log2(e)
   int negate;                        // scale < 0
+  int wide;                          // rows of O start on 32-byte sectors
   int* status;
   uint64_t timeout_ns;
 };
@@ -312,6 +313,21 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   } else {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
+  }
+}
+
+// 32 columns of a row that the thread owns: whole 32-byte sectors where all rows start on one.
+template <bool F16>
+__device__ __forceinline__ void store_row(uint16_t* out, const float* x, bool wide) {
+  uint32_t w[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) w[k] = pack<F16>(x[2 * k], x[2 * k + 1]);
+  if (wide) {
+    stg256(out, w);
+    stg256(out + 16, w + 8);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(out + 8 * k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
   }
 }
 
@@ -678,6 +694,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(&p_full[2 * t + i]);
           };
+          bool fresh = j == it.j0;  // no maximum yet
 #pragma unroll 1
           while (true) {
 #pragma unroll
@@ -698,10 +715,13 @@ __global__ void __launch_bounds__(THREADS, 1)
               for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
             }
             const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
-            sum[0] = sum[1] = 0;
+            if (!fresh) {
+              sum[0] = sum[1] = 0;
 #pragma unroll
-            for (int i = 0; i < EARLY; ++i) weights(i);
-            if (!__any_sync(0xffffffffu, (top - m) * c > 8.0f)) break;
+              for (int i = 0; i < EARLY; ++i) weights(i);
+              if (!__any_sync(0xffffffffu, (top - m) * c > 8.0f)) break;
+            }
+            fresh = false;
             const float up = fmaxf(m, top);
             const float f = m > -INFINITY ? fast_exp2((m - up) * c) : 1.0f;  // (nothing was seen before: zeros)
             m = up;
@@ -743,13 +763,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (idle && it.parts == 1) continue;
       uint16_t* out = g.o + (int64_t)(it.q0 + token) * g.ldo + (int64_t)(it.head * g.group + h) * D;
-      auto store = [&](int i, const float* x) {  // 32 columns
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          *reinterpret_cast<uint4*>(out + i * 32 + k * 8) =
-              make_uint4(pack<F16>(x[8 * k], x[8 * k + 1]), pack<F16>(x[8 * k + 2], x[8 * k + 3]),
-                         pack<F16>(x[8 * k + 4], x[8 * k + 5]), pack<F16>(x[8 * k + 6], x[8 * k + 7]));
-      };
+      auto store = [&](int i, const float* x) { store_row<F16>(out + i * 32, x, g.wide); };
       if (it.parts == 1) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
@@ -857,13 +871,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         const float inv = all == 0.0f ? 0.0f : 1.0f / all;
         uint16_t* out = g.o + (int64_t)(q0 + token) * g.ldo + (int64_t)(head * g.group + h) * D + i * 32;
-        if (real) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<uint4*>(out + q * 8) =
-                make_uint4(pack<F16>(x[8 * q] * inv, x[8 * q + 1] * inv), pack<F16>(x[8 * q + 2] * inv, x[8 * q + 3] * inv),
-                           pack<F16>(x[8 * q + 4] * inv, x[8 * q + 5] * inv), pack<F16>(x[8 * q + 6] * inv, x[8 * q + 7] * inv));
-        }
+        for (int q = 0; q < 32; ++q) x[q] *= inv;
+        if (real) store_row<F16>(out, x, g.wide);
       }
     }
   }
@@ -916,6 +926,7 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   g.page_size = (int)a.cache.page_size;
   while ((1 << g.page_shift) < g.page_size) ++g.page_shift;
   g.negate = a.scale_log2 < 0.0f;
+  g.wide = ((reinterpret_cast<uintptr_t>(a.o) | (uintptr_t)(a.ldo * 2)) & 31u) == 0;
   // equal weights for a scale of zero: the masked scores, -inf, still have to vanish
   g.c = a.scale_log2 == 0.0f ? 1e-30f : std::fabs(a.scale_log2);
   g.status = status;
