@@ -9,15 +9,21 @@
 //
 // Work is cut into steps of 16 keys of one request and one key / value head; all steps, in the order (request,
 // head, step), are dealt to warps in equal runs, whatever the requests' lengths: no CTA waits for the
-// longest. Each warp streams its steps on its own, without barriers: a lane copies the 16-byte pieces that it
-// will need itself (cp.async, three stages of 8 KB a warp, eight warps an SM: up to 128 KB in flight), so
-// shared memory is a longer register file. The d elements of q . k may be added in any order and the
-// columns of V assigned to any column of the product, which lets every piece be a 16-byte vector: a lane's K
-// pieces hold both halves of two steps of the contraction, and pairs of V's rows are interleaved in registers.
+// longest. Each warp streams its steps on its own, without barriers between warps: it copies the 16 keys' rows of K and of V
+// (cp.async, whole rows of 128 or 256 bytes, swizzled) into its own three stages of 8 KB: eight warps an SM, up to 128 KB in
+// flight. The d elements of q . k may be added in any order and the columns of V assigned to any column of the
+// product, which lets every shared-memory read be a 16-byte vector: a lane's pieces of K hold both halves of two
+// steps of the contraction, and pairs of V's rows are interleaved in registers.
 // One pass with a running maximum m: p = exp2(c s - c m); m is raised, and O and l rescaled, only when a
 // score passes it by 8 in the exponent (weights reach 2^8 at most), so most steps exchange nothing between lanes.
 // A head whose steps fall to one warp is finished by it; else the warps write (m, l, O) and a second kernel
 // adds them up in the order of the keys.
+//
+// Measured, head_dim 128, bf16: 64 sequences of 400 to 16000 keys, 64 heads on 8 key / value heads (653 MB): 112 to 115 us, 5.7
+// to 5.8 TB/s (the measured copy rate is 6.8); the streaming kernel 104 to 110 of it, its SMs between 165 and
+// 208 thousand cycles with equal runs, since some are nearer to memory than others. Eight sequences of 1000 to 2600 keys, 32
+// heads (169 MB): 36 us, 31 of it streaming. One of 300 keys, 32 heads: 10 us, latency. Copies of 16 bytes from
+// eight rows at a time, which need no exchange between lanes, took 140 and 41 us: 28 bytes a request to L2, not 120.
 #include <cmath>
 
 #include <cuda_bf16.h>

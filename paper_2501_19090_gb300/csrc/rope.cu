@@ -11,6 +11,8 @@
 // A CTA takes whole tokens: it computes their cosines and sines once, into shared memory, for all heads (a
 // thread's own would cost more issue slots than the loads and stores), and its threads deal the heads' units
 // of 16 elements: two 16-byte vectors, pairs across the vectors (half) or within them (interleaved).
+// Measured, head_dim 128, bf16: 8192 tokens of 64 + 8 + 8 heads into the cache (336 MB) 54 us, 6.2 TB/s (the measured copy rate
+// is 6.8); 2048 tokens of 32 heads, forward and gradient (two launches, 67 MB) 15.1 us.
 #include <cmath>
 
 #include <cuda_bf16.h>
@@ -171,7 +173,7 @@ int launch(RopeArgs g, int dtype, int layout, void* cuda_stream) {
   g.status = pifa_status_word(&e);
   if (!g.status) return pifa_fail_cuda("device status word", e);
   // Whole tokens, as many to a CTA as make one round of the five CTAs that an SM holds, up to MAX_TOKENS (2048 tokens
-  // of 32 heads, forward and gradient: 16.1 us; one to a CTA 19.3). Few tokens: the heads of one are dealt to CTAs until
+  // of 32 heads, forward and gradient: 16.1 us when this was chosen; one to a CTA 19.3). Few tokens: the heads of one are dealt to CTAs until
   // those make two for every SM, one unit for a thread at the finest.
   const int nh = g.hq + 2 * g.hk, sms = pifa_sm_count(), round = 5 * sms;
   g.tokens = g.T > round * MAX_TOKENS ? MAX_TOKENS : (g.T + round - 1) / round;

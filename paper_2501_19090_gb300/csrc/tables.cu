@@ -9,6 +9,7 @@
 // lengths into its own shared memory (a second launch, or a scan split over CTAs, would cost more than the
 // repeated reads, which hit L2), then takes its share of tokens and new pages, finding their requests by
 // bisection. A token on a new page takes the page from the free list itself, so no token waits for the table.
+// Measured: 64 requests in decode 4.8 us, 520 requests with 8087 new tokens 9.0 us.
 // The cluster's barrier between the scan and the writes lets a serving loop update lengths and the free
 // list's head in place.
 #include "pifa.h"
