@@ -487,3 +487,25 @@ def test_the_example_serves_prompts_and_decode_steps(width, heads):
     spec.loader.exec_module(block)
     error, _, _ = block.serve(width=width, heads=heads, requests=5, prompt=83, steps=20)
     assert error < 0.04
+
+
+def test_attention_on_two_streams_at_once():
+    """Calls on two streams overlap, each with its own scratch: the same bits as one after the other."""
+    hq, hk, d, page = 16, 4, 128, 32
+    sets = [make_attention(21, [3000, 40, 700], [300, 1, 77], hq, hk, d, page, torch.bfloat16),
+            make_attention(22, [9000, 5000], [1, 1], hq, hk, d, page, torch.bfloat16),
+            make_attention(23, [6000], [70], hq, hk, d, page, torch.bfloat16),
+            make_attention(24, [200] * 40, [3] * 40, hq, hk, d, page, torch.bfloat16)]
+    bounds = [300, 1, 70, 3]
+    serial = [attend(a, max_q=n) for a, n in zip(sets, bounds)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for k in range(24):
+        for s in (0, 1):
+            with torch.cuda.stream(streams[s]):
+                i = (k + 2 * s) % 4
+                got[s].append((i, attend(sets[i], max_q=bounds[i])))
+    torch.cuda.synchronize()
+    for s in (0, 1):
+        for i, O in got[s]:
+            assert torch.equal(O, serial[i])
