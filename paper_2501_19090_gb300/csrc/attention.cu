@@ -483,7 +483,7 @@ cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cudaError_t e = cudaFuncSetAttribute(attention_rows<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 256);
+  cudaError_t e = pifa_allow_smem<attention_rows<F16, D>>(227 * 1024 - 256);
   if (e == cudaSuccess) e = pifa_launch_ex(&cfg, attention_rows<F16, D>, g);
   if (e != cudaSuccess) return e;
   cfg.dynamicSmemBytes = 0;

@@ -899,6 +899,13 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
 }
 
+template <bool F16, int D>
+cudaError_t launch_tc(cudaLaunchConfig_t& cfg, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap, const TcArgs& g) {
+  cfg.dynamicSmemBytes = Cfg<D>::SMEM;
+  const cudaError_t e = pifa_allow_smem<attention_tc<F16, D>>((int)Cfg<D>::SMEM);
+  return e != cudaSuccess ? e : pifa_launch_ex(&cfg, attention_tc<F16, D>, qmap, kmap, vmap, g);
+}
+
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 
 int64_t list_bytes(int64_t T, int64_t group, int64_t B) {
@@ -964,20 +971,15 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cudaError_t e = cudaFuncSetAttribute(attention_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(4096 * sizeof(Lengths) + 4097 * 4));
+  cudaError_t e = pifa_allow_smem<attention_plan>((int)(4096 * sizeof(Lengths) + 4097 * 4));
   if (e != cudaSuccess) return pifa_fail_cuda("cudaFuncSetAttribute(attention_plan)", e);
   e = pifa_launch_ex(&cfg, attention_plan, g, grid);
   if (e != cudaSuccess) return pifa_fail_cuda("attention_plan launch", e);
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);
-  auto go = [&](auto kernel, uint32_t smem) {
-    cfg.dynamicSmemBytes = smem;
-    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    return err != cudaSuccess ? err : pifa_launch_ex(&cfg, kernel, qmap, kmap, vmap, g);
-  };
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
-  if (a.cache.dim == 64) e = f16 ? go(attention_tc<true, 64>, Cfg<64>::SMEM) : go(attention_tc<false, 64>, Cfg<64>::SMEM);
-  else e = f16 ? go(attention_tc<true, 128>, Cfg<128>::SMEM) : go(attention_tc<false, 128>, Cfg<128>::SMEM);
+  if (a.cache.dim == 64) e = f16 ? launch_tc<true, 64>(cfg, qmap, kmap, vmap, g) : launch_tc<false, 64>(cfg, qmap, kmap, vmap, g);
+  else e = f16 ? launch_tc<true, 128>(cfg, qmap, kmap, vmap, g) : launch_tc<false, 128>(cfg, qmap, kmap, vmap, g);
   if (e != cudaSuccess) return pifa_fail_cuda("attention_tc launch", e);
   return PIFA_OK;
 }

@@ -27,8 +27,27 @@ void pifa_count_launch();
 // SMs of the current device (status.cu); 1 if the query fails, which the next call makes again.
 int pifa_sm_count();
 
+// The current device's number, below kMaxKnown, or -1.
+constexpr int kMaxKnown = 64;
+inline int pifa_device() {
+  int dev = 0;
+  return cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxKnown ? dev : -1;
+}
+
 #ifdef __CUDACC__
+#include <atomic>
 #include <utility>
+// Lets `Kernel` have `bytes` of dynamic shared memory (always the same number for one kernel): asked of the driver
+// once for each device.
+template <auto Kernel>
+inline cudaError_t pifa_allow_smem(int bytes) {
+  static std::atomic<bool> done[kMaxKnown];
+  const int dev = pifa_device();
+  if (dev >= 0 && done[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0) done[dev].store(true, std::memory_order_relaxed);
+  return e;
+}
 // cudaLaunchKernelEx, counted.
 template <typename... K, typename... A>
 inline cudaError_t pifa_launch_ex(const cudaLaunchConfig_t* cfg, void (*kernel)(K...), A&&... args) {

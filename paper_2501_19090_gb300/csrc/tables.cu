@@ -212,7 +212,7 @@ extern "C" int pifa_page_tables(const int32_t* cached_len, const int32_t* new_le
   const TableArgs g = {cached_len, new_len, free_pages, free_first, table, q_start, kv_len, positions, free_next, slots,
                        ldt, (int)B, (int)page_size, (int)n_free, (int)cols, (int)T, status};
   const size_t bytes = (size_t)(3 * B + 2) * 4;
-  if ((e = cudaFuncSetAttribute(page_tables, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)((3 * MAX_B + 2) * 4))) != cudaSuccess)
+  if ((e = pifa_allow_smem<page_tables>((int)((3 * MAX_B + 2) * 4))) != cudaSuccess)
     return pifa_fail_cuda("cudaFuncSetAttribute(page_tables)", e);
   unsigned ctas = 1;  // four tokens a thread before another CTA joins
   while (ctas < MAX_CTAS && (int64_t)ctas * THREADS * 4 < T) ctas *= 2;
