@@ -37,7 +37,7 @@
 // What made it so, on the first case: 3.6 ms with spilled rows of S and one issuing warp; registers moved to the softmax
 // warps 1.72; operands of the MMAs in uniform registers (one elected thread in a converged warp: 50 cycles an
 // instruction, not 80), a warp for each tile's MMAs, the tiles in turn and the weights of half a tile handed over first 1.30;
-// Q by TMA and the turn passed before S 1.22. Cut items cost six tiles' time: 200 tokens over 8000 took 67 us with
+// Q by TMA 1.22. Cut items cost six tiles' time: 200 tokens over 8000 took 67 us with
 // a cut that left a second round, 45 with one round, 39 since all warps add up the pieces.
 #include <cmath>
 
@@ -533,13 +533,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     // S = Q K^T; then K's slot is given back, and Q after the item's last S
     auto score = [&](int slot, bool last, bool pass) {
       if (elect_one()) {
-        if (pass) mbar_arrive(&turn[1 - t]);  // the other tile's PV may follow on: after S it came too late by a wait
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
           const uint32_t at = (uint32_t)(kk / 4) * (HALF / 16) + (uint32_t)(kk % 4) * 2;
           mma_ss_words(s_at, q_desc + at, k_desc + slot * (TILE / 16) + at, hi, qk_desc, kk > 0);
         }
         mma_commit(&s_full[t]);
+        if (pass) mbar_arrive(&turn[1 - t]);  // after S: the other tile's products between PV and S would delay this softmax
         mma_commit(&empty[slot]);
         if (last) mma_commit(&q_free[t]);
       }
