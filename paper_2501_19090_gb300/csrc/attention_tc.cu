@@ -228,7 +228,8 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     // The time, in key tiles, if the longest of those items is cut into `want` pieces and the others into pieces
     // no longer: one round if there is a CTA for each piece; else an even share for every CTA, and the wait for
     // the last pieces: of alike ones, what is left of their last round, of unlike ones about half a piece. An item
-    // costs about two tiles on top (rows of Q, first and last products), a piece with partial sums six.
+    // costs about two tiles on top (rows of Q, first and last products), a piece with its sums four, and adding them up
+    // at the end four more.
     int longest = 0;
     for (int i = 0; i < min(rest, MAX_REST); ++i) longest = max(longest, rest_cost[i]);
     const int want = tid < 16 ? tid + 1 : (int)(16.0f * exp2f(0.21f * (float)(tid - 15)));
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     float work = 0.0f;
     for (int i = 0; i < min(rest, MAX_REST); ++i) {
       const int c = rest_cost[i], n = max((c + size - 1) / size, 1);
-      const float extra = n > 1 ? 6.0f : 2.0f;
+      const float extra = n > 1 ? 4.0f : 2.0f;
       pieces += n;
       most = max(most, (c + n - 1) / n + (int)extra);
       work += (float)c + extra * (float)n;
@@ -248,6 +249,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     float t = whole == 0 && rounds <= 1.0f ? (float)most
                                             : share + (float)most * (alike * (ceilf(rounds) - rounds) + (1.0f - alike) * 0.5f);
     t = fmaxf(t, fmaxf((float)most, (float)(whole_most + 2)));
+    if (pieces > rest) t += 4.0f;
     // more than there is room for
     if (tid > 0 && ((int64_t)pieces * g.heads > MAX_PARTS || rest > MAX_REST || want > longest)) t = 3e38f;
     int who = tid;
