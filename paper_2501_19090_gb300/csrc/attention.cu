@@ -355,10 +355,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
 }
 
 // Adds up the pieces of a request's head whose steps fell to several warps, in the order of the keys: `split` CTAs
-// for each, a share of the columns apiece, a thread for four columns of a row, up to eight threads with every
+// for each, a share of the columns apiece, a thread for four columns of a row, up to 16 threads with every
 // so many-th piece where a CTA has fewer of those. Pieces and their weights are loaded together, four at a time: with few
 // pieces the kernel is two latencies long, and one long sequence (144 pieces of each head) spreads over the SMs (64
-// heads, 8 key / value heads, 16000 keys: 63 -> 33 us).
+// heads, 8 key / value heads, 16000 keys, both kernels: 63 us with one CTA a head, 34 with up to 8 shares and 8 threads,
+// 29 with 16 and 16, 30.5 with 32 and 32; eight pieces at a time cost 64 requests 3 %).
 template <bool F16, int D>
 __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int split) {
   __shared__ float2 sh_ml[THREADS];
@@ -366,7 +367,7 @@ __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int s
   pdl_launch_dependents();
   const int item = (int)blockIdx.x / split, b = item / g.heads, head = item - b * g.heads;
   const int quads = D / 4 / split, col0 = ((int)blockIdx.x - item * split) * quads * 4;  // of this CTA: fours of columns, first one
-  const int slots = g.max_rows * quads, groups = min(max(THREADS / slots, 1), 8);
+  const int slots = g.max_rows * quads, groups = min(max(THREADS / slots, 1), 16);
   pdl_wait_primary();
   const Lengths x = lengths_of(g, b);
   const int run = g.sums[g.B + 1], steps = steps_of(x), from = g.sums[b] + head * steps;
@@ -489,7 +490,7 @@ cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
   cfg.dynamicSmemBytes = 0;
   const int64_t items = (int64_t)g.B * g.heads;
   int split = 1;
-  while (split < 8 && items * split * 2 <= 8 * sms && g.max_rows * (D / 4) / (split * 2) >= THREADS / 8) split *= 2;
+  while (split < 16 && items * split * 2 <= 8 * sms && g.max_rows * (D / 4) / (split * 2) >= THREADS / 16) split *= 2;
   cfg.gridDim = dim3((unsigned)(items * split));
   return pifa_launch_ex(&cfg, attention_join<F16, D>, g, split);
 }
