@@ -503,6 +503,11 @@ int pifa_validate_indices(const int32_t* pivot_idx, const int32_t* nonpivot_idx,
  * kernels latch on the current device (PIFA_OK, PIFA_ERR_TIMEOUT or PIFA_ERR_DEVICE_INDEX). */
 int pifa_device_status(void* cuda_stream);
 
+/* pifa_stream_captures -- 1 if what is enqueued on `cuda_stream` is being captured into a CUDA graph, 0 if not, a negative
+ * pifa_status if the stream cannot say. A workspace that a captured call was given must live, and not be used by
+ * other calls, as long as the graph may be replayed. */
+int pifa_stream_captures(void* cuda_stream);
+
 /* pifa_set_wait_timeout -- bound, in nanoseconds, of every device-side wait of kernels launched
  * after this call (default 1 s, or the environment variable PIFA_WAIT_TIMEOUT_NS at load time;
  * ns == 0 restores that default). A wait that runs out makes its CTA latch PIFA_ERR_TIMEOUT, wait

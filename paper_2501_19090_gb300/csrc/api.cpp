@@ -201,6 +201,14 @@ int pifa_set_wait_timeout(int64_t ns) {
   return PIFA_OK;
 }
 
+int pifa_stream_captures(void* cuda_stream) {
+  pifa_clear_error();
+  cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+  const cudaError_t e = cudaStreamIsCapturing(reinterpret_cast<cudaStream_t>(cuda_stream), &st);
+  if (e != cudaSuccess) return pifa_fail_cuda("cudaStreamIsCapturing", e);
+  return st != cudaStreamCaptureStatusNone;
+}
+
 const char* pifa_last_error(void) { return g_last_error.c_str(); }
 
 const char* pifa_status_string(int status) {

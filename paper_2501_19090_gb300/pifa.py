@@ -63,7 +63,7 @@ EXPORTS = (
     "pifa_backward", "pifa_backward_workspace_size", "pifa_m_accumulate", "pifa_m_accumulate_workspace_size",
     "pifa_m_reconstruct", "pifa_m_reconstruct_workspace_size",
     "pifa_page_tables", "pifa_rope_frequencies", "pifa_rope", "pifa_rope_cache",
-    "pifa_paged_attention", "pifa_paged_attention_workspace_size",
+    "pifa_paged_attention", "pifa_paged_attention_workspace_size", "pifa_stream_captures",
 )
 
 
@@ -167,6 +167,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.pifa_set_wait_timeout.restype = ctypes.c_int
         lib.pifa_selftest_wait_timeout.argtypes = [_VP]
         lib.pifa_selftest_wait_timeout.restype = ctypes.c_int
+        lib.pifa_stream_captures.argtypes = [_VP]
+        lib.pifa_stream_captures.restype = ctypes.c_int
         lib.pifa_launch_count.argtypes = []
         lib.pifa_launch_count.restype = ctypes.c_int64
         lib.pifa_set_decode_grid.argtypes = [ctypes.c_int]
@@ -327,6 +329,50 @@ def _stream_ptr(stream):
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _on(stream):
+    """A context in which torch allocates and fills on `stream`, where the call's kernels will run."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
+# Scratch of a call that is captured into a graph belongs to that graph: its address is in the graph, which may be
+# replayed on any stream, long after the scratch that eager calls share has been replaced by a larger one.
+def _captured(run_on) -> bool:
+    """Whether calls on a stream (its _stream_ptr) are being captured into a graph."""
+    captures = _lib().pifa_stream_captures(run_on)
+    if captures < 0:
+        _check(captures, "pifa_stream_captures")
+    return captures != 0
+
+
+_graph_scratches: list = []
+
+
+def _in_graph_pool(buf) -> bool:
+    """Whether `buf` lies in the memory pool of a graph (torch's captures have one; it lives as long as the graph)."""
+    import torch
+    at = buf.data_ptr()
+    try:
+        segments = torch.cuda.memory_snapshot()
+    except RuntimeError:  # another allocator
+        return False
+    return any(s["address"] <= at < s["address"] + s["total_size"] and tuple(s["segment_pool_id"]) != (0, 0)
+               for s in segments)
+
+
+def _graph_scratch(nbytes, device, stream):
+    """Scratch for one call of a graph that is being captured. In the graph's pool torch may use its memory
+    again, for later calls of this graph alone. A capture that torch did not begin has no pool: then it is never given back."""
+    import torch
+    with _on(stream):
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not _in_graph_pool(buf):
+        _graph_scratches.append(buf)
+    return buf
 
 
 _workspaces: dict = {}
@@ -658,14 +704,6 @@ def _refuse(msg):
     raise ValueError(f"pifa: {msg}")
 
 
-def _on(stream):
-    """A context in which torch allocates and fills on `stream`, where the call's kernels will run."""
-    if stream is None:
-        return contextlib.nullcontext()
-    import torch
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-
-
 def _vector(name, t, n, dtype, device):
     """`t`, a contiguous 1-D tensor of n elements of `dtype` on `device` (n None: any number)."""
     import torch
@@ -889,7 +927,12 @@ _attention_workspaces: dict = {}
 
 
 def _attention_workspace(need, dev, run_on, stream):
-    """(256-byte aligned address, bytes, tensor) of scratch kept for one device and one stream that calls run on."""
+    """(256-byte aligned address, bytes, tensor) of scratch: kept for one device and one stream that calls run on, or
+    the captured graph's own."""
+    if _captured(run_on):
+        buf = _graph_scratch(need + 256, f"cuda:{dev}", stream)
+        pad = -buf.data_ptr() % 256
+        return buf.data_ptr() + pad, need + 256 - pad, buf
     key = (dev, run_on if isinstance(run_on, int) else getattr(run_on, "value", None))
     ws = _attention_workspaces.get(key)
     if ws is None or ws[1] < need:
@@ -906,7 +949,8 @@ def pifa_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, max_q: int
     """Causal attention of each request's new tokens over its pages (pifa_paged_attention): Q (T x heads x
     head_dim), caches as pifa_rope_cache, table int32 (B x columns), q_start int32 (B + 1), kv_len int32 (B),
     max_q at least every request's number of new tokens. scale: 1 / sqrt(head_dim) if not given. Returns O,
-    shaped like Q (allocated as zeros if not given: rows of no request are not written)."""
+    shaped like Q (allocated as zeros if not given: rows of no request are not written). Without workspace_tensor eager
+    calls share scratch that is kept for each stream, and a captured call has its own, from the graph's pool."""
     torch = sys.modules["torch"]
     run_on = _stream_ptr(stream)
     try:

@@ -1,0 +1,85 @@
+"""Who owns the binding's default scratch, without a GPU: torch's allocations go to the host, and its answers
+about captures and pools are the test's."""
+import contextlib
+import gc
+import weakref
+
+import pytest
+import torch
+
+from paper_2501_19090_gb300 import pifa as P
+
+
+class Torch:
+    """torch.empty on the host, keeping a weak reference to every buffer, and whether a capture runs."""
+
+    def __init__(self, monkeypatch):
+        self.capturing, self.pool, self.made = False, True, []
+        empty = torch.empty
+
+        def host_empty(*shape, dtype, device):
+            buf = empty(*shape, dtype=dtype)
+            self.made.append(weakref.ref(buf))
+            return buf
+        monkeypatch.setattr(torch, "empty", host_empty)
+        monkeypatch.setattr(P, "_captured", lambda run_on: self.capturing, raising=False)
+        monkeypatch.setattr(torch.cuda, "memory_snapshot", self.snapshot)
+        monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+        for name in ("_attention_workspaces", "_workspaces"):
+            monkeypatch.setattr(P, name, {})
+        monkeypatch.setattr(P, "_graph_scratches", [], raising=False)
+
+    def snapshot(self):
+        return [{"address": 0, "total_size": 2 ** 63, "segment_pool_id": (0, 7) if self.pool else (0, 0)}]
+
+    def alive(self):
+        gc.collect()
+        return [r() is not None for r in self.made]
+
+
+@pytest.fixture
+def fake(monkeypatch):
+    return Torch(monkeypatch)
+
+
+def attention(need, stream=5):
+    return P._attention_workspace(need, 0, stream, None)[:2]
+
+
+def disjoint(a, b):
+    return a[0] + a[1] <= b[0] or b[0] + b[1] <= a[0]
+
+
+def test_attention_scratch_of_eager_calls_is_kept_for_each_stream(fake):
+    a = attention(1000)
+    assert a[0] % 256 == 0 and a[1] >= 1000
+    assert attention(900) == a and attention(1000) == a and len(fake.made) == 1
+    assert disjoint(a, attention(1000, stream=6))
+    b = attention(50000)
+    assert b[1] >= 50000 and attention(1000) == b
+
+
+@pytest.mark.parametrize("warm", [False, True])
+def test_attention_scratch_of_a_capture_is_the_graphs(fake, warm):
+    """Neither what eager calls use, before or after, nor what another capture uses while its own tensors live."""
+    fake.pool = False                      # (kept alive, so that addresses can be told apart)
+    eager = [attention(1000)] if warm else []
+    fake.capturing = True
+    first = attention(1000)
+    fake.capturing = False
+    eager += [attention(1000), attention(70000)]
+    fake.capturing = True
+    second = attention(1000)
+    assert all(disjoint(first, x) for x in eager + [second])
+    assert disjoint(second, eager[-1])     # (the smaller one before it has been given back)
+
+
+def test_attention_scratch_of_a_capture_outlives_larger_calls(fake):
+    """In a graph's pool the memory is the graph's and the tensor may go; without one the tensor is kept."""
+    for pool in (True, False):
+        fake.pool, fake.capturing = pool, True
+        fake.made.clear()
+        attention(1000)
+        fake.capturing = False
+        attention(10 ** 6 * (2 - pool))
+        assert fake.alive() == [not pool, True]
