@@ -382,9 +382,12 @@ def workspace(nbytes: int, device, stream=None, tag: str = ""):
     """A cached device scratch tensor of at least nbytes on `device` (grown, never shrunk).
 
     The cache is keyed by device, stream and `tag`, so calls on different streams never share
-    scratch, and a caller that keeps several calls' scratch apart on one stream tags them.
+    scratch, and a caller that keeps several calls' scratch apart on one stream tags them. While
+    the stream is being captured into a graph, every call gets scratch of that graph instead.
     """
     import torch
+    if _captured(_stream_ptr(stream)):
+        return _graph_scratch(max(nbytes, 256) + 256, device, stream)
     key = (str(device), 0 if stream is None else getattr(stream, "cuda_stream", stream), str(tag))
     buf = _workspaces.get(key)
     if buf is None or buf.numel() < nbytes:

@@ -50,3 +50,50 @@ def test_attention_graph_with_default_scratch(news, lens, warm):
     assert torch.equal(O, want) and torch.equal(big_O, big_want)
     check_attention(a, O, d ** -0.5)
     assert P.pifa_device_status() == P.PIFA_OK
+
+
+def small_layer(m, n, r, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    order = torch.randperm(m, device=DEV, generator=g)
+    rand = lambda *shape: (torch.randn(shape, device=DEV, generator=g) * r ** -0.5).to(torch.bfloat16)
+    return (rand(r, n), rand(m - r, r), order[:r].sort().values.int(), order[r:].sort().values.int()), rand
+
+
+@pytest.mark.parametrize("what", ["forward", "grouped", "backward", "accumulate"])
+def test_projections_graph_with_default_scratch(what):
+    """As above for a captured projection, its gradient and the calibration's accumulators."""
+    n, r = 1024, 512
+    layer, rand = small_layer(n, n, r, 5)
+    pair = [torch.cat([w, w]) for w in layer[:2]] + [torch.cat([i, i + n]) for i in layer[2:]]
+
+    def call(T, X, dY, out):
+        if what == "forward":
+            out["Y"] = P.pifa_forward(X, *layer)
+        elif what == "grouped":
+            out["Y"] = P.pifa_forward_grouped(2, X, *pair)
+        elif what == "backward":
+            out.update(zip(("dX", "dWp", "dC"), P.pifa_backward(X, *layer, dY)))
+        else:
+            out["XXt"] = torch.zeros((n, n), device=DEV)
+            P.pifa_m_accumulate(None, X, None, 0.5, out["XXt"])
+
+    X, dY, big = rand(24, n), rand(24, n), rand(4096, n)
+    want, got, rest = {}, {}, {}
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        call(24, X, dY, want)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            call(24, X, dY, got)
+        call(4096, big, big, rest)
+        torch.cuda.synchronize()
+        fill = [torch.full((k,), 77, dtype=torch.uint8, device=DEV) for k in (2 ** 12, 2 ** 16, 2 ** 20, 2 ** 22, 2 ** 24) * 6]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert set(got) == set(want) and all(torch.equal(got[k], want[k]) for k in want)
+    assert all(bool((x == 77).all()) for x in fill)
+    assert P.pifa_device_status() == P.PIFA_OK

@@ -83,3 +83,24 @@ def test_attention_scratch_of_a_capture_outlives_larger_calls(fake):
         fake.capturing = False
         attention(10 ** 6 * (2 - pool))
         assert fake.alive() == [not pool, True]
+
+
+# ---- the scratch of the projections, their gradients and the accumulators ---------------------------------
+def test_workspace_of_eager_calls_is_kept(fake):
+    a = P.workspace(1000, "cuda:0")
+    assert P.workspace(1256, "cuda:0") is a and P.workspace(1000, "cuda:0", tag="x") is not a
+    assert P.workspace(5000, "cuda:0") is not a
+
+
+@pytest.mark.parametrize("pool", [True, False])
+@pytest.mark.parametrize("tag", ["", "backward"])
+def test_workspace_of_a_capture_is_the_graphs(fake, pool, tag):
+    fake.pool = pool
+    eager = P.workspace(1000, "cuda:0", tag=tag)
+    fake.capturing = True
+    first, second = P.workspace(1000, "cuda:0", tag=tag), P.workspace(900, "cuda:0", tag=tag)
+    assert len({t.data_ptr() for t in (eager, first, second)}) == 3
+    fake.capturing = False
+    assert P.workspace(1000, "cuda:0", tag=tag) is eager
+    del first, second
+    assert fake.alive() == [True, not pool, not pool]
