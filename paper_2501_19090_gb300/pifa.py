@@ -386,12 +386,14 @@ def workspace(nbytes: int, device, stream=None, tag: str = ""):
     the stream is being captured into a graph, every call gets scratch of that graph instead.
     """
     import torch
-    if _captured(_stream_ptr(stream)):
+    run_on = _stream_ptr(stream)
+    if _captured(run_on):
         return _graph_scratch(max(nbytes, 256) + 256, device, stream)
-    key = (str(device), 0 if stream is None else getattr(stream, "cuda_stream", stream), str(tag))
+    key = (str(device), getattr(run_on, "value", run_on) or 0, str(tag))  # without `stream`: the current one
     buf = _workspaces.get(key)
     if buf is None or buf.numel() < nbytes:
-        buf = torch.empty(max(nbytes, 256) + 256, dtype=torch.uint8, device=device)
+        with _on(stream):
+            buf = torch.empty(max(nbytes, 256) + 256, dtype=torch.uint8, device=device)
         _workspaces[key] = buf
     return buf
 

@@ -1,6 +1,7 @@
 """Who owns the binding's default scratch, without a GPU: torch's allocations go to the host, and its answers
 about captures and pools are the test's."""
 import contextlib
+import ctypes
 import gc
 import weakref
 
@@ -14,20 +15,29 @@ class Torch:
     """torch.empty on the host, keeping a weak reference to every buffer, and whether a capture runs."""
 
     def __init__(self, monkeypatch):
-        self.capturing, self.pool, self.made = False, True, []
+        self.capturing, self.pool, self.made, self.current, self.made_on = False, True, [], 0, []
         empty = torch.empty
 
         def host_empty(*shape, dtype, device):
             buf = empty(*shape, dtype=dtype)
             self.made.append(weakref.ref(buf))
+            self.made_on.append(self.current)
             return buf
         monkeypatch.setattr(torch, "empty", host_empty)
         monkeypatch.setattr(P, "_captured", lambda run_on: self.capturing, raising=False)
         monkeypatch.setattr(torch.cuda, "memory_snapshot", self.snapshot)
-        monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+        monkeypatch.setattr(torch.cuda, "stream", self.on)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda ptr: ptr)
+        monkeypatch.setattr(P, "_stream_ptr", lambda s: self.current if s is None else ctypes.c_void_p(s))
         for name in ("_attention_workspaces", "_workspaces"):
             monkeypatch.setattr(P, name, {})
         monkeypatch.setattr(P, "_graph_scratches", [], raising=False)
+
+    @contextlib.contextmanager
+    def on(self, stream):
+        before, self.current = self.current, stream
+        yield
+        self.current = before
 
     def snapshot(self):
         return [{"address": 0, "total_size": 2 ** 63, "segment_pool_id": (0, 7) if self.pool else (0, 0)}]
@@ -104,3 +114,16 @@ def test_workspace_of_a_capture_is_the_graphs(fake, pool, tag):
     assert P.workspace(1000, "cuda:0", tag=tag) is eager
     del first, second
     assert fake.alive() == [True, not pool, not pool]
+
+
+def test_workspace_of_streams_differs(fake):
+    """Also where the stream is the current one, unnamed; and the memory is allocated on the stream that uses it."""
+    first = P.workspace(1000, "cuda:0")
+    fake.current = 9
+    second = P.workspace(1000, "cuda:0")
+    assert second is not first and P.workspace(1000, "cuda:0", stream=9) is second
+    third = P.workspace(1000, "cuda:0", stream=11)
+    assert third is not second and third is not first
+    fake.current = 0
+    assert P.workspace(1000, "cuda:0") is first and P.workspace(1000, "cuda:0", stream=11) is third
+    assert fake.made_on == [0, 9, 11]
