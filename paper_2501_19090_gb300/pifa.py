@@ -375,6 +375,18 @@ def _graph_scratch(nbytes, device, stream):
     return buf
 
 
+# ctypes lets other host threads run during a call: two of them on one stream (the default one, say) share its scratch, and
+# the kernels of one call must all be enqueued before those of the other.
+_shared_scratch = threading.Lock()
+
+
+def _enqueue(call, workspace_tensor, *args) -> int:
+    if workspace_tensor is not None:
+        return call(*args)
+    with _shared_scratch:
+        return call(*args)
+
+
 _workspaces: dict = {}
 
 
@@ -519,7 +531,8 @@ def pifa_forward(X, Wp, C, pivot_idx, nonpivot_idx, Y=None, variant: int = PIFA_
     if ws is not None and ws_ptr % 256:
         ws_ptr += 256 - ws_ptr % 256
     ws_bytes = 0 if ws is None else ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _lib().pifa_forward_variant(
+    st = _enqueue(
+        _lib().pifa_forward_variant, workspace_tensor,
         X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp),
         C.data_ptr() if has_np else None, m, _ld(C) if has_np else r, cdt,
         pivot_idx.data_ptr(), nonpivot_idx.data_ptr() if has_np else None,
@@ -556,7 +569,8 @@ def pifa_forward_grouped(groups: int, X, Wp, C, pivot_idx, nonpivot_idx, Y=None,
     if ws is not None and ws_ptr % 256:
         ws_ptr += 256 - ws_ptr % 256
     ws_bytes = 0 if ws is None else ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _lib().pifa_forward_grouped(
+    st = _enqueue(
+        _lib().pifa_forward_grouped, workspace_tensor,
         G, X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp), C.data_ptr(), m, _ld(C), cdt,
         pivot_idx.data_ptr(), nonpivot_idx.data_ptr(), Y.data_ptr(), _ld(Y), ws_ptr or None, ws_bytes,
         _stream_ptr(stream))
@@ -617,7 +631,8 @@ def pifa_backward(X, Wp, C, pivot_idx, nonpivot_idx, dY, want=("dX", "dWp", "dC"
     ws = workspace_tensor if workspace_tensor is not None else workspace(need, dev, stream, tag="backward")
     ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
     ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _lib().pifa_backward(
+    st = _enqueue(
+        _lib().pifa_backward, workspace_tensor,
         X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp), C.data_ptr() if has_np else None, m,
         _ld(C) if has_np else r, pivot_idx.data_ptr(), nonpivot_idx.data_ptr() if has_np else None,
         dY.data_ptr(), _ld(dY), dX.data_ptr() if dX is not None else None, _ld(dX) if dX is not None else n,
@@ -659,7 +674,8 @@ def pifa_m_accumulate(Xo, Xu, W, lam, XXt, YtXt=None, workspace_tensor=None, str
     ws = workspace_tensor if workspace_tensor is not None else workspace(need, Xu.device, stream, tag="macc")
     ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
     ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _lib().pifa_m_accumulate(
+    st = _enqueue(
+        _lib().pifa_m_accumulate, workspace_tensor,
         Xo.data_ptr() if YtXt is not None else None, Xu.data_ptr(), T, n, _ld(Xu),
         W.data_ptr() if YtXt is not None else None, m, _ld(W) if YtXt is not None else n, float(lam),
         XXt.data_ptr(), _ld(XXt), YtXt.data_ptr() if YtXt is not None else None,
@@ -1001,7 +1017,8 @@ def pifa_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, max_q: int
             _refuse("workspace_tensor must be a tensor on Q's device")
         ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
         ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _lib().pifa_paged_attention(
+    st = _enqueue(
+        _lib().pifa_paged_attention, workspace_tensor,
         Q.data_ptr(), ldq, T, h, hk, d, PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16,
         k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh,
         table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), B, int(max_q),

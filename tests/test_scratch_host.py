@@ -3,6 +3,8 @@ about captures and pools are the test's."""
 import contextlib
 import ctypes
 import gc
+import threading
+import time
 import weakref
 
 import pytest
@@ -127,3 +129,52 @@ def test_workspace_of_streams_differs(fake):
     fake.current = 0
     assert P.workspace(1000, "cuda:0") is first and P.workspace(1000, "cuda:0", stream=11) is third
     assert fake.made_on == [0, 9, 11]
+
+
+class Library:
+    """Entry points that take a while and note how many there were and how many ran at once."""
+
+    def __init__(self):
+        self.running, self.most, self.calls = 0, 0, 0
+
+    def __getattr__(self, name):
+        if "workspace_size" in name:
+            return lambda *args: 1000
+
+        def call(*args):
+            self.running += 1
+            self.calls += 1
+            self.most = max(self.most, self.running)
+            time.sleep(0.02)
+            self.running -= 1
+            return P.PIFA_OK
+        return call
+
+
+@pytest.mark.parametrize("what", ["forward", "grouped", "backward", "accumulate", "attention"])
+def test_threads_that_share_scratch_enqueue_one_after_another(fake, monkeypatch, what):
+    lib, bf16, i32 = Library(), torch.bfloat16, torch.int32
+    monkeypatch.setattr(P, "_lib", lambda: lib)
+    monkeypatch.setattr(P, "_operands", lambda *a, **k: (4, 16, 8, 16))
+    monkeypatch.setattr(torch.Tensor, "device", torch.device("cuda:0"), raising=False)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    z = lambda *shape, dtype=bf16: torch.zeros(shape, dtype=dtype)
+    X, Wp, C, piv, nonp = z(4, 16), z(8, 16), z(8, 8), z(8, dtype=i32), z(8, dtype=i32)
+    P._workspace_size.cache_clear()
+    P._attention_workspace_size.cache_clear()
+    calls = {
+        "forward": lambda: P.pifa_forward(X, Wp, C, piv, nonp, Y=z(4, 16)),
+        "grouped": lambda: P.pifa_forward_grouped(1, X, Wp, C, piv, nonp, Y=z(4, 16)),
+        "backward": lambda: P.pifa_backward(X, Wp, C, piv, nonp, z(4, 16)),
+        "accumulate": lambda: P.pifa_m_accumulate(None, X, None, 0.5, z(16, 16, dtype=torch.float32)),
+        "attention": lambda: P.pifa_paged_attention(z(4, 2, 64), z(3, 16, 2, 64), z(3, 16, 2, 64), z(1, 3, dtype=i32),
+                                                      z(2, dtype=i32), z(1, dtype=i32), 4, O=z(4, 2, 64)),
+    }
+    threads = [threading.Thread(target=calls[what]) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    P._workspace_size.cache_clear()
+    P._attention_workspace_size.cache_clear()
+    assert lib.most == 1 and lib.calls == 4
