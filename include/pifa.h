@@ -463,7 +463,8 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
  *                ceil(kv_len / page_size). A request with kv_len > cols * page_size is cut to that and latches
  *                PIFA_ERR_CAPACITY; keys of a page outside [0, pages) read as zeros and latch
  *                PIFA_ERR_DEVICE_INDEX.
- *   q_start      DEVICE, int32[B + 1], ascending from 0; kv_len DEVICE, int32[B].
+ *   q_start      DEVICE, int32[B + 1], ascending from 0 (where an entry is less than the one before, nothing is written and
+ *                PIFA_ERR_DEVICE_INDEX is latched); kv_len DEVICE, int32[B].
  *   max_q        at least every request's number of new tokens, at least 1 (host): picks the kernel (group max_q <= 16
  *                rows: streamed by warps; more: on the tensor cores). A request with more
  *                latches PIFA_ERR_CAPACITY and its further rows are not written.

@@ -50,7 +50,7 @@ struct RowArgs {
   const uint16_t *q, *k, *v;
   uint16_t* o;
   const int32_t *table, *q_start, *kv_len;
-  int* sums;          // B + 1: first step of each request (times heads), then the steps of one warp
+  int* sums;          // B + 1: first step of each request (times heads), then the steps of one warp (0: nothing is done)
   float* partial;     // for each warp two of max_rows x (D + 2): O, m, l
   int64_t ldq, ldo, ldt, page_stride, token_stride, head_stride, pages;
   int T, heads, group, page_size, page_shift, cols, B, max_q, max_rows;
@@ -130,13 +130,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // ---- the requests' first steps ----
   int total = 0;
-  bool over = false;
+  bool over = false, falls = false;
   for (int b0 = 0; b0 < g.B; b0 += THREADS) {
     const int b = b0 + tid;
     int v = 0;
     if (b < g.B) {
       const Lengths x = lengths_of(g, b);
       over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
+      falls |= g.q_start[b + 1] < g.q_start[b];
       v = steps_of(x) * g.heads;
     }
     int a = v;
@@ -158,12 +159,17 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
     total += all;
   }
   if (tid == 0) first[g.B] = total;
-  __syncthreads();
+  // requests that overlap: which of them a row belongs to is not said, so nothing is done
+  const bool overlap = __syncthreads_or(falls);
+  if (overlap) total = 0;
   const int workers = (int)gridDim.x * WARPS;
   const int run = max((total + workers - 1) / workers, MIN_STEPS);
   if (blockIdx.x == 0) {
     for (int b = tid; b <= g.B; b += THREADS) g.sums[b] = first[b];
-    if (tid == 0) g.sums[g.B + 1] = run;
+    if (tid == 0) {
+      g.sums[g.B + 1] = overlap ? 0 : run;
+      if (overlap) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+    }
     if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
   }
 
@@ -371,7 +377,7 @@ __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int s
   pdl_wait_primary();
   const Lengths x = lengths_of(g, b);
   const int run = g.sums[g.B + 1], steps = steps_of(x), from = g.sums[b] + head * steps;
-  if (steps == 0) return;
+  if (steps == 0 || run == 0) return;
   const int w0 = from / run, w1 = (from + steps - 1) / run;
   if (w0 == w1) return;  // the warp has finished it
   const int place = g.max_rows * (D + 2);  // a warp has two: the head that began before its run, and the last one

@@ -112,7 +112,7 @@ struct Lengths {
   int ahead;      // token i sees ahead + i keys
 };
 
-// Lengths of request b, kept within the buffers whatever the arrays hold.
+// Lengths of request b, kept within the buffers whatever the arrays hold. Ascending starts make the tokens of all requests T at most.
 __device__ __forceinline__ Lengths lengths_of(const TcArgs& g, int b) {
   Lengths x;
   x.q0 = min(max(g.q_start[b], 0), g.T);
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     whole_sum = 0;
   }
   pdl_wait_primary();
-  bool over = false;
+  bool over = false, falls = false;
   int items = 0;
   for (int b0 = 0; b0 < g.B; b0 += PLAN_THREADS) {
     const int b = b0 + tid;
@@ -176,6 +176,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
       const Lengths x = lengths_of(g, b);
       len[b] = x;
       over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
+      falls |= g.q_start[b + 1] < g.q_start[b];
       n = (x.n + 2 * g.tpt - 1) / (2 * g.tpt);
     }
     unsigned long long total;
@@ -185,7 +186,11 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   }
   if (tid == 0) first[g.B] = items;
   if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
-  __syncthreads();
+  // Requests that overlap could have more rows than T, and more items than the list has room for: nothing is done then.
+  if (__syncthreads_or(falls)) {
+    items = 0;
+    if (tid == 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+  }
 
   // the item at place k of the list, later rows of a request first, and its cost in key tiles
   auto item_at = [&](int k, Item& x) {
