@@ -378,14 +378,15 @@ int64_t pifa_m_reconstruct_workspace_size(int64_t m, int64_t n, int64_t r);
  *                the order of its tokens. Entries [ceil(cached / page_size), ceil((cached + new) / page_size))
  *                are written, request after request, with the next free pages; others are left as they are.
  *   q_start      DEVICE out, int32[B + 1]: first row of each request's new tokens; q_start[B] is their number.
- *   kv_len       DEVICE out, int32[B]: cached + new.
+ *   kv_len       DEVICE out, int32[B]: cached + new (q_start[b + 1] - q_start[b]).
  *   positions    DEVICE out, int32[T]: the position of each new token in its request; 0 in rows past q_start[B].
  *   slots        DEVICE out, int64[T]: the slot of each new token; -1 in rows past q_start[B].
  *   free_next    DEVICE out, int32[1]: free_first after this step.
  *
  *   B <= 4096 (PIFA_ERR_UNSUPPORTED). Where the new tokens exceed T, the pages n_free or a request's pages
- *   cols, nothing is written out of bounds, tokens without a page get slot -1, free_next stops at n_free and
- *   PIFA_ERR_CAPACITY is latched. A serving loop may pass kv_len = cached_len and free_next = free_first (each
+ *   cols, nothing is written out of bounds and PIFA_ERR_CAPACITY is latched. Tokens past T are no part of the step:
+ *   q_start, kv_len, the table and free_next are those of the tokens before. Tokens without a page get slot -1 and
+ *   free_next stops at n_free. A serving loop may pass kv_len = cached_len and free_next = free_first (each
  *   exactly; they are written after every block has read them); outputs must not overlap otherwise.
  */
 int pifa_page_tables(const int32_t* cached_len, const int32_t* new_len, int64_t B, int64_t page_size,

@@ -92,45 +92,53 @@ __global__ void __launch_bounds__(THREADS, 1) page_tables(const TableArgs g) {
   pdl_wait_primary();
   const int first = *g.free_first;
   const int lim = 0x7fffffff;
-  if (tid == 0) carry[0] = carry[1] = 0;
   bool negative = first < 0, over = false;
-  for (int b0 = 0; b0 < g.B; b0 += THREADS) {
-    const int b = b0 + tid;
-    int c = 0, n = 0;
-    if (b < g.B) {
-      c = g.cached[b];
-      n = g.fresh[b];
-      negative |= c < 0 || n < 0;
-      c = max(c, 0);
-      n = max(n, 0);
-      if (n > lim - c) {
-        n = lim - c;
-        over = true;
+  // Where the new tokens are more than T, those past it are no part of the step: a second round counts the pages of
+  // the ones before.
+  for (bool cut = false;; cut = true) {
+    if (tid == 0) carry[0] = carry[1] = 0;
+    for (int b0 = 0; b0 < g.B; b0 += THREADS) {
+      const int b = b0 + tid;
+      int c = 0, n = 0;
+      if (b < g.B) {
+        c = g.cached[b];
+        n = g.fresh[b];
+        negative |= c < 0 || n < 0;
+        c = max(c, 0);
+        n = max(n, 0);
+        if (n > lim - c) {
+          n = lim - c;
+          over = true;
+        }
+        if (cut) n = q_off[b + 1] - q_off[b];
+        cached[b] = c;
       }
-      cached[b] = c;
-    }
-    const int pages = (int)(((int64_t)c + n + g.P - 1) / g.P - ((int64_t)c + g.P - 1) / g.P);
-    int64_t a = n, p = pages;
-    __syncthreads();  // the last round's carry and partial sums have been read
-    block_scan(a, p, part);
-    const int64_t ca = carry[0], cp = carry[1];
-    if (b < g.B) {
-      q_off[b] = (int)min(ca + a - n, (int64_t)g.T);
-      p_off[b] = (int)min(cp + p - pages, (int64_t)lim);
+      const int pages = (int)(((int64_t)c + n + g.P - 1) / g.P - ((int64_t)c + g.P - 1) / g.P);
+      int64_t a = n, p = pages;
+      __syncthreads();  // the last round's carry and partial sums have been read
+      block_scan(a, p, part);
+      const int64_t ca = carry[0], cp = carry[1];
+      if (b < g.B) {
+        q_off[b] = (int)min(ca + a - n, (int64_t)g.T);
+        p_off[b] = (int)min(cp + p - pages, (int64_t)lim);
+      }
+      __syncthreads();
+      if (tid == THREADS - 1) {
+        carry[0] = ca + a;
+        carry[1] = cp + p;
+      }
     }
     __syncthreads();
-    if (tid == THREADS - 1) {
-      carry[0] = ca + a;
-      carry[1] = cp + p;
+    const bool fits = carry[0] <= g.T;
+    if (tid == 0) {
+      q_off[g.B] = (int)min(carry[0], (int64_t)g.T);
+      p_off[g.B] = (int)min(carry[1], (int64_t)lim);
     }
+    over |= carry[1] > (int64_t)g.n_free - max(first, 0);
+    if (fits) break;
+    over = true;
+    __syncthreads();
   }
-  __syncthreads();
-  const int64_t all = carry[0], fresh_pages = carry[1];
-  if (tid == 0) {
-    q_off[g.B] = (int)min(all, (int64_t)g.T);
-    p_off[g.B] = (int)min(fresh_pages, (int64_t)lim);
-  }
-  over |= all > g.T || fresh_pages > (int64_t)g.n_free - max(first, 0);
   cluster_sync_all();  // every CTA has read the lengths and the free list's head
 
   const int me = (int)blockIdx.x * THREADS + tid, step = (int)gridDim.x * THREADS;
@@ -166,10 +174,7 @@ __global__ void __launch_bounds__(THREADS, 1) page_tables(const TableArgs g) {
   }
   for (int b = me; b <= g.B; b += step) {
     g.q_start[b] = q_off[b];
-    if (b < g.B) {
-      // the new tokens as the scan counted them: q_off is cut at T, the lengths are not
-      g.kv_len[b] = cached[b] + min(max(g.fresh[b], 0), lim - cached[b]);
-    }
+    if (b < g.B) g.kv_len[b] = cached[b] + (q_off[b + 1] - q_off[b]);
   }
   if (me == 0) *g.free_next = (int)min((int64_t)head + p_off[g.B], (int64_t)max(g.n_free, head));
   if (negative) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
