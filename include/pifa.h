@@ -361,8 +361,9 @@ int64_t pifa_m_reconstruct_workspace_size(int64_t m, int64_t n, int64_t r);
  * heads or heads of tokens. A token's slot is p * page_size + o. Offsets are 64-bit.
  * Activations are rows of heads: element e of head h of token t is at t * ld + h * head_dim + e.
  * Alignment: bases 16 bytes, strides and leading dimensions multiples of 8 elements (PIFA_ERR_ALIGNMENT).
- * The calls are asynchronous on cuda_stream, allocate nothing, take T == 0 (and B == 0) as a no-op, and can be captured into
- * a CUDA graph: sizes that the host passes are capacities, lengths are read on the device.
+ * The calls are asynchronous on cuda_stream, allocate nothing, take T == 0 (page tables: B == 0; attention: either) as a
+ * no-op that writes nothing, and can be captured into a CUDA graph: sizes that the host passes are capacities, lengths are
+ * read on the device.
  */
 
 /*
@@ -383,7 +384,7 @@ int64_t pifa_m_reconstruct_workspace_size(int64_t m, int64_t n, int64_t r);
  *   slots        DEVICE out, int64[T]: the slot of each new token; -1 in rows past q_start[B].
  *   free_next    DEVICE out, int32[1]: free_first after this step.
  *
- *   B <= 4096 (PIFA_ERR_UNSUPPORTED). Where the new tokens exceed T, the pages n_free or a request's pages
+ *   B <= 4096 (PIFA_ERR_UNSUPPORTED); with B == 0 no output is written. Where the new tokens exceed T, the pages n_free or a request's pages
  *   cols, nothing is written out of bounds and PIFA_ERR_CAPACITY is latched. Tokens past T are no part of the step:
  *   q_start, kv_len, the table and free_next are those of the tokens before. Tokens without a page get slot -1 and
  *   free_next stops at n_free. A serving loop may pass kv_len = cached_len and free_next = free_first (each

@@ -828,6 +828,12 @@ def pifa_page_tables(cached_len, new_len, page_size: int, free_pages, free_first
         _vector("positions", positions, T, i32, dev)
         _vector("slots", slots, T, torch.int64, dev)
         _vector("free_next", free_next, 1, i32, dev)
+    if B == 0:  # the library writes nothing then
+        with _on(stream):
+            q_start.zero_()
+            positions.zero_()
+            slots.fill_(-1)
+            free_next.copy_(free_first)
     st = _lib().pifa_page_tables(
         cached_len.data_ptr(), new_len.data_ptr(), B, int(page_size), free_pages.data_ptr(), free_pages.shape[0],
         free_first.data_ptr(), table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), positions.data_ptr(),

@@ -1,4 +1,4 @@
-"""Page tables of steps that do not fit."""
+"""Page tables of steps that do not fit, and of no requests."""
 import random
 
 import pytest
@@ -52,3 +52,16 @@ def test_attention_of_a_step_that_does_not_fit():
     assert P.pifa_device_status() == P.PIFA_ERR_CAPACITY and int(nxt) == len(spare)
     O = attend(dict(a, table=table, q_start=q_start, kv_len=kv_len))
     check_attention(a, O, d ** -0.5)
+
+
+@pytest.mark.parametrize("T", [0, 1, 40])
+@pytest.mark.parametrize("given", [False, True])
+def test_no_requests(T, given):
+    empty = lambda n, dtype=torch.int32: torch.full((n,), -3, dtype=dtype, device=DEV)
+    out = (empty(1), empty(0), empty(T), empty(T, torch.int64), empty(1)) if given else None
+    if not given:  # memory that the call's outputs are likely to get
+        before = [empty(n, dt) for n in (1, 1, T, T) for dt in (torch.int32, torch.int64)]
+        del before
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    got = P.pifa_page_tables(none, none, 16, i32([4, 5, 6]), i32([2]), torch.empty((0, 3), dtype=torch.int32, device=DEV), T, out=out)
+    assert [x.tolist() for x in got] == [[0], [], [0] * T, [-1] * T, [2]]
