@@ -442,7 +442,8 @@ int pifa_rope(const void* X, int64_t T, int64_t heads, int64_t ldx, int64_t head
  *                of one projection's output).
  *   positions    DEVICE, int32[T]; slots DEVICE, int64[T]: a slot of -1 stores nothing; others outside
  *                [0, pages * page_size) store nothing and latch PIFA_ERR_DEVICE_INDEX. Slots of one call differ.
- *   Qr           DEVICE out, ldqr; may be Q itself (ldqr == ldq), must not overlap an input otherwise.
+ *   Qr           DEVICE out, ldqr; may be Q itself (ldqr == ldq), must not overlap an input otherwise. In place K and V must
+ *                not share elements with Q (they may be other columns of the same rows).
  *   freq, rot_dim, layout, scale as pifa_rope.
  */
 int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T,

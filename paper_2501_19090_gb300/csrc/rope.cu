@@ -155,6 +155,23 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeArgs g) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Whether T rows of `na` elements and T rows of `nb` have an element in common: columns of one matrix may interleave.
+bool rows_overlap(const void* a, int64_t na, int64_t lda, const void* b, int64_t nb, int64_t ldb, int64_t T) {
+  if (!pifa_spans_overlap(pifa_span(a, T, na, lda, 2), pifa_span(b, T, nb, ldb, 2))) return false;
+  // a's element 0 is column 0; b's is element `from`
+  const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)) / 2;
+  if (lda == ldb) {
+    const int64_t at = (from % lda + lda) % lda;
+    return at < na || at + nb > lda;
+  }
+  for (int64_t i = 0; i < T; ++i) {  // the first row of b that ends behind the start of a's row i
+    const int64_t behind = i * lda - from - nb;
+    const int64_t j = behind < 0 ? 0 : behind / ldb + 1;
+    if (j < T && from + j * ldb < i * lda + na) return true;
+  }
+  return false;
+}
+
 int check_heads(int64_t T, int64_t heads, int64_t dim, int dtype, int64_t rot, int layout, float scale) {
   const int64_t lim = (int64_t)1 << 30;
   if (T < 0 || T >= lim) return pifa_fail(PIFA_ERR_INVALID_ARG, "T must be in [0, 2^30)");
@@ -281,7 +298,8 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
   // the two caches may interleave (pages of keys and values in turn), so their spans may overlap; a row of Q that
   // interleaves with K and V (columns of one projection) may too, but Qr then has to be Q itself or apart
   const bool in_place = Qr == Q && ldqr == ldq;
-  bool bad = !in_place && (pifa_spans_overlap(qr, q) || pifa_spans_overlap(qr, in[0]) || pifa_spans_overlap(qr, in[1]));
+  bool bad = in_place ? rows_overlap(Q, qrow, ldq, K, krow, ldk, T) || rows_overlap(Q, qrow, ldq, V, krow, ldv, T)
+                      : pifa_spans_overlap(qr, q) || pifa_spans_overlap(qr, in[0]) || pifa_spans_overlap(qr, in[1]);
   for (const PifaSpan& cache : {kc, vc})
     bad = bad || pifa_spans_overlap(cache, q) || pifa_spans_overlap(cache, in[0]) || pifa_spans_overlap(cache, in[1]) ||
           pifa_spans_overlap(cache, qr);
