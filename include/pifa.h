@@ -41,9 +41,11 @@ typedef enum {
   PIFA_ERR_TIMEOUT = -5,         /* a device-side bounded wait gave up (kernel returned early) */
   PIFA_ERR_RANK_DEFICIENT = -6,  /* W' = U V^T has fewer than r independent rows               */
   PIFA_ERR_WORKSPACE = -7,       /* workspace missing or smaller than pifa_workspace_size()    */
-  PIFA_ERR_DEVICE_INDEX = -8,    /* a kernel met a pivot/non-pivot index outside [0, m)       */
+  PIFA_ERR_DEVICE_INDEX = -8,    /* a kernel met an index outside its range: a pivot or non-pivot, a slot, a page, a length,
+                                    a request's start                                          */
   PIFA_ERR_RANGE = -9,           /* a Y_p value exceeded the fp16 range (C stored as fp16)      */
-  PIFA_ERR_CAPACITY = -10        /* page tables: more tokens, pages or columns than there are   */
+  PIFA_ERR_CAPACITY = -10        /* page tables: more tokens, pages or columns than there are; attention: more keys than
+                                    the table's columns hold, more new tokens than max_q or rows */
 } pifa_status;
 
 /* Storage type of C. W_p, X and Y are always bf16. C may be bf16 or fp16 (both 2 bytes per
@@ -504,7 +506,8 @@ int pifa_validate_indices(const int32_t* pivot_idx, const int32_t* nonpivot_idx,
                           int64_t m, int64_t r);
 
 /* pifa_device_status -- synchronizes `cuda_stream`, then returns and clears the error word the
- * kernels latch on the current device (PIFA_OK, PIFA_ERR_TIMEOUT or PIFA_ERR_DEVICE_INDEX). */
+ * kernels latch on the current device (PIFA_OK, PIFA_ERR_TIMEOUT, PIFA_ERR_DEVICE_INDEX, PIFA_ERR_RANGE or
+ * PIFA_ERR_CAPACITY). */
 int pifa_device_status(void* cuda_stream);
 
 /* pifa_stream_captures -- 1 if what is enqueued on `cuda_stream` is being captured into a CUDA graph, 0 if not, a negative

@@ -99,7 +99,7 @@ struct TcArgs {
   int64_t ldo, ldt, pages;
   int T, heads, group, tpt, B, max_q,   // tpt: tokens of a tile
        cols, page_size, page_shift;
-  int token_at, head_at, page_at;    // their places among the tensor maps' coordinates 1 to 3
+  int token_at, head_at;             // their places among the tensor maps' coordinates 1 to 3; the page has the third
   float c;                           // |scale| log2(e)
   int negate;                        // scale < 0
   int wide;                          // rows of O start on 32-byte sectors
@@ -966,7 +966,6 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   if ((st = make_tmap_cache(&vmap, a.dtype, a.v, a.cache, rows, order)) != PIFA_OK) return st;
   g.token_at = order[0];
   g.head_at = order[1];
-  g.page_at = order[2];
   const int grid = pifa_sm_count();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(1);
