@@ -167,30 +167,32 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     whole_sum = 0;
   }
   pdl_wait_primary();
-  bool over = false, falls = false;
+  bool over = false;
   int items = 0;
+  unsigned falls = 0;  // starts that are less than the one before: counted with the items, from bit 40 on
   for (int b0 = 0; b0 < g.B; b0 += PLAN_THREADS) {
     const int b = b0 + tid;
-    int n = 0;
+    unsigned long long n = 0;
     if (b < g.B) {
       const Lengths x = lengths_of(g, b);
-      len[b] = x;
       over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
-      falls |= g.q_start[b + 1] < g.q_start[b];
-      n = (x.n + 2 * g.tpt - 1) / (2 * g.tpt);
+      n = (unsigned)((x.n + 2 * g.tpt - 1) / (2 * g.tpt)) | (unsigned long long)(g.q_start[b + 1] < g.q_start[b]) << 40;
+      len[b] = x;
     }
     unsigned long long total;
     const int at = (int)block_scan(n, part, total);
     if (b < g.B) first[b] = items + at;
     items += (int)total;
+    falls += (unsigned)(total >> 40);
   }
   if (tid == 0) first[g.B] = items;
   if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
   // Requests that overlap could have more rows than T, and more items than the list has room for: nothing is done then.
-  if (__syncthreads_or(falls)) {
+  if (falls > 0) {
     items = 0;
     if (tid == 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
   }
+  __syncthreads();
 
   // the item at place k of the list, later rows of a request first, and its cost in key tiles
   auto item_at = [&](int k, Item& x) {

@@ -378,13 +378,7 @@ def _graph_scratch(nbytes, device, stream):
 # ctypes lets other host threads run during a call: two of them on one stream (the default one, say) share its scratch, and
 # the kernels of one call must all be enqueued before those of the other.
 _shared_scratch = threading.Lock()
-
-
-def _enqueue(call, workspace_tensor, *args) -> int:
-    if workspace_tensor is not None:
-        return call(*args)
-    with _shared_scratch:
-        return call(*args)
+_own_scratch = contextlib.nullcontext()
 
 
 _workspaces: dict = {}
@@ -531,12 +525,12 @@ def pifa_forward(X, Wp, C, pivot_idx, nonpivot_idx, Y=None, variant: int = PIFA_
     if ws is not None and ws_ptr % 256:
         ws_ptr += 256 - ws_ptr % 256
     ws_bytes = 0 if ws is None else ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _enqueue(
-        _lib().pifa_forward_variant, workspace_tensor,
-        X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp),
-        C.data_ptr() if has_np else None, m, _ld(C) if has_np else r, cdt,
-        pivot_idx.data_ptr(), nonpivot_idx.data_ptr() if has_np else None,
-        Y.data_ptr(), _ld(Y), ws_ptr or None, ws_bytes, variant, _stream_ptr(stream))
+    with _shared_scratch if workspace_tensor is None else _own_scratch:
+        st = _lib().pifa_forward_variant(
+            X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp),
+            C.data_ptr() if has_np else None, m, _ld(C) if has_np else r, cdt,
+            pivot_idx.data_ptr(), nonpivot_idx.data_ptr() if has_np else None,
+            Y.data_ptr(), _ld(Y), ws_ptr or None, ws_bytes, variant, _stream_ptr(stream))
     _check(st, "pifa_forward")
     return Y
 
@@ -569,11 +563,11 @@ def pifa_forward_grouped(groups: int, X, Wp, C, pivot_idx, nonpivot_idx, Y=None,
     if ws is not None and ws_ptr % 256:
         ws_ptr += 256 - ws_ptr % 256
     ws_bytes = 0 if ws is None else ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _enqueue(
-        _lib().pifa_forward_grouped, workspace_tensor,
-        G, X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp), C.data_ptr(), m, _ld(C), cdt,
-        pivot_idx.data_ptr(), nonpivot_idx.data_ptr(), Y.data_ptr(), _ld(Y), ws_ptr or None, ws_bytes,
-        _stream_ptr(stream))
+    with _shared_scratch if workspace_tensor is None else _own_scratch:
+        st = _lib().pifa_forward_grouped(
+            G, X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp), C.data_ptr(), m, _ld(C), cdt,
+            pivot_idx.data_ptr(), nonpivot_idx.data_ptr(), Y.data_ptr(), _ld(Y), ws_ptr or None, ws_bytes,
+            _stream_ptr(stream))
     _check(st, "pifa_forward_grouped")
     return Y
 
@@ -631,14 +625,14 @@ def pifa_backward(X, Wp, C, pivot_idx, nonpivot_idx, dY, want=("dX", "dWp", "dC"
     ws = workspace_tensor if workspace_tensor is not None else workspace(need, dev, stream, tag="backward")
     ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
     ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _enqueue(
-        _lib().pifa_backward, workspace_tensor,
-        X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp), C.data_ptr() if has_np else None, m,
-        _ld(C) if has_np else r, pivot_idx.data_ptr(), nonpivot_idx.data_ptr() if has_np else None,
-        dY.data_ptr(), _ld(dY), dX.data_ptr() if dX is not None else None, _ld(dX) if dX is not None else n,
-        dWp.data_ptr() if dWp is not None else None, _ld(dWp) if dWp is not None else n,
-        dC.data_ptr() if dC is not None else None, _ld(dC) if dC is not None else r,
-        ws_ptr, ws_bytes, _stream_ptr(stream))
+    with _shared_scratch if workspace_tensor is None else _own_scratch:
+        st = _lib().pifa_backward(
+            X.data_ptr(), T, n, _ld(X), Wp.data_ptr(), r, _ld(Wp), C.data_ptr() if has_np else None, m,
+            _ld(C) if has_np else r, pivot_idx.data_ptr(), nonpivot_idx.data_ptr() if has_np else None,
+            dY.data_ptr(), _ld(dY), dX.data_ptr() if dX is not None else None, _ld(dX) if dX is not None else n,
+            dWp.data_ptr() if dWp is not None else None, _ld(dWp) if dWp is not None else n,
+            dC.data_ptr() if dC is not None else None, _ld(dC) if dC is not None else r,
+            ws_ptr, ws_bytes, _stream_ptr(stream))
     _check(st, "pifa_backward")
     return dX, dWp, dC
 
@@ -674,12 +668,12 @@ def pifa_m_accumulate(Xo, Xu, W, lam, XXt, YtXt=None, workspace_tensor=None, str
     ws = workspace_tensor if workspace_tensor is not None else workspace(need, Xu.device, stream, tag="macc")
     ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
     ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _enqueue(
-        _lib().pifa_m_accumulate, workspace_tensor,
-        Xo.data_ptr() if YtXt is not None else None, Xu.data_ptr(), T, n, _ld(Xu),
-        W.data_ptr() if YtXt is not None else None, m, _ld(W) if YtXt is not None else n, float(lam),
-        XXt.data_ptr(), _ld(XXt), YtXt.data_ptr() if YtXt is not None else None,
-        _ld(YtXt) if YtXt is not None else n, ws_ptr, ws_bytes, _stream_ptr(stream))
+    with _shared_scratch if workspace_tensor is None else _own_scratch:
+        st = _lib().pifa_m_accumulate(
+            Xo.data_ptr() if YtXt is not None else None, Xu.data_ptr(), T, n, _ld(Xu),
+            W.data_ptr() if YtXt is not None else None, m, _ld(W) if YtXt is not None else n, float(lam),
+            XXt.data_ptr(), _ld(XXt), YtXt.data_ptr() if YtXt is not None else None,
+            _ld(YtXt) if YtXt is not None else n, ws_ptr, ws_bytes, _stream_ptr(stream))
     _check(st, "pifa_m_accumulate")
     return XXt, YtXt
 
@@ -1023,11 +1017,11 @@ def pifa_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, max_q: int
             _refuse("workspace_tensor must be a tensor on Q's device")
         ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
         ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
-    st = _enqueue(
-        _lib().pifa_paged_attention, workspace_tensor,
-        Q.data_ptr(), ldq, T, h, hk, d, PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16,
-        k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh,
-        table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), B, int(max_q),
-        d ** -0.5 if scale is None else float(scale), O.data_ptr(), ldo, ws_ptr, ws_bytes, run_on)
+    with _shared_scratch if workspace_tensor is None else _own_scratch:
+        st = _lib().pifa_paged_attention(
+            Q.data_ptr(), ldq, T, h, hk, d, PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16,
+            k_cache.data_ptr(), v_cache.data_ptr(), pages, size, sp, st_, sh,
+            table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), B, int(max_q),
+            d ** -0.5 if scale is None else float(scale), O.data_ptr(), ldo, ws_ptr, ws_bytes, run_on)
     _check(st, "pifa_paged_attention")
     return O
