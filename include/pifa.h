@@ -353,9 +353,10 @@ int64_t pifa_m_reconstruct_workspace_size(int64_t m, int64_t n, int64_t r);
 
 /*
  * Attention between the projections. A PIFA layer replaces a linear layer; the calls below are what lies between
- * a decoder layer's q / k / v projections and its output projection when it serves or trains: page tables for a
+ * a decoder layer's q / k / v projections and its output projection when it serves: page tables for a
  * step's requests, rotary positions with the write into a paged key / value cache, and attention of each
- * request's new tokens over its pages. The paper has no counterpart.
+ * request's new tokens over its pages. The rotation alone has a gradient too (pifa_rope, inverse). The paper has no
+ * counterpart.
  *
  * The cache of one layer is two DEVICE buffers of `dtype` (a pifa_dtype), k_cache and v_cache, of `pages` pages
  * of `page_size` tokens of `kv_heads` heads of `head_dim` elements; element e of head h of token o of page p is
@@ -474,9 +475,10 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
  *                rows: streamed by warps; more: on the tensor cores). A request with more
  *                latches PIFA_ERR_CAPACITY and its further rows are not written.
  *   workspace    DEVICE scratch of pifa_paged_attention_workspace_size() bytes, 256-byte aligned, no
- *                initialisation needed.
+ *                initialisation needed; not used by another call that may run at the same time, replays of a graph that
+ *                captured this one among them.
  *   head_dim 64 or 128; page_size a power of two from 16 to 256; q_heads a multiple of kv_heads, at most 64 query heads to a
- *   key / value head; B <= 4096 (PIFA_ERR_UNSUPPORTED).
+ *   key / value head; B <= 4096; T q_heads < 2^32; B kv_heads (cols page_size / 16 + 1) < 2^31 (PIFA_ERR_UNSUPPORTED).
  *   What the cache holds past a request's kv_len, or in pages of no request, is not used, whatever its bits. A key
  *   that some new token of its request sees is part of that request's products: an infinity or NaN in its V
  *   may reach the request's other new tokens too (0 times infinity). A K that is not finite stays with the tokens

@@ -10,7 +10,9 @@
 // and sum need no exchange; p = exp2(c s - c m) goes back to tensor memory as bf16 or fp16 over S's columns
 // and is the first operand of O += P V. m is only raised, and O and l rescaled, when the row's maximum
 // has grown by more than 8 in the exponent (then O's columns are read and written by the row's warp);
-// until then weights reach 2^8 at most, which costs neither format precision.
+// until then weights reach 2^8 at most, which costs neither format precision. The rounding of the weights, which l
+// adds up as they were, takes the outputs' error from 0.0017 of their size to 0.0022 in bf16, from 0.00021 to 0.00026 in fp16; a
+// product of their lower parts as well, half as many MMAs again, was not taken.
 //
 // CTA of 384 threads, one per SM, persistent:
 //   warps 0-3, 4-7   softmax and epilogue of tile 0 and 1 (tensor memory quarter = warp % 4)
