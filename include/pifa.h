@@ -501,6 +501,67 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
 int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
                                             int64_t max_q);
 
+/*
+ * The same cache in 8 bits: half the bytes to hold and to read. Elements are e4m3 (1 sign, 4 exponent, 3 mantissa bits, no
+ * infinity, 0x7f and 0xff NaN), with a scale for each block of PIFA_Q8_BLOCK tokens of a page and each head: a power of two, held
+ * as the byte b of 2^(b - 127) (e8m0; 255: NaN). A value is element times scale.
+ * Two buffers of elements, k_cache and v_cache, laid out as above with strides in elements (bytes; multiples of 16), and two of
+ * scales, k_scale and v_scale: the scale of block o / PIFA_Q8_BLOCK of page p and head h is at p * scale_page_stride +
+ * (o / PIFA_Q8_BLOCK) * scale_block_stride + h * scale_head_stride. page_size is a multiple of PIFA_Q8_BLOCK. page tables,
+ * slots and positions are those of pifa_page_tables.
+ */
+#define PIFA_Q8_BLOCK 16
+
+/*
+ * pifa_rope_cache_q8 -- pifa_rope_cache into a cache in 8 bits: K turned, V as it is, each in fp32 and rounded once to e4m3 (to
+ * nearest even) in units of its block's scale.
+ *   The scale is the smallest power of two, from 2^-126 on, that brings the largest finite magnitude of the block's tokens to 448 or
+ *   less. A block whose first token is among those written begins anew: what else it holds, and its scale, may be anything. Otherwise
+ *   its scale is raised if the new tokens need it and stays if not, and when it rises the elements that are not written are rounded
+ *   anew to it. Tokens that come one by one give the scales of tokens that come at once. A block whose scale is NaN keeps it.
+ *   Infinities and NaN are stored as NaN.
+ *   Q, K, V, T, heads, positions, freq, rot_dim, layout, scale, Qr: as pifa_rope_cache.
+ *   slots        DEVICE, int64[T], as pifa_rope_cache. Slots of one call differ, and rows whose slots lie in one block are
+ *                neighbours (in any order), as pifa_page_tables makes them. What a block whose rows are apart, or with a slot that comes
+ *                twice, holds afterwards is not specified; neighbouring rows with the same slot latch PIFA_ERR_DEVICE_INDEX.
+ */
+int pifa_rope_cache_q8(const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv, int64_t T,
+                       int64_t q_heads, int64_t kv_heads, int64_t head_dim, int dtype,
+                       const int32_t* positions, const int64_t* slots,
+                       const int64_t* freq, int64_t rot_dim, int layout, float scale,
+                       void* Qr, int64_t ldqr, void* k_cache, void* v_cache, void* k_scale, void* v_scale,
+                       int64_t pages, int64_t page_size, int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                       int64_t scale_page_stride, int64_t scale_block_stride, int64_t scale_head_stride, void* cuda_stream);
+
+/*
+ * pifa_cache_read_q8 -- tokens of a cache in 8 bits, read back: row t of K and V gets what slots[t] holds, as T rows of kv_heads
+ * heads, dtype, rounded once (bf16: exact from 2^-117 on). A value beyond the type's largest finite number becomes that.
+ *   slots        DEVICE, int64[T], in any order, also the same one twice; a row whose slot is -1 is not written, nor is one whose slot
+ *                lies outside [0, pages * page_size), which latches PIFA_ERR_DEVICE_INDEX.
+ *   K, V         DEVICE out, ldk and ldv >= kv_heads * head_dim; head_dim a multiple of 16 up to 512.
+ */
+int pifa_cache_read_q8(const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
+                       int64_t pages, int64_t page_size, int64_t kv_heads, int64_t head_dim,
+                       int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                       int64_t scale_page_stride, int64_t scale_block_stride, int64_t scale_head_stride,
+                       const int64_t* slots, int64_t T, int dtype, void* K, int64_t ldk, void* V, int64_t ldv,
+                       void* cuda_stream);
+
+/*
+ * pifa_paged_attention_q8 -- pifa_paged_attention over a cache in 8 bits.
+ *   As there, but for: the caches and scales, as above; page_size a power of two from 16 to 256.
+ *   Numerics: Q enters the first product in fp16, in bf16's case times a power of two for each row that brings its largest
+ *   magnitude to [2^14, 2^15); keys and values enter as fp16, which holds e4m3 exactly, without their scales, which are applied in fp32
+ *   (the keys') or as part of the weights' exponent (the values'). Weights are fp16, at most 2^8; scores, running maximum and sums fp32.
+ */
+int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                            int dtype, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
+                            int64_t pages, int64_t page_size, int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                            int64_t scale_page_stride, int64_t scale_block_stride, int64_t scale_head_stride,
+                            const int32_t* table, int64_t cols, int64_t ldt,
+                            const int32_t* q_start, const int32_t* kv_len, int64_t B, int64_t max_q, float scale,
+                            void* O, int64_t ldo, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
 /* pifa_validate_indices -- HOST copies: PIFA_OK iff pivot_idx (r entries) and nonpivot_idx
  * (m - r entries) are strictly ascending, inside [0, m) and disjoint (so together a partition
  * of [0, m), as Algorithm 1 step 2 defines I^c); else PIFA_ERR_INVALID_ARG. */

@@ -186,8 +186,37 @@ int pifa_check_cache(const PifaCacheShape& c, int64_t least, int64_t most) {
   return PIFA_OK;
 }
 
-PifaSpan pifa_cache_span(const void* base, const PifaCacheShape& c) {
-  return pifa_span(base, 1, (c.pages - 1) * c.page_stride + (c.page_size - 1) * c.token_stride + (c.heads - 1) * c.head_stride + c.dim, 0, 2);
+PifaSpan pifa_cache_span(const void* base, const PifaCacheShape& c, int64_t elem) {
+  return pifa_span(base, 1, (c.pages - 1) * c.page_stride + (c.page_size - 1) * c.token_stride + (c.heads - 1) * c.head_stride + c.dim, 0, elem);
+}
+
+int pifa_check_cache_q8(const PifaCacheShape& c, const PifaScaleShape& s, int64_t most) {
+  const int st = pifa_check_cache(c, PIFA_Q8_BLOCK, most);
+  if (st != PIFA_OK) return st;
+  if (c.page_size % PIFA_Q8_BLOCK) return pifa_fail(PIFA_ERR_UNSUPPORTED, "cache: page_size must be a multiple of 16 tokens");
+  if ((c.page_stride | c.token_stride | c.head_stride) & 15)
+    return pifa_fail(PIFA_ERR_ALIGNMENT, "cache: strides must be multiples of 16 elements");
+  const int64_t far = (int64_t)1 << 46;
+  struct { int64_t n, stride; } d[3] = {
+      {c.heads, s.head_stride}, {c.page_size / PIFA_Q8_BLOCK, s.block_stride}, {c.pages, s.page_stride}};
+  for (const auto& x : d)
+    if (x.stride < 0 || x.stride >= far || x.stride > ((int64_t)1 << 60) / x.n)
+      return pifa_fail(PIFA_ERR_INVALID_ARG, "scales: a stride out of range");
+  for (int i = 0; i < 3; ++i)
+    for (int j = 0; j < i; ++j)
+      if (d[i].stride < d[j].stride) std::swap(d[i], d[j]);
+  int64_t extent = 1;
+  for (const auto& x : d) {
+    if (x.n == 1) continue;
+    if (x.stride < extent) return pifa_fail(PIFA_ERR_INVALID_ARG, "scales: strides make elements overlap");
+    extent += (x.n - 1) * x.stride;
+  }
+  return PIFA_OK;
+}
+
+PifaSpan pifa_scale_span(const void* base, const PifaCacheShape& c, const PifaScaleShape& s) {
+  return pifa_span(base, 1, (c.pages - 1) * s.page_stride + (c.page_size / PIFA_Q8_BLOCK - 1) * s.block_stride +
+                                (c.heads - 1) * s.head_stride + 1, 0, 1);
 }
 
 // ---- public API ---------------------------------------------------------------------------------

@@ -504,33 +504,18 @@ cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
   return pifa_launch_ex(&cfg, attention_join<F16, D>, g, split);
 }
 
-}  // namespace
-
-extern "C" {
-
-int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
-                                            int64_t max_q) {
-  pifa_clear_error();
-  const int st = check_sizes(T, q_heads, kv_heads, head_dim, B, max_q);
-  if (st != PIFA_OK) return st;
-  if (T == 0 || B == 0) return 0;
-  const int64_t group = q_heads / kv_heads;
-  return kWorkspaceReserve + (takes_tc(group, max_q) ? attention_tc_workspace_bytes(T, q_heads, kv_heads, head_dim, B)
-                                                     : rows_workspace_bytes(group * max_q, head_dim, B));
-}
-
-int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
-                         int dtype, const void* k_cache, const void* v_cache, int64_t pages, int64_t page_size,
-                         int64_t page_stride, int64_t token_stride, int64_t head_stride, const int32_t* table,
-                         int64_t cols, int64_t ldt, const int32_t* q_start, const int32_t* kv_len, int64_t B,
-                         int64_t max_q, float scale, void* O, int64_t ldo, void* workspace, int64_t workspace_bytes,
-                         void* cuda_stream) {
+// Both forms of the cache; q8: the scales of one in 8 bits, else null.
+int attend(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int dtype,
+           const void* k_cache, const void* v_cache, const PifaScales* q8, int64_t pages, int64_t page_size, int64_t page_stride,
+           int64_t token_stride, int64_t head_stride, const int32_t* table, int64_t cols, int64_t ldt, const int32_t* q_start,
+           const int32_t* kv_len, int64_t B, int64_t max_q, float scale, void* O, int64_t ldo, void* workspace,
+           int64_t workspace_bytes, void* cuda_stream) {
   pifa_clear_error();
   const int64_t need = pifa_paged_attention_workspace_size(T, q_heads, kv_heads, head_dim, B, max_q);
   if (need < 0) return (int)need;
   if (dtype != PIFA_DTYPE_BF16 && dtype != PIFA_DTYPE_FP16) return pifa_fail(PIFA_ERR_INVALID_ARG, "unknown dtype");
   const PifaCacheShape c = {pages, page_size, kv_heads, head_dim, page_stride, token_stride, head_stride};
-  int st = pifa_check_cache(c, 16, 256);
+  int st = q8 ? pifa_check_cache_q8(c, q8->shape, 256) : pifa_check_cache(c, 16, 256);
   if (st != PIFA_OK) return st;
   if (page_size & (page_size - 1)) return pifa_fail(PIFA_ERR_UNSUPPORTED, "attention takes a page_size that is a power of two");
   const int64_t lim = (int64_t)1 << 30;
@@ -539,7 +524,7 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   if (B * kv_heads * (cols * page_size / STEP + 1) >= 2 * lim)
     return pifa_fail(PIFA_ERR_UNSUPPORTED, "attention takes at most 2^35 keys, over all requests and heads, in the tables");
   if (T == 0 || B == 0) return PIFA_OK;
-  if (!Q || !k_cache || !v_cache || !O || !q_start || !kv_len || (cols && !table))
+  if (!Q || !k_cache || !v_cache || !O || !q_start || !kv_len || (cols && !table) || (q8 && (!q8->k || !q8->v)))
     return pifa_fail(PIFA_ERR_INVALID_ARG, "null argument");
   const int64_t row = q_heads * head_dim;
   if (ldq < row || ldo < row) return pifa_fail(PIFA_ERR_INVALID_ARG, "leading dimension smaller than the row length");
@@ -550,9 +535,12 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   if (reinterpret_cast<uintptr_t>(workspace) & 255u)
     return pifa_fail(PIFA_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
   const PifaSpan o = pifa_span(O, T, row, ldo, 2), ws = pifa_span(workspace, 1, need, need, 1);
-  const PifaSpan in[] = {pifa_span(Q, T, row, ldq, 2), pifa_cache_span(k_cache, c), pifa_cache_span(v_cache, c),
+  const int64_t elem = q8 ? 1 : 2;
+  const PifaSpan none = {0, 0};
+  const PifaSpan in[] = {pifa_span(Q, T, row, ldq, 2), pifa_cache_span(k_cache, c, elem), pifa_cache_span(v_cache, c, elem),
                          pifa_span(table, B, cols, ldt, 4), pifa_span(q_start, 1, B + 1, B + 1, 4),
-                         pifa_span(kv_len, 1, B, B, 4)};
+                         pifa_span(kv_len, 1, B, B, 4), q8 ? pifa_scale_span(q8->k, c, q8->shape) : none,
+                         q8 ? pifa_scale_span(q8->v, c, q8->shape) : none};
   bool bad = pifa_spans_overlap(o, ws);
   for (const PifaSpan& x : in) bad = bad || pifa_spans_overlap(o, x) || pifa_spans_overlap(ws, x);
   if (bad) return pifa_fail(PIFA_ERR_INVALID_ARG, "O or workspace overlaps another buffer");
@@ -560,7 +548,8 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   int* status = pifa_status_word(&e);
   if (!status) return pifa_fail_cuda("device status word", e);
   const PifaAttention a = {Q, k_cache, v_cache, O, table, q_start, kv_len, T, ldq, ldo, ldt, cols, B, max_q, q_heads, c, dtype,
-                           scale * 1.4426950408889634f, static_cast<uint8_t*>(workspace) + kWorkspaceReserve};
+                           scale * 1.4426950408889634f, static_cast<uint8_t*>(workspace) + kWorkspaceReserve, q8};
+  if (q8) return launch_attention_q8(a, status, reinterpret_cast<cudaStream_t>(cuda_stream));
   if (takes_tc(q_heads / kv_heads, max_q))
     return launch_attention_tc(a, status, pifa_wait_timeout_ns(), reinterpret_cast<cudaStream_t>(cuda_stream));
   RowArgs g = {};
@@ -599,6 +588,44 @@ int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads,
   else e = f16 ? launch_rows<true, 128>(g, stream) : launch_rows<false, 128>(g, stream);
   if (e != cudaSuccess) return pifa_fail_cuda("attention launch", e);
   return PIFA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
+                                            int64_t max_q) {
+  pifa_clear_error();
+  const int st = check_sizes(T, q_heads, kv_heads, head_dim, B, max_q);
+  if (st != PIFA_OK) return st;
+  if (T == 0 || B == 0) return 0;
+  const int64_t group = q_heads / kv_heads;
+  return kWorkspaceReserve + (takes_tc(group, max_q) ? attention_tc_workspace_bytes(T, q_heads, kv_heads, head_dim, B)
+                                                     : rows_workspace_bytes(group * max_q, head_dim, B));
+}
+
+int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                         int dtype, const void* k_cache, const void* v_cache, int64_t pages, int64_t page_size,
+                         int64_t page_stride, int64_t token_stride, int64_t head_stride, const int32_t* table,
+                         int64_t cols, int64_t ldt, const int32_t* q_start, const int32_t* kv_len, int64_t B,
+                         int64_t max_q, float scale, void* O, int64_t ldo, void* workspace, int64_t workspace_bytes,
+                         void* cuda_stream) {
+  return attend(Q, ldq, T, q_heads, kv_heads, head_dim, dtype, k_cache, v_cache, nullptr, pages, page_size, page_stride, token_stride,
+                head_stride, table, cols, ldt, q_start, kv_len, B, max_q, scale, O, ldo, workspace, workspace_bytes, cuda_stream);
+}
+
+int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                            int dtype, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
+                            int64_t pages, int64_t page_size, int64_t page_stride, int64_t token_stride, int64_t head_stride,
+                            int64_t scale_page_stride, int64_t scale_block_stride, int64_t scale_head_stride,
+                            const int32_t* table, int64_t cols, int64_t ldt, const int32_t* q_start, const int32_t* kv_len,
+                            int64_t B, int64_t max_q, float scale, void* O, int64_t ldo, void* workspace,
+                            int64_t workspace_bytes, void* cuda_stream) {
+  const PifaScales q8 = {static_cast<const uint8_t*>(k_scale), static_cast<const uint8_t*>(v_scale),
+                         {scale_page_stride, scale_block_stride, scale_head_stride}};
+  return attend(Q, ldq, T, q_heads, kv_heads, head_dim, dtype, k_cache, v_cache, &q8, pages, page_size, page_stride, token_stride,
+                head_stride, table, cols, ldt, q_start, kv_len, B, max_q, scale, O, ldo, workspace, workspace_bytes, cuda_stream);
 }
 
 }  // extern "C"

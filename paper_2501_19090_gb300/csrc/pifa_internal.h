@@ -107,10 +107,27 @@ struct PifaCacheShape {
 };
 // PIFA_OK, or the failure, for sizes and strides; page_size in [least, most].
 int pifa_check_cache(const PifaCacheShape& c, int64_t least, int64_t most);
-// The bytes from the first to the last element of one buffer.
-PifaSpan pifa_cache_span(const void* base, const PifaCacheShape& c);
+// The bytes from the first to the last element of one buffer; `elem`: bytes of one.
+PifaSpan pifa_cache_span(const void* base, const PifaCacheShape& c, int64_t elem = 2);
+// Scales of a cache in 8 bits: bytes from page to page, from block of PIFA_Q8_BLOCK tokens to block, from head to head.
+struct PifaScaleShape {
+  int64_t page_stride, block_stride, head_stride;
+};
+// As pifa_check_cache, for a cache in 8 bits and its scales.
+int pifa_check_cache_q8(const PifaCacheShape& c, const PifaScaleShape& s, int64_t most);
+PifaSpan pifa_scale_span(const void* base, const PifaCacheShape& c, const PifaScaleShape& s);
 
-// ---- attention over a paged cache (attention.cu, attention_tc.cu) --------------------------------
+// ---- rows of heads that are rotated (rope.cu) -----------------------------------------------------
+int pifa_check_heads(int64_t T, int64_t heads, int64_t dim, int dtype, int64_t rot, int layout, float scale);
+// Whether T rows of `na` 2-byte elements and T rows of `nb` have an element in common: columns of one matrix may interleave.
+bool pifa_rows_overlap(const void* a, int64_t na, int64_t lda, const void* b, int64_t nb, int64_t ldb, int64_t T);
+
+// ---- attention over a paged cache (attention.cu, attention_q8.cu, attention_tc.cu) ----------------
+// The scales of a cache in 8 bits.
+struct PifaScales {
+  const uint8_t *k, *v;
+  PifaScaleShape shape;
+};
 struct PifaAttention {
   const void *q, *k, *v;
   void* o;
@@ -120,7 +137,10 @@ struct PifaAttention {
   int dtype;          // PIFA_DTYPE_*
   float scale_log2;   // scale log2(e)
   void* ws;           // after the reserve
+  const PifaScales* q8;  // null: elements of dtype
 };
+// Over a cache in 8 bits.
+int launch_attention_q8(const PifaAttention& a, int* status, cudaStream_t stream);
 // Chunks of new tokens on the tensor cores.
 int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B);
 int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream);

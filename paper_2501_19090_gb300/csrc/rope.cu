@@ -15,174 +15,17 @@
 // is 6.8); 2048 tokens of 32 heads, forward and gradient (two launches, 67 MB) 15.1 us.
 #include <cmath>
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "pifa.h"
-#include "pifa_internal.h"
-#include "ptx.cuh"
+#include "rope.cuh"
 
 namespace {
 
-using namespace pifa;
-
-constexpr int THREADS = 256;
-constexpr int MAX_TOKENS = 4;     // tokens of one CTA
-constexpr int MAX_DIM = 512;
-
-struct RopeArgs {
-  const uint16_t *q, *k, *v;
-  uint16_t *qr, *kc, *vc;
-  const int32_t* positions;
-  const int64_t* slots;
-  const int64_t* freq;
-  int64_t ldq, ldk, ldv, ldqr;
-  int64_t page_stride, token_stride, head_stride, n_slots;
-  int page_size;
-  int T, hq, hk, dim, rot;
-  int tokens;                     // of one CTA
-  int heads;                      // of one CTA (blockIdx.y)
-  float scale;
-  int inverse;
-  int* status;
-};
-
-template <bool F16>
-__device__ __forceinline__ float2 unpack(uint32_t w) {
-  if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
-  else return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-}
-template <bool F16>
-__device__ __forceinline__ uint32_t pack(float a, float b) {
-  if constexpr (F16) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  } else {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-}
+constexpr int THREADS = ROPE_THREADS;
 
 template <bool F16, bool HALF>
 __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeArgs g) {
-  __shared__ __align__(16) float2 turn[MAX_TOKENS][MAX_DIM / 2];
-  __shared__ int64_t place[MAX_TOKENS];  // the token's offset in the cache, -1: not stored
   pdl_launch_dependents();
   pdl_wait_primary();
-  const int t0 = (int)blockIdx.x * g.tokens, nt = min(g.tokens, g.T - t0);
-  const int pairs = g.rot / 2;
-  const int units = g.dim / 16, turned = g.rot / 16;
-  const int h0 = (int)blockIdx.y * g.heads, nh = min(g.heads, g.hq + 2 * g.hk - h0), n = nt * nh * units;
-  // a unit's two vectors: halves of the turned part, or neighbours; those of a thread's next unit are in flight
-  // while it works on one, the first ones while the CTA computes its cosines and sines
-  struct Unit {
-    int tt, h, u, a0, a1;
-    uint4 va, vb;
-  } next;
-  auto fetch = [&](int i) {
-    const int hh = i / units;
-    next.u = i - hh * units;
-    next.tt = hh / nh;
-    next.h = h0 + hh - next.tt * nh;
-    const int64_t t = t0 + next.tt;
-    const uint16_t* src = next.h < g.hq           ? g.q + t * g.ldq + (int64_t)next.h * g.dim
-                          : next.h < g.hq + g.hk ? g.k + t * g.ldk + (int64_t)(next.h - g.hq) * g.dim
-                                                  : g.v + t * g.ldv + (int64_t)(next.h - g.hq - g.hk) * g.dim;
-    const bool apart = HALF && next.u < turned;
-    next.a0 = apart ? next.u * 8 : next.u * 16;
-    next.a1 = apart ? next.u * 8 + pairs : next.u * 16 + 8;
-    next.va = *reinterpret_cast<const uint4*>(src + next.a0);
-    next.vb = *reinterpret_cast<const uint4*>(src + next.a1);
-  };
-  if ((int)threadIdx.x < n) fetch(threadIdx.x);
-  for (int i = threadIdx.x; i < nt * pairs; i += THREADS) {
-    const int tt = i / pairs, p = i - tt * pairs;
-    const uint64_t phase = (uint64_t)(int64_t)g.positions[t0 + tt] * (uint64_t)g.freq[p];
-    float s, c;
-    sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);
-    // two pairs make a float4; those that a unit's lanes read together lie together
-    turn[tt][2 * ((p & 7) / 2 * turned + p / 8) + (p & 1)] = make_float2(c * g.scale, (g.inverse ? -s : s) * g.scale);
-  }
-  if (g.hk && threadIdx.x < nt) {
-    const int64_t slot = g.slots[t0 + threadIdx.x];
-    int64_t at = -1;
-    if (slot >= 0 && slot < g.n_slots) {
-      const int64_t page = slot / g.page_size;
-      at = page * g.page_stride + (slot - page * g.page_size) * g.token_stride;
-    } else if (slot != -1) {
-      latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-    }
-    place[threadIdx.x] = at;
-  }
-  __syncthreads();
-
-  for (int i = threadIdx.x; i < n; i += THREADS) {
-    Unit x = next;
-    if (i + THREADS < n) fetch(i + THREADS);
-    uint16_t* dst;
-    if (x.h < g.hq) {
-      dst = g.qr + (int64_t)(t0 + x.tt) * g.ldqr + (int64_t)x.h * g.dim;
-    } else {
-      const bool is_v = x.h >= g.hq + g.hk;
-      const int64_t at = place[x.tt];
-      if (at < 0) continue;
-      dst = (is_v ? g.vc : g.kc) + at + (x.h - g.hq - (is_v ? g.hk : 0)) * g.head_stride;
-    }
-    const bool turns = x.u < turned && x.h < g.hq + g.hk;
-    if (turns) {
-      uint32_t* wa = reinterpret_cast<uint32_t*>(&x.va);
-      uint32_t* wb = reinterpret_cast<uint32_t*>(&x.vb);
-      const float4* cs = reinterpret_cast<const float4*>(turn[x.tt]) + x.u;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 r = cs[j * turned];
-        if constexpr (HALF) {
-          const float2 v = unpack<F16>(wa[j]), y = unpack<F16>(wb[j]);
-          wa[j] = pack<F16>(v.x * r.x - y.x * r.y, v.y * r.z - y.y * r.w);
-          wb[j] = pack<F16>(y.x * r.x + v.x * r.y, y.y * r.z + v.y * r.w);
-        } else {
-          uint32_t* w = (j < 2 ? wa : wb) + 2 * (j & 1);
-          const float2 p = unpack<F16>(w[0]), q = unpack<F16>(w[1]);
-          w[0] = pack<F16>(p.x * r.x - p.y * r.y, p.y * r.x + p.x * r.y);
-          w[1] = pack<F16>(q.x * r.z - q.y * r.w, q.y * r.z + q.x * r.w);
-        }
-      }
-    }
-    *reinterpret_cast<uint4*>(dst + x.a0) = x.va;
-    *reinterpret_cast<uint4*>(dst + x.a1) = x.vb;
-  }
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// Whether T rows of `na` elements and T rows of `nb` have an element in common: columns of one matrix may interleave.
-bool rows_overlap(const void* a, int64_t na, int64_t lda, const void* b, int64_t nb, int64_t ldb, int64_t T) {
-  if (!pifa_spans_overlap(pifa_span(a, T, na, lda, 2), pifa_span(b, T, nb, ldb, 2))) return false;
-  // a's element 0 is column 0; b's is element `from`
-  const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)) / 2;
-  if (lda == ldb) {
-    const int64_t at = (from % lda + lda) % lda;
-    return at < na || at + nb > lda;
-  }
-  for (int64_t i = 0; i < T; ++i) {  // the first row of b that ends behind the start of a's row i
-    const int64_t behind = i * lda - from - nb;
-    const int64_t j = behind < 0 ? 0 : behind / ldb + 1;
-    if (j < T && from + j * ldb < i * lda + na) return true;
-  }
-  return false;
-}
-
-int check_heads(int64_t T, int64_t heads, int64_t dim, int dtype, int64_t rot, int layout, float scale) {
-  const int64_t lim = (int64_t)1 << 30;
-  if (T < 0 || T >= lim) return pifa_fail(PIFA_ERR_INVALID_ARG, "T must be in [0, 2^30)");
-  if (heads < 1 || heads > 65536) return pifa_fail(PIFA_ERR_INVALID_ARG, "heads must be in [1, 65536]");
-  if (dtype != PIFA_DTYPE_BF16 && dtype != PIFA_DTYPE_FP16) return pifa_fail(PIFA_ERR_INVALID_ARG, "unknown dtype");
-  if (layout != PIFA_ROPE_HALF && layout != PIFA_ROPE_INTERLEAVED) return pifa_fail(PIFA_ERR_INVALID_ARG, "unknown layout");
-  if (!std::isfinite(scale)) return pifa_fail(PIFA_ERR_INVALID_ARG, "scale must be finite");
-  if (dim < 1 || rot < 2 || rot > dim) return pifa_fail(PIFA_ERR_INVALID_ARG, "need 2 <= rot_dim <= head_dim");
-  if (dim % 16 || dim > MAX_DIM || rot % 16)
-    return pifa_fail(PIFA_ERR_UNSUPPORTED, "head_dim and rot_dim must be multiples of 16, head_dim at most 512");
-  return PIFA_OK;
+  rope_tokens<F16, HALF>(g, (int)blockIdx.x, (int)blockIdx.y);
 }
 
 int launch(RopeArgs g, int dtype, int layout, void* cuda_stream) {
@@ -214,6 +57,36 @@ int launch(RopeArgs g, int dtype, int layout, void* cuda_stream) {
 }
 
 }  // namespace
+
+// Whether T rows of `na` elements and T rows of `nb` have an element in common: columns of one matrix may interleave.
+bool pifa_rows_overlap(const void* a, int64_t na, int64_t lda, const void* b, int64_t nb, int64_t ldb, int64_t T) {
+  if (!pifa_spans_overlap(pifa_span(a, T, na, lda, 2), pifa_span(b, T, nb, ldb, 2))) return false;
+  // a's element 0 is column 0; b's is element `from`
+  const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)) / 2;
+  if (lda == ldb) {
+    const int64_t at = (from % lda + lda) % lda;
+    return at < na || at + nb > lda;
+  }
+  for (int64_t i = 0; i < T; ++i) {  // the first row of b that ends behind the start of a's row i
+    const int64_t behind = i * lda - from - nb;
+    const int64_t j = behind < 0 ? 0 : behind / ldb + 1;
+    if (j < T && from + j * ldb < i * lda + na) return true;
+  }
+  return false;
+}
+
+int pifa_check_heads(int64_t T, int64_t heads, int64_t dim, int dtype, int64_t rot, int layout, float scale) {
+  const int64_t lim = (int64_t)1 << 30;
+  if (T < 0 || T >= lim) return pifa_fail(PIFA_ERR_INVALID_ARG, "T must be in [0, 2^30)");
+  if (heads < 1 || heads > 65536) return pifa_fail(PIFA_ERR_INVALID_ARG, "heads must be in [1, 65536]");
+  if (dtype != PIFA_DTYPE_BF16 && dtype != PIFA_DTYPE_FP16) return pifa_fail(PIFA_ERR_INVALID_ARG, "unknown dtype");
+  if (layout != PIFA_ROPE_HALF && layout != PIFA_ROPE_INTERLEAVED) return pifa_fail(PIFA_ERR_INVALID_ARG, "unknown layout");
+  if (!std::isfinite(scale)) return pifa_fail(PIFA_ERR_INVALID_ARG, "scale must be finite");
+  if (dim < 1 || rot < 2 || rot > dim) return pifa_fail(PIFA_ERR_INVALID_ARG, "need 2 <= rot_dim <= head_dim");
+  if (dim % 16 || dim > MAX_DIM || rot % 16)
+    return pifa_fail(PIFA_ERR_UNSUPPORTED, "head_dim and rot_dim must be multiples of 16, head_dim at most 512");
+  return PIFA_OK;
+}
 
 extern "C" {
 
@@ -248,7 +121,7 @@ int pifa_rope(const void* X, int64_t T, int64_t heads, int64_t ldx, int64_t head
               const int32_t* positions, const int64_t* freq, int64_t rot_dim, int layout, float scale, int inverse,
               void* Y, int64_t ldy, void* cuda_stream) {
   pifa_clear_error();
-  int st = check_heads(T, heads, head_dim, dtype, rot_dim, layout, scale);
+  int st = pifa_check_heads(T, heads, head_dim, dtype, rot_dim, layout, scale);
   if (st != PIFA_OK) return st;
   if (T == 0) return PIFA_OK;
   if (!X || !Y || !positions || !freq) return pifa_fail(PIFA_ERR_INVALID_ARG, "null X, Y, positions or freq");
@@ -280,7 +153,7 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
                     int64_t ldqr, void* k_cache, void* v_cache, int64_t pages, int64_t page_size, int64_t page_stride,
                     int64_t token_stride, int64_t head_stride, void* cuda_stream) {
   pifa_clear_error();
-  int st = check_heads(T, q_heads, head_dim, dtype, rot_dim, layout, scale);
+  int st = pifa_check_heads(T, q_heads, head_dim, dtype, rot_dim, layout, scale);
   if (st != PIFA_OK) return st;
   const PifaCacheShape c = {pages, page_size, kv_heads, head_dim, page_stride, token_stride, head_stride};
   if ((st = pifa_check_cache(c, 1, 65536)) != PIFA_OK) return st;
@@ -298,7 +171,7 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
   // the two caches may interleave (pages of keys and values in turn), so their spans may overlap; a row of Q that
   // interleaves with K and V (columns of one projection) may too, but Qr then has to be Q itself or apart
   const bool in_place = Qr == Q && ldqr == ldq;
-  bool bad = in_place ? rows_overlap(Q, qrow, ldq, K, krow, ldk, T) || rows_overlap(Q, qrow, ldq, V, krow, ldv, T)
+  bool bad = in_place ? pifa_rows_overlap(Q, qrow, ldq, K, krow, ldk, T) || pifa_rows_overlap(Q, qrow, ldq, V, krow, ldv, T)
                       : pifa_spans_overlap(qr, q) || pifa_spans_overlap(qr, in[0]) || pifa_spans_overlap(qr, in[1]);
   for (const PifaSpan& cache : {kc, vc})
     bad = bad || pifa_spans_overlap(cache, q) || pifa_spans_overlap(cache, in[0]) || pifa_spans_overlap(cache, in[1]) ||

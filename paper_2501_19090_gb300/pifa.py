@@ -44,6 +44,8 @@ PIFA_DECODE_GRID_WAVES = 1
 PIFA_DECODE_GRID_PERSISTENT = 2
 PIFA_DECODE_GRID_SPLITK = 3
 
+PIFA_Q8_BLOCK = 16
+
 PIFA_ROPE_HALF = 0
 PIFA_ROPE_INTERLEAVED = 1
 
@@ -64,6 +66,7 @@ EXPORTS = (
     "pifa_m_reconstruct", "pifa_m_reconstruct_workspace_size",
     "pifa_page_tables", "pifa_rope_frequencies", "pifa_rope", "pifa_rope_cache",
     "pifa_paged_attention", "pifa_paged_attention_workspace_size", "pifa_stream_captures",
+    "pifa_rope_cache_q8", "pifa_cache_read_q8", "pifa_paged_attention_q8",
 )
 
 
@@ -153,6 +156,17 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                              _I64, _I64, _I64, _VP, _I64, _I64, _VP, _VP, _I64, _I64, ctypes.c_float,
                                              _VP, _I64, _VP, _I64, _VP]
         lib.pifa_paged_attention.restype = ctypes.c_int
+        lib.pifa_rope_cache_q8.argtypes = [_VP, _I64, _VP, _I64, _VP, _I64, _I64, _I64, _I64, _I64, ctypes.c_int, _VP,
+                                           _VP, _VP, _I64, ctypes.c_int, ctypes.c_float, _VP, _I64, _VP, _VP, _VP, _VP,
+                                           _I64, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _VP]
+        lib.pifa_rope_cache_q8.restype = ctypes.c_int
+        lib.pifa_cache_read_q8.argtypes = [_VP, _VP, _VP, _VP, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _I64, _I64,
+                                           _VP, _I64, ctypes.c_int, _VP, _I64, _VP, _I64, _VP]
+        lib.pifa_cache_read_q8.restype = ctypes.c_int
+        lib.pifa_paged_attention_q8.argtypes = [_VP, _I64, _I64, _I64, _I64, _I64, ctypes.c_int, _VP, _VP, _VP, _VP, _I64,
+                                                _I64, _I64, _I64, _I64, _I64, _I64, _I64, _VP, _I64, _I64, _VP, _VP, _I64,
+                                                _I64, ctypes.c_float, _VP, _I64, _VP, _I64, _VP]
+        lib.pifa_paged_attention_q8.restype = ctypes.c_int
         lib.pifa_paged_attention_workspace_size.argtypes = [_I64] * 6
         lib.pifa_paged_attention_workspace_size.restype = _I64
         lib.pifa_validate_indices.argtypes = [_VP, _VP, _I64, _I64]
@@ -1024,4 +1038,188 @@ def pifa_paged_attention(Q, k_cache, v_cache, table, q_start, kv_len, max_q: int
             table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), B, int(max_q),
             d ** -0.5 if scale is None else float(scale), O.data_ptr(), ldo, ws_ptr, ws_bytes, run_on)
     _check(st, "pifa_paged_attention")
+    return O
+
+
+# ---- the cache in 8 bits: e4m3 elements, a power-of-two scale (e8m0) for each block of 16 tokens and head ----------
+def _scale_strides(k_scale, v_scale, k_cache):
+    """(page, block, head) strides of two pages x page_size / 16 x kv_heads tensors of one set of strides."""
+    import torch
+    pages, size, heads, _ = k_cache.shape
+    if size % PIFA_Q8_BLOCK:
+        _refuse(f"k_cache: page_size must be a multiple of {PIFA_Q8_BLOCK} (it is {size})")
+    shape = (pages, size // PIFA_Q8_BLOCK, heads)
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.float8_e8m0fnu or t.shape != shape:
+            _refuse(f"{name} must be a torch.float8_e8m0fnu tensor of shape {shape}")
+        if t.device != k_cache.device:
+            _refuse(f"{name} is on {t.device}, not on {k_cache.device}")
+    if v_scale.stride() != k_scale.stride():
+        _refuse("k_scale and v_scale must have one set of strides")
+    return k_scale.stride()
+
+
+def pifa_rope_cache_q8(Q, K, V, positions, slots, freq, k_cache, v_cache, k_scale, v_scale, layout: int = PIFA_ROPE_HALF,
+                       scale: float = 1.0, Qr=None, stream=None):
+    """pifa_rope_cache into a cache in 8 bits (pifa_rope_cache_q8): k_cache and v_cache float8_e4m3fn (pages x page_size x
+    kv_heads x head_dim), k_scale and v_scale float8_e8m0fnu (pages x page_size / 16 x kv_heads), all updated in place."""
+    torch = sys.modules["torch"]
+    try:
+        dev, dt, qs, ks, cs, strides = Q.get_device(), Q.dtype, Q.shape, K.shape, k_cache.shape, k_cache.stride()
+        (T, h, d), (_, hk, _), (pages, size, _, _), (sp, st_, sh, se) = qs, ks, cs, strides
+        (ldq, qh, qe), (ldk, kh, ke), (ldv, vh, ve), (ldqr, rh, re) = Q.stride(), K.stride(), V.stride(), Qr.stride()
+        ss = cp, cb, ch = k_scale.stride()
+        if T == 1:
+            ldq, ldk, ldv, ldqr = h * d, hk * d, hk * d, h * d
+        fast = (dev >= 0 and se == qe == ke == ve == re == 1 and qh == kh == vh == rh == d
+                and ks == V.shape == (T, hk, d) and Qr.shape == qs and cs == v_cache.shape == (pages, size, hk, d)
+                and v_cache.stride() == strides and (dt is torch.bfloat16 or dt is torch.float16)
+                and dt is K.dtype is V.dtype is Qr.dtype and k_cache.dtype is v_cache.dtype is torch.float8_e4m3fn
+                and k_scale.dtype is v_scale.dtype is torch.float8_e8m0fnu and size % PIFA_Q8_BLOCK == 0
+                and k_scale.shape == v_scale.shape == (pages, size // PIFA_Q8_BLOCK, hk) and v_scale.stride() == ss
+                and positions.dtype is torch.int32 and slots.dtype is freq.dtype is torch.int64
+                and positions.shape == slots.shape == (T,) and freq.dim() == 1
+                and dev == K.get_device() == V.get_device() == Qr.get_device() == k_cache.get_device() == v_cache.get_device()
+                and dev == positions.get_device() == slots.get_device() == freq.get_device()
+                and dev == k_scale.get_device() == v_scale.get_device()
+                and positions.is_contiguous() and slots.is_contiguous() and freq.is_contiguous())
+    except (AttributeError, TypeError, ValueError):
+        fast = False
+    if not fast:
+        T, h, d, ldq = _rows_of_heads("Q", Q)
+        dev, dt = Q.device, Q.dtype
+        *ks, ldk = _rows_of_heads("K", K, dt, dev)
+        *vs, ldv = _rows_of_heads("V", V, dt, dev)
+        pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, torch.float8_e4m3fn, dev)
+        cp, cb, ch = _scale_strides(k_scale, v_scale, k_cache)
+        if ks != [T, hk, d] or vs != [T, hk, d]:
+            _refuse(f"K and V must be tensors of shape {(T, hk, d)}")
+        _vector("positions", positions, T, torch.int32, dev)
+        _vector("slots", slots, T, torch.int64, dev)
+        _vector("freq", freq, None, torch.int64, dev)
+        if Qr is None:
+            with _on(stream):
+                Qr = torch.empty((T, h, d), dtype=dt, device=dev)
+        *qs, ldqr = _rows_of_heads("Qr", Qr, dt, dev)
+        if qs != [T, h, d]:
+            _refuse(f"Qr must be a tensor of shape {(T, h, d)}")
+    st = _lib().pifa_rope_cache_q8(
+        Q.data_ptr(), ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, T, h, hk, d,
+        PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16, positions.data_ptr(), slots.data_ptr(),
+        freq.data_ptr(), 2 * freq.shape[0], int(layout), float(scale), Qr.data_ptr(), ldqr,
+        k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, size, sp, st_, sh, cp, cb, ch,
+        _stream_ptr(stream))
+    _check(st, "pifa_rope_cache_q8")
+    return Qr
+
+
+def pifa_cache_read_q8(k_cache, v_cache, k_scale, v_scale, slots, K=None, V=None, dtype=None, stream=None):
+    """Tokens of a cache in 8 bits at `slots` int64 (T), read back (pifa_cache_read_q8): returns (K, V), T x kv_heads x
+    head_dim. K and V give those tensors; else they are allocated as zeros (rows whose slot is -1 are not written) in
+    `dtype`, bfloat16 if not given, or that of the one that is."""
+    torch = sys.modules["torch"]
+    try:
+        dev, dt, shape, (T,), strides = k_cache.get_device(), K.dtype, K.shape, slots.shape, k_cache.stride()
+        (pages, size, hk, d), (sp, st_, sh, se), (cp, cb, ch) = k_cache.shape, strides, k_scale.stride()
+        (ldk, kh, ke), (ldv, vh, ve) = K.stride(), V.stride()
+        if T == 1:
+            ldk = ldv = hk * d
+        fast = (dev >= 0 and se == ke == ve == 1 and kh == vh == d and shape == V.shape == (T, hk, d)
+                and (dt is torch.bfloat16 or dt is torch.float16) and V.dtype is dt and (dtype is None or dtype is dt)
+                and v_cache.shape == (pages, size, hk, d) and v_cache.stride() == strides
+                and k_cache.dtype is v_cache.dtype is torch.float8_e4m3fn and size % PIFA_Q8_BLOCK == 0
+                and k_scale.dtype is v_scale.dtype is torch.float8_e8m0fnu and v_scale.stride() == (cp, cb, ch)
+                and k_scale.shape == v_scale.shape == (pages, size // PIFA_Q8_BLOCK, hk)
+                and slots.dtype is torch.int64 and slots.is_contiguous()
+                and dev == v_cache.get_device() == k_scale.get_device() == v_scale.get_device() == slots.get_device()
+                and dev == K.get_device() == V.get_device())
+    except (AttributeError, TypeError, ValueError):
+        fast = False
+    if not fast:
+        if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4 or k_cache.device.type != "cuda":
+            _refuse("k_cache must be a CUDA tensor of pages x page_size x kv_heads x head_dim")
+        dev, d = k_cache.device, k_cache.shape[3]
+        pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, torch.float8_e4m3fn, dev)
+        cp, cb, ch = _scale_strides(k_scale, v_scale, k_cache)
+        _vector("slots", slots, None, torch.int64, dev)
+        T = slots.shape[0]
+        given = [t.dtype for t in (K, V) if isinstance(t, torch.Tensor)]
+        dt = dtype or (given[0] if given else torch.bfloat16)
+        if dt is not torch.bfloat16 and dt is not torch.float16:
+            _refuse(f"dtype must be bfloat16 or float16, not {dt}")
+        with _on(stream):
+            K, V = (torch.zeros((T, hk, d), dtype=dt, device=dev) if t is None else t for t in (K, V))
+        *ks, ldk = _rows_of_heads("K", K, dt, dev)
+        *vs, ldv = _rows_of_heads("V", V, dt, dev)
+        if ks != [T, hk, d] or vs != [T, hk, d]:
+            _refuse(f"K and V must be tensors of shape {(T, hk, d)}")
+    st = _lib().pifa_cache_read_q8(
+        k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, size, hk, d, sp, st_, sh, cp, cb, ch,
+        slots.data_ptr(), T, PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16, K.data_ptr(), ldk, V.data_ptr(), ldv,
+        _stream_ptr(stream))
+    _check(st, "pifa_cache_read_q8")
+    return K, V
+
+
+def pifa_paged_attention_q8(Q, k_cache, v_cache, k_scale, v_scale, table, q_start, kv_len, max_q: int, scale=None, O=None,
+                            workspace_tensor=None, stream=None):
+    """pifa_paged_attention over a cache in 8 bits (pifa_paged_attention_q8): caches and scales as pifa_rope_cache_q8."""
+    torch = sys.modules["torch"]
+    run_on = _stream_ptr(stream)
+    try:
+        dev, dt, qs, cs, strides = Q.get_device(), Q.dtype, Q.shape, k_cache.shape, k_cache.stride()
+        (T, h, d), (pages, size, hk, _), (sp, st_, sh, se) = qs, cs, strides
+        (ldq, qh, qe), (ldo, oh, oe), (ldt, te), (B, cols) = Q.stride(), O.stride(), table.stride(), table.shape
+        ss = cp, cb, ch = k_scale.stride()
+        if T == 1:
+            ldq = ldo = h * d
+        if B == 1:
+            ldt = cols
+        fast = (dev >= 0 and se == qe == oe == te == 1 and qh == oh == d and ldt >= cols and O.shape == qs
+                and cs == v_cache.shape == (pages, size, hk, d) and v_cache.stride() == strides
+                and (dt is torch.bfloat16 or dt is torch.float16) and dt is O.dtype
+                and k_cache.dtype is v_cache.dtype is torch.float8_e4m3fn and size % PIFA_Q8_BLOCK == 0
+                and k_scale.dtype is v_scale.dtype is torch.float8_e8m0fnu and v_scale.stride() == ss
+                and k_scale.shape == v_scale.shape == (pages, size // PIFA_Q8_BLOCK, hk)
+                and table.dtype is q_start.dtype is kv_len.dtype is torch.int32
+                and q_start.shape == (B + 1,) and kv_len.shape == (B,)
+                and dev == O.get_device() == k_cache.get_device() == v_cache.get_device()
+                and dev == k_scale.get_device() == v_scale.get_device()
+                and dev == table.get_device() == q_start.get_device() == kv_len.get_device()
+                and q_start.is_contiguous() and kv_len.is_contiguous())
+    except (AttributeError, TypeError, ValueError):
+        fast = False
+    if not fast:
+        T, h, d, ldq = _rows_of_heads("Q", Q)
+        dt = Q.dtype
+        pages, size, hk, sp, st_, sh = _cache_strides(k_cache, v_cache, d, torch.float8_e4m3fn, Q.device)
+        cp, cb, ch = _scale_strides(k_scale, v_scale, k_cache)
+        _vector("kv_len", kv_len, None, torch.int32, Q.device)
+        B = kv_len.shape[0]
+        _vector("q_start", q_start, B + 1, torch.int32, Q.device)
+        ldt = _table_ld(table, B, Q.device)
+        cols = table.shape[1]
+        if O is None:
+            with _on(stream):
+                O = torch.zeros((T, h, d), dtype=dt, device=Q.device)
+        *os_, ldo = _rows_of_heads("O", O, dt, Q.device)
+        if os_ != [T, h, d]:
+            _refuse(f"O must be a tensor of shape {(T, h, d)}")
+        dev = Q.get_device()
+    need = _attention_workspace_size(T, h, hk, d, B, int(max_q))
+    if workspace_tensor is None:
+        ws_ptr, ws_bytes, _ = _attention_workspace(need, dev, run_on, stream)
+    else:
+        ws = workspace_tensor
+        if not isinstance(ws, torch.Tensor) or ws.get_device() != dev:
+            _refuse("workspace_tensor must be a tensor on Q's device")
+        ws_ptr = ws.data_ptr() + (-ws.data_ptr()) % 256
+        ws_bytes = ws.numel() * ws.element_size() - (ws_ptr - ws.data_ptr())
+    with _shared_scratch if workspace_tensor is None else _own_scratch:
+        st = _lib().pifa_paged_attention_q8(
+            Q.data_ptr(), ldq, T, h, hk, d, PIFA_DTYPE_FP16 if dt is torch.float16 else PIFA_DTYPE_BF16,
+            k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, size, sp, st_, sh, cp, cb, ch,
+            table.data_ptr(), cols, ldt, q_start.data_ptr(), kv_len.data_ptr(), B, int(max_q),
+            d ** -0.5 if scale is None else float(scale), O.data_ptr(), ldo, ws_ptr, ws_bytes, run_on)
+    _check(st, "pifa_paged_attention_q8")
     return O
