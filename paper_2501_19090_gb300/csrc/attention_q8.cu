@@ -6,18 +6,304 @@
 // A warp takes one row of one query head and walks its keys: the simplest form, right for every shape.
 #include <cmath>
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "pifa.h"
-#include "pifa_internal.h"
-#include "ptx.cuh"
+#include "attention_rows.cuh"
+#include "q8.cuh"
 
 namespace {
 
-using namespace pifa;
+// ---- few rows --------------------------------------------------------------------------------------
+struct RowsQ8 {
+  const uint8_t *k, *v, *ks, *vs;
+  int64_t scale_page, scale_block, scale_head;
+};
 
-constexpr int THREADS = 128;
+template <int D>
+constexpr int kStages = 768 / D;  // of 16 keys: 4 KB (D = 128) or 2 KB
+
+// Where a 16-byte piece of a key's row lies among its stage's K or V, so that the lanes that read together meet different bank
+// groups: of K two keys' four neighbouring pieces at a time; of V, of every other key, two pieces (D = 64: halves of two).
+template <int D>
+__device__ __forceinline__ int k_place(int key, int piece) {
+  return D == 128 ? key * 128 + ((piece ^ (key & 1) << 2) << 4) : key * 64 + (piece << 4);
+}
+template <int D>
+__device__ __forceinline__ int v_place(int key, int piece) {
+  return D == 128 ? key * 128 + ((piece ^ (key & 6)) << 4) : (key >> 1) * 128 + ((((key & 1) * 4 + piece) ^ (key & 6)) << 4);
+}
+__device__ __forceinline__ uint32_t halves_of(uint32_t e4m3x2) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)e4m3x2));
+  return h;
+}
+
+template <bool F16, int D>
+__global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g, const RowsQ8 c8) {
+  constexpr int KC = D / 64, VC = D / 8;               // of a lane: 16-byte pieces of a key of K; columns of a key of V
+  constexpr int PIECES = D / 16, KEYS = 32 / PIECES;   // of a key's row; keys that a warp copies at once
+  constexpr int STAGE_BYTES = 2 * STEP * D;            // K and V of a step
+  constexpr int STAGES = kStages<D>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  int* first = reinterpret_cast<int*>(smem + WARPS * STAGES * STAGE_BYTES);  // B + 1
+  __shared__ int part[32];
+  pdl_launch_dependents();
+  pdl_wait_primary();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Run dealt = deal_steps(g, first, part);
+  const int total = dealt.total, run = dealt.run;
+
+  // ---- this warp's run of steps: segments of one request and head each ----
+  const int worker = warp * (int)gridDim.x + (int)blockIdx.x;  // neighbours on different SMs
+  const int64_t at64 = (int64_t)worker * run;
+  int at = (int)min(at64, (int64_t)total);
+  const int stop = (int)min(at64 + run, (int64_t)total);
+  const int gr = lane >> 2, c4 = lane & 3;
+  const uint8_t* ring = smem + warp * STAGES * STAGE_BYTES;
+  const uint32_t ring_at = smem_u32(ring);
+  const int piece = lane % PIECES, key0 = lane / PIECES;
+  while (at < stop) {
+    const int b = find(first, g.B, at);
+    const Lengths x = lengths_of(g, b);
+    const int steps = steps_of(x), head = (at - first[b]) / steps, s0 = at - first[b] - head * steps;
+    const int s1 = min(steps, s0 + stop - at);
+    const int rows = x.n * g.group;
+    const int32_t* pages = g.table + b * g.ldt;
+    const int n_pages = (x.L + g.page_size - 1) >> g.page_shift;
+    // Lane i holds the page, and the two scales, of step i of 32: of those that are being loaded and the next, of those that
+    // are being computed and the next. A page comes two loads' time, its scales some steps, before what needs it.
+    auto page_of = [&](int s) {
+      const int p = (s * STEP) >> g.page_shift;
+      return s < s1 && p < n_pages ? pages[p] : 0;
+    };
+    auto scales_of = [&](int s, int id) {
+      if (s >= s1 || id < 0 || id >= g.pages || x.L <= 0) return 127 | 127 << 8;  // ones, for the zeros that are read there
+      const int64_t from = id * c8.scale_page + ((s * STEP & (g.page_size - 1)) / PIFA_Q8_BLOCK) * c8.scale_block + head * c8.scale_head;
+      return (int)c8.ks[from] | (int)c8.vs[from] << 8;
+    };
+    int known = s0, ids = page_of(s0 + lane), ids_next = page_of(s0 + 32 + lane);
+    int scales = scales_of(s0 + lane, ids), scales_next = 0, scaled = s0;
+    // the rows of Q: this lane's are gr and gr + 8; as fp16, times a power of two that brings bf16's into its range
+    uint32_t q[2][KC][8];
+    int seen[2];
+    float c[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int row = gr + 8 * r, token = row / g.group;
+      seen[r] = row < rows ? max(x.ahead + token, 0) : 0;
+      c[r] = g.c;
+#pragma unroll
+      for (int i = 0; i < KC; ++i) {
+        uint4 w[2] = {};
+        if (row < rows) {
+          const uint4* from = reinterpret_cast<const uint4*>(g.q + (int64_t)(x.q0 + token) * g.ldq +
+                                                             (int64_t)(head * g.group + row - token * g.group) * D + (c4 + 4 * i) * 16);
+          w[0] = from[0];
+          w[1] = from[1];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) q[r][i][k] = (&w[k / 4].x)[k % 4] ^ g.flip;
+      }
+      if constexpr (!F16) {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KC; ++i)
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            most = max3(most, fabsf(__uint_as_float(q[r][i][k] << 16)), fabsf(__uint_as_float(q[r][i][k] & 0xffff0000u)));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int e = row_exponent(most);
+        const float up = exponent_of_2(e);
+        c[r] *= exponent_of_2(-e);
+#pragma unroll
+        for (int i = 0; i < KC; ++i)
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            q[r][i][k] = pack<true>(__uint_as_float(q[r][i][k] << 16) * up, __uint_as_float(q[r][i][k] & 0xffff0000u) * up);
+      }
+    }
+    auto load = [&](int s, int stage) {  // K, then V, as two groups; nothing past s1
+      if (s < s1) {
+        if (s == known + 32) {
+          known = s;
+          ids = ids_next;
+          ids_next = page_of(s + 32 + lane);
+          scales_next = scales_of(s + lane, ids);
+        }
+        const int id = __shfl_sync(0xffffffffu, ids, s - known);
+        const bool bad = id < 0 || id >= g.pages;
+        if (bad && x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+        // this lane's piece of every KEYS-th key: a warp's copy is whole rows
+        const int64_t from = (bad ? 0 : (int64_t)id) * g.page_stride + head * g.head_stride +
+                             (((s * STEP) & (g.page_size - 1)) + key0) * g.token_stride + piece * 16;
+        const int left = bad ? 0 : x.L - s * STEP - key0;  // keys from this lane's first on
+        const uint32_t dst = ring_at + stage * STAGE_BYTES;
+        const int64_t back = left > 0 ? 0 : key0 * g.token_stride;
+#pragma unroll
+        for (int i = 0; i < STEP / KEYS; ++i) {
+          const bool in = i * KEYS < left;
+          cp_async16(dst + k_place<D>(key0 + i * KEYS, piece), c8.k + from + (in ? i * KEYS * g.token_stride : 0) - back, in ? 16 : 0);
+        }
+        cp_commit();
+#pragma unroll
+        for (int i = 0; i < STEP / KEYS; ++i) {
+          const bool in = i * KEYS < left;
+          cp_async16(dst + STEP * D + v_place<D>(key0 + i * KEYS, piece), c8.v + from + (in ? i * KEYS * g.token_stride : 0) - back,
+                     in ? 16 : 0);
+        }
+      } else {
+        cp_commit();
+      }
+      cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) load(s0 + i, i);
+    float o[VC][4] = {};
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
+    float base = NO_BASE;  // exponent that the values' scales are held against
+    int stage = 0;
+    for (int s = s0; s < s1; ++s) {
+      __syncwarp();  // all lanes have read the stage that is filled next
+      load(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+      if (s == scaled + 32) {
+        scaled = s;
+        scales = scales_next;
+      }
+      const int two = __shfl_sync(0xffffffffu, scales, s - scaled);
+      const float key_scale = scale_of(two & 0xff);
+      const ValueScale vs = value_scale(two >> 8, base);
+      if (vs.up > 0.0f) {  // the sums so far, in units of the larger exponent
+        const float f = exponent_of_2(-(int)fminf(vs.up, 126.0f));
+#pragma unroll
+        for (int i = 0; i < VC; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[i][k] *= f;
+      }
+      const uint8_t* buf = ring + stage * STAGE_BYTES;
+      cp_wait<2 * STAGES - 1>();
+      __syncwarp();
+      float sc[2][4] = {};
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+          const uint4 k = *reinterpret_cast<const uint4*>(buf + k_place<D>(gr + 8 * nb, c4 + 4 * i));
+          const uint32_t w[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            mma_m16n8k16_f16(sc[nb], q[0][i][2 * j], q[1][i][2 * j], q[0][i][2 * j + 1], q[1][i][2 * j + 1], halves_of(w[j] & 0xffffu),
+                             halves_of(w[j] >> 16));
+        }
+      // keys that a row does not see; exponents of the weights times their value's scale, relative to m
+      float v[2][4];
+      bool grows = false;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float cr = c[r] * key_scale;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int key = s * STEP + 8 * (k >> 1) + c4 * 2 + (k & 1);
+          v[r][k] = key < seen[r] ? fmaf(sc[k >> 1][2 * r + (k & 1)], cr, vs.exponent) : -INFINITY;
+          grows |= v[r][k] > m[r] + 8.0f;
+        }
+      }
+      if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float top = fmaxf(fmaxf(v[r][0], v[r][1]), fmaxf(v[r][2], v[r][3]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          top = fmaxf(top, m[r]);
+          const float f = top > m[r] ? fast_exp2(m[r] - top) : 1.0f;  // 0 where nothing was seen before
+          m[r] = top;
+          l[r] *= f;
+#pragma unroll
+          for (int i = 0; i < VC; ++i) {
+            o[i][2 * r] *= f;
+            o[i][2 * r + 1] *= f;
+          }
+        }
+      }
+      uint32_t p[2][2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float from = m[r] > -INFINITY ? m[r] : 0.0f;
+        float e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] = fast_exp2(v[r][k] - from);
+        l[r] += ((e[0] + e[1]) + (e[2] + e[3])) * vs.inverse;
+        p[r][0] = pack<true>(e[0], e[1]);
+        p[r][1] = pack<true>(e[2], e[3]);
+      }
+      cp_wait<2 * STAGES - 2>();
+      __syncwarp();
+      // this lane's columns VC gr to VC gr + VC - 1 of four keys
+      uint32_t w[4][VC / 4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int key = c4 * 2 + (k & 1) + 8 * (k >> 1);
+        if constexpr (D == 128) {
+          const uint4 u = *reinterpret_cast<const uint4*>(buf + STEP * D + v_place<D>(key, gr));
+          w[k][0] = u.x, w[k][1] = u.y, w[k][2] = u.z, w[k][3] = u.w;
+        } else {
+          const uint2 u = *reinterpret_cast<const uint2*>(buf + STEP * D + v_place<D>(key, gr >> 1) + 8 * (gr & 1));
+          w[k][0] = u.x, w[k][1] = u.y;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < VC / 4; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // columns 4 i + 2 h and the next
+          const uint32_t lo = __byte_perm(w[0][i], w[1][i], h ? 0x7362 : 0x5140), hi = __byte_perm(w[2][i], w[3][i], h ? 0x7362 : 0x5140);
+          mma_m16n8k16_f16(o[4 * i + 2 * h], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo & 0xffffu), halves_of(hi & 0xffffu));
+          mma_m16n8k16_f16(o[4 * i + 2 * h + 1], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo >> 16), halves_of(hi >> 16));
+        }
+      stage = stage == STAGES - 1 ? 0 : stage + 1;
+    }
+    cp_wait<0>();
+    // o[i][2 r + e]: row gr + 8 r, column VC (2 c4 + e) + i, in units of 2^base
+    const float unit = base > NO_BASE ? exponent_of_2((int)base) : 1.0f;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      const int row = gr + 8 * r, token = row / g.group;
+      if (row >= rows) continue;
+      if (s0 == 0 && s1 == steps) {
+        const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+        uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + 2 * VC * c4;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int i = 0; i < VC / 8; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              w[k] = pack<F16>(o[8 * i + 2 * k][2 * r + e] * inv * unit, o[8 * i + 2 * k + 1][2 * r + e] * inv * unit);
+            *reinterpret_cast<uint4*>(out + VC * e + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+      } else {  // a head that began before this run: the first of the warp's two places, else the second
+        float* to = g.partial + (((int64_t)worker * 2 + (s0 > 0 ? 0 : 1)) * g.max_rows + row) * (D + 2);
+        float2* ml = reinterpret_cast<float2*>(to + D);
+        if (c4 == 0) *ml = make_float2(m[r], l[r]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int i = 0; i < VC / 2; ++i)
+            *reinterpret_cast<float2*>(to + VC * (2 * c4 + e) + 2 * i) =
+                make_float2(o[2 * i][2 * r + e] * unit, o[2 * i + 1][2 * r + e] * unit);
+      }
+    }
+    at += s1 - s0;
+  }
+}
+
+template <bool F16, int D>
+cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
+  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * kStages<D> * 2 * STEP * D, stream, c8);
+}
+
+// ---- more rows: a warp for each, key by key -----------------------------------------------------------
+constexpr int EACH_THREADS = 128;
 
 struct Q8Args {
   const uint16_t* q;
@@ -35,15 +321,11 @@ __device__ __forceinline__ float from_e4m3(uint32_t e) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)e));
   return __half22float2(*reinterpret_cast<const __half2*>(&h)).x;
 }
-__device__ __forceinline__ float scale_of(int byte) {
-  return byte == 0 ? __uint_as_float(0x00400000u) : byte == 255 ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)byte << 23);
-}
-
 template <bool F16, int D>
-__global__ void __launch_bounds__(THREADS) attention_q8(const Q8Args g) {
+__global__ void __launch_bounds__(EACH_THREADS) attention_q8(const Q8Args g) {
   const int tid = threadIdx.x, lane = tid & 31, t = (int)blockIdx.x;
   bool over = false, falls = false;
-  for (int b = tid; b < g.B; b += THREADS) {
+  for (int b = tid; b < g.B; b += EACH_THREADS) {
     const int64_t n = (int64_t)g.q_start[b + 1] - g.q_start[b];
     falls |= n < 0;
     over |= n > 0 && (n > g.max_q || g.q_start[b + 1] > g.T);
@@ -62,7 +344,7 @@ __global__ void __launch_bounds__(THREADS) attention_q8(const Q8Args g) {
   const int L = min(max(g.kv_len[b], 0), g.cols * g.page_size);
   const int seen = min(L, L - (g.q_start[b + 1] - q0) + 1 + token);
   constexpr int E = D / 32;
-  for (int h = (int)blockIdx.y * (THREADS / 32) + (tid >> 5); h < g.heads * g.group; h += (int)gridDim.y * (THREADS / 32)) {
+  for (int h = (int)blockIdx.y * (EACH_THREADS / 32) + (tid >> 5); h < g.heads * g.group; h += (int)gridDim.y * (EACH_THREADS / 32)) {
     const int head = h / g.group;
     float q[E], o[E] = {}, m = -INFINITY, l = 0.0f;
     for (int e = 0; e < E; ++e) {
@@ -96,7 +378,16 @@ __global__ void __launch_bounds__(THREADS) attention_q8(const Q8Args g) {
 
 }  // namespace
 
-int launch_attention_q8(const PifaAttention& a, int* status, cudaStream_t stream) {
+int launch_attention_q8(const PifaAttention& a, bool few_rows, int* status, cudaStream_t stream) {
+  if (few_rows) {
+    const RowArgs g = row_args(a, status);
+    const RowsQ8 c8 = {static_cast<const uint8_t*>(a.k), static_cast<const uint8_t*>(a.v), a.q8->k, a.q8->v, a.q8->shape.page_stride,
+                       a.q8->shape.block_stride, a.q8->shape.head_stride};
+    const bool half = a.dtype == PIFA_DTYPE_FP16;
+    const cudaError_t e = a.cache.dim == 64 ? (half ? launch_rows_q8<true, 64>(g, c8, stream) : launch_rows_q8<false, 64>(g, c8, stream))
+                                            : (half ? launch_rows_q8<true, 128>(g, c8, stream) : launch_rows_q8<false, 128>(g, c8, stream));
+    return e == cudaSuccess ? PIFA_OK : pifa_fail_cuda("attention_rows_q8 launch", e);
+  }
   Q8Args g = {};
   g.q = static_cast<const uint16_t*>(a.q);
   g.o = static_cast<uint16_t*>(a.o);
@@ -128,7 +419,7 @@ int launch_attention_q8(const PifaAttention& a, int* status, cudaStream_t stream
   g.status = status;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)a.T, (unsigned)((a.q_heads + 3) / 4 < 65535 ? (a.q_heads + 3) / 4 : 65535));
-  cfg.blockDim = dim3(THREADS);
+  cfg.blockDim = dim3(EACH_THREADS);
   cfg.stream = stream;
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
   cudaError_t e;

@@ -140,7 +140,7 @@ struct PifaAttention {
   const PifaScales* q8;  // null: elements of dtype
 };
 // Over a cache in 8 bits.
-int launch_attention_q8(const PifaAttention& a, int* status, cudaStream_t stream);
+int launch_attention_q8(const PifaAttention& a, bool few_rows, int* status, cudaStream_t stream);
 // Chunks of new tokens on the tensor cores.
 int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B);
 int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream);

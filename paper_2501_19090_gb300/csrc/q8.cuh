@@ -1,0 +1,59 @@
+// q8.cuh -- scales of a paged cache in 8 bits, as the attention kernels take them (attention_q8.cu, attention_tc.cu).
+//
+// Both products run on fp16: e4m3 numbers are fp16 numbers, and rows of Q are brought into its range by a power of two. Of
+// the scales the keys' multiply the scores. The values' become part of the weights' exponents: with x_j the score of key j
+// (times log2(e)) and t its value's scale,
+//   w_j = 2^(x_j + log2 t - base - m),  O = sum_j w_j v_j,  l = sum_j w_j 2^(base - log2 t),  o = 2^base O / l
+// so that a weight costs no operation more, and fp16's range is spent on what the weights contribute. `base`, whole, is near
+// the largest log2 t so far: a larger one than base + 40 raises it, and O is brought into
+// the new unit; smaller ones than base - 40 count as
+// that, in w and in l alike, which puts an error of less than 2^-39 of the largest value into o. In between neither w nor l leaves
+// fp32's range where it matters (a w below 2^-126 belongs to a weight of less than 2^-46 of the largest).
+#ifndef PIFA_Q8_CUH_
+#define PIFA_Q8_CUH_
+
+#include <stdint.h>
+
+namespace pifa {
+
+constexpr float NO_BASE = -1000.0f;
+constexpr float FAR = 40.0f;
+
+// 2^e for e in [-126, 127].
+__device__ __forceinline__ float exponent_of_2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// The scale that a byte b stands for, 2^(b - 127); 255: NaN.
+__device__ __forceinline__ float scale_of(int byte) {
+  return byte == 0 ? __uint_as_float(0x00400000u) : byte == 255 ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)byte << 23);
+}
+
+struct ValueScale {
+  float exponent, inverse;  // log2 t - base, and 2^ the negative of it
+  float up;                 // by which base has risen
+};
+// A block's scale byte against `base`, which is set by the first block and rises when it has to. A scale of NaN gives weights of
+// NaN to the keys that are seen, and leaves l alone where none is.
+__device__ __forceinline__ ValueScale value_scale(int byte, float& base) {
+  ValueScale r = {__uint_as_float(0x7fffffffu), 0.0f, 0.0f};
+  if (byte == 255) return r;
+  const float e = (float)(byte - 127);
+  if (base == NO_BASE) base = fmaxf(e, -126.0f);
+  if (e > base + FAR) {
+    r.up = e - base;
+    base = e;
+  }
+  r.exponent = fmaxf(e - base, -FAR);
+  r.inverse = exponent_of_2(-(int)r.exponent);
+  return r;
+}
+
+// The power of two that brings a row of bf16 magnitudes up to `most` to [2^14, 2^15); what is that small that this would leave
+// fp32's range, zeros and what is not finite are taken as they come.
+__device__ __forceinline__ int row_exponent(float most) {
+  const int e = (int)(__float_as_uint(most) >> 23) - 127;
+  return most == 0.0f || e == 128 ? 0 : 14 - max(e, -100);
+}
+
+}  // namespace pifa
+
+#endif  // PIFA_Q8_CUH_

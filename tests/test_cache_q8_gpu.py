@@ -423,6 +423,31 @@ def test_attention_scales_far_apart(name):
     check_attention(a, attend(a), d ** -0.5)
 
 
+@pytest.mark.parametrize("order", ["up", "down", "mixed"])
+@pytest.mark.parametrize("new", [1, 5, 150])
+def test_attention_blocks_of_zeros_and_of_any_size(new, order):
+    """Values whose blocks are nothing but zeros (the smallest scale) or differ by 2^120 in size: each key / value head against its own
+    largest value, the weights' sum with all keys in it."""
+    L, hq, hk, d, page = 900, 8, 4, 128, 32
+    a = make_q8(17, [L], [new], hq, hk, d, page, torch.bfloat16)
+    pages, g = a["table"][0, :-(-L // page)].long(), gen(18)
+    blocks = len(pages) * page // 16
+    size = torch.tensor([1, 1, 60, 100, 121, 160, 180], device=DEV)[torch.randint(0, 7, (blocks, hk), device=DEV, generator=g)]
+    size[:, 0] = torch.where(torch.arange(blocks, device=DEV) % 3 > 0, 1, 121)       # a head whose values are mostly zeros
+    if order != "mixed":
+        size[:, 1:] = size[:, 1:].sort(0, descending=order == "down").values
+    vs, v8 = a["vs"].view(U8), a["v8"].view(U8)
+    vs[pages] = size.to(U8).view(len(pages), page // 16, hk)
+    v8[pages] = torch.where(size.view(len(pages), page // 16, 1, hk, 1) == 1, 0, v8[pages].view(len(pages), page // 16, 16, hk, d)).view(len(pages), page, hk, d).to(U8)
+    a["v_cache"] = values(a["v8"], a["vs"])
+    O = attend(a)
+    want, s, keys = plain_attention(a, d ** -0.5)
+    most = a["v_cache"][pages].flatten(0, 1)[:L].abs().amax((0, 2)).repeat_interleave(hq // hk)[None, :, None]
+    err = (O.double() - want).abs()
+    tol = U[O.dtype] * want.abs() + (1.1 * 2.0 ** -11 + 2e-4) * s + 2.0 ** -24 * (1.0 + keys) * most
+    assert bool((err <= tol).all()), (float((err - tol).max()), (err > tol).nonzero()[:4].tolist())
+
+
 @pytest.mark.parametrize("size", [1e-30, 3e-5, 2e4, 1e30])
 @pytest.mark.parametrize("name", ["decode_ragged_gqa", "prompt_1000_gqa"])
 def test_attention_queries_of_any_size(name, size):
