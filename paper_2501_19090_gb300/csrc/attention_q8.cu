@@ -11,7 +11,6 @@
 
 namespace {
 
-// ---- few rows --------------------------------------------------------------------------------------
 struct RowsQ8 {
   const uint8_t *k, *v, *ks, *vs;
   int64_t scale_page, scale_block, scale_head;
@@ -30,12 +29,6 @@ template <int D>
 __device__ __forceinline__ int v_place(int key, int piece) {
   return D == 128 ? key * 128 + ((piece ^ (key & 6)) << 4) : (key >> 1) * 128 + ((((key & 1) * 4 + piece) ^ (key & 6)) << 4);
 }
-__device__ __forceinline__ uint32_t halves_of(uint32_t e4m3x2) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)e4m3x2));
-  return h;
-}
-
 template <bool F16, int D>
 __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g, const RowsQ8 c8) {
   constexpr int KC = D / 64, VC = D / 8;               // of a lane: 16-byte pieces of a key of K; columns of a key of V
@@ -75,7 +68,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
       return s < s1 && p < n_pages ? pages[p] : 0;
     };
     auto scales_of = [&](int s, int id) {
-      if (s >= s1 || id < 0 || id >= g.pages || x.L <= 0) return 127 | 127 << 8;  // ones, for the zeros that are read there
+      if (s >= s1 || id < 0 || id >= g.pages || x.L <= 0) return NO_SCALE << 8 | 127;
       const int64_t from = id * c8.scale_page + ((s * STEP & (g.page_size - 1)) / PIFA_Q8_BLOCK) * c8.scale_block + head * c8.scale_head;
       return (int)c8.ks[from] | (int)c8.vs[from] << 8;
     };
@@ -170,9 +163,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
       }
       const int two = __shfl_sync(0xffffffffu, scales, s - scaled);
       const float key_scale = scale_of(two & 0xff);
+      const float up = raise_base(two >> 8 < 255 ? (two >> 8) - 127 : -1000, base);
       const ValueScale vs = value_scale(two >> 8, base);
-      if (vs.up > 0.0f) {  // the sums so far, in units of the larger exponent
-        const float f = exponent_of_2(-(int)fminf(vs.up, 126.0f));
+      if (up > 0.0f) {  // the sums so far, in units of the larger exponent
+        const float f = exponent_of_2(-(int)fminf(up, 126.0f));
 #pragma unroll
         for (int i = 0; i < VC; ++i)
 #pragma unroll
@@ -302,129 +296,14 @@ cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stre
   return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * kStages<D> * 2 * STEP * D, stream, c8);
 }
 
-// ---- more rows: a warp for each, key by key -----------------------------------------------------------
-constexpr int EACH_THREADS = 128;
-
-struct Q8Args {
-  const uint16_t* q;
-  uint16_t* o;
-  const uint8_t *k, *v, *ks, *vs;
-  const int32_t *table, *q_start, *kv_len;
-  int64_t ldq, ldo, ldt, page_stride, token_stride, head_stride, scale_page, scale_block, scale_head, pages;
-  int T, heads, group, page_size, cols, B, max_q;
-  float c;  // scale log2(e)
-  int* status;
-};
-
-__device__ __forceinline__ float from_e4m3(uint32_t e) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)e));
-  return __half22float2(*reinterpret_cast<const __half2*>(&h)).x;
-}
-template <bool F16, int D>
-__global__ void __launch_bounds__(EACH_THREADS) attention_q8(const Q8Args g) {
-  const int tid = threadIdx.x, lane = tid & 31, t = (int)blockIdx.x;
-  bool over = false, falls = false;
-  for (int b = tid; b < g.B; b += EACH_THREADS) {
-    const int64_t n = (int64_t)g.q_start[b + 1] - g.q_start[b];
-    falls |= n < 0;
-    over |= n > 0 && (n > g.max_q || g.q_start[b + 1] > g.T);
-    over |= g.kv_len[b] > g.cols * g.page_size;
-  }
-  if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
-  if (__syncthreads_or(falls)) {
-    if (tid == 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-    return;
-  }
-  int b = 0;  // the request of row t: the last that does not start after it
-  for (int i = 1; i < g.B; ++i)
-    if (g.q_start[i] <= t) b = i;
-  const int q0 = g.q_start[b], token = t - q0;
-  if (token < 0 || t >= g.q_start[b + 1] || token >= g.max_q) return;
-  const int L = min(max(g.kv_len[b], 0), g.cols * g.page_size);
-  const int seen = min(L, L - (g.q_start[b + 1] - q0) + 1 + token);
-  constexpr int E = D / 32;
-  for (int h = (int)blockIdx.y * (EACH_THREADS / 32) + (tid >> 5); h < g.heads * g.group; h += (int)gridDim.y * (EACH_THREADS / 32)) {
-    const int head = h / g.group;
-    float q[E], o[E] = {}, m = -INFINITY, l = 0.0f;
-    for (int e = 0; e < E; ++e) {
-      const uint16_t w = g.q[(int64_t)t * g.ldq + (int64_t)h * D + e * 32 + lane];
-      q[e] = F16 ? __half2float(__ushort_as_half(w)) : __uint_as_float((uint32_t)w << 16);
-    }
-    for (int j = 0; j < seen; ++j) {
-      const int id = g.table[b * g.ldt + j / g.page_size], at = j % g.page_size;
-      const bool bad = id < 0 || id >= g.pages;
-      if (bad) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-      const int64_t from = bad ? 0 : id * g.page_stride + at * g.token_stride + head * g.head_stride;
-      const int64_t sc = bad ? 0 : id * g.scale_page + at / PIFA_Q8_BLOCK * g.scale_block + head * g.scale_head;
-      float s = 0.0f;
-      if (!bad)
-        for (int e = 0; e < E; ++e) s += q[e] * from_e4m3(g.k[from + e * 32 + lane]);
-      for (int x = 16; x; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
-      s *= bad ? 0.0f : g.c * scale_of(g.ks[sc]);
-      const float up = fmaxf(m, s), f = m > -INFINITY ? exp2f(m - up) : 0.0f, p = exp2f(s - up);
-      m = up;
-      l = l * f + p;
-      const float pv = bad ? 0.0f : p * scale_of(g.vs[sc]);
-      for (int e = 0; e < E; ++e) o[e] = o[e] * f + (bad ? 0.0f : pv * from_e4m3(g.v[from + e * 32 + lane]));
-    }
-    for (int e = 0; e < E; ++e) {
-      const float x = l == 0.0f ? 0.0f : o[e] / l;
-      const uint16_t w = F16 ? __half_as_ushort(__float2half_rn(x)) : __bfloat16_as_ushort(__float2bfloat16_rn(x));
-      g.o[(int64_t)t * g.ldo + (int64_t)h * D + e * 32 + lane] = w;
-    }
-  }
-}
-
 }  // namespace
 
-int launch_attention_q8(const PifaAttention& a, bool few_rows, int* status, cudaStream_t stream) {
-  if (few_rows) {
-    const RowArgs g = row_args(a, status);
-    const RowsQ8 c8 = {static_cast<const uint8_t*>(a.k), static_cast<const uint8_t*>(a.v), a.q8->k, a.q8->v, a.q8->shape.page_stride,
-                       a.q8->shape.block_stride, a.q8->shape.head_stride};
-    const bool half = a.dtype == PIFA_DTYPE_FP16;
-    const cudaError_t e = a.cache.dim == 64 ? (half ? launch_rows_q8<true, 64>(g, c8, stream) : launch_rows_q8<false, 64>(g, c8, stream))
-                                            : (half ? launch_rows_q8<true, 128>(g, c8, stream) : launch_rows_q8<false, 128>(g, c8, stream));
-    return e == cudaSuccess ? PIFA_OK : pifa_fail_cuda("attention_rows_q8 launch", e);
-  }
-  Q8Args g = {};
-  g.q = static_cast<const uint16_t*>(a.q);
-  g.o = static_cast<uint16_t*>(a.o);
-  g.k = static_cast<const uint8_t*>(a.k);
-  g.v = static_cast<const uint8_t*>(a.v);
-  g.ks = a.q8->k;
-  g.vs = a.q8->v;
-  g.table = a.table;
-  g.q_start = a.q_start;
-  g.kv_len = a.kv_len;
-  g.ldq = a.ldq;
-  g.ldo = a.ldo;
-  g.ldt = a.ldt;
-  g.page_stride = a.cache.page_stride;
-  g.token_stride = a.cache.token_stride;
-  g.head_stride = a.cache.head_stride;
-  g.scale_page = a.q8->shape.page_stride;
-  g.scale_block = a.q8->shape.block_stride;
-  g.scale_head = a.q8->shape.head_stride;
-  g.pages = a.cache.pages;
-  g.T = (int)a.T;
-  g.heads = (int)a.cache.heads;
-  g.group = (int)(a.q_heads / a.cache.heads);
-  g.page_size = (int)a.cache.page_size;
-  g.cols = (int)a.cols;
-  g.B = (int)a.B;
-  g.max_q = (int)(a.max_q < a.T ? a.max_q : a.T);
-  g.c = a.scale_log2;
-  g.status = status;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.T, (unsigned)((a.q_heads + 3) / 4 < 65535 ? (a.q_heads + 3) / 4 : 65535));
-  cfg.blockDim = dim3(EACH_THREADS);
-  cfg.stream = stream;
+int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream) {
+  const RowArgs g = row_args(a, status);
+  const RowsQ8 c8 = {static_cast<const uint8_t*>(a.k), static_cast<const uint8_t*>(a.v), a.q8->k, a.q8->v, a.q8->shape.page_stride,
+                     a.q8->shape.block_stride, a.q8->shape.head_stride};
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
-  cudaError_t e;
-  if (a.cache.dim == 64) e = f16 ? pifa_launch_ex(&cfg, attention_q8<true, 64>, g) : pifa_launch_ex(&cfg, attention_q8<false, 64>, g);
-  else e = f16 ? pifa_launch_ex(&cfg, attention_q8<true, 128>, g) : pifa_launch_ex(&cfg, attention_q8<false, 128>, g);
-  if (e != cudaSuccess) return pifa_fail_cuda("attention_q8 launch", e);
-  return PIFA_OK;
+  const cudaError_t e = a.cache.dim == 64 ? (f16 ? launch_rows_q8<true, 64>(g, c8, stream) : launch_rows_q8<false, 64>(g, c8, stream))
+                                          : (f16 ? launch_rows_q8<true, 128>(g, c8, stream) : launch_rows_q8<false, 128>(g, c8, stream));
+  return e == cudaSuccess ? PIFA_OK : pifa_fail_cuda("attention_rows_q8 launch", e);
 }

@@ -49,6 +49,7 @@
 #include "pifa.h"
 #include "pifa_internal.h"
 #include "ptx.cuh"
+#include "q8.cuh"
 
 namespace {
 
@@ -57,19 +58,28 @@ using namespace pifa;
 constexpr int BM = 128;             // rows of a tile
 constexpr int ROWS = 2 * BM;        // rows of an item (with those that a group's size leaves unused)
 constexpr int BN = 128;             // keys of a tile
-constexpr int THREADS = 384;
+template <bool Q8>
+constexpr int kThreads = Q8 ? 512 : 384;
 constexpr int PLAN_THREADS = 256;
 constexpr int MAX_REST = 512;       // items that may be cut: fewer than a round's, and one more for each head
 constexpr int MAX_PARTS = 456;      // pieces (times heads) that may leave partial sums: three for each SM
 constexpr int EARLY = 2;            // of four times 32 keys: those whose weights are handed to the MMAs first
 constexpr uint32_t HALF = BN * 128;  // 128 rows of 64 columns: 16 KB
 
-template <int D>
+template <int D, bool Q8 = false>
 struct Cfg {
   static constexpr uint32_t TILE = D / 64 * HALF;
-  static constexpr int SLOTS = D == 128 ? 5 : 8;
-  static constexpr uint32_t SMEM = 1024 + (2 + SLOTS) * TILE + 1024;
+  static constexpr int SLOTS = Q8 ? (D == 128 ? 4 : 6) : (D == 128 ? 5 : 8);
+  static constexpr uint32_t RAW = BN * D;                      // a tile of K or V in 8 bits
+  static constexpr int RAWS = Q8 ? (D == 128 ? 2 : 4) : 0;     // of those; they go through SLOTS as fp16
+  static constexpr uint32_t SMEM = 1024 + (2 + SLOTS) * TILE + RAWS * RAW + (Q8 ? 1536 : 1024);
   static constexpr int64_t PART_FLOATS = ROWS * D + 2 * ROWS;  // O, then (m, l) of each row
+};
+constexpr int SCALED = 4;  // key tiles whose blocks' scales are in shared memory
+// Of a key tile: its eight blocks' scales as q8.cuh has them, and what the values' are held against.
+struct TileScales {
+  float4 block[BN / PIFA_Q8_BLOCK];  // the keys' scale; the values' exponent and its inverse
+  float base, up;
 };
 
 // A work item: 16 words. The plan lists those of head 0 with everything that a CTA has to know; a CTA takes one
@@ -107,6 +117,8 @@ struct TcArgs {
   int wide;                          // rows of O start on 32-byte sectors
   int* status;
   uint64_t timeout_ns;
+  const uint8_t *ks, *vs;            // scales of a cache in 8 bits
+  int64_t scale_page, scale_block, scale_head;
 };
 
 struct Lengths {
@@ -354,17 +366,19 @@ __device__ __forceinline__ void store_row(uint16_t* out, const float* x, bool wi
   }
 }
 
-template <bool F16, int D>
-__global__ void __launch_bounds__(THREADS, 1)
+template <bool F16, int D, bool Q8>
+__global__ void __launch_bounds__(kThreads<Q8>, 1)
     attention_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                  const __grid_constant__ CUtensorMap vmap, const TcArgs g) {
-  using C = Cfg<D>;
-  constexpr int SLOTS = C::SLOTS;
+  using C = Cfg<D, Q8>;
+  constexpr int SLOTS = C::SLOTS, LOADS = Q8 ? C::RAWS : SLOTS;  // of tiles: as the MMAs take them, and as TMA fills them
   constexpr uint32_t TILE = C::TILE;
+  constexpr bool AS_F16 = F16 || Q8;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = smem + 2 * TILE;
-  uint64_t* full = reinterpret_cast<uint64_t*>(ring + SLOTS * TILE);
+  uint8_t* raw = ring + SLOTS * TILE;  // Q8: what TMA fills
+  uint64_t* full = reinterpret_cast<uint64_t*>(raw + C::RAWS * C::RAW);
   uint64_t* empty = full + SLOTS;
   uint64_t* s_full = empty + SLOTS;   // S of a tile is in tensor memory
   uint64_t* p_full = s_full + 2;      // half of its P is, and its O may be added to: two for each tile
@@ -376,14 +390,24 @@ __global__ void __launch_bounds__(THREADS, 1)
   uint64_t* v_clean = item_free + 2;  // of a slot: rows of V past the last key are zero
   uint64_t* turn = v_clean + SLOTS;   // the tiles' MMAs alternate
   uint64_t* drain = turn + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 2);
-  Item* items = reinterpret_cast<Item*>(tmem_slot + 2);
+  uint64_t* raw_full = drain + 2;     // Q8: tiles in 8 bits, scales of a key tile, rows of Q as fp16
+  uint64_t* raw_empty = raw_full + C::RAWS;
+  uint64_t* scales_full = raw_empty + C::RAWS;
+  uint64_t* q_ready = scales_full + SCALED;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_ready + 2);
+  Item* items = reinterpret_cast<Item*>((reinterpret_cast<uintptr_t>(tmem_slot + 2) + 15) & ~uintptr_t(15));
+  TileScales* scales = reinterpret_cast<TileScales*>(items + 2);
+  static_assert(C::SMEM >= 1024 + (2 + SLOTS) * TILE + C::RAWS * C::RAW + 8 * (3 * SLOTS + 2 * C::RAWS + SCALED + 22) + 8 + 16 +
+                               2 * sizeof(Item) + (Q8 ? SCALED * sizeof(TileScales) : 0), "what lies behind the tiles");
+  // what TMA fills
+  const uint32_t loads_at = smem_u32(Q8 ? raw : ring);
+  uint64_t *load_full = Q8 ? raw_full : full, *load_empty = Q8 ? raw_empty : empty;
 
   pdl_launch_dependents();
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < SLOTS; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&full[s], Q8 ? 2 : 1);
       mbar_init(&empty[s], 2);
       mbar_init(&v_clean[s], 1);
     }
@@ -397,8 +421,14 @@ __global__ void __launch_bounds__(THREADS, 1)
       mbar_init(&q_full[t], 1);
       mbar_init(&q_free[t], 1);
       mbar_init(&item_full[t], 1);
-      mbar_init(&item_free[t], 11);
+      mbar_init(&item_free[t], Q8 ? 15 : 11);
+      mbar_init(&q_ready[t], 4);
     }
+    for (int s = 0; s < C::RAWS; ++s) {
+      mbar_init(&raw_full[s], 1);
+      mbar_init(&raw_empty[s], 2);
+    }
+    for (int s = 0; s < SCALED; ++s) mbar_init(&scales_full[s], 1);
     fence_mbar_init();
     prefetch_tmap(&qmap);
     prefetch_tmap(&kmap);
@@ -424,14 +454,15 @@ __global__ void __launch_bounds__(THREADS, 1)
     return ok;
   };
 
-  // Registers: a softmax thread holds a row of S. 2 x 128 x 208 + 128 x 88 = 384 x 168, as launched.
+  // Registers: a softmax thread holds a row of S. 2 x 128 x 208 + 128 x 88 = 384 x 168, as launched; with the warps that convert
+  // 2 x 128 x 208 + 2 x 128 x 48 = 512 x 128.
   if (warp >= 8) {
-  regs_lower<88>();
+  regs_lower<Q8 ? 48 : 88>();
   // K (kv = 0) or V of an item's key tiles, fill after fill of the ring: K and V take its slots in turn. A lane
   // copies 64 columns of a page's rows (or of 128 of them). One warp issuing both was the bound for pages of 16.
   auto stream = [&](int kv, int& tiles, int b, int L, int head, int j0, int j1, auto&& every) {
     const int per_tile = g.page_size >= BN ? 1 : BN / g.page_size, box_rows = min(g.page_size, BN);
-    const int mine = lane / (D / 64), half = lane % (D / 64);
+    const int mine = Q8 ? lane : lane / (D / 64), half = Q8 ? 0 : lane % (D / 64);
     const int n_pages = (L + g.page_size - 1) >> g.page_shift;
     const int32_t* row = g.table + b * g.ldt;
     auto page_of = [&](int j) {
@@ -447,26 +478,27 @@ __global__ void __launch_bounds__(THREADS, 1)
         latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
         id = (int)g.pages;  // outside the tensor map: zeros
       }
-      const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, has)) * (uint32_t)box_rows * 128u;
+      const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, has)) * (uint32_t)box_rows * (Q8 ? (uint32_t)D : 128u);
       const int token = (j * BN) & (g.page_size - 1);
       const int y = g.token_at == 0 ? token : g.head_at == 0 ? head : id;
       const int z = g.token_at == 1 ? token : g.head_at == 1 ? head : id;
       const int w = g.token_at == 2 ? token : g.head_at == 2 ? head : id;
-      const int fill = 2 * tiles + kv, s = fill % SLOTS;
-      if (!wait(&empty[s], ((uint32_t)(fill / SLOTS) & 1u) ^ 1u)) break;
-      if (lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
+      const int fill = 2 * tiles + kv, s = fill % LOADS;
+      if (!wait(&load_empty[s], ((uint32_t)(fill / LOADS) & 1u) ^ 1u)) break;
+      if (lane == 0) mbar_arrive_expect_tx(&load_full[s], bytes);
       __syncwarp();
       if (has)
-        tma_load_4d(smem_u32(ring) + (uint32_t)s * TILE + (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u,
-                    kv ? &vmap : &kmap, half * 64, y, z, w, &full[s]);
+        tma_load_4d(Q8 ? loads_at + (uint32_t)s * C::RAW + (uint32_t)(mine * box_rows) * (uint32_t)D
+                       : loads_at + (uint32_t)s * TILE + (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u,
+                    kv ? &vmap : &kmap, half * 64, y, z, w, &load_full[s]);
       ++tiles;
       id = next;
     }
   };
   // nothing may land in shared memory after the CTA has left
   auto landed = [&](int kv, int tiles) {
-    for (int i = max(2 * tiles - 2 * SLOTS, 0) + kv; i < 2 * tiles; i += 2)
-      if (i + SLOTS >= 2 * tiles && !mbar_wait(&full[i % SLOTS], (uint32_t)(i / SLOTS) & 1u, 100000000ull))
+    for (int i = max(2 * tiles - 2 * LOADS, 0) + kv; i < 2 * tiles; i += 2)
+      if (i + LOADS >= 2 * tiles && !mbar_wait(&load_full[i % LOADS], (uint32_t)(i / LOADS) & 1u, 100000000ull))
         latch_status(g.status, PIFA_ERR_TIMEOUT);
   };
   if (warp == 8) {
@@ -525,9 +557,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp < 11) {
     // ---------------- MMAs of a tile ----------------
     const int t = warp - 9;
-    const uint32_t kind = F16 ? idesc_f16_f32(BM, BN) : idesc_bf16_f32(BM, BN);
+    const uint32_t kind = AS_F16 ? idesc_f16_f32(BM, BN) : idesc_bf16_f32(BM, BN);
     const uint32_t qk_desc = kind | (g.negate ? 1u << 13 : 0u);
-    const uint32_t pv_desc = (F16 ? idesc_f16_f32(BM, D) : idesc_bf16_f32(BM, D)) | (1u << 16);
+    const uint32_t pv_desc = (AS_F16 ? idesc_f16_f32(BM, D) : idesc_bf16_f32(BM, D)) | (1u << 16);
     // descriptors: the low word holds the address, which alone changes
     const uint32_t q_desc = (uint32_t)sw128_desc(smem_u32(smem) + (uint32_t)t * TILE);
     const uint32_t k_desc = (uint32_t)sw128_desc(smem_u32(ring)), v_desc = (uint32_t)sw128_mn_desc(smem_u32(ring));
@@ -568,7 +600,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (j0 >= j1) continue;
       if (!wait(&full[s], ph)) break;
       if (j0 < e) {
-        if (!wait(&q_full[t], q_ph)) break;
+        if (!wait(Q8 && !F16 ? &q_ready[t] : &q_full[t], q_ph)) break;
         q_ph ^= 1u;
         tc_fence_after();
         score(s, j0 + 1 >= e, false);
@@ -586,7 +618,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           advance();
         }
         const int tail = L - j * BN;  // keys of this tile
-        if (tail < BN) {
+        if (!Q8 && tail < BN) {
           if (t == 0) {
             uint8_t* v = ring + vs * TILE;
             for (int i = max(tail, 0) * 8 + lane; i < BN * 8; i += 32)
@@ -637,6 +669,87 @@ __global__ void __launch_bounds__(THREADS, 1)
       mma_commit(&drain[t]);  // every MMA has completed before the tensor memory is freed
       if (!mbar_wait(&drain[t], 0, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
     }
+  } else if (Q8 && warp >= 12) {
+    // ---------------- tiles of K (warps 12, 13) and V (14, 15) from 8 bits to fp16, and the blocks' scales (12) ----------------
+    if constexpr (Q8) {
+      constexpr int PIECES = D / 16;                       // of a row: 16 bytes in, 32 out
+      const int kv = (warp - 12) >> 1, sub = (warp - 12) & 1, piece = lane % PIECES, row0 = sub * (BN / 2) + lane / PIECES;
+      int tiles = 0;
+      for (int n = 0; !dead; ++n) {
+        if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
+        const int end = items[n & 1].end, j0 = items[n & 1].j0, j1 = items[n & 1].j1, L = items[n & 1].L, head = items[n & 1].head;
+        const int b = items[n & 1].b;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&item_free[n & 1]);
+        if (end) break;
+        // Lanes 0 to 7 have the keys' scales of a tile, 8 to 15 the values'; pages two tiles ahead, scales one.
+        const int32_t* pages = g.table + b * g.ldt;
+        auto page_of = [&](int j) {
+          const int key = j * BN + (lane & 7) * PIFA_Q8_BLOCK;
+          return lane < 16 && j < j1 && key < L ? pages[key >> g.page_shift] : -1;
+        };
+        auto scale_at = [&](int j, int id) {
+          if (id < 0 || id >= g.pages) return NO_SCALE;
+          const int at = (j * BN + (lane & 7) * PIFA_Q8_BLOCK) & (g.page_size - 1);
+          return (int)(lane < 8 ? g.ks : g.vs)[id * g.scale_page + at / PIFA_Q8_BLOCK * g.scale_block + head * g.scale_head];
+        };
+        int next_page = 0, next_scale = 0;
+        float base = NO_BASE;
+        if (warp == 12) {
+          next_scale = scale_at(j0, page_of(j0));
+          next_page = page_of(j0 + 1);
+        }
+        for (int j = j0; j < j1; ++j, ++tiles) {
+          const int fill = 2 * tiles + kv, from = fill % LOADS, to = fill % SLOTS;
+          if (!wait(&empty[to], ((uint32_t)(fill / SLOTS) & 1u) ^ 1u)) break;
+          if (warp == 12) {
+            // The scales of this tile take the place of those of four tiles ago: both tiles' S of the last K in this slot, or of a
+            // later one, is done, and so is what their softmax did before.
+            const int scale = next_scale;
+            next_scale = scale_at(j + 1, next_page);
+            next_page = page_of(j + 2);
+            TileScales& out = scales[tiles % SCALED];
+            const bool counts = lane >= 8 && lane < 16 && scale != NO_SCALE && scale != 255;
+            const int most = __reduce_max_sync(0xffffffffu, counts ? scale - 127 : -1000);
+            const float up = raise_base(most, base);
+            const ValueScale v = value_scale(scale, base);
+            const float k = __shfl_sync(0xffffffffu, scale == NO_SCALE ? 1.0f : scale_of(scale), lane & 7);
+            if (lane >= 8 && lane < 16) out.block[lane - 8] = make_float4(k, v.exponent, v.inverse, 0.0f);
+            if (lane == 0) {
+              out.base = base;
+              out.up = up;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&scales_full[tiles % SCALED]);
+          }
+          if (!wait(&raw_full[from], (uint32_t)(fill / LOADS) & 1u)) break;
+          const uint8_t* src = raw + from * C::RAW;
+          uint8_t* dst = ring + to * TILE + (piece >> 2) * HALF;
+          const int tail = kv ? L - j * BN : BN;           // rows of V past the last key may hold anything: zeros
+#pragma unroll 4
+          for (int i = 0; i < BN / 2; i += 32 / PIECES) {
+            const int r = row0 + i;
+            const uint4 x = *reinterpret_cast<const uint4*>(src + r * D + piece * 16);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            uint32_t h[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[k] = r < tail ? halves_of(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu) : 0u;
+            // the lanes of a row's second half the other way round: the eight of a quarter warp then meet eight bank groups
+            const int first = D == 128 ? piece >> 2 : 0;
+            const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+            const int at = (piece & 3) * 2;
+            *reinterpret_cast<uint4*>(dst + r * 128 + (((at + first) ^ (r & 7)) << 4)) = first ? hi : lo;
+            *reinterpret_cast<uint4*>(dst + r * 128 + (((at + 1 - first) ^ (r & 7)) << 4)) = first ? lo : hi;
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&full[to]);
+            mbar_arrive(&raw_empty[from]);
+          }
+        }
+      }
+    }
   } else {
     // ---------------- rows of Q, and V ----------------
     int loads[2] = {0, 0}, tiles = 0;
@@ -674,8 +787,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int t = warp >> 2, quarter = warp & 3;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_at = tmem + lanes + t * BN, o_at = tmem + lanes + 2 * BN + t * D;
-    const float c = g.c;
-    uint32_t s_ph = 0, o_ph = 0;
+    float c = g.c;
+    uint32_t s_ph = 0, o_ph = 0, q_ph = 0;
+    int tiles = 0;  // Q8: key tiles of the items before
     const int my_tok = (quarter * 32 + lane) / g.group, h = quarter * 32 + lane - my_tok * g.group;
     for (int n = 0; !dead; ++n) {
       if (!wait(&item_full[n & 1], ((uint32_t)n >> 1) & 1u)) break;
@@ -688,10 +802,50 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool real = my_tok < g.tpt && token < it.n;
       const int seen = real ? max(it.ahead + token, 0) : 0;
       const bool idle = !__any_sync(0xffffffffu, real);
-      float m = -INFINITY, l = 0.0f;
+      float m = -INFINITY, l = 0.0f, base = NO_BASE;
+      if constexpr (Q8 && !F16) {
+        if (it.j0 < end) {
+          // this row of Q from bf16 to fp16, times a power of two that brings it into its range, which c takes back
+          if (!wait(&q_full[t], q_ph)) break;
+          q_ph ^= 1u;
+          if (real) {
+            const int r = quarter * 32 + lane;
+            uint8_t* row = smem + t * TILE + r * 128;
+            uint4 x[D / 8];
+            float most = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+              x[i] = *reinterpret_cast<const uint4*>(row + (i / 8) * HALF + (((i & 7) ^ (r & 7)) << 4));
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t w = (&x[i].x)[k];
+                most = max3(most, fabsf(__uint_as_float(w << 16)), fabsf(__uint_as_float(w & 0xffff0000u)));
+              }
+            }
+            const int e = row_exponent(most);
+            const float up = exponent_of_2(e);
+            c = g.c * exponent_of_2(-e);
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t w = (&x[i].x)[k];
+                (&x[i].x)[k] = pack<true>(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
+              }
+              *reinterpret_cast<uint4*>(row + (i / 8) * HALF + (((i & 7) ^ (r & 7)) << 4)) = x[i];
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&q_ready[t]);
+        }
+      }
       for (int j = it.j0; j < end; ++j) {
         if (!wait(&s_full[t], s_ph)) break;
         s_ph ^= 1u;
+        const int tile = tiles + j - it.j0;
+        if (Q8 && !wait(&scales_full[tile % SCALED], (uint32_t)(tile / SCALED) & 1u)) break;
+        const TileScales& scale = scales[Q8 ? tile % SCALED : 0];
         if (!idle) {
           tc_fence_after();
           uint32_t v[4][32];
@@ -700,7 +854,33 @@ __global__ void __launch_bounds__(THREADS, 1)
           uint64_t sum[2];
           uint32_t w[4][16];
           const uint64_t c2 = f32x2(c, c);
+          const int lim = seen - j * BN;  // keys of this tile that the row sees
+          // Q8: of a block's scales, what the row's scores are multiplied by, and exponent and inverse of its values'; those of a
+          // block that the row does not see may be anything
+          auto block = [&](int i) {
+            const float4 x = scale.block[i];
+            const bool sees = PIFA_Q8_BLOCK * i < lim;
+            return make_float3(sees ? max_nan(c * x.x, 1e-37f) : 1.0f, sees ? x.y : 0.0f, sees ? x.z : 0.0f);  // (-inf times 0 is NaN)
+          };
+          auto weights_q8 = [&](int i) {  // of two blocks
+            const float from = m > -INFINITY ? m : 0.0f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float3 b = block(2 * i + h);
+              const uint64_t by = f32x2(b.x, b.x), off = f32x2(b.y - from, b.y - from);
+              uint64_t part = 0;
+#pragma unroll
+              for (int k = 8 * h; k < 8 * h + 8; ++k) {
+                const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), by, off));
+                const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+                part = add_f32x2(part, f32x2(p0, p1));
+                w[i][k] = pack<true>(p0, p1);
+              }
+              sum[h] = fma_f32x2(part, f32x2(b.z, b.z), sum[h]);
+            }
+          };
           auto weights = [&](int i) {  // keys 32 i to 32 i + 31
+            if constexpr (Q8) return weights_q8(i);
             const float mc = m > -INFINITY ? -m * c : 0.0f;
             const uint64_t mc2 = f32x2(mc, mc);
 #pragma unroll
@@ -718,12 +898,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (lane == 0) mbar_arrive(&p_full[2 * t + i]);
           };
           bool fresh = j == it.j0;  // no maximum yet
+          const float up = Q8 ? scale.up : 0.0f;
+          if (Q8) base = scale.base;
+          bool raised = up > 0.0f;
 #pragma unroll 1
           while (true) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
             tmem_ld_wait();
-            const int lim = seen - j * BN;  // keys of this tile that the row sees
             if (__any_sync(0xffffffffu, lim < BN)) {
 #pragma unroll
               for (int i = 0; i < 4; ++i)
@@ -732,23 +914,39 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             float mx[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; !Q8 && i < 4; ++i) {
               mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
 #pragma unroll
               for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
             }
-            const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
-            if (!fresh) {
+            float top;  // Q8: times c, and with the values' exponents
+            if constexpr (Q8) {
+              top = -INFINITY;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float most = fmaxf(__uint_as_float(v[i / 2][16 * (i & 1)]), __uint_as_float(v[i / 2][16 * (i & 1) + 1]));
+#pragma unroll
+                for (int k = 2; k < 16; k += 2)
+                  most = max3(most, __uint_as_float(v[i / 2][16 * (i & 1) + k]), __uint_as_float(v[i / 2][16 * (i & 1) + k + 1]));
+                const float3 b = block(i);
+                top = fmaxf(top, fmaf(most, b.x, b.y));
+              }
+            } else {
+              top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
+            }
+            if (!fresh && !raised) {
               sum[0] = sum[1] = 0;
 #pragma unroll
               for (int i = 0; i < EARLY; ++i) weights(i);
-              if (!__any_sync(0xffffffffu, (top - m) * c > 8.0f)) break;
+              if (!__any_sync(0xffffffffu, (Q8 ? top - m : (top - m) * c) > 8.0f)) break;
             }
             fresh = false;
-            const float up = fmaxf(m, top);
-            const float f = m > -INFINITY ? fast_exp2((m - up) * c) : 1.0f;  // (nothing was seen before: zeros)
-            m = up;
+            const float most = fmaxf(m, top);
+            float f = m > -INFINITY ? fast_exp2(Q8 ? m - most : (m - most) * c) : 1.0f;  // (nothing was seen before: zeros)
+            m = most;
             l *= f;
+            if (raised) f *= exponent_of_2(-(int)fminf(up, 126.0f));  // O, but not l, is in units of 2^base
+            raised = false;
             if (j > it.j0) {  // S(j) is in: so is PV(j - 1), issued before it, and O may be touched
 #pragma unroll 1
               for (int i = 0; i < D / 16; ++i) {
@@ -777,8 +975,10 @@ __global__ void __launch_bounds__(THREADS, 1)
           mbar_arrive(&p_full[2 * t + 1]);
         }
       }
+      tiles += it.j1 - it.j0;
       if (dead) break;
       const bool any = it.j0 < end;
+      const float unit = Q8 && base > NO_BASE ? exponent_of_2((int)base) : 1.0f;
       if (any) {
         if (!wait(&o_full[t], o_ph)) break;
         o_ph ^= 1u;
@@ -799,6 +999,10 @@ __global__ void __launch_bounds__(THREADS, 1)
           float x[32];
 #pragma unroll
           for (int k = 0; k < 32; ++k) x[k] = any && seen > 0 ? __uint_as_float(o[k]) * inv : 0.0f;
+          if (Q8) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) x[k] *= unit;
+          }
           if (real) store(i, x);
         }
       } else {
@@ -813,12 +1017,16 @@ __global__ void __launch_bounds__(THREADS, 1)
               tmem_ld_32x32b_x32(o_at + i * 32, o);
               tmem_ld_wait();
             }
+            if (Q8) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * unit);
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k)
               __stcg(reinterpret_cast<uint4*>(mine) + (w8 * (D / 4) + i * 8 + k) * 32 + lane,
                      make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
           }
-          __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, make_float2(m * c, l));
+          __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, make_float2(Q8 ? m : m * c, l));
           __threadfence();
           __syncwarp();
         }
@@ -910,11 +1118,17 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
 }
 
-template <bool F16, int D>
+template <bool F16, int D, bool Q8>
 cudaError_t launch_tc(cudaLaunchConfig_t& cfg, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap, const TcArgs& g) {
-  cfg.dynamicSmemBytes = Cfg<D>::SMEM;
-  const cudaError_t e = pifa_allow_smem<attention_tc<F16, D>>((int)Cfg<D>::SMEM);
-  return e != cudaSuccess ? e : pifa_launch_ex(&cfg, attention_tc<F16, D>, qmap, kmap, vmap, g);
+  cfg.blockDim = dim3(kThreads<Q8>);
+  cfg.dynamicSmemBytes = Cfg<D, Q8>::SMEM;
+  const cudaError_t e = pifa_allow_smem<attention_tc<F16, D, Q8>>((int)Cfg<D, Q8>::SMEM);
+  return e != cudaSuccess ? e : pifa_launch_ex(&cfg, attention_tc<F16, D, Q8>, qmap, kmap, vmap, g);
+}
+template <int D, bool Q8>
+cudaError_t launch_tc(bool f16, cudaLaunchConfig_t& cfg, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap,
+                      const TcArgs& g) {
+  return f16 ? launch_tc<true, D, Q8>(cfg, qmap, kmap, vmap, g) : launch_tc<false, D, Q8>(cfg, qmap, kmap, vmap, g);
 }
 
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
@@ -966,8 +1180,16 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   const uint32_t rows = (uint32_t)(a.cache.page_size < BN ? a.cache.page_size : BN);
   if ((st = make_tmap_heads(&qmap, a.dtype, a.q, a.T, a.q_heads, a.cache.dim, a.ldq, (uint32_t)group, (uint32_t)g.tpt)) != PIFA_OK)
     return st;
-  if ((st = make_tmap_cache(&kmap, a.dtype, a.k, a.cache, rows, order)) != PIFA_OK) return st;
-  if ((st = make_tmap_cache(&vmap, a.dtype, a.v, a.cache, rows, order)) != PIFA_OK) return st;
+  const bool q8 = a.q8 != nullptr;
+  if ((st = make_tmap_cache(&kmap, a.dtype, q8, a.k, a.cache, rows, order)) != PIFA_OK) return st;
+  if ((st = make_tmap_cache(&vmap, a.dtype, q8, a.v, a.cache, rows, order)) != PIFA_OK) return st;
+  if (q8) {
+    g.ks = a.q8->k;
+    g.vs = a.q8->v;
+    g.scale_page = a.q8->shape.page_stride;
+    g.scale_block = a.q8->shape.block_stride;
+    g.scale_head = a.q8->shape.head_stride;
+  }
   g.token_at = order[0];
   g.head_at = order[1];
   const int grid = pifa_sm_count();
@@ -986,10 +1208,9 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   e = pifa_launch_ex(&cfg, attention_plan, g, grid);
   if (e != cudaSuccess) return pifa_fail_cuda("attention_plan launch", e);
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(THREADS);
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
-  if (a.cache.dim == 64) e = f16 ? launch_tc<true, 64>(cfg, qmap, kmap, vmap, g) : launch_tc<false, 64>(cfg, qmap, kmap, vmap, g);
-  else e = f16 ? launch_tc<true, 128>(cfg, qmap, kmap, vmap, g) : launch_tc<false, 128>(cfg, qmap, kmap, vmap, g);
+  if (a.cache.dim == 64) e = q8 ? launch_tc<64, true>(f16, cfg, qmap, kmap, vmap, g) : launch_tc<64, false>(f16, cfg, qmap, kmap, vmap, g);
+  else e = q8 ? launch_tc<128, true>(f16, cfg, qmap, kmap, vmap, g) : launch_tc<128, false>(f16, cfg, qmap, kmap, vmap, g);
   if (e != cudaSuccess) return pifa_fail_cuda("attention_tc launch", e);
   return PIFA_OK;
 }

@@ -139,8 +139,8 @@ struct PifaAttention {
   void* ws;           // after the reserve
   const PifaScales* q8;  // null: elements of dtype
 };
-// Over a cache in 8 bits.
-int launch_attention_q8(const PifaAttention& a, bool few_rows, int* status, cudaStream_t stream);
+// Few rows over a cache in 8 bits.
+int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream);
 // Chunks of new tokens on the tensor cores.
 int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B);
 int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream);
@@ -261,7 +261,8 @@ int make_tmap_heads(CUtensorMap* map, int dtype, const void* base, int64_t T, in
                     uint32_t box_heads, uint32_t box_rows);
 // 4-D tensor map over one buffer of a paged cache, innermost the head's elements, then tokens, heads and pages by
 // rising stride; box of 64 elements x `rows` tokens, 128-byte swizzle, zero fill outside. order[0..2]: which of
-// the map's coordinates 1 to 3 the token, the head and the page are.
-int make_tmap_cache(CUtensorMap* map, int dtype, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]);
+// the map's coordinates 1 to 3 the token, the head and the page are. q8: elements of one byte, box of a head's elements x `rows`
+// tokens, no swizzle.
+int make_tmap_cache(CUtensorMap* map, int dtype, bool q8, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]);
 
 #endif  // PIFA_INTERNAL_H_

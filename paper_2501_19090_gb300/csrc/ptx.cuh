@@ -263,6 +263,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// The larger of two; NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // Two fp32 operations at once, each rounded to nearest: a b + c, a + b.
 __device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
   uint64_t r;

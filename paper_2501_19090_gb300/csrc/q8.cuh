@@ -27,24 +27,37 @@ __device__ __forceinline__ float scale_of(int byte) {
   return byte == 0 ? __uint_as_float(0x00400000u) : byte == 255 ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)byte << 23);
 }
 
+// What stands for the scale of a block that is not read (zeros do as its keys and values).
+constexpr int NO_SCALE = 256;
+
+// Sets `base` by the largest exponent (-1000: none) of the first blocks that have one, and raises it by that of later ones where
+// it has to; returns by how much it has risen.
+__device__ __forceinline__ float raise_base(int exponent, float& base) {
+  if (exponent == -1000) return 0.0f;
+  const float e = fmaxf((float)exponent, -126.0f);
+  if (base != NO_BASE && e <= base + FAR) return 0.0f;
+  const float up = base == NO_BASE ? 0.0f : e - base;
+  base = e;
+  return up;
+}
+
 struct ValueScale {
   float exponent, inverse;  // log2 t - base, and 2^ the negative of it
-  float up;                 // by which base has risen
 };
-// A block's scale byte against `base`, which is set by the first block and rises when it has to. A scale of NaN gives weights of
-// NaN to the keys that are seen, and leaves l alone where none is.
-__device__ __forceinline__ ValueScale value_scale(int byte, float& base) {
-  ValueScale r = {__uint_as_float(0x7fffffffu), 0.0f, 0.0f};
-  if (byte == 255) return r;
-  const float e = (float)(byte - 127);
-  if (base == NO_BASE) base = fmaxf(e, -126.0f);
-  if (e > base + FAR) {
-    r.up = e - base;
-    base = e;
-  }
-  r.exponent = fmaxf(e - base, -FAR);
-  r.inverse = exponent_of_2(-(int)r.exponent);
-  return r;
+// A block's scale byte against `base`. A scale of NaN gives weights of NaN to the keys that are seen, and leaves l alone where
+// none is.
+__device__ __forceinline__ ValueScale value_scale(int byte, float base) {
+  if (byte == 255) return {__uint_as_float(0x7fffffffu), 0.0f};
+  if (byte == NO_SCALE) return {0.0f, 1.0f};
+  const float e = fminf(fmaxf((float)(byte - 127) - base, -FAR), FAR);
+  return {e, exponent_of_2(-(int)e)};
+}
+
+// Two e4m3 numbers as fp16, the lower byte's in the lower half.
+__device__ __forceinline__ uint32_t halves_of(uint32_t e4m3x2) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)e4m3x2));
+  return h;
 }
 
 // The power of two that brings a row of bf16 magnitudes up to `most` to [2^14, 2^15); what is that small that this would leave

@@ -47,11 +47,6 @@ struct Stretch {
   int64_t at, scale;   // offsets of the block's first token and of its scale, for head 0
 };
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 // Two e4m3 numbers, the first in the low byte, rounded to nearest even; a NaN stays one.
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
   uint16_t r;
