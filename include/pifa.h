@@ -553,6 +553,8 @@ int pifa_cache_read_q8(const void* k_cache, const void* v_cache, const void* k_s
  *   Numerics: Q enters the first product in fp16, in bf16's case times a power of two for each row that brings its largest
  *   magnitude to [2^14, 2^15); keys and values enter as fp16, which holds e4m3 exactly, without their scales, which are applied in fp32
  *   (the keys') or as part of the weights' exponent (the values'). Weights are fp16, at most 2^8; scores, running maximum and sums fp32.
+ *   Of long chunks, with room for it (pifa_paged_attention_q8_workspace_size), keys and values are rounded to dtype once, and all else
+ *   is as in pifa_paged_attention.
  */
 int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                             int dtype, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
@@ -561,6 +563,12 @@ int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_hea
                             const int32_t* table, int64_t cols, int64_t ldt,
                             const int32_t* q_start, const int32_t* kv_len, int64_t B, int64_t max_q, float scale,
                             void* O, int64_t ldo, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* pifa_paged_attention_q8_workspace_size -- bytes of device scratch with which pifa_paged_attention_q8 is fastest:
+ * pifa_paged_attention_workspace_size() is enough, more is room for the keys and values of long chunks in 16 bits (group max_q > 512
+ * rows, and at most 1 GB for B requests of cols * page_size tokens). Negative pifa_status on bad arguments. Pure host arithmetic. */
+int64_t pifa_paged_attention_q8_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
+                                               int64_t max_q, int64_t cols, int64_t page_size);
 
 /* pifa_validate_indices -- HOST copies: PIFA_OK iff pivot_idx (r entries) and nonpivot_idx
  * (m - r entries) are strictly ascending, inside [0, m) and disjoint (so together a partition

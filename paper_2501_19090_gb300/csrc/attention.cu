@@ -263,6 +263,13 @@ int check_sizes(int64_t T, int64_t hq, int64_t hk, int64_t dim, int64_t B, int64
   return PIFA_OK;
 }
 
+// Whether a cache in 8 bits is brought to 16 before a call on the tensor cores, given the room: where a head's rows may make several
+// items, and the room, for the most keys that the tables can hold, is at most a gigabyte.
+constexpr int64_t WIDE_ROWS_FROM = 512, WIDE_BYTES = (int64_t)1 << 30;
+bool widens(int64_t group, int64_t kv_heads, int64_t dim, int64_t B, int64_t max_q, int64_t keys) {
+  return keys > 0 && group * max_q > WIDE_ROWS_FROM && attention_wide_bytes(kv_heads, dim, B, keys) <= WIDE_BYTES;
+}
+
 // Whether a request's rows for one key / value head may be more than one 16-row product.
 bool takes_tc(int64_t group, int64_t max_q) { return max_q > MAX_ROWS || group * max_q > MAX_ROWS; }
 
@@ -300,7 +307,12 @@ int attend(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_he
     return pifa_fail(PIFA_ERR_WORKSPACE, "workspace missing or smaller than pifa_paged_attention_workspace_size()");
   if (reinterpret_cast<uintptr_t>(workspace) & 255u)
     return pifa_fail(PIFA_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
-  const PifaSpan o = pifa_span(O, T, row, ldo, 2), ws = pifa_span(workspace, 1, need, need, 1);
+  const bool tc = takes_tc(q_heads / kv_heads, max_q);
+  const int64_t room = q8 && tc && widens(q_heads / kv_heads, kv_heads, head_dim, B, max_q, cols * page_size)
+                           ? need + attention_wide_bytes(kv_heads, head_dim, B, cols * page_size) : need;
+  const bool wide = room > need && workspace_bytes >= room;
+  const int64_t used = wide ? room : need;
+  const PifaSpan o = pifa_span(O, T, row, ldo, 2), ws = pifa_span(workspace, 1, used, used, 1);
   const int64_t elem = q8 ? 1 : 2;
   const PifaSpan none = {0, 0};
   const PifaSpan in[] = {pifa_span(Q, T, row, ldq, 2), pifa_cache_span(k_cache, c, elem), pifa_cache_span(v_cache, c, elem),
@@ -315,8 +327,7 @@ int attend(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_he
   if (!status) return pifa_fail_cuda("device status word", e);
   const PifaAttention a = {Q, k_cache, v_cache, O, table, q_start, kv_len, T, ldq, ldo, ldt, cols, B, max_q, q_heads, c, dtype,
                            scale * 1.4426950408889634f, static_cast<uint8_t*>(workspace) + kWorkspaceReserve, q8};
-  if (takes_tc(q_heads / kv_heads, max_q))
-    return launch_attention_tc(a, status, pifa_wait_timeout_ns(), reinterpret_cast<cudaStream_t>(cuda_stream));
+  if (tc) return launch_attention_tc(a, wide, status, pifa_wait_timeout_ns(), reinterpret_cast<cudaStream_t>(cuda_stream));
   if (q8) return launch_attention_rows_q8(a, status, reinterpret_cast<cudaStream_t>(cuda_stream));
   RowArgs g = row_args(a, status);
   g.k = static_cast<const uint16_t*>(k_cache);
@@ -342,6 +353,18 @@ int64_t pifa_paged_attention_workspace_size(int64_t T, int64_t q_heads, int64_t 
   const int64_t group = q_heads / kv_heads;
   return kWorkspaceReserve + (takes_tc(group, max_q) ? attention_tc_workspace_bytes(T, q_heads, kv_heads, head_dim, B)
                                                      : rows_workspace_bytes(group * max_q, head_dim, B));
+}
+
+int64_t pifa_paged_attention_q8_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
+                                               int64_t max_q, int64_t cols, int64_t page_size) {
+  const int64_t need = pifa_paged_attention_workspace_size(T, q_heads, kv_heads, head_dim, B, max_q);
+  if (need <= 0) return need;
+  const int64_t lim = (int64_t)1 << 30;
+  if (cols < 0 || cols >= lim || page_size < 1 || page_size > 256 || cols * page_size > lim)
+    return pifa_fail(PIFA_ERR_INVALID_ARG, "cols or page_size out of range");
+  const int64_t group = q_heads / kv_heads, keys = cols * page_size;
+  return need + (takes_tc(group, max_q) && widens(group, kv_heads, head_dim, B, max_q, keys)
+                     ? attention_wide_bytes(kv_heads, head_dim, B, keys) : 0);
 }
 
 int pifa_paged_attention(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,

@@ -71,15 +71,14 @@ struct Cfg {
   static constexpr uint32_t TILE = D / 64 * HALF;
   static constexpr int SLOTS = Q8 ? (D == 128 ? 4 : 6) : (D == 128 ? 5 : 8);
   static constexpr uint32_t RAW = BN * D;                      // a tile of K or V in 8 bits
-  static constexpr int RAWS = Q8 ? (D == 128 ? 2 : 4) : 0;     // of those; they go through SLOTS as fp16
+  static constexpr int RAWS = Q8 ? (D == 128 ? 2 : 8) : 0;     // of those; they go through SLOTS as fp16
   static constexpr uint32_t SMEM = 1024 + (2 + SLOTS) * TILE + RAWS * RAW + (Q8 ? 1536 : 1024);
   static constexpr int64_t PART_FLOATS = ROWS * D + 2 * ROWS;  // O, then (m, l) of each row
 };
-constexpr int SCALED = 4;  // key tiles whose blocks' scales are in shared memory
-// Of a key tile: its eight blocks' scales as q8.cuh has them, and what the values' are held against.
-struct TileScales {
-  float4 block[BN / PIFA_Q8_BLOCK];  // the keys' scale; the values' exponent and its inverse
-  float base, up;
+constexpr int SCALED = 4;  // key tiles whose scales are in shared memory
+// Of a key tile: the largest scale of its keys' blocks, which the others are brought to, and the same of its values as q8.cuh has it.
+struct alignas(16) TileScales {
+  float key, exponent, inverse, up, base;
 };
 
 // A work item: 16 words. The plan lists those of head 0 with everything that a CTA has to know; a CTA takes one
@@ -110,7 +109,7 @@ struct TcArgs {
   float* partial;
   int64_t ldo, ldt, pages;
   int T, heads, group, tpt, B, max_q,   // tpt: tokens of a tile
-       cols, page_size, page_shift;
+       most_keys, page_size, page_shift;  // most_keys: that the table has room for
   int token_at, head_at;             // their places among the tensor maps' coordinates 1 to 3; the page has the third
   float c;                           // |scale| log2(e)
   int negate;                        // scale < 0
@@ -131,7 +130,7 @@ __device__ __forceinline__ Lengths lengths_of(const TcArgs& g, int b) {
   Lengths x;
   x.q0 = min(max(g.q_start[b], 0), g.T);
   x.n = min(min(max(g.q_start[b + 1], x.q0), g.T) - x.q0, g.max_q);
-  x.L = min(max(g.kv_len[b], 0), g.cols << g.page_shift);
+  x.L = min(max(g.kv_len[b], 0), g.most_keys);
   x.ahead = x.L - (max(g.q_start[b + 1], x.q0) - x.q0) + 1;
   return x;
 }
@@ -166,21 +165,18 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
   return a - v + before;
 }
 
-__global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g, int grid) {
-  extern __shared__ __align__(16) uint8_t plan_smem[];
+__device__ __forceinline__ void make_plan(const TcArgs& g, int grid, uint8_t* plan_smem) {
   Lengths* len = reinterpret_cast<Lengths*>(plan_smem);          // B
   int* first = reinterpret_cast<int*>(plan_smem + (size_t)g.B * sizeof(Lengths));  // B + 1: first item of each request
   __shared__ unsigned long long part[PLAN_THREADS / 32];
   __shared__ int rest_cost[MAX_REST], whole_most;
   __shared__ unsigned long long whole_sum;
   __shared__ int cut;             // key tiles of a piece
-  pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31;
   if (tid == 0) {
     whole_most = 0;
     whole_sum = 0;
   }
-  pdl_wait_primary();
   bool over = false;
   int items = 0;
   unsigned falls = 0;  // starts that are less than the one before: counted with the items, from bit 40 on
@@ -189,7 +185,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
     unsigned long long n = 0;
     if (b < g.B) {
       const Lengths x = lengths_of(g, b);
-      over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
+      over |= g.kv_len[b] > g.most_keys || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
       n = (unsigned)((x.n + 2 * g.tpt - 1) / (2 * g.tpt)) | (unsigned long long)(g.q_start[b + 1] < g.q_start[b]) << 40;
       len[b] = x;
     }
@@ -319,6 +315,106 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
   if (tid == 0) {
     const Plan p = {0, (int)(done >> 32), (int)(done & 0xffffu), (int)(done >> 16 & 0xffffu), 0, {0, 0, 0}};
     *g.plan = p;
+  }
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g, int grid) {
+  extern __shared__ __align__(16) uint8_t plan_smem[];
+  pdl_launch_dependents();
+  pdl_wait_primary();
+  make_plan(g, grid, plan_smem);
+}
+
+// ---- a cache in 8 bits, brought to 16 ----------------------------------------------------------------
+// Where the rows of a key / value head make several items, each would bring the same tiles from 8 bits to 16: then a kernel does
+// it once, beside the plan, into pages of the workspace (of a key tile; of heads of tokens; request b's are b wide_cols and the
+// following), and attention reads those. Rounded to dtype: exact in bf16 from 2^-117 on; in fp16 a finite value stays one.
+constexpr int WIDE_PAGE = BN;
+constexpr int WIDE_ROWS = 64;  // tokens times heads that a CTA takes at a time: of a block of tokens, 4 heads
+
+struct WideArgs {
+  const uint8_t *k, *v;
+  uint16_t *to_k, *to_v;
+  const int32_t* table;        // of the pages in 8 bits
+  int32_t* to_table;
+  int64_t ldt, page_stride, token_stride, head_stride;
+  int wide_cols, page_size, page_shift;
+  int64_t pages;
+};
+
+template <bool F16, int D>
+__global__ void __launch_bounds__(PLAN_THREADS) attention_plan_widen(const TcArgs g, const WideArgs x, int grid) {
+  extern __shared__ __align__(16) uint8_t plan_smem[];
+  __shared__ unsigned long long part[PLAN_THREADS / 32];
+  pdl_launch_dependents();
+  pdl_wait_primary();
+  if (blockIdx.x == 0) return make_plan(g, grid, plan_smem);
+  const int tid = threadIdx.x;
+  int* first = reinterpret_cast<int*>(plan_smem);  // B + 1: blocks of 16 tokens of the requests before
+  int blocks = 0;
+  for (int b0 = 0; b0 < g.B; b0 += PLAN_THREADS) {
+    const int b = b0 + tid;
+    int n = 0;
+    if (b < g.B) {
+      const Lengths len = lengths_of(g, b);
+      n = len.n > 0 ? (len.L + PIFA_Q8_BLOCK - 1) / PIFA_Q8_BLOCK : 0;
+    }
+    unsigned long long total;
+    const int at = (int)block_scan((unsigned long long)n, part, total);
+    if (b < g.B) first[b] = blocks + at;
+    blocks += (int)total;
+  }
+  if (tid == 0) first[g.B] = blocks;
+  __syncthreads();
+  constexpr int PIECES = D / 16;                                // of a row: 16 bytes in, 32 out
+  constexpr int EACH = WIDE_ROWS * PIECES / PLAN_THREADS;       // of a thread
+  const int parts = (2 * g.heads + 3) / 4;                      // four heads of K's and V's
+  const int64_t units = (int64_t)blocks * parts;
+  for (int64_t unit = blockIdx.x - 1; unit < units; unit += gridDim.x - 1) {
+    const int block = (int)(unit / parts), h0 = (int)(unit - (int64_t)block * parts) * 4;
+    int lo = 0, hi = g.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= block) lo = mid;
+      else hi = mid;
+    }
+    const int b = lo, token0 = (block - first[b]) * PIFA_Q8_BLOCK;
+    const int id = x.table[b * x.ldt + (token0 >> x.page_shift)];
+    const bool bad = id < 0 || id >= x.pages;
+    const int page = b * x.wide_cols + token0 / WIDE_PAGE;
+    if (tid == 0) {
+      if (bad) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+      if (h0 == 0 && token0 % WIDE_PAGE == 0) x.to_table[page] = page;
+    }
+    uint4 in[EACH];
+    float s[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int row = (tid + i * PLAN_THREADS) / PIECES, piece = (tid + i * PLAN_THREADS) % PIECES;
+      const int hh = h0 + row / PIFA_Q8_BLOCK, token = row % PIFA_Q8_BLOCK, head = hh < g.heads ? hh : hh - g.heads;
+      in[i] = make_uint4(0, 0, 0, 0);
+      s[i] = 1.0f;
+      if (hh < 2 * g.heads && !bad) {
+        const int in_page = token0 & (x.page_size - 1);
+        const int64_t from = id * x.page_stride + (in_page + token) * x.token_stride + head * x.head_stride + piece * 16;
+        in[i] = __ldg(reinterpret_cast<const uint4*>((hh < g.heads ? x.k : x.v) + from));
+        s[i] = scale_of((hh < g.heads ? g.ks : g.vs)[id * g.scale_page + in_page / PIFA_Q8_BLOCK * g.scale_block + head * g.scale_head]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int row = (tid + i * PLAN_THREADS) / PIECES, piece = (tid + i * PLAN_THREADS) % PIECES;
+      const int hh = h0 + row / PIFA_Q8_BLOCK, token = token0 + row % PIFA_Q8_BLOCK, head = hh < g.heads ? hh : hh - g.heads;
+      if (hh >= 2 * g.heads) continue;
+      uint32_t out[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t w = (&in[i].x)[k / 2];
+        out[k] = scaled_from_e4m3x2<F16>(k & 1 ? w >> 16 : w & 0xffffu, s[i]);
+      }
+      uint16_t* to = (hh < g.heads ? x.to_k : x.to_v) + (((int64_t)page * g.heads + head) * WIDE_PAGE + token % WIDE_PAGE) * D + piece * 16;
+      stg256(to, out);
+    }
   }
 }
 
@@ -455,9 +551,9 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
   };
 
   // Registers: a softmax thread holds a row of S. 2 x 128 x 208 + 128 x 88 = 384 x 168, as launched; with the warps that convert
-  // 2 x 128 x 208 + 2 x 128 x 48 = 512 x 128.
+  // 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128.
   if (warp >= 8) {
-  regs_lower<Q8 ? 48 : 88>();
+  regs_lower<Q8 ? 64 : 88>();
   // K (kv = 0) or V of an item's key tiles, fill after fill of the ring: K and V take its slots in turn. A lane
   // copies 64 columns of a page's rows (or of 128 of them). One warp issuing both was the bound for pages of 16.
   auto stream = [&](int kv, int& tiles, int b, int L, int head, int j0, int j1, auto&& every) {
@@ -672,7 +768,7 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
   } else if (Q8 && warp >= 12) {
     // ---------------- tiles of K (warps 12, 13) and V (14, 15) from 8 bits to fp16, and the blocks' scales (12) ----------------
     if constexpr (Q8) {
-      constexpr int PIECES = D / 16;                       // of a row: 16 bytes in, 32 out
+      constexpr int PIECES = D / 16, BATCH = PIECES / 2;   // of a row: 16 bytes in, 32 out; accesses of a warp to a block's rows
       const int kv = (warp - 12) >> 1, sub = (warp - 12) & 1, piece = lane % PIECES, row0 = sub * (BN / 2) + lane / PIECES;
       int tiles = 0;
       for (int n = 0; !dead; ++n) {
@@ -682,64 +778,84 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&item_free[n & 1]);
         if (end) break;
-        // Lanes 0 to 7 have the keys' scales of a tile, 8 to 15 the values'; pages two tiles ahead, scales one.
+        // Lane i has the scale of the tile's block i (every warp of its own kind, the warp for K's scales the values' too, in lanes 8
+        // to 15); pages are read two tiles ahead, scales one.
         const int32_t* pages = g.table + b * g.ldt;
+        const bool both = warp == 12;
+        const uint8_t* from_scales = kv || lane >= 8 ? g.vs : g.ks;
         auto page_of = [&](int j) {
           const int key = j * BN + (lane & 7) * PIFA_Q8_BLOCK;
-          return lane < 16 && j < j1 && key < L ? pages[key >> g.page_shift] : -1;
+          return lane < (both ? 16 : 8) && j < j1 && key < L ? pages[key >> g.page_shift] : -1;
         };
         auto scale_at = [&](int j, int id) {
           if (id < 0 || id >= g.pages) return NO_SCALE;
           const int at = (j * BN + (lane & 7) * PIFA_Q8_BLOCK) & (g.page_size - 1);
-          return (int)(lane < 8 ? g.ks : g.vs)[id * g.scale_page + at / PIFA_Q8_BLOCK * g.scale_block + head * g.scale_head];
+          return (int)from_scales[id * g.scale_page + at / PIFA_Q8_BLOCK * g.scale_block + head * g.scale_head];
         };
-        int next_page = 0, next_scale = 0;
+        int next_scale = scale_at(j0, page_of(j0)), next_page = page_of(j0 + 1);
         float base = NO_BASE;
-        if (warp == 12) {
-          next_scale = scale_at(j0, page_of(j0));
-          next_page = page_of(j0 + 1);
-        }
         for (int j = j0; j < j1; ++j, ++tiles) {
           const int fill = 2 * tiles + kv, from = fill % LOADS, to = fill % SLOTS;
+          const int scale = next_scale;
+          next_scale = scale_at(j + 1, next_page);
+          next_page = page_of(j + 2);
+          const bool counts = scale != NO_SCALE && scale != 255;
+          const int most = __reduce_max_sync(0xffffffffu, counts && lane < 8 ? scale : -1);
+          // Blocks are brought to the tile's largest scale by a power of two in fp16: exact unless that is below 2^-15, and
+          // then off by 2^-25 at most, in units of which the tile's largest element is 224 or more.
+          const int down = scale - most;
+          const uint32_t by = scale == NO_SCALE ? 0x3c00u : scale == 255 ? 0x7fffu : down >= -14 ? (uint32_t)(15 + down) << 10
+                              : down >= -24 ? 1u << (24 + down) : 0u;
           if (!wait(&empty[to], ((uint32_t)(fill / SLOTS) & 1u) ^ 1u)) break;
-          if (warp == 12) {
+          if (both) {
             // The scales of this tile take the place of those of four tiles ago: both tiles' S of the last K in this slot, or of a
             // later one, is done, and so is what their softmax did before.
-            const int scale = next_scale;
-            next_scale = scale_at(j + 1, next_page);
-            next_page = page_of(j + 2);
-            TileScales& out = scales[tiles % SCALED];
-            const bool counts = lane >= 8 && lane < 16 && scale != NO_SCALE && scale != 255;
-            const int most = __reduce_max_sync(0xffffffffu, counts ? scale - 127 : -1000);
-            const float up = raise_base(most, base);
-            const ValueScale v = value_scale(scale, base);
-            const float k = __shfl_sync(0xffffffffu, scale == NO_SCALE ? 1.0f : scale_of(scale), lane & 7);
-            if (lane >= 8 && lane < 16) out.block[lane - 8] = make_float4(k, v.exponent, v.inverse, 0.0f);
+            const int most_v = __reduce_max_sync(0xffffffffu, counts && lane >= 8 ? scale : -1);
+            const float up = raise_base(most_v < 0 ? -1000 : most_v - 127, base);
+            const ValueScale v = value_scale(most_v < 0 ? NO_SCALE : most_v, base);
             if (lane == 0) {
-              out.base = base;
-              out.up = up;
+              scales[tiles % SCALED] = {most < 0 ? 1.0f : scale_of(most), v.exponent, v.inverse, up, base};
+              mbar_arrive(&scales_full[tiles % SCALED]);
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&scales_full[tiles % SCALED]);
           }
           if (!wait(&raw_full[from], (uint32_t)(fill / LOADS) & 1u)) break;
-          const uint8_t* src = raw + from * C::RAW;
-          uint8_t* dst = ring + to * TILE + (piece >> 2) * HALF;
-          const int tail = kv ? L - j * BN : BN;           // rows of V past the last key may hold anything: zeros
-#pragma unroll 4
-          for (int i = 0; i < BN / 2; i += 32 / PIECES) {
-            const int r = row0 + i;
-            const uint4 x = *reinterpret_cast<const uint4*>(src + r * D + piece * 16);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-            uint32_t h[8];
+          // Blocks of 16 rows, BATCH accesses of 32 / PIECES rows each. Lanes of a row's second half store
+          // their two vectors the other way round: the eight of a quarter warp then meet eight bank groups.
+          const uint8_t* src = raw + from * C::RAW + row0 * D + piece * 16;
+          uint8_t* dst = ring + to * TILE + (piece >> 2) * HALF + row0 * 128;
+          const int second = D == 128 ? piece >> 2 : 0, at = ((piece & 3) * 2 + second) ^ (row0 & 7);
+          constexpr int BLOCKS = BN / 2 / PIFA_Q8_BLOCK;
+#pragma unroll 1  // (all of it unrolled takes room that the softmax's instructions need: 2.06 ms became 2.42)
+          for (int i = 0; i < BLOCKS; ++i) {
+            uint4 x[BATCH];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[k] = r < tail ? halves_of(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu) : 0u;
-            // the lanes of a row's second half the other way round: the eight of a quarter warp then meet eight bank groups
-            const int first = D == 128 ? piece >> 2 : 0;
-            const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
-            const int at = (piece & 3) * 2;
-            *reinterpret_cast<uint4*>(dst + r * 128 + (((at + first) ^ (r & 7)) << 4)) = first ? hi : lo;
-            *reinterpret_cast<uint4*>(dst + r * 128 + (((at + 1 - first) ^ (r & 7)) << 4)) = first ? lo : hi;
+            for (int k = 0; k < BATCH; ++k) x[k] = *reinterpret_cast<const uint4*>(src + (i * PIFA_Q8_BLOCK + k * (32 / PIECES)) * D);
+            const uint32_t f = __shfl_sync(0xffffffffu, by * 0x10001u, sub * BLOCKS + i);
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+              uint32_t h[8];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const uint32_t w = (&x[k].x)[q];
+                h[2 * q] = mul_f16x2(halves_of(w & 0xffffu), f);
+                h[2 * q + 1] = mul_f16x2(halves_of(w >> 16), f);
+              }
+              const int r = i * PIFA_Q8_BLOCK + k * (32 / PIECES);
+              uint8_t* to_row = dst + r * 128;
+              const int place = (at ^ (r & 7)) << 4;
+              const uint4 lo = make_uint4(h[0], h[1], h[2], h[3]), hi = make_uint4(h[4], h[5], h[6], h[7]);
+              *reinterpret_cast<uint4*>(to_row + place) = second ? hi : lo;
+              *reinterpret_cast<uint4*>(to_row + (place ^ 16)) = second ? lo : hi;
+            }
+          }
+          const int tail = L - j * BN - sub * (BN / 2);   // rows of V past the last key may hold anything: zeros
+          if (kv && tail < BN / 2) {
+            __syncwarp();
+            for (int i = max(tail, 0) * 8 + lane; i < BN / 2 * 8; i += 32)
+#pragma unroll
+              for (int h = 0; h < D / 64; ++h)
+                *reinterpret_cast<uint4*>(ring + to * TILE + h * HALF + sub * (BN / 2) * 128 + i * 16) = make_uint4(0, 0, 0, 0);
           }
           fence_proxy_async_smem();
           __syncwarp();
@@ -782,7 +898,7 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
       if (loads[t] && !mbar_wait(&q_full[t], (uint32_t)(loads[t] - 1) & 1u, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
   }
   } else {
-    regs_raise<208>();
+    regs_raise<Q8 ? 192 : 208>();
     // ---------------- softmax and epilogue: a row per thread ----------------
     const int t = warp >> 2, quarter = warp & 3;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
@@ -843,10 +959,100 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
       for (int j = it.j0; j < end; ++j) {
         if (!wait(&s_full[t], s_ph)) break;
         s_ph ^= 1u;
-        const int tile = tiles + j - it.j0;
-        if (Q8 && !wait(&scales_full[tile % SCALED], (uint32_t)(tile / SCALED) & 1u)) break;
-        const TileScales& scale = scales[Q8 ? tile % SCALED : 0];
-        if (!idle) {
+        auto hand_over = [&](int i) {
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_full[2 * t + i]);
+        };
+        const int lim = seen - j * BN;  // keys of this tile that the row sees
+        bool fresh = j == it.j0;        // no maximum yet
+        auto rescale = [&](float f) {   // S(j) is in: so is PV(j - 1), issued before it, and O may be touched
+#pragma unroll 1
+          for (int i = 0; i < D / 16; ++i) {
+            uint32_t o[16];
+            tmem_ld_32x32b_x16(o_at + i * 16, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tmem_st_32x32b_x16(o_at + i * 16, o);
+          }
+        };
+        if (idle) {
+          if (lane == 0) {
+            mbar_arrive(&p_full[2 * t]);
+            mbar_arrive(&p_full[2 * t + 1]);
+          }
+        } else if constexpr (Q8) {
+          // As below, but that m is in the exponents' units and holds the values' scale.
+          const int tile = tiles + j - it.j0;
+          if (!wait(&scales_full[tile % SCALED], (uint32_t)(tile / SCALED) & 1u)) break;
+          const TileScales sc = scales[tile % SCALED];
+          base = sc.base;
+          tc_fence_after();
+          const float ct = fmaxf(c * sc.key, 1e-37f);  // (-inf times 0 is NaN)
+          const uint64_t c2 = f32x2(ct, ct);
+          const bool partly = __any_sync(0xffffffffu, lim < BN);
+          uint64_t sum[2];
+          uint32_t v[4][32], w[4][16];
+          auto weights = [&](int i) {  // keys 32 i to 32 i + 31
+            const float off = sc.exponent - (m > -INFINITY ? m : 0.0f);
+            const uint64_t off2 = f32x2(off, off);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), c2, off2));
+              const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+              sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
+              w[i][k] = pack<true>(p0, p1);
+            }
+          };
+          bool raised = sc.up > 0.0f;
+#pragma unroll 1
+          while (true) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
+            tmem_ld_wait();
+            if (partly) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
+            }
+            float mx[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
+#pragma unroll
+              for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
+            }
+            const float top = fmaf(max3(mx[0], mx[1], fmaxf(mx[2], mx[3])), ct, sc.exponent);
+            if (!fresh && !raised) {
+              sum[0] = sum[1] = 0;
+#pragma unroll
+              for (int i = 0; i < EARLY; ++i) weights(i);
+              if (!__any_sync(0xffffffffu, top - m > 8.0f)) break;
+            }
+            fresh = false;
+            const float most = fmaxf(m, top);
+            float f = m > -INFINITY ? fast_exp2(m - most) : 1.0f;  // (nothing was seen before: zeros)
+            m = most;
+            l *= f;
+            if (raised) f *= exponent_of_2(-(int)fminf(sc.up, 126.0f));  // O, but not l, is in units of 2^base
+            raised = false;
+            if (j > it.j0) rescale(f);
+          }
+#pragma unroll
+          for (int i = 0; i < EARLY; ++i) tmem_st_32x32b_x16(s_at + i * 16, w[i]);
+          hand_over(0);
+#pragma unroll
+          for (int i = EARLY; i < 4; ++i) {
+            weights(i);
+            tmem_st_32x32b_x16(s_at + i * 16, w[i]);
+          }
+          hand_over(1);
+          const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
+          l = fmaf(both.x + both.y, sc.inverse, l);
+        } else {
           tc_fence_after();
           uint32_t v[4][32];
           // The weights of the first 64 keys with the maximum as it was, beside the search for the new one; they
@@ -854,33 +1060,7 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
           uint64_t sum[2];
           uint32_t w[4][16];
           const uint64_t c2 = f32x2(c, c);
-          const int lim = seen - j * BN;  // keys of this tile that the row sees
-          // Q8: of a block's scales, what the row's scores are multiplied by, and exponent and inverse of its values'; those of a
-          // block that the row does not see may be anything
-          auto block = [&](int i) {
-            const float4 x = scale.block[i];
-            const bool sees = PIFA_Q8_BLOCK * i < lim;
-            return make_float3(sees ? max_nan(c * x.x, 1e-37f) : 1.0f, sees ? x.y : 0.0f, sees ? x.z : 0.0f);  // (-inf times 0 is NaN)
-          };
-          auto weights_q8 = [&](int i) {  // of two blocks
-            const float from = m > -INFINITY ? m : 0.0f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float3 b = block(2 * i + h);
-              const uint64_t by = f32x2(b.x, b.x), off = f32x2(b.y - from, b.y - from);
-              uint64_t part = 0;
-#pragma unroll
-              for (int k = 8 * h; k < 8 * h + 8; ++k) {
-                const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), by, off));
-                const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
-                part = add_f32x2(part, f32x2(p0, p1));
-                w[i][k] = pack<true>(p0, p1);
-              }
-              sum[h] = fma_f32x2(part, f32x2(b.z, b.z), sum[h]);
-            }
-          };
           auto weights = [&](int i) {  // keys 32 i to 32 i + 31
-            if constexpr (Q8) return weights_q8(i);
             const float mc = m > -INFINITY ? -m * c : 0.0f;
             const uint64_t mc2 = f32x2(mc, mc);
 #pragma unroll
@@ -891,16 +1071,6 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
               w[i][k] = pack<F16>(p0, p1);
             }
           };
-          auto hand_over = [&](int i) {
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[2 * t + i]);
-          };
-          bool fresh = j == it.j0;  // no maximum yet
-          const float up = Q8 ? scale.up : 0.0f;
-          if (Q8) base = scale.base;
-          bool raised = up > 0.0f;
 #pragma unroll 1
           while (true) {
 #pragma unroll
@@ -914,50 +1084,24 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
             }
             float mx[4];
 #pragma unroll
-            for (int i = 0; !Q8 && i < 4; ++i) {
+            for (int i = 0; i < 4; ++i) {
               mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
 #pragma unroll
               for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
             }
-            float top;  // Q8: times c, and with the values' exponents
-            if constexpr (Q8) {
-              top = -INFINITY;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                float most = fmaxf(__uint_as_float(v[i / 2][16 * (i & 1)]), __uint_as_float(v[i / 2][16 * (i & 1) + 1]));
-#pragma unroll
-                for (int k = 2; k < 16; k += 2)
-                  most = max3(most, __uint_as_float(v[i / 2][16 * (i & 1) + k]), __uint_as_float(v[i / 2][16 * (i & 1) + k + 1]));
-                const float3 b = block(i);
-                top = fmaxf(top, fmaf(most, b.x, b.y));
-              }
-            } else {
-              top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
-            }
-            if (!fresh && !raised) {
+            const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
+            if (!fresh) {
               sum[0] = sum[1] = 0;
 #pragma unroll
               for (int i = 0; i < EARLY; ++i) weights(i);
-              if (!__any_sync(0xffffffffu, (Q8 ? top - m : (top - m) * c) > 8.0f)) break;
+              if (!__any_sync(0xffffffffu, (top - m) * c > 8.0f)) break;
             }
             fresh = false;
-            const float most = fmaxf(m, top);
-            float f = m > -INFINITY ? fast_exp2(Q8 ? m - most : (m - most) * c) : 1.0f;  // (nothing was seen before: zeros)
-            m = most;
+            const float up = fmaxf(m, top);
+            const float f = m > -INFINITY ? fast_exp2((m - up) * c) : 1.0f;  // (nothing was seen before: zeros)
+            m = up;
             l *= f;
-            if (raised) f *= exponent_of_2(-(int)fminf(up, 126.0f));  // O, but not l, is in units of 2^base
-            raised = false;
-            if (j > it.j0) {  // S(j) is in: so is PV(j - 1), issued before it, and O may be touched
-#pragma unroll 1
-              for (int i = 0; i < D / 16; ++i) {
-                uint32_t o[16];
-                tmem_ld_32x32b_x16(o_at + i * 16, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                tmem_st_32x32b_x16(o_at + i * 16, o);
-              }
-            }
+            if (j > it.j0) rescale(f);
           }
 #pragma unroll
           for (int i = 0; i < EARLY; ++i) tmem_st_32x32b_x16(s_at + i * 16, w[i]);
@@ -970,9 +1114,6 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
           hand_over(1);
           const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
           l += both.x + both.y;
-        } else if (lane == 0) {
-          mbar_arrive(&p_full[2 * t]);
-          mbar_arrive(&p_full[2 * t + 1]);
         }
       }
       tiles += it.j1 - it.j0;
@@ -1062,7 +1203,7 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
         if (!__any_sync(0xffffffffu, real)) continue;
         const float* from = g.partial + ((int64_t)__ldcg(&at->slot) * g.heads + head) * C::PART_FLOATS;
         const int64_t pitch = (int64_t)g.heads * C::PART_FLOATS;
-        constexpr int FLIGHT = 4;  // pieces and their weights in flight
+        constexpr int FLIGHT = Q8 ? 2 : 4;  // pieces and their weights in flight
         float x[32] = {}, top = -INFINITY, all = 0.0f;
 #pragma unroll 1
         for (int p0 = 0; p0 < parts; p0 += FLIGHT) {
@@ -1131,6 +1272,17 @@ cudaError_t launch_tc(bool f16, cudaLaunchConfig_t& cfg, const CUtensorMap& qmap
   return f16 ? launch_tc<true, D, Q8>(cfg, qmap, kmap, vmap, g) : launch_tc<false, D, Q8>(cfg, qmap, kmap, vmap, g);
 }
 
+template <auto Kernel, typename... A>
+cudaError_t launch_plan(const cudaLaunchConfig_t& cfg, const A&... args) {
+  const cudaError_t e = pifa_allow_smem<Kernel>((int)(4096 * sizeof(Lengths) + 4097 * 4));
+  return e != cudaSuccess ? e : pifa_launch_ex(&cfg, Kernel, args...);
+}
+template <int D>
+cudaError_t launch_widen(bool f16, cudaLaunchConfig_t cfg, const TcArgs& g, const WideArgs& x, int grid) {
+  cfg.gridDim = dim3((unsigned)(1 + 4 * grid));  // the plan, and four CTAs for each SM
+  return f16 ? launch_plan<attention_plan_widen<true, D>>(cfg, g, x, grid) : launch_plan<attention_plan_widen<false, D>>(cfg, g, x, grid);
+}
+
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 
 int64_t list_bytes(int64_t T, int64_t group, int64_t B) {
@@ -1145,8 +1297,15 @@ int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_head
   return round256(kPlanBytes) + list_bytes(T, q_heads / kv_heads, B) + MAX_PARTS * part;
 }
 
-int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream) {
+int64_t attention_wide_bytes(int64_t kv_heads, int64_t dim, int64_t B, int64_t keys) {
+  const int64_t pages = B * ((keys + WIDE_PAGE - 1) / WIDE_PAGE);
+  return round256(pages * 4) + 2 * pages * WIDE_PAGE * kv_heads * dim * 2;
+}
+
+int launch_attention_tc(const PifaAttention& given, bool wide, int* status, uint64_t timeout_ns, cudaStream_t stream) {
+  PifaAttention a = given;
   TcArgs g = {};
+  WideArgs x = {};
   uint8_t* ws = static_cast<uint8_t*>(a.ws);
   const int64_t group = a.q_heads / a.cache.heads;
   g.o = static_cast<uint16_t*>(a.o);
@@ -1166,7 +1325,39 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   g.tpt = BM / g.group;
   g.B = (int)a.B;
   g.max_q = (int)(a.max_q < a.T ? a.max_q : a.T);
-  g.cols = (int)a.cols;
+  g.most_keys = (int)(a.cols * a.cache.page_size);
+  if (a.q8) {
+    g.ks = a.q8->k;
+    g.vs = a.q8->v;
+    g.scale_page = a.q8->shape.page_stride;
+    g.scale_block = a.q8->shape.block_stride;
+    g.scale_head = a.q8->shape.head_stride;
+  }
+  if (wide) {  // from here on a cache in 16 bits: the workspace's
+    uint8_t* at = ws + attention_tc_workspace_bytes(a.T, a.q_heads, a.cache.heads, a.cache.dim, a.B);
+    x.k = static_cast<const uint8_t*>(a.k);
+    x.v = static_cast<const uint8_t*>(a.v);
+    x.table = a.table;
+    x.ldt = a.ldt;
+    x.page_stride = a.cache.page_stride;
+    x.token_stride = a.cache.token_stride;
+    x.head_stride = a.cache.head_stride;
+    x.pages = a.cache.pages;
+    x.page_size = (int)a.cache.page_size;
+    while ((1 << x.page_shift) < x.page_size) ++x.page_shift;
+    x.wide_cols = (g.most_keys + WIDE_PAGE - 1) / WIDE_PAGE;
+    const int64_t pages = a.B * x.wide_cols, row = WIDE_PAGE * a.cache.dim;
+    x.to_table = reinterpret_cast<int32_t*>(at);
+    x.to_k = reinterpret_cast<uint16_t*>(at + round256(pages * 4));
+    x.to_v = x.to_k + pages * a.cache.heads * row;
+    a.k = x.to_k;
+    a.v = x.to_v;
+    a.q8 = nullptr;
+    a.cache = {pages, WIDE_PAGE, a.cache.heads, a.cache.dim, a.cache.heads * row, a.cache.dim, row};
+    g.table = x.to_table;
+    g.ldt = x.wide_cols;
+    g.pages = pages;
+  }
   g.page_size = (int)a.cache.page_size;
   while ((1 << g.page_shift) < g.page_size) ++g.page_shift;
   g.negate = a.scale_log2 < 0.0f;
@@ -1183,13 +1374,6 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   const bool q8 = a.q8 != nullptr;
   if ((st = make_tmap_cache(&kmap, a.dtype, q8, a.k, a.cache, rows, order)) != PIFA_OK) return st;
   if ((st = make_tmap_cache(&vmap, a.dtype, q8, a.v, a.cache, rows, order)) != PIFA_OK) return st;
-  if (q8) {
-    g.ks = a.q8->k;
-    g.vs = a.q8->v;
-    g.scale_page = a.q8->shape.page_stride;
-    g.scale_block = a.q8->shape.block_stride;
-    g.scale_head = a.q8->shape.head_stride;
-  }
   g.token_at = order[0];
   g.head_at = order[1];
   const int grid = pifa_sm_count();
@@ -1203,12 +1387,12 @@ int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cudaError_t e = pifa_allow_smem<attention_plan>((int)(4096 * sizeof(Lengths) + 4097 * 4));
-  if (e != cudaSuccess) return pifa_fail_cuda("cudaFuncSetAttribute(attention_plan)", e);
-  e = pifa_launch_ex(&cfg, attention_plan, g, grid);
+  const bool f16 = a.dtype == PIFA_DTYPE_FP16;
+  cudaError_t e;
+  if (wide) e = a.cache.dim == 64 ? launch_widen<64>(f16, cfg, g, x, grid) : launch_widen<128>(f16, cfg, g, x, grid);
+  else e = launch_plan<attention_plan>(cfg, g, grid);
   if (e != cudaSuccess) return pifa_fail_cuda("attention_plan launch", e);
   cfg.gridDim = dim3((unsigned)grid);
-  const bool f16 = a.dtype == PIFA_DTYPE_FP16;
   if (a.cache.dim == 64) e = q8 ? launch_tc<64, true>(f16, cfg, qmap, kmap, vmap, g) : launch_tc<64, false>(f16, cfg, qmap, kmap, vmap, g);
   else e = q8 ? launch_tc<128, true>(f16, cfg, qmap, kmap, vmap, g) : launch_tc<128, false>(f16, cfg, qmap, kmap, vmap, g);
   if (e != cudaSuccess) return pifa_fail_cuda("attention_tc launch", e);

@@ -143,7 +143,10 @@ struct PifaAttention {
 int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream);
 // Chunks of new tokens on the tensor cores.
 int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B);
-int launch_attention_tc(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream);
+// `wide`: a cache in 8 bits is brought to 16 first, in attention_wide_bytes() of workspace behind the rest (keys: that a request's
+// row of the table has room for).
+int launch_attention_tc(const PifaAttention& a, bool wide, int* status, uint64_t timeout_ns, cudaStream_t stream);
+int64_t attention_wide_bytes(int64_t kv_heads, int64_t dim, int64_t B, int64_t keys);
 
 // ---- decode (decode.cu) ----------------------------------------------------------------------
 int64_t decode_workspace_bytes(const PifaShape& s);

@@ -1,4 +1,4 @@
-// q8.cuh -- scales of a paged cache in 8 bits, as the attention kernels take them (attention_q8.cu, attention_tc.cu).
+// q8.cuh -- elements and scales of a paged cache in 8 bits (rope_q8.cu), and how attention takes them (attention_q8.cu, attention_tc.cu).
 //
 // Both products run on fp16: e4m3 numbers are fp16 numbers, and rows of Q are brought into its range by a power of two. Of
 // the scales the keys' multiply the scores. The values' become part of the weights' exponents: with x_j the score of key j
@@ -13,6 +13,8 @@
 #define PIFA_Q8_CUH_
 
 #include <stdint.h>
+
+#include <cuda_fp16.h>
 
 namespace pifa {
 
@@ -53,6 +55,11 @@ __device__ __forceinline__ ValueScale value_scale(int byte, float base) {
   return {e, exponent_of_2(-(int)e)};
 }
 
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // Two e4m3 numbers as fp16, the lower byte's in the lower half.
 __device__ __forceinline__ uint32_t halves_of(uint32_t e4m3x2) {
   uint32_t h;
@@ -65,6 +72,17 @@ __device__ __forceinline__ uint32_t halves_of(uint32_t e4m3x2) {
 __device__ __forceinline__ int row_exponent(float most) {
   const int e = (int)(__float_as_uint(most) >> 23) - 127;
   return most == 0.0f || e == 128 ? 0 : 14 - max(e, -100);
+}
+
+// Two e4m3 numbers times s in 16 bits, each rounded once; a finite product stays finite, at most the type's largest number.
+template <bool F16>
+__device__ __forceinline__ uint32_t scaled_from_e4m3x2(uint32_t two, float s) {
+  const uint32_t h = halves_of(two);
+  const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  uint32_t r;
+  if constexpr (F16) asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(p.y * s), "f"(p.x * s));
+  else asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(p.y * s), "f"(p.x * s));
+  return r;
 }
 
 }  // namespace pifa

@@ -7,6 +7,7 @@
 // scale of a block does not depend on how its tokens were dealt to calls, and a float's relative precision does not depend on it.
 #include <cmath>
 
+#include "q8.cuh"
 #include "rope.cuh"
 
 namespace {
@@ -54,13 +55,8 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
   return r;
 }
 __device__ __forceinline__ float2 from_e4m3x2(uint32_t two) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+  const uint32_t h = halves_of(two);
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
-// 2^(byte - 127)
-__device__ __forceinline__ float scale_of(int byte) {
-  return byte == 0 ? __uint_as_float(0x00400000u) : byte == 255 ? __uint_as_float(0x7fffffffu) : __uint_as_float((uint32_t)byte << 23);
 }
 // 2^(127 - byte); 0 for a scale that is not a number
 __device__ __forceinline__ float inverse_scale_of(int byte) {
@@ -289,12 +285,7 @@ __global__ void __launch_bounds__(THREADS) cache_read_q8(const ReadArgs g) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     uint32_t o[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float2 p = from_e4m3x2(w[j / 2] >> (16 * (j & 1)) & 0xffffu);
-      // a finite value stays one: fp16's 65504 was held as 65536, bf16's largest as 2^128
-      if constexpr (F16) asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(o[j]) : "f"(p.y * s), "f"(p.x * s));
-      else asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(o[j]) : "f"(p.y * s), "f"(p.x * s));
-    }
+    for (int j = 0; j < 8; ++j) o[j] = scaled_from_e4m3x2<F16>(w[j / 2] >> (16 * (j & 1)) & 0xffffu, s);
     uint16_t* dst = (is_k ? g.k + (t0 + tt) * g.ldk : g.v + (t0 + tt) * g.ldv) + (int64_t)head * g.dim + u * 16;
     *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
     *reinterpret_cast<uint4*>(dst + 8) = make_uint4(o[4], o[5], o[6], o[7]);

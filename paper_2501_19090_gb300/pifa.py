@@ -66,7 +66,7 @@ EXPORTS = (
     "pifa_m_reconstruct", "pifa_m_reconstruct_workspace_size",
     "pifa_page_tables", "pifa_rope_frequencies", "pifa_rope", "pifa_rope_cache",
     "pifa_paged_attention", "pifa_paged_attention_workspace_size", "pifa_stream_captures",
-    "pifa_rope_cache_q8", "pifa_cache_read_q8", "pifa_paged_attention_q8",
+    "pifa_rope_cache_q8", "pifa_cache_read_q8", "pifa_paged_attention_q8", "pifa_paged_attention_q8_workspace_size",
 )
 
 
@@ -167,6 +167,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                                 _I64, _I64, _I64, _I64, _I64, _I64, _I64, _VP, _I64, _I64, _VP, _VP, _I64,
                                                 _I64, ctypes.c_float, _VP, _I64, _VP, _I64, _VP]
         lib.pifa_paged_attention_q8.restype = ctypes.c_int
+        lib.pifa_paged_attention_q8_workspace_size.argtypes = [_I64] * 8
+        lib.pifa_paged_attention_q8_workspace_size.restype = _I64
         lib.pifa_paged_attention_workspace_size.argtypes = [_I64] * 6
         lib.pifa_paged_attention_workspace_size.restype = _I64
         lib.pifa_validate_indices.argtypes = [_VP, _VP, _I64, _I64]
@@ -1161,9 +1163,23 @@ def pifa_cache_read_q8(k_cache, v_cache, k_scale, v_scale, slots, K=None, V=None
     return K, V
 
 
+@functools.lru_cache(maxsize=1024)  # host arithmetic on plain ints
+def _attention_q8_workspace_size(T, q_heads, kv_heads, head_dim, B, max_q, cols, page_size) -> int:
+    v = int(_lib().pifa_paged_attention_q8_workspace_size(T, q_heads, kv_heads, head_dim, B, max_q, cols, page_size))
+    if v < 0:
+        _check(v, "pifa_paged_attention_q8_workspace_size")
+    return v
+
+
+def pifa_paged_attention_q8_workspace_size(T: int, q_heads: int, kv_heads: int, head_dim: int, B: int, max_q: int, cols: int,
+                                           page_size: int) -> int:
+    return _attention_q8_workspace_size(int(T), int(q_heads), int(kv_heads), int(head_dim), int(B), int(max_q), int(cols), int(page_size))
+
+
 def pifa_paged_attention_q8(Q, k_cache, v_cache, k_scale, v_scale, table, q_start, kv_len, max_q: int, scale=None, O=None,
                             workspace_tensor=None, stream=None):
-    """pifa_paged_attention over a cache in 8 bits (pifa_paged_attention_q8): caches and scales as pifa_rope_cache_q8."""
+    """pifa_paged_attention over a cache in 8 bits (pifa_paged_attention_q8): caches and scales as pifa_rope_cache_q8. Scratch as
+    there, of pifa_paged_attention_q8_workspace_size bytes; a workspace_tensor may be smaller, as that says."""
     torch = sys.modules["torch"]
     run_on = _stream_ptr(stream)
     try:
@@ -1206,7 +1222,7 @@ def pifa_paged_attention_q8(Q, k_cache, v_cache, k_scale, v_scale, table, q_star
         if os_ != [T, h, d]:
             _refuse(f"O must be a tensor of shape {(T, h, d)}")
         dev = Q.get_device()
-    need = _attention_workspace_size(T, h, hk, d, B, int(max_q))
+    need = _attention_q8_workspace_size(T, h, hk, d, B, int(max_q), cols, size)
     if workspace_tensor is None:
         ws_ptr, ws_bytes, _ = _attention_workspace(need, dev, run_on, stream)
     else:

@@ -5,8 +5,9 @@ Bounds:
               value within half an e4m3 step of the exact one, max(2^-4 |x|, 2^-10 s), and 1e-6 (|x| + |partner|) for the rotation
               in fp32. Elements that a call keeps are rounded anew to a scale 2^k higher: e4m3's rounding of q / 2^k, exactly.
   read        element times scale, rounded once: exact in bf16, u |x| + 2^-25 in fp16
-  attention   of the values that the cache stands for. Weights are fp16 and the output is rounded once: u |o| + 2^-11 sum p |v|
-              (first order, 10% over for the rest), 2e-4 sum p |v| for fp32 scores, exponentials and sums, and 2^-24 max |v| a
+  attention   of the values that the cache stands for. Weights are fp16 (of long chunks that are brought to 16 bits first, dtype: w) and
+              the output is rounded once: u |o| + w sum p |v| (first order, 10% over for the rest), 2e-4 sum p |v| for fp32
+              scores, exponentials and sums, and 2^-24 max |v| a
               key, for weights below fp16's normal range: a weight, times its value's scale, is held relative to the largest of them,
               which is at least 1 there, so its error of 2^-25 times an element of at most 448 is at most 2^-24 max |v| in the sum.
               Q in fp16 is exact but for elements less than 2^-28 of their row's largest.
@@ -384,9 +385,21 @@ def make_q8(seed, lens, news, hq, hk, d, page, dtype, heads_first=False, spread=
     return a
 
 
-def attend(a, max_q=None, scale=None, **kw):
+def sizes(a, max_q):
+    B, cols = a["table"].shape
+    pages, page, hk, d = a["k8"].shape
+    return a["Q"].shape[0], a["Q"].shape[1], hk, d, B, max_q, cols, page
+
+
+def attend(a, max_q=None, scale=None, room=True, **kw):
+    """room: for the keys and values of long chunks in 16 bits, if the call has a use for it."""
     if max_q is None:
         max_q = max([1] + (a["q_start"][1:] - a["q_start"][:-1]).tolist())
+    size = sizes(a, max_q)
+    need, most = P.pifa_paged_attention_workspace_size(*size[:6]), P.pifa_paged_attention_q8_workspace_size(*size)
+    a["wide"] = room and most > need
+    if not room:
+        kw["workspace_tensor"] = torch.empty(need + 256, dtype=U8, device=DEV)
     return P.pifa_paged_attention_q8(a["Q"], a["k8"], a["v8"], a["ks"], a["vs"], a["table"], a["q_start"], a["kv_len"], max_q,
                                      scale=scale, **kw)
 
@@ -395,7 +408,8 @@ def check_attention(a, O, scale, slack=0.0):
     want, size, keys = plain_attention(a, scale)
     most = a["v_cache"].double().nan_to_num(0.0, 0.0, 0.0)
     most = float(most[a["table"].clamp(min=0).long().unique()].abs().max())
-    tol = U[O.dtype] * want.abs() + (1.1 * 2.0 ** -11 + 2e-4 + slack) * size + 2.0 ** -24 * (1.0 + keys) * most
+    w = U[O.dtype] if a.get("wide") else 2.0 ** -11
+    tol = U[O.dtype] * want.abs() + (1.1 * w + 2e-4 + slack) * size + 2.0 ** -24 * (1.0 + keys) * most
     err = (O.double() - want).abs()
     assert bool((err <= tol).all()), (float((err - tol).max()), int((err > tol).sum()), (err > tol).nonzero()[:4].tolist())
 
@@ -405,10 +419,25 @@ def check_attention(a, O, scale, slack=0.0):
 def test_attention(name, dtype):
     lens, news, hq, hk, d, page = SHAPES[name]
     a = make_q8(len(name), lens, news, hq, hk, d, page, dtype)
-    O = torch.full_like(a["Q"], math.nan)
-    attend(a, O=O)
-    check_attention(a, O, d ** -0.5)
-    assert torch.equal(attend(a), O)     # and whatever order blocks run in
+    for room in (False, True):
+        O = torch.full_like(a["Q"], math.nan)
+        attend(a, O=O, room=room)
+        check_attention(a, O, d ** -0.5)
+        assert torch.equal(attend(a, room=room), O)     # and whatever order blocks run in
+        if not a["wide"] and room:
+            assert torch.equal(O, last)
+        last = O
+
+
+def test_long_chunks_take_the_room():
+    """Which of the shapes above are brought to 16 bits first: those with more than 512 rows of a head."""
+    for name, (lens, news, hq, hk, d, page) in SHAPES.items():
+        cols = max(-(-n // page) for n in lens + [1]) + 1
+        size = (sum(news), hq, hk, d, len(lens), max(news + [1]), cols, page)
+        wide = P.pifa_paged_attention_q8_workspace_size(*size) > P.pifa_paged_attention_workspace_size(*size[:6])
+        assert wide == (max(news) * hq // hk > 512), name
+    assert P.pifa_paged_attention_q8_workspace_size(2048, 64, 8, 128, 200, 2048, 1000, 64) == P.pifa_paged_attention_workspace_size(
+        2048, 64, 8, 128, 200, 2048)                    # 200 requests of up to 64000 tokens: more than a gigabyte
 
 
 @pytest.mark.parametrize("name", ["decode_ragged_gqa", "few_tokens", "mixed", "prompt_1000_gqa", "chunk_group_3"])
@@ -417,14 +446,16 @@ def test_attention_scales_far_apart(name):
     lens, news, hq, hk, d, page = SHAPES[name]
     a = make_q8(3, lens, news, hq, hk, d, page, torch.bfloat16, spread=5)
     a["Q"] = (a["Q"].float() / 32).to(torch.bfloat16)
+    check_attention(a, attend(a, room=False), d ** -0.5)
     check_attention(a, attend(a), d ** -0.5)
     a = make_q8(4, lens, news, hq, hk, d, page, torch.bfloat16, spread=10)
     a["Q"] = (a["Q"].float() / 1024).to(torch.bfloat16)
+    check_attention(a, attend(a, room=False), d ** -0.5)
     check_attention(a, attend(a), d ** -0.5)
 
 
 @pytest.mark.parametrize("order", ["up", "down", "mixed"])
-@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("new", [1, 5, 150, 300])
 def test_attention_blocks_of_zeros_and_of_any_size(new, order):
     """Values whose blocks are nothing but zeros (the smallest scale) or differ by 2^120 in size: each key / value head against its own
     largest value, the weights' sum with all keys in it."""
@@ -440,12 +471,14 @@ def test_attention_blocks_of_zeros_and_of_any_size(new, order):
     vs[pages] = size.to(U8).view(len(pages), page // 16, hk)
     v8[pages] = torch.where(size.view(len(pages), page // 16, 1, hk, 1) == 1, 0, v8[pages].view(len(pages), page // 16, 16, hk, d)).view(len(pages), page, hk, d).to(U8)
     a["v_cache"] = values(a["v8"], a["vs"])
-    O = attend(a)
     want, s, keys = plain_attention(a, d ** -0.5)
     most = a["v_cache"][pages].flatten(0, 1)[:L].abs().amax((0, 2)).repeat_interleave(hq // hk)[None, :, None]
-    err = (O.double() - want).abs()
-    tol = U[O.dtype] * want.abs() + (1.1 * 2.0 ** -11 + 2e-4) * s + 2.0 ** -24 * (1.0 + keys) * most
-    assert bool((err <= tol).all()), (float((err - tol).max()), (err > tol).nonzero()[:4].tolist())
+    for room in (False, True):
+        O = attend(a, room=room)
+        w = U[O.dtype] if a["wide"] else 2.0 ** -11
+        err = (O.double() - want).abs()
+        tol = U[O.dtype] * want.abs() + (1.1 * w + 2e-4) * s + 2.0 ** -24 * (1.0 + keys) * most
+        assert bool((err <= tol).all()), (float((err - tol).max()), (err > tol).nonzero()[:4].tolist())
 
 
 @pytest.mark.parametrize("size", [1e-30, 3e-5, 2e4, 1e30])
@@ -457,7 +490,8 @@ def test_attention_queries_of_any_size(name, size):
     rows = torch.exp2(torch.arange(a["Q"].shape[0], device=DEV) % 3 - 1.0)[:, None, None]
     a["Q"] = (a["Q"].float() * size * rows).to(torch.bfloat16)
     a["Q"][0, 1] = 0.0
-    check_attention(a, attend(a, scale=d ** -0.5 / size), d ** -0.5 / size)
+    for room in (False, True):
+        check_attention(a, attend(a, scale=d ** -0.5 / size, room=room), d ** -0.5 / size)
 
 
 @pytest.mark.parametrize("scale,size", [(1.0, 30.0), (-0.3, 2.0), (0.0, 1.0), (1e-3, 300.0)])
@@ -468,7 +502,8 @@ def test_attention_scores_of_any_size(name, scale, size):
     lens, news, hq, hk, d, page = SHAPES[name]
     a = make_q8(6, lens, news, hq, hk, d, page, torch.bfloat16)
     a["Q"] = (a["Q"].float() * size / 1.5).to(torch.bfloat16)
-    check_attention(a, attend(a, scale=scale), scale, slack=2e-3)
+    for room in (False, True):
+        check_attention(a, attend(a, scale=scale, room=room), scale, slack=2e-3)
 
 
 @pytest.mark.parametrize("name", ["tokens_at_page_ends", "few_tokens_gqa", "mixed", "prompt_1000_gqa"])
@@ -477,23 +512,25 @@ def test_attention_bound_on_new_tokens_may_be_loose(name):
     a = make_q8(5, lens, news, hq, hk, d, page, torch.bfloat16)
     for loose in (16, 100, 5000):
         if loose >= max(news):
-            check_attention(a, attend(a, max_q=loose), d ** -0.5)
+            for room in (False, True):
+                check_attention(a, attend(a, max_q=loose, room=room), d ** -0.5)
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("name", ["one_token", "few_tokens", "chunk_in_context", "mixed"])
-def test_attention_strides_and_guards(name):
+def test_attention_strides_and_guards(name, room):
     lens, news, hq, hk, d, page = SHAPES[name]
     a = make_q8(9, lens, news, hq, hk, d, page, torch.bfloat16, heads_first=True)
     T = a["Q"].shape[0]
     wide = torch.full((T + 3, hq + 5, d), 3.0, dtype=torch.bfloat16, device=DEV)
     wide[:T, 2:2 + hq] = a["Q"]
     a["Q"] = wide[:, 2:2 + hq]
-    room = torch.full((T + 5, hq * d + 40), 9.0, dtype=torch.bfloat16, device=DEV)
-    O = room[1:-1, 16:16 + hq * d].unflatten(1, (hq, d))
-    attend(a, O=O)
+    frame = torch.full((T + 5, hq * d + 40), 9.0, dtype=torch.bfloat16, device=DEV)
+    O = frame[1:-1, 16:16 + hq * d].unflatten(1, (hq, d))
+    attend(a, O=O, room=room)
     a["Q"] = a["Q"][:T]
     check_attention(a, O[:T], d ** -0.5)
-    assert (room[0] == 9).all() and (room[T + 1:] == 9).all() and (room[:, :16] == 9).all() and (room[:, 16 + hq * d:] == 9).all()
+    assert (frame[0] == 9).all() and (frame[T + 1:] == 9).all() and (frame[:, :16] == 9).all() and (frame[:, 16 + hq * d:] == 9).all()
 
 
 @pytest.mark.parametrize("dead,dead_scale", [(0x7f, 0xff), (0xff, 0xff), (0x7e, 0xfe), (0x55, 0), (0x7f, 127)])
@@ -503,10 +540,11 @@ def test_attention_ignores_what_no_request_owns(name, dead, dead_scale):
     for dtype in DTYPES:
         a = make_q8(2, lens, news, hq, hk, d, page, dtype, dead=dead, dead_scale=dead_scale)
         b = make_q8(2, lens, news, hq, hk, d, page, dtype, dead=0, dead_scale=127)
-        assert torch.equal(attend(a), attend(b))
+        for room in (False, True):
+            assert torch.equal(attend(a, room=room), attend(b, room=room))
 
 
-@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("new", [1, 40, 280])
 @pytest.mark.parametrize("what", ["k8", "ks", "vs"])
 def test_attention_nan_stays_with_the_tokens_that_see_it(what, new):
     """A NaN key, or a scale of NaN: NaN for the rows that see (a token of) it, nothing for the others."""
@@ -529,8 +567,8 @@ def test_attention_nan_stays_with_the_tokens_that_see_it(what, new):
 
 
 def test_attention_reports_bad_tables_and_bounds():
-    for new in (1, 40):
-        a = make_q8(7, [200, 90], [new, 1], 4, 2, 128, 16, torch.bfloat16)
+    for new in (300, 1, 40):
+        a = make_q8(7, [200 + new, 90], [new, 1], 4, 2, 128, 16, torch.bfloat16)
         good = attend(a)
         for bad in (-1, 10 ** 6, 2 ** 31 - 1):
             b = dict(a, table=a["table"].clone())
@@ -538,14 +576,15 @@ def test_attention_reports_bad_tables_and_bounds():
             O = attend(b)
             assert P.pifa_device_status() == P.PIFA_ERR_DEVICE_INDEX
             assert torch.equal(O[new:], good[new:])
-            z = dict(a, k_cache=a["k_cache"].clone(), v_cache=a["v_cache"].clone())
+            z = dict(a, k_cache=a["k_cache"].clone(), v_cache=a["v_cache"].clone(), wide=b["wide"])
             z["k_cache"][int(a["table"][0, 3])] = 0.0
             z["v_cache"][int(a["table"][0, 3])] = 0.0
             check_attention(z, O, 128 ** -0.5)
         b = dict(a, kv_len=i32([10 ** 6, 90]))
-        O = attend(b)
-        assert P.pifa_device_status() in (P.PIFA_ERR_CAPACITY, P.PIFA_ERR_DEVICE_INDEX)
-        check_attention(a, torch.cat([good[:new], O[new:]]), 128 ** -0.5)
+        for room in (False, True):
+            O = attend(b, room=room)
+            assert P.pifa_device_status() in (P.PIFA_ERR_CAPACITY, P.PIFA_ERR_DEVICE_INDEX)
+            check_attention(a, torch.cat([good[:new], O[new:]]), 128 ** -0.5)
         O = torch.full_like(a["Q"], 5.0)
         attend(dict(a, q_start=i32([0, new + 1, new])), max_q=new + 1, O=O)
         assert P.pifa_device_status() == P.PIFA_ERR_DEVICE_INDEX and (O == 5.0).all()
@@ -601,16 +640,17 @@ def test_a_serving_loop(dtype):
                  torch.empty(T, dtype=torch.int64, device=DEV), head),
                 torch.empty((T, hq, d), dtype=dtype, device=DEV), torch.zeros((T, hq, d), dtype=dtype, device=DEV))
 
-    def check(out, Qr, O):
+    def check(out, Qr, O, max_q):
         n = int(out[0][-1])
-        a = dict(Q=Qr[:n], k_cache=values(cache[0], cache[2]), v_cache=values(cache[1], cache[3]), table=table, q_start=out[0], kv_len=lens)
+        a = dict(Q=Qr[:n], k_cache=values(cache[0], cache[2]), v_cache=values(cache[1], cache[3]), table=table, q_start=out[0], kv_len=lens,
+                 wide=max_q * hq // hk > 512)
         check_attention(a, O[:n], d ** -0.5)
 
     T = sum(prompt) + 4                                          # padded
     x = torch.randn((T, hq + 2 * hk, d), device=DEV, generator=g).to(dtype)
     buf = buffers(T)
     step(x, i32(prompt), T, max(prompt), *buf)
-    check(*buf)
+    check(*buf, max(prompt))
     at = 0
     for b, n in enumerate(prompt):
         sent[b] += list(x[at:at + n, hq + hk:])
@@ -626,7 +666,7 @@ def test_a_serving_loop(dtype):
         graph.replay()
         torch.cuda.synchronize()
         if k % 6 == 5:
-            check(*buf)
+            check(*buf, 1)
         for b in range(B):
             sent[b].append(x1[b, hq + hk:].clone())
     for b in range(B):                                           # values are not turned: what went in, within the roundings
