@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   pdl_launch_dependents();
   pdl_wait_primary();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Run steps_here = deal_steps(g, first, part);
+  const Run steps_here = deal_steps(g, first, part, (int)gridDim.x * WARPS, MIN_STEPS);
   const int total = steps_here.total, run = steps_here.run;
 
   // ---- this warp's run of steps: segments of one request and head each ----

@@ -17,7 +17,13 @@ struct RowsQ8 {
 };
 
 template <int D>
-constexpr int kStages = 768 / D;  // of 16 keys: 4 KB (D = 128) or 2 KB
+constexpr int kStages = 512 / D;  // of 16 keys: 4 KB (D = 128) or 2 KB
+constexpr int LEAST = 2 * WARPS;  // steps of a CTA
+
+// What a warp has summed up of a head that it did not finish alone: in shared memory, for the CTA to add up.
+struct Piece {
+  int item, b, from, steps;  // (first step of the head) -1: none
+};
 
 // Where a 16-byte piece of a key's row lies among its stage's K or V, so that the lanes that read together meet different bank
 // groups: of K two keys' four neighbouring pieces at a time; of V, of every other key, two pieces (D = 64: halves of two).
@@ -36,19 +42,27 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
   constexpr int STAGE_BYTES = 2 * STEP * D;            // K and V of a step
   constexpr int STAGES = kStages<D>;
   extern __shared__ __align__(16) uint8_t smem[];
-  int* first = reinterpret_cast<int*>(smem + WARPS * STAGES * STAGE_BYTES);  // B + 1
+  // of each warp its first head's piece; its last one's takes the place of its stages when those are done
+  float* sums = reinterpret_cast<float*>(smem + WARPS * STAGES * STAGE_BYTES);
+  int* first = reinterpret_cast<int*>(sums + WARPS * g.max_rows * D);  // B + 1
+  static_assert(STAGES * STAGE_BYTES >= MAX_ROWS * D * 4, "a piece fits into a warp's stages");
   __shared__ int part[32];
+  __shared__ Piece pieces[2 * WARPS];
+  __shared__ float2 ml[2 * WARPS][MAX_ROWS];
   pdl_launch_dependents();
   pdl_wait_primary();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Run dealt = deal_steps(g, first, part);
-  const int total = dealt.total, run = dealt.run;
+  const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST);
 
-  // ---- this warp's run of steps: segments of one request and head each ----
-  const int worker = warp * (int)gridDim.x + (int)blockIdx.x;  // neighbours on different SMs
-  const int64_t at64 = (int64_t)worker * run;
-  int at = (int)min(at64, (int64_t)total);
-  const int stop = (int)min(at64 + run, (int64_t)total);
+  // ---- this CTA's run of steps, this warp's share of it: segments of one request and head each ----
+  const int64_t c64 = (int64_t)blockIdx.x * dealt.run;
+  const int c0 = (int)min(c64, (int64_t)dealt.total), c1 = (int)min(c64 + dealt.run, (int64_t)dealt.total);
+  if (c0 == c1) return;
+  const int share = (c1 - c0 + WARPS - 1) / WARPS;
+  int at = min(c0 + warp * share, c1);
+  const int stop = min(at + share, c1);
+  if (lane < 2) pieces[2 * warp + lane].item = -1;
+  __syncwarp();
   const int gr = lane >> 2, c4 = lane & 3;
   const uint8_t* ring = smem + warp * STAGES * STAGE_BYTES;
   const uint32_t ring_at = smem_u32(ring);
@@ -256,13 +270,20 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
     cp_wait<0>();
     // o[i][2 r + e]: row gr + 8 r, column VC (2 c4 + e) + i, in units of 2^base
     const float unit = base > NO_BASE ? exponent_of_2((int)base) : 1.0f;
+    const bool alone = s0 == 0 && s1 == steps;
+    const int which = 2 * warp + (at + s1 - s0 == stop ? 1 : 0);  // a piece's place: the warp's first, or what it ends with
+    float* sum = which & 1 ? reinterpret_cast<float*>(smem + warp * STAGES * STAGE_BYTES) : sums + warp * g.max_rows * D;
+    if (!alone) {
+      __syncwarp();  // the stages have been read
+      if (lane == 0) pieces[which] = {b * g.heads + head, b, first[b] + head * steps, steps};
+    }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
       const int row = gr + 8 * r, token = row / g.group;
       if (row >= rows) continue;
-      if (s0 == 0 && s1 == steps) {
+      if (alone) {
         const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
         uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + 2 * VC * c4;
 #pragma unroll
@@ -275,25 +296,70 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
               w[k] = pack<F16>(o[8 * i + 2 * k][2 * r + e] * inv * unit, o[8 * i + 2 * k + 1][2 * r + e] * inv * unit);
             *reinterpret_cast<uint4*>(out + VC * e + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-      } else {  // a head that began before this run: the first of the warp's two places, else the second
-        float* to = g.partial + (((int64_t)worker * 2 + (s0 > 0 ? 0 : 1)) * g.max_rows + row) * (D + 2);
-        float2* ml = reinterpret_cast<float2*>(to + D);
-        if (c4 == 0) *ml = make_float2(m[r], l[r]);
+      } else {
+        if (c4 == 0) ml[which][row] = make_float2(m[r], l[r]);
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int i = 0; i < VC / 2; ++i)
-            *reinterpret_cast<float2*>(to + VC * (2 * c4 + e) + 2 * i) =
-                make_float2(o[2 * i][2 * r + e] * unit, o[2 * i + 1][2 * r + e] * unit);
+          for (int i = 0; i < VC / 4; ++i)
+            *reinterpret_cast<float4*>(sum + row * D + VC * (2 * c4 + e) + 4 * i) =
+                make_float4(o[4 * i][2 * r + e] * unit, o[4 * i + 1][2 * r + e] * unit, o[4 * i + 2][2 * r + e] * unit, o[4 * i + 3][2 * r + e] * unit);
       }
     }
     at += s1 - s0;
+  }
+  // ---- the CTA's pieces, those of one head added up in the order of the keys; heads of several CTAs are left to the join ----
+  __syncthreads();
+  for (int k0 = 0; k0 < 2 * WARPS;) {
+    const Piece x = pieces[k0];
+    int k1 = k0 + 1;
+    while (k1 < 2 * WARPS && (pieces[k1].item == x.item || pieces[k1].item < 0)) ++k1;
+    if (x.item < 0) {
+      ++k0;
+      continue;
+    }
+    const int head = x.item - x.b * g.heads;
+    const Lengths len = lengths_of(g, x.b);
+    const bool whole = x.from >= c0 && x.from + x.steps <= c1;
+    const int rows = len.n * g.group;
+    for (int slot = threadIdx.x; slot < rows * (D / 4); slot += THREADS) {
+      const int row = slot / (D / 4), col = slot % (D / 4) * 4;
+      float top = -INFINITY;
+      for (int k = k0; k < k1; ++k)
+        if (pieces[k].item >= 0 && ml[k][row].y != 0.0f) top = fmaxf(top, ml[k][row].x);
+      float all = 0.0f;
+      float4 acc = make_float4(0, 0, 0, 0);
+      for (int k = k0; k < k1; ++k) {
+        if (pieces[k].item < 0) continue;
+        const float2 v = ml[k][row];
+        const float e = v.y != 0.0f ? fast_exp2(v.x - top) : 0.0f;
+        const float* from = k & 1 ? reinterpret_cast<const float*>(smem + (k >> 1) * STAGES * STAGE_BYTES) : sums + (k >> 1) * g.max_rows * D;
+        const float4 o = *reinterpret_cast<const float4*>(from + row * D + col);
+        all += v.y * e;
+        acc.x += o.x * e;
+        acc.y += o.y * e;
+        acc.z += o.z * e;
+        acc.w += o.w * e;
+      }
+      if (whole) {
+        const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+        const int token = row / g.group;
+        uint16_t* out = g.o + (int64_t)(len.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + col;
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack<F16>(acc.x * inv, acc.y * inv), pack<F16>(acc.z * inv, acc.w * inv));
+      } else {  // a head that began before this CTA's run: the first of its two places, else the second
+        float* to = g.partial + (((int64_t)blockIdx.x * 2 + (x.from < c0 ? 0 : 1)) * g.max_rows + row) * (D + 2);
+        if (col == 0) *reinterpret_cast<float2*>(to + D) = make_float2(top, all);
+        *reinterpret_cast<float2*>(to + col) = make_float2(acc.x, acc.y);
+        *reinterpret_cast<float2*>(to + col + 2) = make_float2(acc.z, acc.w);
+      }
+    }
+    k0 = k1;
   }
 }
 
 template <bool F16, int D>
 cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
-  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * kStages<D> * 2 * STEP * D, stream, c8);
+  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4), stream, c8);
 }
 
 }  // namespace

@@ -27,8 +27,8 @@ struct RowArgs {
   const uint16_t *q, *k, *v;
   uint16_t* o;
   const int32_t *table, *q_start, *kv_len;
-  int* sums;          // B + 1: first step of each request (times heads), then the steps of one warp (0: nothing is done)
-  float* partial;     // for each warp two of max_rows x (D + 2): O, m, l
+  int* sums;          // B + 1: first step of each request (times heads), then the steps of one worker (0: nothing is done)
+  float* partial;     // for each worker, a warp or a CTA, two of max_rows x (D + 2): O, m, l
   int64_t ldq, ldo, ldt, page_stride, token_stride, head_stride, pages;
   int T, heads, group, page_size, page_shift, cols, B, max_q, max_rows;
   float c;            // |scale| log2(e), with scale's sign in `flip`
@@ -87,12 +87,12 @@ __device__ __forceinline__ int find(const int* first, int n, int v) {
   return lo;
 }
 
-// The requests' first steps, into first[0, B], how many there are, and a warp's share of them (all threads of the CTA; CTA 0
-// writes them down for the join).
+// The requests' first steps, into first[0, B], how many there are, and the share of each worker, at least `least` (all threads of
+// the CTA; CTA 0 writes them down for the join).
 struct Run {
   int total, run;
 };
-__device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* part) {
+__device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* part, int workers, int least) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int total = 0;
   bool over = false, falls = false;
@@ -127,8 +127,7 @@ __device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* par
   // requests that overlap: which of them a row belongs to is not said, so nothing is done
   const bool overlap = __syncthreads_or(falls);
   if (overlap) total = 0;
-  const int workers = (int)gridDim.x * WARPS;
-  const int run = max((total + workers - 1) / workers, MIN_STEPS);
+  const int run = max((total + workers - 1) / workers, least);
   if (blockIdx.x == 0) {
     for (int b = tid; b <= g.B; b += THREADS) g.sums[b] = first[b];
     if (tid == 0) {
@@ -140,7 +139,7 @@ __device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* par
   return {total, run};
 }
 
-// Adds up the pieces of a request's head whose steps fell to several warps, in the order of the keys: `split` CTAs
+// Adds up the pieces of a request's head whose steps fell to several workers, in the order of the keys: `split` CTAs
 // for each, a share of the columns apiece, a thread for four columns of a row, up to 16 threads with every
 // so many-th piece where a CTA has fewer of those. Pieces and their weights are loaded together, four at a time: with few
 // pieces the kernel is two latencies long, and one long sequence (144 pieces of each head) spreads over the SMs (64
@@ -159,8 +158,8 @@ __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int s
   const int run = g.sums[g.B + 1], steps = steps_of(x), from = g.sums[b] + head * steps;
   if (steps == 0 || run == 0) return;
   const int w0 = from / run, w1 = (from + steps - 1) / run;
-  if (w0 == w1) return;  // the warp has finished it
-  const int place = g.max_rows * (D + 2);  // a warp has two: the head that began before its run, and the last one
+  if (w0 == w1) return;  // the worker has finished it
+  const int place = g.max_rows * (D + 2);  // a worker has two: the head that began before its run, and the last one
   for (int slot = (int)threadIdx.x % (slots * groups); slot < slots * groups; slot += THREADS) {
     const int group = slot / slots, row = (slot - group * slots) / quads, col = col0 + (slot - group * slots) % quads * 4;
     const bool here = row < x.n * g.group && (int)threadIdx.x < slots * groups;
@@ -249,7 +248,7 @@ cudaError_t launch_rows_and_join(const RowArgs& g, size_t smem, cudaStream_t str
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cudaError_t e = pifa_allow_smem<Kernel>(227 * 1024 - 256);
+  cudaError_t e = pifa_allow_smem<Kernel>(223 * 1024);  // (the rest is static)
   if (e == cudaSuccess) e = pifa_launch_ex(&cfg, Kernel, g, more...);
   if (e != cudaSuccess) return e;
   cfg.dynamicSmemBytes = 0;
