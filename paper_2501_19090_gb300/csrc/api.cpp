@@ -126,14 +126,14 @@ int make_tmap_heads(CUtensorMap* map, int dtype, const void* base, int64_t T, in
   return PIFA_OK;
 }
 
-int make_tmap_cache(CUtensorMap* map, int dtype, bool q8, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]) {
+static int encode_cache(CUtensorMap* map, CUtensorMapDataType dt, int64_t elem, uint32_t box_cols, CUtensorMapSwizzle swizzle,
+                        const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) return pifa_fail(PIFA_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   struct { int64_t n, stride; uint32_t box; int is; } d[3] = {
       {c.page_size, c.token_stride, rows, 0}, {c.heads, c.head_stride, 1, 1}, {c.pages, c.page_stride, 1, 2}};
   // a dimension of one element is never stepped over: whatever its stride says, it takes the largest one
-  int64_t most = q8 ? 16 : 8;
-  const int64_t elem = q8 ? 1 : 2;
+  int64_t most = 16 / elem;
   for (const auto& x : d)
     if (x.n > 1 && x.stride > most) most = x.stride;
   for (auto& x : d)
@@ -141,8 +141,12 @@ int make_tmap_cache(CUtensorMap* map, int dtype, bool q8, const void* base, cons
   for (int i = 0; i < 3; ++i)
     for (int j = 0; j < i; ++j)
       if (d[i].stride < d[j].stride) std::swap(d[i], d[j]);
+  // L2 fetches no more than a row: what lies behind it is another head's (64 sequences, 8 heads of 128 bytes: 77 us became 69)
+  const CUtensorMapL2promotion promotion = c.dim * elem >= 256   ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B
+                                           : c.dim * elem >= 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B
+                                                                 : CU_TENSOR_MAP_L2_PROMOTION_L2_64B;
   cuuint64_t dims[4] = {(cuuint64_t)c.dim}, strides[3];
-  cuuint32_t box[4] = {q8 ? (cuuint32_t)c.dim : 64u}, estr[4] = {1, 1, 1, 1};
+  cuuint32_t box[4] = {box_cols}, estr[4] = {1, 1, 1, 1};
   for (int i = 0; i < 3; ++i) {
     if (d[i].stride * elem >= ((int64_t)1 << 40)) return pifa_fail(PIFA_ERR_UNSUPPORTED, "cache: a stride of 2^40 bytes or more");
     dims[i + 1] = (cuuint64_t)d[i].n;
@@ -150,16 +154,23 @@ int make_tmap_cache(CUtensorMap* map, int dtype, bool q8, const void* base, cons
     box[i + 1] = d[i].box;
     order[d[i].is] = i;
   }
-  const CUtensorMapDataType dt =
-      q8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : dtype == PIFA_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   CUresult r = fn(map, dt, 4, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  q8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                  swizzle, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     char buf[120];
     std::snprintf(buf, sizeof buf, "cuTensorMapEncodeTiled failed (CUresult %d) for a paged cache", (int)r);
     return pifa_fail(PIFA_ERR_CUDA, buf);
   }
   return PIFA_OK;
+}
+
+int make_tmap_cache(CUtensorMap* map, int dtype, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]) {
+  return encode_cache(map, dtype == PIFA_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, 64,
+                      CU_TENSOR_MAP_SWIZZLE_128B, base, c, rows, order);
+}
+int make_tmap_cache_q8(CUtensorMap* map, const void* base, const PifaCacheShape& c, uint32_t rows, bool swizzle, int order[3]) {
+  return encode_cache(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, (uint32_t)c.dim,
+                      !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE : c.dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, base, c, rows, order);
 }
 
 int pifa_check_cache(const PifaCacheShape& c, int64_t least, int64_t most) {

@@ -12,8 +12,10 @@
 namespace {
 
 struct RowsQ8 {
-  const uint8_t *k, *v, *ks, *vs;
+  const uint8_t *ks, *vs;
   int64_t scale_page, scale_block, scale_head;
+  int token_at, head_at;  // their places among the tensor maps' coordinates 1 to 3; the page has the third
+  uint64_t timeout_ns;
 };
 
 template <int D>
@@ -25,23 +27,26 @@ struct Piece {
   int item, b, from, steps;  // (first step of the head) -1: none
 };
 
-// Where a 16-byte piece of a key's row lies among its stage's K or V, so that the lanes that read together meet different bank
-// groups: of K two keys' four neighbouring pieces at a time; of V, of every other key, two pieces (D = 64: halves of two).
+// TMA leaves the 16-byte pieces of a key's row swizzled (its index xor the row's, in the 128 bytes that eight, or with D = 64 two
+// rows of 64, lie in). Which of a product's 16 keys is which of the step's, and which of its columns are a lane's, is free: chosen so
+// that the eight lanes that read together meet eight bank groups.
 template <int D>
-__device__ __forceinline__ int k_place(int key, int piece) {
-  return D == 128 ? key * 128 + ((piece ^ (key & 1) << 2) << 4) : key * 64 + (piece << 4);
+__device__ __forceinline__ int key_of(int n) {  // of a product's key: the step's; D = 128: 0, 4, 1, 5, ... of each eight
+  return D == 128 ? (n & 8) | (n >> 1 & 3) | (n & 1) << 2 : n;
 }
 template <int D>
-__device__ __forceinline__ int v_place(int key, int piece) {
-  return D == 128 ? key * 128 + ((piece ^ (key & 6)) << 4) : (key >> 1) * 128 + ((((key & 1) * 4 + piece) ^ (key & 6)) << 4);
+__device__ __forceinline__ int place(int key, int piece) {
+  return D == 128 ? key * 128 + ((piece ^ (key & 7)) << 4) : key * 64 + ((piece ^ (key >> 1 & 3)) << 4);
 }
+
 template <bool F16, int D>
-__global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g, const RowsQ8 c8) {
+__global__ void __launch_bounds__(THREADS, 1)
+    attention_rows_q8(const RowArgs g, const RowsQ8 c8, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
   constexpr int KC = D / 64, VC = D / 8;               // of a lane: 16-byte pieces of a key of K; columns of a key of V
-  constexpr int PIECES = D / 16, KEYS = 32 / PIECES;   // of a key's row; keys that a warp copies at once
   constexpr int STAGE_BYTES = 2 * STEP * D;            // K and V of a step
   constexpr int STAGES = kStages<D>;
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   // of each warp its first head's piece; its last one's takes the place of its stages when those are done
   float* sums = reinterpret_cast<float*>(smem + WARPS * STAGES * STAGE_BYTES);
   int* first = reinterpret_cast<int*>(sums + WARPS * g.max_rows * D);  // B + 1
@@ -49,9 +54,18 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
   __shared__ int part[32];
   __shared__ Piece pieces[2 * WARPS];
   __shared__ float2 ml[2 * WARPS][MAX_ROWS];
+  __shared__ uint64_t landed[WARPS][STAGES];
   pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5);
+  if (lane == 0) {
+    for (int i = 0; i < STAGES; ++i) mbar_init(&landed[warp][i], 1);
+    fence_mbar_init();
+  }
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&kmap);
+    prefetch_tmap(&vmap);
+  }
   pdl_wait_primary();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST);
 
   // ---- this CTA's run of steps, this warp's share of it: segments of one request and head each ----
@@ -66,8 +80,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
   const int gr = lane >> 2, c4 = lane & 3;
   const uint8_t* ring = smem + warp * STAGES * STAGE_BYTES;
   const uint32_t ring_at = smem_u32(ring);
-  const int piece = lane % PIECES, key0 = lane / PIECES;
-  while (at < stop) {
+  int put = 0, get = 0, flying = 0;  // stages that are filled, and read, next; loads that have not been waited for
+  uint32_t parity = 0;
+  bool dead = false;
+  while (at < stop && !dead) {
     const int b = find(first, g.B, at);
     const Lengths x = lengths_of(g, b);
     const int steps = steps_of(x), head = (at - first[b]) / steps, s0 = at - first[b] - head * steps;
@@ -75,19 +91,45 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
     const int rows = x.n * g.group;
     const int32_t* pages = g.table + b * g.ldt;
     const int n_pages = (x.L + g.page_size - 1) >> g.page_shift;
-    // Lane i holds the page, and the two scales, of step i of 32: of those that are being loaded and the next, of those that
-    // are being computed and the next. A page comes two loads' time, its scales some steps, before what needs it.
+    // Lane i holds the page of step i of 32, and what its scales come to: of those that are being loaded and the next, of those
+    // that are being computed and the next. A page comes 32 steps, its scales some steps, before what needs them.
     auto page_of = [&](int s) {
       const int p = (s * STEP) >> g.page_shift;
-      return s < s1 && p < n_pages ? pages[p] : 0;
+      return s < s1 && p < n_pages ? pages[p] : -1;
     };
     auto scales_of = [&](int s, int id) {
-      if (s >= s1 || id < 0 || id >= g.pages || x.L <= 0) return NO_SCALE << 8 | 127;
+      if (s >= s1 || id < 0 || id >= g.pages) return NO_SCALE << 8 | 127;
       const int64_t from = id * c8.scale_page + ((s * STEP & (g.page_size - 1)) / PIFA_Q8_BLOCK) * c8.scale_block + head * c8.scale_head;
       return (int)c8.ks[from] | (int)c8.vs[from] << 8;
     };
     int known = s0, ids = page_of(s0 + lane), ids_next = page_of(s0 + 32 + lane);
-    int scales = scales_of(s0 + lane, ids), scales_next = 0, scaled = s0;
+    int scales_next = scales_of(s0 + lane, ids);
+    auto load = [&](int s) {
+      if (s == known + 32) {
+        known = s;
+        ids = ids_next;
+        ids_next = page_of(s + 32 + lane);
+        scales_next = scales_of(s + lane, ids);
+      }
+      int id = __shfl_sync(0xffffffffu, ids, s - known);
+      if (id < 0 || id >= g.pages) {
+        if (x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+        id = (int)g.pages;  // outside the tensor map: zeros
+      }
+      if (elect_one()) {
+        const int token = (s * STEP) & (g.page_size - 1);
+        const int y = c8.token_at == 0 ? token : c8.head_at == 0 ? head : id;
+        const int z = c8.token_at == 1 ? token : c8.head_at == 1 ? head : id;
+        const int w = c8.token_at == 2 ? token : c8.head_at == 2 ? head : id;
+        const uint32_t dst = ring_at + put * STAGE_BYTES;
+        mbar_arrive_expect_tx(&landed[warp][put], STAGE_BYTES);
+        tma_load_4d(dst, &kmap, 0, y, z, w, &landed[warp][put]);
+        tma_load_4d(dst + STEP * D, &vmap, 0, y, z, w, &landed[warp][put]);
+      }
+      put = put == STAGES - 1 ? 0 : put + 1;
+      ++flying;
+    };
+    for (int i = 0; i < STAGES - 1 && s0 + i < s1; ++i) load(s0 + i);
     // the rows of Q: this lane's are gr and gr + 8; as fp16, times a power of two that brings bf16's into its range
     uint32_t q[2][KC][8];
     int seen[2];
@@ -95,7 +137,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int row = gr + 8 * r, token = row / g.group;
-      seen[r] = row < rows ? max(x.ahead + token, 0) : 0;
+      seen[r] = row < rows ? max(x.ahead + token, 0) : 0x7fffffff;
       c[r] = g.c;
 #pragma unroll
       for (int i = 0; i < KC; ++i) {
@@ -128,101 +170,84 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
             q[r][i][k] = pack<true>(__uint_as_float(q[r][i][k] << 16) * up, __uint_as_float(q[r][i][k] & 0xffff0000u) * up);
       }
     }
-    auto load = [&](int s, int stage) {  // K, then V, as two groups; nothing past s1
-      if (s < s1) {
-        if (s == known + 32) {
-          known = s;
-          ids = ids_next;
-          ids_next = page_of(s + 32 + lane);
-          scales_next = scales_of(s + lane, ids);
-        }
-        const int id = __shfl_sync(0xffffffffu, ids, s - known);
-        const bool bad = id < 0 || id >= g.pages;
-        if (bad && x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-        // this lane's piece of every KEYS-th key: a warp's copy is whole rows
-        const int64_t from = (bad ? 0 : (int64_t)id) * g.page_stride + head * g.head_stride +
-                             (((s * STEP) & (g.page_size - 1)) + key0) * g.token_stride + piece * 16;
-        const int left = bad ? 0 : x.L - s * STEP - key0;  // keys from this lane's first on
-        const uint32_t dst = ring_at + stage * STAGE_BYTES;
-        const int64_t back = left > 0 ? 0 : key0 * g.token_stride;
-#pragma unroll
-        for (int i = 0; i < STEP / KEYS; ++i) {
-          const bool in = i * KEYS < left;
-          cp_async16(dst + k_place<D>(key0 + i * KEYS, piece), c8.k + from + (in ? i * KEYS * g.token_stride : 0) - back, in ? 16 : 0);
-        }
-        cp_commit();
-#pragma unroll
-        for (int i = 0; i < STEP / KEYS; ++i) {
-          const bool in = i * KEYS < left;
-          cp_async16(dst + STEP * D + v_place<D>(key0 + i * KEYS, piece), c8.v + from + (in ? i * KEYS * g.token_stride : 0) - back,
-                     in ? 16 : 0);
-        }
-      } else {
-        cp_commit();
-      }
-      cp_commit();
-    };
-#pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) load(s0 + i, i);
+    const int all_see = __reduce_min_sync(0xffffffffu, min(seen[0], seen[1]));  // keys before this are seen by every row
     float o[VC][4] = {};
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
     float base = NO_BASE;  // exponent that the values' scales are held against
-    int stage = 0;
+    float key_scales = 0.0f, exponents = 0.0f, inverses = 0.0f;  // of step i of 32
+    int scaled = s0 - 32;
     for (int s = s0; s < s1; ++s) {
       __syncwarp();  // all lanes have read the stage that is filled next
-      load(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
       if (s == scaled + 32) {
         scaled = s;
-        scales = scales_next;
-      }
-      const int two = __shfl_sync(0xffffffffu, scales, s - scaled);
-      const float key_scale = scale_of(two & 0xff);
-      const float up = raise_base(two >> 8 < 255 ? (two >> 8) - 127 : -1000, base);
-      const ValueScale vs = value_scale(two >> 8, base);
-      if (up > 0.0f) {  // the sums so far, in units of the larger exponent
-        const float f = exponent_of_2(-(int)fminf(up, 126.0f));
+        const int now = scales_next >> 8;
+        const float up = raise_base(__reduce_max_sync(0xffffffffu, now < 255 ? now - 127 : -1000), base);
+        const ValueScale v = value_scale(now, base);
+        key_scales = scale_of(scales_next & 0xff);
+        exponents = v.exponent;
+        inverses = v.inverse;
+        if (up > 0.0f) {  // the sums so far, in units of the larger exponent
+          const float f = exponent_of_2(-(int)fminf(up, 126.0f));
 #pragma unroll
-        for (int i = 0; i < VC; ++i)
+          for (int i = 0; i < VC; ++i)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[i][k] *= f;
+            for (int k = 0; k < 4; ++k) o[i][k] *= f;
+        }
       }
-      const uint8_t* buf = ring + stage * STAGE_BYTES;
-      cp_wait<2 * STAGES - 1>();
-      __syncwarp();
+      if (s + STAGES - 1 < s1) load(s + STAGES - 1);
+      const float key_scale = __shfl_sync(0xffffffffu, key_scales, s - scaled);
+      const float exponent = __shfl_sync(0xffffffffu, exponents, s - scaled);
+      const float inverse = __shfl_sync(0xffffffffu, inverses, s - scaled);
+      const uint8_t* buf = ring + get * STAGE_BYTES;
+      if (!__all_sync(0xffffffffu, mbar_wait(&landed[warp][get], parity >> get & 1u, c8.timeout_ns))) {
+        latch_status(g.status, PIFA_ERR_TIMEOUT);
+        dead = true;
+        break;
+      }
+      parity ^= 1u << get;
+      --flying;
       float sc[2][4] = {};
 #pragma unroll
       for (int i = 0; i < KC; ++i)
 #pragma unroll
         for (int nb = 0; nb < 2; ++nb) {
-          const uint4 k = *reinterpret_cast<const uint4*>(buf + k_place<D>(gr + 8 * nb, c4 + 4 * i));
+          const uint4 k = *reinterpret_cast<const uint4*>(buf + place<D>(key_of<D>(gr + 8 * nb), c4 + 4 * i));
           const uint32_t w[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             mma_m16n8k16_f16(sc[nb], q[0][i][2 * j], q[1][i][2 * j], q[0][i][2 * j + 1], q[1][i][2 * j + 1], halves_of(w[j] & 0xffffu),
                              halves_of(w[j] >> 16));
         }
-      // keys that a row does not see; exponents of the weights times their value's scale, relative to m
+      // exponents of the weights times their value's scale, relative to m; keys that a row does not see
       float v[2][4];
       bool grows = false;
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float cr = c[r] * key_scale;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int key = s * STEP + 8 * (k >> 1) + c4 * 2 + (k & 1);
-          v[r][k] = key < seen[r] ? fmaf(sc[k >> 1][2 * r + (k & 1)], cr, vs.exponent) : -INFINITY;
-          grows |= v[r][k] > m[r] + 8.0f;
-        }
+        for (int k = 0; k < 4; ++k) v[r][k] = fmaf(sc[k >> 1][2 * r + (k & 1)], cr, exponent);
+      }
+      if ((s + 1) * STEP > all_see) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (s * STEP + key_of<D>(8 * (k >> 1) + c4 * 2 + (k & 1)) >= seen[r]) v[r][k] = -INFINITY;
+      }
+      float top[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        top[r] = max3(v[r][0], v[r][1], fmaxf(v[r][2], v[r][3]));
+        grows |= top[r] > m[r] + 8.0f;
       }
       if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float top = fmaxf(fmaxf(v[r][0], v[r][1]), fmaxf(v[r][2], v[r][3]));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          top = fmaxf(top, m[r]);
-          const float f = top > m[r] ? fast_exp2(m[r] - top) : 1.0f;  // 0 where nothing was seen before
-          m[r] = top;
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          top[r] = fmaxf(top[r], m[r]);
+          const float f = top[r] > m[r] ? fast_exp2(m[r] - top[r]) : 1.0f;  // 0 where nothing was seen before
+          m[r] = top[r];
           l[r] *= f;
 #pragma unroll
           for (int i = 0; i < VC; ++i) {
@@ -238,24 +263,30 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
         float e[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) e[k] = fast_exp2(v[r][k] - from);
-        l[r] += ((e[0] + e[1]) + (e[2] + e[3])) * vs.inverse;
+        l[r] = fmaf((e[0] + e[1]) + (e[2] + e[3]), inverse, l[r]);
         p[r][0] = pack<true>(e[0], e[1]);
         p[r][1] = pack<true>(e[2], e[3]);
       }
-      cp_wait<2 * STAGES - 2>();
-      __syncwarp();
-      // this lane's columns VC gr to VC gr + VC - 1 of four keys
+      // this lane's columns of four keys: VC from `from` on
+      const int group = D == 128 ? (gr >> 1) | (gr & 1) << 2 : gr;
       uint32_t w[4][VC / 4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int key = c4 * 2 + (k & 1) + 8 * (k >> 1);
+        const int key = key_of<D>(c4 * 2 + (k & 1) + 8 * (k >> 1));
         if constexpr (D == 128) {
-          const uint4 u = *reinterpret_cast<const uint4*>(buf + STEP * D + v_place<D>(key, gr));
+          const uint4 u = *reinterpret_cast<const uint4*>(buf + STEP * D + place<D>(key, group));
           w[k][0] = u.x, w[k][1] = u.y, w[k][2] = u.z, w[k][3] = u.w;
         } else {
-          const uint2 u = *reinterpret_cast<const uint2*>(buf + STEP * D + v_place<D>(key, gr >> 1) + 8 * (gr & 1));
+          const uint2 u = *reinterpret_cast<const uint2*>(buf + STEP * D + place<D>(key, group >> 1) + 8 * (group & 1));
           w[k][0] = u.x, w[k][1] = u.y;
         }
+      }
+      if ((s + 1) * STEP > x.L) {  // rows past the last key may hold anything: 0 times NaN is NaN
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < VC / 4; ++i)
+            if (s * STEP + key_of<D>(c4 * 2 + (k & 1) + 8 * (k >> 1)) >= x.L) w[k][i] = 0u;
       }
 #pragma unroll
       for (int i = 0; i < VC / 4; ++i)
@@ -265,10 +296,17 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
           mma_m16n8k16_f16(o[4 * i + 2 * h], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo & 0xffffu), halves_of(hi & 0xffffu));
           mma_m16n8k16_f16(o[4 * i + 2 * h + 1], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo >> 16), halves_of(hi >> 16));
         }
-      stage = stage == STAGES - 1 ? 0 : stage + 1;
+      get = get == STAGES - 1 ? 0 : get + 1;
     }
-    cp_wait<0>();
-    // o[i][2 r + e]: row gr + 8 r, column VC (2 c4 + e) + i, in units of 2^base
+    if (dead) {  // nothing may land in shared memory after the CTA has left
+      for (; flying > 0; --flying) {
+        mbar_wait(&landed[warp][get], parity >> get & 1u, 100000000ull);
+        parity ^= 1u << get;
+        get = get == STAGES - 1 ? 0 : get + 1;
+      }
+      break;
+    }
+    // o[i][2 r + e]: row gr + 8 r, column VC group(2 c4 + e) + i, in units of 2^base
     const float unit = base > NO_BASE ? exponent_of_2((int)base) : 1.0f;
     const bool alone = s0 == 0 && s1 == steps;
     const int which = 2 * warp + (at + s1 - s0 == stop ? 1 : 0);  // a piece's place: the warp's first, or what it ends with
@@ -283,27 +321,27 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
       l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
       const int row = gr + 8 * r, token = row / g.group;
       if (row >= rows) continue;
-      if (alone) {
-        const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
-        uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + 2 * VC * c4;
+      const float inv = !alone ? 1.0f : l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+      auto value = [&](int i, int e) { return o[i][2 * r + e] * inv * unit; };
+      if (!alone && c4 == 0) ml[which][row] = make_float2(m[r], l[r]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < 2; ++e) {
+        const int n = 2 * c4 + e, col = VC * (D == 128 ? (n >> 1) | (n & 1) << 2 : n);
+        if (alone) {
+          uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + col;
 #pragma unroll
           for (int i = 0; i < VC / 8; ++i) {
             uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              w[k] = pack<F16>(o[8 * i + 2 * k][2 * r + e] * inv * unit, o[8 * i + 2 * k + 1][2 * r + e] * inv * unit);
-            *reinterpret_cast<uint4*>(out + VC * e + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int k = 0; k < 4; ++k) w[k] = pack<F16>(value(8 * i + 2 * k, e), value(8 * i + 2 * k + 1, e));
+            *reinterpret_cast<uint4*>(out + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-      } else {
-        if (c4 == 0) ml[which][row] = make_float2(m[r], l[r]);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
+        } else {
 #pragma unroll
           for (int i = 0; i < VC / 4; ++i)
-            *reinterpret_cast<float4*>(sum + row * D + VC * (2 * c4 + e) + 4 * i) =
-                make_float4(o[4 * i][2 * r + e] * unit, o[4 * i + 1][2 * r + e] * unit, o[4 * i + 2][2 * r + e] * unit, o[4 * i + 3][2 * r + e] * unit);
+            *reinterpret_cast<float4*>(sum + row * D + col + 4 * i) =
+                make_float4(value(4 * i, e), value(4 * i + 1, e), value(4 * i + 2, e), value(4 * i + 3, e));
+        }
       }
     }
     at += s1 - s0;
@@ -358,18 +396,24 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
 }
 
 template <bool F16, int D>
-cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
-  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4), stream, c8);
+cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, const CUtensorMap& kmap, const CUtensorMap& vmap, cudaStream_t stream) {
+  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, 1024 + (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4),
+                                                                 stream, c8, kmap, vmap);
 }
 
 }  // namespace
 
-int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream) {
+int launch_attention_rows_q8(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream) {
   const RowArgs g = row_args(a, status);
-  const RowsQ8 c8 = {static_cast<const uint8_t*>(a.k), static_cast<const uint8_t*>(a.v), a.q8->k, a.q8->v, a.q8->shape.page_stride,
-                     a.q8->shape.block_stride, a.q8->shape.head_stride};
+  CUtensorMap kmap, vmap;
+  int order[3], st;
+  if ((st = make_tmap_cache_q8(&kmap, a.k, a.cache, STEP, true, order)) != PIFA_OK) return st;
+  if ((st = make_tmap_cache_q8(&vmap, a.v, a.cache, STEP, true, order)) != PIFA_OK) return st;
+  const RowsQ8 c8 = {a.q8->k, a.q8->v, a.q8->shape.page_stride, a.q8->shape.block_stride, a.q8->shape.head_stride, order[0], order[1],
+                     timeout_ns};
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
-  const cudaError_t e = a.cache.dim == 64 ? (f16 ? launch_rows_q8<true, 64>(g, c8, stream) : launch_rows_q8<false, 64>(g, c8, stream))
-                                          : (f16 ? launch_rows_q8<true, 128>(g, c8, stream) : launch_rows_q8<false, 128>(g, c8, stream));
+  cudaError_t e;
+  if (a.cache.dim == 64) e = f16 ? launch_rows_q8<true, 64>(g, c8, kmap, vmap, stream) : launch_rows_q8<false, 64>(g, c8, kmap, vmap, stream);
+  else e = f16 ? launch_rows_q8<true, 128>(g, c8, kmap, vmap, stream) : launch_rows_q8<false, 128>(g, c8, kmap, vmap, stream);
   return e == cudaSuccess ? PIFA_OK : pifa_fail_cuda("attention_rows_q8 launch", e);
 }

@@ -42,6 +42,7 @@
 // Q by TMA 1.22. Cut items cost six tiles' time: 200 tokens over 8000 took 67 us with
 // a cut that left a second round, 45 with one round, 39 since all warps add up the pieces.
 #include <cmath>
+#include <utility>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -1372,8 +1373,10 @@ int launch_attention_tc(const PifaAttention& given, bool wide, int* status, uint
   if ((st = make_tmap_heads(&qmap, a.dtype, a.q, a.T, a.q_heads, a.cache.dim, a.ldq, (uint32_t)group, (uint32_t)g.tpt)) != PIFA_OK)
     return st;
   const bool q8 = a.q8 != nullptr;
-  if ((st = make_tmap_cache(&kmap, a.dtype, q8, a.k, a.cache, rows, order)) != PIFA_OK) return st;
-  if ((st = make_tmap_cache(&vmap, a.dtype, q8, a.v, a.cache, rows, order)) != PIFA_OK) return st;
+  for (const auto& x : {std::make_pair(&kmap, a.k), std::make_pair(&vmap, a.v)}) {
+    st = q8 ? make_tmap_cache_q8(x.first, x.second, a.cache, rows, false, order) : make_tmap_cache(x.first, a.dtype, x.second, a.cache, rows, order);
+    if (st != PIFA_OK) return st;
+  }
   g.token_at = order[0];
   g.head_at = order[1];
   const int grid = pifa_sm_count();
