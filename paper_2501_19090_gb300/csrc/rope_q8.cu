@@ -27,7 +27,7 @@ struct StoreArgs {
   int64_t scale_page, scale_block, scale_head;
   int page_size, hk;
   int window, kv_heads, kv_parts, kv_ctas;  // rows and heads (of 2 hk) of a CTA that stores; CTAs of a window; all of them
-  int q_parts;
+  int q_parts, stride;  // every stride-th CTA stores, as long as there are such
 };
 
 struct ReadArgs {
@@ -63,9 +63,9 @@ __device__ __forceinline__ float inverse_scale_of(int byte) {
   return byte < 254 ? __uint_as_float((uint32_t)(254 - byte) << 23) : byte == 254 ? __uint_as_float(0x00400000u) : 0.0f;
 }
 
-// Keys and values of the stretches that begin in a window of rows. GW warps take a stretch of one head: up to 16 rows, four
+// Keys and values of the stretches that begin in a window of rows. GW warps take a stretch of one head: up to 16 rows, EACH
 // units of 16 elements a lane (a unit: two vectors of 8, as in rope_tokens).
-template <bool F16, bool HALF, int GW>
+template <bool F16, bool HALF, int EACH, int GW>
 __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int part) {
   extern __shared__ __align__(16) float2 turns[];  // of a row: as rope_tokens lays them out
   __shared__ int64_t slot_of[MAX_WINDOW + BLOCK];  // from the row before the window on
@@ -76,7 +76,18 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
   const int t0 = wx * g.window, rows = min(g.window + BLOCK - 1, T - t0), inside = min(g.window, T - t0);
   const int pairs = g.q.rot / 2, units = dim / 16, turned = g.q.rot / 16;
   const int h0 = part * g.kv_heads, nh = min(g.kv_heads, 2 * g.hk - h0);
+  // cosines and sines of rows [from, to)
+  auto turn_rows = [&](int from, int to) {
+    for (int i = from * pairs + tid; i < to * pairs; i += THREADS) {
+      const int tt = i / pairs, p = i - tt * pairs;
+      const uint64_t phase = (uint64_t)(int64_t)g.q.positions[t0 + tt] * (uint64_t)g.q.freq[p];
+      float s, c;
+      sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);
+      turns[tt * pairs + 2 * ((p & 7) / 2 * turned + p / 8) + (p & 1)] = make_float2(c * g.q.scale, s * g.q.scale);
+    }
+  };
   for (int i = tid; i <= rows; i += THREADS) slot_of[i] = t0 + i > 0 ? g.slots[t0 + i - 1] : -1;
+  if (h0 < g.hk) turn_rows(0, inside);  // a stretch that goes on behind the window: later, when that is known
   __syncthreads();
   if (tid < 32) {
     auto good = [&](int64_t s) { return s >= 0 && s < g.n_slots; };
@@ -113,14 +124,8 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
     }
   }
   __syncthreads();
-  if (h0 < g.hk) {
-    for (int i = tid; i < last * pairs; i += THREADS) {
-      const int tt = i / pairs, p = i - tt * pairs;
-      const uint64_t phase = (uint64_t)(int64_t)g.q.positions[t0 + tt] * (uint64_t)g.q.freq[p];
-      float s, c;
-      sincospif((float)(int32_t)(phase >> 32) * 0x1p-31f, &s, &c);
-      turns[tt * pairs + 2 * ((p & 7) / 2 * turned + p / 8) + (p & 1)] = make_float2(c * g.q.scale, s * g.q.scale);
-    }
+  if (h0 < g.hk && last > inside) {
+    turn_rows(inside, last);
     __syncthreads();
   }
 
@@ -137,7 +142,7 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
     uint8_t* scale = (is_k ? g.ks : g.vs) + x.scale + (int64_t)head * g.scale_head;
     const bool held = !(x.written & 1u);  // tokens before these: a block begins anew with its first one
     const int was = held ? *scale : 0;
-    float e[4][16];
+    float e[EACH][16];
     float most = 0.0f;
     const int n = x.n * units;
     auto places = [&](int u, int& a0, int& a1) {
@@ -146,7 +151,7 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
       a1 = apart ? u * 8 + pairs : u * 16 + 8;
     };
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < EACH; ++k) {
       const int i = l + k * GW * 32, r = i / units, u = i - r * units;
       if (i >= n) continue;
       int a0, a1;
@@ -197,7 +202,7 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
     if (top >= 0x7f800000u) {  // what is not finite is stored as NaN and leaves the scale to the others
       most = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < EACH; ++k)
 #pragma unroll
         for (int j = 0; j < 16; ++j)
           if (l + k * GW * 32 < n) {
@@ -211,7 +216,7 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
     const int byte = max(fresh, was);
     const float inv = inverse_scale_of(byte);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < EACH; ++k) {
       const int i = l + k * GW * 32, r = i / units, u = i - r * units;
       if (i >= n) continue;
       int a0, a1;
@@ -245,13 +250,18 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
   }
 }
 
-template <bool F16, bool HALF, int GW>
-__global__ void __launch_bounds__(THREADS, 2) rope_cache_q8(const StoreArgs g) {
+template <bool F16, bool HALF, int EACH, int GW>
+__global__ void __launch_bounds__(THREADS, EACH == 2 ? 4 : 2) rope_cache_q8(const StoreArgs g) {
   pdl_launch_dependents();
   pdl_wait_primary();
-  const int b = (int)blockIdx.x - g.kv_ctas;
-  if (b < 0) store_blocks<F16, HALF, GW>(g, (int)blockIdx.x / g.kv_parts, (int)blockIdx.x % g.kv_parts);
-  else rope_tokens<F16, HALF>(g.q, b / g.q_parts, b % g.q_parts);
+  // CTAs that store keys and values take longer and come first, of many tokens in turn with those that turn queries
+  const int b = (int)blockIdx.x, at = b / g.stride;
+  if (b == at * g.stride && at < g.kv_ctas) {
+    store_blocks<F16, HALF, EACH, GW>(g, at / g.kv_parts, at % g.kv_parts);
+  } else {
+    const int q = b - min((b + g.stride - 1) / g.stride, g.kv_ctas);
+    rope_tokens<F16, HALF>(g.q, q / g.q_parts, q % g.q_parts);
+  }
 }
 
 // A thread takes 16 elements at a time: 16 bytes in, 32 out.
@@ -292,11 +302,20 @@ __global__ void __launch_bounds__(THREADS) cache_read_q8(const ReadArgs g) {
   }
 }
 
+// Few tokens make short stretches: a warp for each (four units a lane) spares the exchange between two. Many make whole blocks: two
+// units a lane leave the registers, and with them the loads in flight, to twice the CTAs. (8192 tokens, 64 + 8 + 8 heads: 83 us with
+// four units, 61 with two; 200 sequences in decode: 5.8 and 7.0.)
+constexpr int FEW_TOKENS = 1024;
+template <bool F16, bool HALF, int EACH>
+cudaError_t launch_store(const cudaLaunchConfig_t* cfg, const StoreArgs& g) {
+  if (g.q.dim <= 32 * EACH) return pifa_launch_ex(cfg, rope_cache_q8<F16, HALF, EACH, 1>, g);
+  if (g.q.dim <= 64 * EACH) return pifa_launch_ex(cfg, rope_cache_q8<F16, HALF, EACH, 2>, g);
+  if (EACH == 4 || g.q.dim <= 128 * EACH) return pifa_launch_ex(cfg, rope_cache_q8<F16, HALF, EACH, 4>, g);
+  return pifa_launch_ex(cfg, rope_cache_q8<F16, HALF, EACH, EACH == 4 ? 4 : 8>, g);
+}
 template <bool F16, bool HALF>
 cudaError_t launch_store(const cudaLaunchConfig_t* cfg, const StoreArgs& g) {
-  return g.q.dim <= 128   ? pifa_launch_ex(cfg, rope_cache_q8<F16, HALF, 1>, g)
-         : g.q.dim <= 256 ? pifa_launch_ex(cfg, rope_cache_q8<F16, HALF, 2>, g)
-                          : pifa_launch_ex(cfg, rope_cache_q8<F16, HALF, 4>, g);
+  return g.q.T < FEW_TOKENS ? launch_store<F16, HALF, 4>(cfg, g) : launch_store<F16, HALF, 2>(cfg, g);
 }
 
 void overlap_launches(cudaLaunchConfig_t& cfg, cudaLaunchAttribute& attr, void* cuda_stream) {
@@ -399,6 +418,7 @@ int pifa_rope_cache_q8(const void* Q, int64_t ldq, const void* K, int64_t ldk, c
   overlap_launches(cfg, attr, cuda_stream);
   const int64_t ctas = (int64_t)windows * g.kv_parts + (int64_t)((t + g.q.tokens - 1) / g.q.tokens) * g.q_parts;
   if (ctas > 0x7fffffff) return pifa_fail(PIFA_ERR_UNSUPPORTED, "too many tokens times heads");
+  g.stride = t >= FEW_TOKENS && ctas >= 2 * (int64_t)g.kv_ctas ? 2 : 1;
   cfg.gridDim = dim3((unsigned)ctas);
   cfg.dynamicSmemBytes = (size_t)(g.window + BLOCK - 1) * (size_t)rot_dim * 4;
   const bool f16 = dtype == PIFA_DTYPE_FP16, half = layout == PIFA_ROPE_HALF;
