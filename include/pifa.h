@@ -565,7 +565,7 @@ int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_hea
                             void* O, int64_t ldo, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
 /* pifa_paged_attention_q8_workspace_size -- bytes of device scratch with which pifa_paged_attention_q8 is fastest:
- * pifa_paged_attention_workspace_size() is enough, more is room for the keys and values of long chunks in 16 bits (group max_q > 512
+ * pifa_paged_attention_workspace_size() is enough, more is room for the keys and values of long chunks in 16 bits (group max_q > 768
  * rows, and at most 1 GB for B requests of cols * page_size tokens). Negative pifa_status on bad arguments. Pure host arithmetic. */
 int64_t pifa_paged_attention_q8_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
                                                int64_t max_q, int64_t cols, int64_t page_size);

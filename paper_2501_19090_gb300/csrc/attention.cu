@@ -51,8 +51,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   extern __shared__ __align__(16) uint8_t smem[];
   int* first = reinterpret_cast<int*>(smem + WARPS * STAGES * STAGE_BYTES);  // B + 1
   __shared__ int part[32];
-  pdl_launch_dependents();
   pdl_wait_primary();
+  pdl_launch_dependents();  // (after the wait: the join reads the lengths before its own)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Run steps_here = deal_steps(g, first, part, (int)gridDim.x * WARPS, MIN_STEPS);
   const int total = steps_here.total, run = steps_here.run;
@@ -265,7 +265,7 @@ int check_sizes(int64_t T, int64_t hq, int64_t hk, int64_t dim, int64_t B, int64
 
 // Whether a cache in 8 bits is brought to 16 before a call on the tensor cores, given the room: where a head's rows may make several
 // items, and the room, for the most keys that the tables can hold, is at most a gigabyte.
-constexpr int64_t WIDE_ROWS_FROM = 512, WIDE_BYTES = (int64_t)1 << 30;
+constexpr int64_t WIDE_ROWS_FROM = 768, WIDE_BYTES = (int64_t)1 << 30;
 bool widens(int64_t group, int64_t kv_heads, int64_t dim, int64_t B, int64_t max_q, int64_t keys) {
   return keys > 0 && group * max_q > WIDE_ROWS_FROM && attention_wide_bytes(kv_heads, dim, B, keys) <= WIDE_BYTES;
 }

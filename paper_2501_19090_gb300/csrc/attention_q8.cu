@@ -55,7 +55,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   __shared__ Piece pieces[2 * WARPS];
   __shared__ float2 ml[2 * WARPS][MAX_ROWS];
   __shared__ uint64_t landed[WARPS][STAGES];
-  pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5);
   if (lane == 0) {
     for (int i = 0; i < STAGES; ++i) mbar_init(&landed[warp][i], 1);
@@ -66,6 +65,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     prefetch_tmap(&vmap);
   }
   pdl_wait_primary();
+  pdl_launch_dependents();  // (after the wait: the join reads the lengths before its own)
   const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST);
 
   // ---- this CTA's run of steps, this warp's share of it: segments of one request and head each ----

@@ -153,8 +153,8 @@ __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int s
   const int item = (int)blockIdx.x / split, b = item / g.heads, head = item - b * g.heads;
   const int quads = D / 4 / split, col0 = ((int)blockIdx.x - item * split) * quads * 4;  // of this CTA: fours of columns, first one
   const int slots = g.max_rows * quads, groups = min(max(THREADS / slots, 1), 16);
+  const Lengths x = lengths_of(g, b);  // (before the wait: the kernel before lets this one begin when it has waited itself)
   pdl_wait_primary();
-  const Lengths x = lengths_of(g, b);
   const int run = g.sums[g.B + 1], steps = steps_of(x), from = g.sums[b] + head * steps;
   if (steps == 0 || run == 0) return;
   const int w0 = from / run, w1 = (from + steps - 1) / run;

@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) attention_plan(const TcArgs g
 // it once, beside the plan, into pages of the workspace (of a key tile; of heads of tokens; request b's are b wide_cols and the
 // following), and attention reads those. Rounded to dtype: exact in bf16 from 2^-117 on; in fp16 a finite value stays one.
 constexpr int WIDE_PAGE = BN;
-constexpr int WIDE_ROWS = 64;  // tokens times heads that a CTA takes at a time: of a block of tokens, 4 heads
+constexpr int WIDE_HEADS = 8;  // a CTA takes a block of 16 tokens of so many heads, K's and V's counted, at a time
 
 struct WideArgs {
   const uint8_t *k, *v;
@@ -368,11 +368,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan_widen(const TcArg
   if (tid == 0) first[g.B] = blocks;
   __syncthreads();
   constexpr int PIECES = D / 16;                                // of a row: 16 bytes in, 32 out
-  constexpr int EACH = WIDE_ROWS * PIECES / PLAN_THREADS;       // of a thread
-  const int parts = (2 * g.heads + 3) / 4;                      // four heads of K's and V's
+  constexpr int EACH = WIDE_HEADS * PIFA_Q8_BLOCK * PIECES / PLAN_THREADS;  // of a thread
+  const int parts = (2 * g.heads + WIDE_HEADS - 1) / WIDE_HEADS;
   const int64_t units = (int64_t)blocks * parts;
   for (int64_t unit = blockIdx.x - 1; unit < units; unit += gridDim.x - 1) {
-    const int block = (int)(unit / parts), h0 = (int)(unit - (int64_t)block * parts) * 4;
+    const int block = (int)(unit / parts), h0 = (int)(unit - (int64_t)block * parts) * WIDE_HEADS;
     int lo = 0, hi = g.B;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -1280,7 +1280,7 @@ cudaError_t launch_plan(const cudaLaunchConfig_t& cfg, const A&... args) {
 }
 template <int D>
 cudaError_t launch_widen(bool f16, cudaLaunchConfig_t cfg, const TcArgs& g, const WideArgs& x, int grid) {
-  cfg.gridDim = dim3((unsigned)(1 + 4 * grid));  // the plan, and four CTAs for each SM
+  cfg.gridDim = dim3((unsigned)(1 + 8 * grid));  // the plan, and eight CTAs for each SM
   return f16 ? launch_plan<attention_plan_widen<true, D>>(cfg, g, x, grid) : launch_plan<attention_plan_widen<false, D>>(cfg, g, x, grid);
 }
 

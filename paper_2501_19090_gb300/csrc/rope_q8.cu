@@ -15,6 +15,7 @@ namespace {
 constexpr int THREADS = ROPE_THREADS;
 constexpr int BLOCK = PIFA_Q8_BLOCK;
 constexpr int MAX_WINDOW = 16;             // rows of a CTA that stores keys and values
+constexpr int READ_WINDOW = 8;             // most rows of a CTA that reads (50001 tokens, 8 heads: 50 us, with 16 rows 52)
 constexpr int TURN_BYTES = 38 * 1024;      // of cosines and sines: with the rest, what a CTA has without asking for more
 
 struct StoreArgs {
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(THREADS, EACH == 2 ? 4 : 2) rope_cache_q8(cons
 // A thread takes 16 elements at a time: 16 bytes in, 32 out.
 template <bool F16>
 __global__ void __launch_bounds__(THREADS) cache_read_q8(const ReadArgs g) {
-  __shared__ int64_t at[MAX_WINDOW], scale_at[MAX_WINDOW];  // -1: the row is not written
+  __shared__ int64_t at[READ_WINDOW], scale_at[READ_WINDOW];  // -1: the row is not written
   pdl_launch_dependents();
   pdl_wait_primary();
   const int t0 = (int)blockIdx.x * g.tokens, nt = min(g.tokens, g.T - t0);
@@ -478,7 +479,7 @@ int pifa_cache_read_q8(const void* k_cache, const void* v_cache, const void* k_s
   g.hk = (int)kv_heads;
   g.dim = (int)head_dim;
   const int round = 8 * pifa_sm_count();
-  g.tokens = (int)T >= round * MAX_WINDOW ? MAX_WINDOW : ((int)T + round - 1) / round;
+  g.tokens = (int)T >= round * READ_WINDOW ? READ_WINDOW : ((int)T + round - 1) / round;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr;
   overlap_launches(cfg, attr, cuda_stream);
