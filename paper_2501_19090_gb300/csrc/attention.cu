@@ -328,7 +328,7 @@ int attend(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_he
   const PifaAttention a = {Q, k_cache, v_cache, O, table, q_start, kv_len, T, ldq, ldo, ldt, cols, B, max_q, q_heads, c, dtype,
                            scale * 1.4426950408889634f, static_cast<uint8_t*>(workspace) + kWorkspaceReserve, q8};
   if (tc) return launch_attention_tc(a, wide, status, pifa_wait_timeout_ns(), reinterpret_cast<cudaStream_t>(cuda_stream));
-  if (q8) return launch_attention_rows_q8(a, status, pifa_wait_timeout_ns(), reinterpret_cast<cudaStream_t>(cuda_stream));
+  if (q8) return launch_attention_rows_q8(a, status, reinterpret_cast<cudaStream_t>(cuda_stream));
   RowArgs g = row_args(a, status);
   g.k = static_cast<const uint16_t*>(k_cache);
   g.v = static_cast<const uint16_t*>(v_cache);

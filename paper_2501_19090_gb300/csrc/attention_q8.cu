@@ -12,10 +12,8 @@
 namespace {
 
 struct RowsQ8 {
-  const uint8_t *ks, *vs;
+  const uint8_t *k, *v, *ks, *vs;
   int64_t scale_page, scale_block, scale_head;
-  int token_at, head_at;  // their places among the tensor maps' coordinates 1 to 3; the page has the third
-  uint64_t timeout_ns;
 };
 
 template <int D>
@@ -27,9 +25,9 @@ struct Piece {
   int item, b, from, steps;  // (first step of the head) -1: none
 };
 
-// TMA leaves the 16-byte pieces of a key's row swizzled (its index xor the row's, in the 128 bytes that eight, or with D = 64 two
-// rows of 64, lie in). Which of a product's 16 keys is which of the step's, and which of its columns are a lane's, is free: chosen so
-// that the eight lanes that read together meet eight bank groups.
+// The 16-byte pieces of a key's row lie swizzled (its index xor the row's, in the 128 bytes that eight, or with D = 64 two rows of 64,
+// lie in). Which of a product's 16 keys is which of the step's, and which of its columns are a lane's, is free: chosen so that the
+// eight lanes that read together meet eight bank groups.
 template <int D>
 __device__ __forceinline__ int key_of(int n) {  // of a product's key: the step's; D = 128: 0, 4, 1, 5, ... of each eight
   return D == 128 ? (n & 8) | (n >> 1 & 3) | (n & 1) << 2 : n;
@@ -41,12 +39,12 @@ __device__ __forceinline__ int place(int key, int piece) {
 
 template <bool F16, int D>
 __global__ void __launch_bounds__(THREADS, 1)
-    attention_rows_q8(const RowArgs g, const RowsQ8 c8, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+    attention_rows_q8(const RowArgs g, const RowsQ8 c8) {
   constexpr int KC = D / 64, VC = D / 8;               // of a lane: 16-byte pieces of a key of K; columns of a key of V
+  constexpr int PIECES = D / 16, KEYS = 32 / PIECES;   // of a key's row; keys that a warp copies at once
   constexpr int STAGE_BYTES = 2 * STEP * D;            // K and V of a step
   constexpr int STAGES = kStages<D>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  extern __shared__ __align__(128) uint8_t smem[];
   // of each warp its first head's piece; its last one's takes the place of its stages when those are done
   float* sums = reinterpret_cast<float*>(smem + WARPS * STAGES * STAGE_BYTES);
   int* first = reinterpret_cast<int*>(sums + WARPS * g.max_rows * D);  // B + 1
@@ -54,16 +52,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   __shared__ int part[32];
   __shared__ Piece pieces[2 * WARPS];
   __shared__ float2 ml[2 * WARPS][MAX_ROWS];
-  __shared__ uint64_t landed[WARPS][STAGES];
   const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5);
-  if (lane == 0) {
-    for (int i = 0; i < STAGES; ++i) mbar_init(&landed[warp][i], 1);
-    fence_mbar_init();
-  }
-  if (threadIdx.x == 0) {
-    prefetch_tmap(&kmap);
-    prefetch_tmap(&vmap);
-  }
   pdl_wait_primary();
   pdl_launch_dependents();  // (after the wait: the join reads the lengths before its own)
   const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST);
@@ -80,10 +69,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int gr = lane >> 2, c4 = lane & 3;
   const uint8_t* ring = smem + warp * STAGES * STAGE_BYTES;
   const uint32_t ring_at = smem_u32(ring);
-  int put = 0, get = 0, flying = 0;  // stages that are filled, and read, next; loads that have not been waited for
-  uint32_t parity = 0;
-  bool dead = false;
-  while (at < stop && !dead) {
+  const int piece = lane % PIECES, key0 = lane / PIECES;
+  while (at < stop) {
     const int b = find(first, g.B, at);
     const Lengths x = lengths_of(g, b);
     const int steps = steps_of(x), head = (at - first[b]) / steps, s0 = at - first[b] - head * steps;
@@ -104,32 +91,44 @@ __global__ void __launch_bounds__(THREADS, 1)
     };
     int known = s0, ids = page_of(s0 + lane), ids_next = page_of(s0 + 32 + lane);
     int scales_next = scales_of(s0 + lane, ids);
-    auto load = [&](int s) {
+    auto load = [&](int s, int stage) {
       if (s == known + 32) {
         known = s;
         ids = ids_next;
         ids_next = page_of(s + 32 + lane);
         scales_next = scales_of(s + lane, ids);
       }
-      int id = __shfl_sync(0xffffffffu, ids, s - known);
-      if (id < 0 || id >= g.pages) {
-        if (x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-        id = (int)g.pages;  // outside the tensor map: zeros
+      const int id = __shfl_sync(0xffffffffu, ids, s - known);
+      const bool bad = id < 0 || id >= g.pages;
+      if (bad && x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+      // this lane's piece of every KEYS-th key: a warp's copy is whole rows
+      const int64_t step = KEYS * g.token_stride;
+      int64_t from = (bad ? 0 : (int64_t)id) * g.page_stride + head * g.head_stride + ((s * STEP) & (g.page_size - 1)) * g.token_stride +
+                     key0 * g.token_stride + piece * 16;
+      const uint32_t dst = ring_at + stage * STAGE_BYTES;
+      if (bad || (s + 1) * STEP > x.L) {  // keys past the last one: zeros, that nothing is read for
+        const int left = bad ? 0 : x.L - s * STEP;
+#pragma unroll
+        for (int i = 0; i < STEP / KEYS; ++i) {
+          const int key = key0 + i * KEYS;
+          const bool in = key < left;
+          cp_async16(dst + place<D>(key, piece), in ? c8.k + from + i * step : c8.k, in ? 16 : 0);
+          cp_async16(dst + STEP * D + place<D>(key, piece), in ? c8.v + from + i * step : c8.v, in ? 16 : 0);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < STEP / KEYS; ++i, from += step) {
+          const int at = place<D>(key0 + i * KEYS, piece);
+          cp_async16(dst + at, c8.k + from, 16);
+          cp_async16(dst + STEP * D + at, c8.v + from, 16);
+        }
       }
-      if (elect_one()) {
-        const int token = (s * STEP) & (g.page_size - 1);
-        const int y = c8.token_at == 0 ? token : c8.head_at == 0 ? head : id;
-        const int z = c8.token_at == 1 ? token : c8.head_at == 1 ? head : id;
-        const int w = c8.token_at == 2 ? token : c8.head_at == 2 ? head : id;
-        const uint32_t dst = ring_at + put * STAGE_BYTES;
-        mbar_arrive_expect_tx(&landed[warp][put], STAGE_BYTES);
-        tma_load_4d(dst, &kmap, 0, y, z, w, &landed[warp][put]);
-        tma_load_4d(dst + STEP * D, &vmap, 0, y, z, w, &landed[warp][put]);
-      }
-      put = put == STAGES - 1 ? 0 : put + 1;
-      ++flying;
     };
-    for (int i = 0; i < STAGES - 1 && s0 + i < s1; ++i) load(s0 + i);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) {
+      if (s0 + i < s1) load(s0 + i, i);
+      cp_commit();
+    }
     // the rows of Q: this lane's are gr and gr + 8; as fp16, times a power of two that brings bf16's into its range
     uint32_t q[2][KC][8];
     int seen[2];
@@ -175,7 +174,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
     float base = NO_BASE;  // exponent that the values' scales are held against
     float key_scales = 0.0f, exponents = 0.0f, inverses = 0.0f;  // of step i of 32
-    int scaled = s0 - 32;
+    int scaled = s0 - 32, stage = 0;
     for (int s = s0; s < s1; ++s) {
       __syncwarp();  // all lanes have read the stage that is filled next
       if (s == scaled + 32) {
@@ -194,18 +193,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int k = 0; k < 4; ++k) o[i][k] *= f;
         }
       }
-      if (s + STAGES - 1 < s1) load(s + STAGES - 1);
+      if (s + STAGES - 1 < s1) load(s + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+      cp_commit();
       const float key_scale = __shfl_sync(0xffffffffu, key_scales, s - scaled);
       const float exponent = __shfl_sync(0xffffffffu, exponents, s - scaled);
       const float inverse = __shfl_sync(0xffffffffu, inverses, s - scaled);
-      const uint8_t* buf = ring + get * STAGE_BYTES;
-      if (!__all_sync(0xffffffffu, mbar_wait(&landed[warp][get], parity >> get & 1u, c8.timeout_ns))) {
-        latch_status(g.status, PIFA_ERR_TIMEOUT);
-        dead = true;
-        break;
-      }
-      parity ^= 1u << get;
-      --flying;
+      const uint8_t* buf = ring + stage * STAGE_BYTES;
+      cp_wait<STAGES - 1>();
+      __syncwarp();
       float sc[2][4] = {};
 #pragma unroll
       for (int i = 0; i < KC; ++i)
@@ -281,13 +276,6 @@ __global__ void __launch_bounds__(THREADS, 1)
           w[k][0] = u.x, w[k][1] = u.y;
         }
       }
-      if ((s + 1) * STEP > x.L) {  // rows past the last key may hold anything: 0 times NaN is NaN
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int i = 0; i < VC / 4; ++i)
-            if (s * STEP + key_of<D>(c4 * 2 + (k & 1) + 8 * (k >> 1)) >= x.L) w[k][i] = 0u;
-      }
 #pragma unroll
       for (int i = 0; i < VC / 4; ++i)
 #pragma unroll
@@ -296,16 +284,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           mma_m16n8k16_f16(o[4 * i + 2 * h], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo & 0xffffu), halves_of(hi & 0xffffu));
           mma_m16n8k16_f16(o[4 * i + 2 * h + 1], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo >> 16), halves_of(hi >> 16));
         }
-      get = get == STAGES - 1 ? 0 : get + 1;
+      stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
-    if (dead) {  // nothing may land in shared memory after the CTA has left
-      for (; flying > 0; --flying) {
-        mbar_wait(&landed[warp][get], parity >> get & 1u, 100000000ull);
-        parity ^= 1u << get;
-        get = get == STAGES - 1 ? 0 : get + 1;
-      }
-      break;
-    }
+    cp_wait<0>();
     // o[i][2 r + e]: row gr + 8 r, column VC group(2 c4 + e) + i, in units of 2^base
     const float unit = base > NO_BASE ? exponent_of_2((int)base) : 1.0f;
     const bool alone = s0 == 0 && s1 == steps;
@@ -396,24 +377,19 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 template <bool F16, int D>
-cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, const CUtensorMap& kmap, const CUtensorMap& vmap, cudaStream_t stream) {
-  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, 1024 + (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4),
-                                                                 stream, c8, kmap, vmap);
+cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
+  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4), stream, c8);
 }
 
 }  // namespace
 
-int launch_attention_rows_q8(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream) {
+int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream) {
   const RowArgs g = row_args(a, status);
-  CUtensorMap kmap, vmap;
-  int order[3], st;
-  if ((st = make_tmap_cache_q8(&kmap, a.k, a.cache, STEP, true, order)) != PIFA_OK) return st;
-  if ((st = make_tmap_cache_q8(&vmap, a.v, a.cache, STEP, true, order)) != PIFA_OK) return st;
-  const RowsQ8 c8 = {a.q8->k, a.q8->v, a.q8->shape.page_stride, a.q8->shape.block_stride, a.q8->shape.head_stride, order[0], order[1],
-                     timeout_ns};
+  const RowsQ8 c8 = {static_cast<const uint8_t*>(a.k), static_cast<const uint8_t*>(a.v), a.q8->k, a.q8->v, a.q8->shape.page_stride,
+                     a.q8->shape.block_stride, a.q8->shape.head_stride};
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
   cudaError_t e;
-  if (a.cache.dim == 64) e = f16 ? launch_rows_q8<true, 64>(g, c8, kmap, vmap, stream) : launch_rows_q8<false, 64>(g, c8, kmap, vmap, stream);
-  else e = f16 ? launch_rows_q8<true, 128>(g, c8, kmap, vmap, stream) : launch_rows_q8<false, 128>(g, c8, kmap, vmap, stream);
+  if (a.cache.dim == 64) e = f16 ? launch_rows_q8<true, 64>(g, c8, stream) : launch_rows_q8<false, 64>(g, c8, stream);
+  else e = f16 ? launch_rows_q8<true, 128>(g, c8, stream) : launch_rows_q8<false, 128>(g, c8, stream);
   return e == cudaSuccess ? PIFA_OK : pifa_fail_cuda("attention_rows_q8 launch", e);
 }

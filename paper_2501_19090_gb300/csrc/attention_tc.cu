@@ -1374,7 +1374,7 @@ int launch_attention_tc(const PifaAttention& given, bool wide, int* status, uint
     return st;
   const bool q8 = a.q8 != nullptr;
   for (const auto& x : {std::make_pair(&kmap, a.k), std::make_pair(&vmap, a.v)}) {
-    st = q8 ? make_tmap_cache_q8(x.first, x.second, a.cache, rows, false, order) : make_tmap_cache(x.first, a.dtype, x.second, a.cache, rows, order);
+    st = q8 ? make_tmap_cache_q8(x.first, x.second, a.cache, rows, order) : make_tmap_cache(x.first, a.dtype, x.second, a.cache, rows, order);
     if (st != PIFA_OK) return st;
   }
   g.token_at = order[0];

@@ -140,7 +140,7 @@ struct PifaAttention {
   const PifaScales* q8;  // null: elements of dtype
 };
 // Few rows over a cache in 8 bits.
-int launch_attention_rows_q8(const PifaAttention& a, int* status, uint64_t timeout_ns, cudaStream_t stream);
+int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream);
 // Chunks of new tokens on the tensor cores.
 int64_t attention_tc_workspace_bytes(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t B);
 // `wide`: a cache in 8 bits is brought to 16 first, in attention_wide_bytes() of workspace behind the rest (keys: that a request's
@@ -266,7 +266,7 @@ int make_tmap_heads(CUtensorMap* map, int dtype, const void* base, int64_t T, in
 // rising stride; box of 64 elements x `rows` tokens, 128-byte swizzle, zero fill outside. order[0..2]: which of
 // the map's coordinates 1 to 3 the token, the head and the page are.
 int make_tmap_cache(CUtensorMap* map, int dtype, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]);
-// The same over elements of one byte: box of a head's elements (64 or 128) x `rows` tokens, swizzled over that many bytes or not.
-int make_tmap_cache_q8(CUtensorMap* map, const void* base, const PifaCacheShape& c, uint32_t rows, bool swizzle, int order[3]);
+// The same over elements of one byte: box of a head's elements x `rows` tokens, not swizzled.
+int make_tmap_cache_q8(CUtensorMap* map, const void* base, const PifaCacheShape& c, uint32_t rows, int order[3]);
 
 #endif  // PIFA_INTERNAL_H_
