@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
 
 template <bool F16, int D>
 cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
-  return launch_rows_and_join<F16, D, attention_rows<F16, D>>(g, (size_t)WARPS * kStages<D> * 2 * STEP * 2 * D, stream);
+  return launch_rows_and_join<F16, D, attention_rows<F16, D>>(g, (size_t)WARPS * kStages<D> * 2 * STEP * 2 * D, true, stream);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -14,11 +14,16 @@ namespace {
 struct RowsQ8 {
   const uint8_t *k, *v, *ks, *vs;
   int64_t scale_page, scale_block, scale_head;
+  int whole;  // heads of a CTA; 0: an equal run of steps, wherever heads end
 };
 
 template <int D>
 constexpr int kStages = 512 / D;  // of 16 keys: 4 KB (D = 128) or 2 KB
-constexpr int LEAST = 2 * WARPS;  // steps of a CTA
+constexpr int LEAST = WARPS;      // steps of a CTA (one sequence of 351 keys, 32 heads: 11.7 us, with twice as many 12.4)
+// Where a CTA's share of the heads has at most so many keys, going by what the tables have room for, heads are not cut and nothing is
+// left to the join. (Measured, cut and whole: 1 sequence of 351 keys, 32 heads 11.7 and 8.3 us; 16 of 1000 to 2000, 8 heads 24.5 and 20.3;
+// 64 of 256 to 500, 8 heads 25.5 and 24.7; 64 of 480 to 940, 8 heads, 3840 keys a CTA, 31.3 and 34.6.)
+constexpr int WHOLE_KEYS = 2048;
 
 // What a warp has summed up of a head that it did not finish alone: in shared memory, for the CTA to add up.
 struct Piece {
@@ -58,8 +63,13 @@ __global__ void __launch_bounds__(THREADS, 1)
   const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST);
 
   // ---- this CTA's run of steps, this warp's share of it: segments of one request and head each ----
-  const int64_t c64 = (int64_t)blockIdx.x * dealt.run;
-  const int c0 = (int)min(c64, (int64_t)dealt.total), c1 = (int)min(c64 + dealt.run, (int64_t)dealt.total);
+  auto begin_of = [&](int i) {  // this CTA's first step (i = 0), the next one's (1)
+    const int64_t k = (int64_t)(blockIdx.x + i) * (c8.whole ? c8.whole : dealt.run);
+    if (c8.whole == 0 || dealt.total == 0 || k >= g.B * g.heads) return (int)(c8.whole ? dealt.total : min(k, (int64_t)dealt.total));
+    const int b = (int)k / g.heads;
+    return first[b] + ((int)k - b * g.heads) * steps_of(lengths_of(g, b));
+  };
+  const int c0 = begin_of(0), c1 = begin_of(1);
   if (c0 == c1) return;
   const int share = (c1 - c0 + WARPS - 1) / WARPS;
   int at = min(c0 + warp * share, c1);
@@ -378,15 +388,18 @@ __global__ void __launch_bounds__(THREADS, 1)
 
 template <bool F16, int D>
 cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
-  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4), stream, c8);
+  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4),
+                                                                 c8.whole == 0, stream, c8);
 }
 
 }  // namespace
 
 int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream) {
   const RowArgs g = row_args(a, status);
+  const int64_t heads = a.B * a.cache.heads, ctas = rows_grid();
+  const int64_t share = (heads + ctas - 1) / ctas, whole = share * a.cols * a.cache.page_size <= WHOLE_KEYS ? share : 0;
   const RowsQ8 c8 = {static_cast<const uint8_t*>(a.k), static_cast<const uint8_t*>(a.v), a.q8->k, a.q8->v, a.q8->shape.page_stride,
-                     a.q8->shape.block_stride, a.q8->shape.head_stride};
+                     a.q8->shape.block_stride, a.q8->shape.head_stride, (int)whole};
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
   cudaError_t e;
   if (a.cache.dim == 64) e = f16 ? launch_rows_q8<true, 64>(g, c8, stream) : launch_rows_q8<false, 64>(g, c8, stream);

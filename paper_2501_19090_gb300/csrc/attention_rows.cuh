@@ -234,10 +234,16 @@ __global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int s
   }
 }
 
-// The launch of `kernel` with `smem` bytes beside the requests' first steps, and of the join.
+// CTAs of the streaming kernel.
+inline int rows_grid() {
+  const int sms = pifa_sm_count();
+  return sms < MAX_CTAS ? sms : MAX_CTAS;
+}
+
+// The launch of `kernel` with `smem` bytes beside the requests' first steps, and of the join if it leaves heads to it.
 template <bool F16, int D, auto Kernel, typename... A>
-cudaError_t launch_rows_and_join(const RowArgs& g, size_t smem, cudaStream_t stream, const A&... more) {
-  const int sms = pifa_sm_count(), grid = sms < MAX_CTAS ? sms : MAX_CTAS;
+cudaError_t launch_rows_and_join(const RowArgs& g, size_t smem, bool joins, cudaStream_t stream, const A&... more) {
+  const int sms = pifa_sm_count(), grid = rows_grid();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);
@@ -250,7 +256,7 @@ cudaError_t launch_rows_and_join(const RowArgs& g, size_t smem, cudaStream_t str
   cfg.numAttrs = 1;
   cudaError_t e = pifa_allow_smem<Kernel>(223 * 1024);  // (the rest is static)
   if (e == cudaSuccess) e = pifa_launch_ex(&cfg, Kernel, g, more...);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || !joins) return e;
   cfg.dynamicSmemBytes = 0;
   const int64_t items = (int64_t)g.B * g.heads;
   int split = 1;
