@@ -1,12 +1,13 @@
 """A decoder layer's attention sublayer with PIFA projections, served: prompts, then decode steps.
 
-    python examples/attention_block.py [--width 4096] [--heads 32] [--requests 8] [--prompt 700] [--steps 32]
+    python examples/attention_block.py [--width 4096] [--heads 32] [--requests 8] [--prompt 700] [--steps 32] [--cache-bits 16]
 
 q, k and v are one grouped call (three layers of one shape that share their input), the output projection another;
 between them the step's page tables, the rotation with the cache write, and the attention over the pages. The
 prompts run as one ragged step; the decode step is captured once into a CUDA graph that updates lengths and
 the free list's head in place, and replayed. Layers are random (drawn like compressed ones); the last
-step's output is checked against the same sublayer computed densely in float64.
+step's output is checked against the same sublayer computed densely in float64. With --cache-bits 8 keys and values are
+held as e4m3 numbers with a scale for each block of 16 tokens and head.
 """
 import argparse
 import os
@@ -42,14 +43,19 @@ def project(layers, X, Y=None):
 class Block:
     """The sublayer's weights and cache, and the state of the requests that it serves."""
 
-    def __init__(self, width, heads, requests, longest, page=16, rank=None, seed=0):
+    def __init__(self, width, heads, requests, longest, page=16, rank=None, seed=0, cache_bits=16):
         gen = torch.Generator(device=DEV).manual_seed(seed)
         rank = width // 2 if rank is None else rank
         self.heads, self.dim, self.page = heads, width // heads, page
         self.qkv, self.out = random_layers(gen, 3, width, rank), random_layers(gen, 1, width, rank)
         cols = -(-longest // page)
         pages = requests * cols
-        self.k_cache, self.v_cache = (torch.empty((pages, page, heads, self.dim), dtype=BF16, device=DEV) for _ in range(2))
+        held = torch.float8_e4m3fn if cache_bits == 8 else BF16
+        self.cache = [torch.empty((pages, page, heads, self.dim), dtype=held, device=DEV) for _ in range(2)]
+        if cache_bits == 8:  # keys, values, and the scales of each
+            self.cache += [torch.empty((pages, page // P.PIFA_Q8_BLOCK, heads), dtype=torch.float8_e8m0fnu, device=DEV) for _ in range(2)]
+        self.write = P.pifa_rope_cache_q8 if cache_bits == 8 else P.pifa_rope_cache
+        self.attend = P.pifa_paged_attention_q8 if cache_bits == 8 else P.pifa_paged_attention
         self.free_pages = torch.randperm(pages, device=DEV, generator=gen).int()
         self.free_first = torch.zeros(1, dtype=torch.int32, device=DEV)
         self.table = torch.full((requests, cols), -1, dtype=torch.int32, device=DEV)
@@ -69,8 +75,8 @@ class Block:
         q_start, kv_len, positions, slots, _ = P.pifa_page_tables(self.lens, new_len, self.page, self.free_pages, self.free_first,
                                                                   self.table, T, out=buf["tables"])
         q, k, v = project(self.qkv, X).view(T, 3, self.heads, self.dim).unbind(1)
-        P.pifa_rope_cache(q, k, v, positions, slots, self.freq, self.k_cache, self.v_cache, Qr=buf["q"])
-        P.pifa_paged_attention(buf["q"], self.k_cache, self.v_cache, self.table, q_start, kv_len, max_q, O=buf["o"])
+        self.write(q, k, v, positions, slots, self.freq, *self.cache, Qr=buf["q"])
+        self.attend(buf["q"], *self.cache, self.table, q_start, kv_len, max_q, O=buf["o"])
         return project(self.out, buf["o"].view(T, -1))
 
 
@@ -99,9 +105,9 @@ def dense_last(block, X):
     return dense(block.out, torch.einsum("hqk,khd->qhd", p, v).reshape(1, H * d))[0]
 
 
-def serve(width=4096, heads=32, requests=8, prompt=700, steps=32, seed=0):
+def serve(width=4096, heads=32, requests=8, prompt=700, steps=32, seed=0, cache_bits=16):
     """Runs the loop; returns (largest error of the last step over the outputs' rms, prompt us, decode us a step)."""
-    block = Block(width, heads, requests, prompt + steps + 1, seed=seed)
+    block = Block(width, heads, requests, prompt + steps + 1, seed=seed, cache_bits=cache_bits)
     gen = torch.Generator(device=DEV).manual_seed(seed + 1)
     lens = [max(1, prompt * (b + 1) // requests) for b in range(requests)]
     X = torch.randn((sum(lens), width), device=DEV, generator=gen).to(BF16)
@@ -152,7 +158,8 @@ if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("width", 4096), ("heads", 32), ("requests", 8), ("prompt", 700), ("steps", 32)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--cache-bits", type=int, default=16, choices=(8, 16))
     a = vars(ap.parse_args())
     error, prompt_us, decode_us = serve(**a)
-    print(f"{a['requests']} requests, width {a['width']}, {a['heads']} heads: prompts {prompt_us:.0f} us, decode step "
+    print(f"{a['requests']} requests, width {a['width']}, {a['heads']} heads, cache in {a['cache_bits']} bits: prompts {prompt_us:.0f} us, decode step "
           f"{decode_us:.1f} us, largest error of the last step {error:.3g} of the outputs' rms")

@@ -31,6 +31,16 @@
 // last round: a piece writes its unnormalised sums, and when all have, all warps add them up, in the order of the
 // keys. Every wait is bounded; on timeout PIFA_ERR_TIMEOUT is latched and the CTA drains.
 //
+// A cache in 8 bits (Q8): both products on fp16. Four more warps (512 threads) bring tiles, which TMA leaves in slots of their own,
+// to fp16 in the slots that the MMAs read: K's and V's two each, an e4m3 number times a power of two (2^-k, the block's scale against
+// the tile's largest), so that the softmax meets one scale of K and one of V a tile (q8.cuh). Softmax threads bring their own row of
+// Q from bf16 to fp16. What bounds it is that work: a tile of K or V takes its two warps 2000 to 2300 cycles, next to 2048 of MMAs
+// that leave little of shared memory's time; and instruction fetch: all of a warp's rows unrolled (10 KB more) took a tile's softmax from
+// 2650 to 3750 cycles. Chunks whose rows would convert the same keys several times have them converted once, by a kernel that makes
+// the plan too, and run as above. Measured, head_dim 128: 2048 tokens over 30000 cached, 64 heads on 8: 1.79 ms with conversion inside,
+// 1.35 to 1.40 with it before (36 us of it; 1.25 in 16 bits); a prompt of 1900, 32 heads, 69 and 53 us (9; 38.5); 512 rows a head
+// over 30000, 8 heads: 88 and 100.
+//
 // Measured, head_dim 128, bf16: 2048 tokens over 30000 cached, 64 heads on 8 key / value heads, pages of 64: 1.20 to 1.27 ms,
 // 1640 to 1740 TFLOP/s of the visible pairs (the measured bf16 rate is 1910 in a burst, 1702 for seconds: the power cap is what
 // bounds it; 82% of the cycles have a tensor instruction). A prompt of 2048, 32 heads: 38 us, 16 tiles at most for a CTA: 3.3 us
@@ -553,8 +563,10 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
 
   // Registers: a softmax thread holds a row of S. 2 x 128 x 208 + 128 x 88 = 384 x 168, as launched; with the warps that convert
   // 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128.
+  constexpr int HIGH = Q8 ? 192 : 208, LOW = Q8 ? 64 : 88;
+  static_assert(256 * HIGH + (kThreads<Q8> - 256) * LOW <= kThreads<Q8> * (65536 / kThreads<Q8> / 8 * 8), "more than the launch has");
   if (warp >= 8) {
-  regs_lower<Q8 ? 64 : 88>();
+  regs_lower<LOW>();
   // K (kv = 0) or V of an item's key tiles, fill after fill of the ring: K and V take its slots in turn. A lane
   // copies 64 columns of a page's rows (or of 128 of them). One warp issuing both was the bound for pages of 16.
   auto stream = [&](int kv, int& tiles, int b, int L, int head, int j0, int j1, auto&& every) {
@@ -899,7 +911,7 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
       if (loads[t] && !mbar_wait(&q_full[t], (uint32_t)(loads[t] - 1) & 1u, 100000000ull)) latch_status(g.status, PIFA_ERR_TIMEOUT);
   }
   } else {
-    regs_raise<Q8 ? 192 : 208>();
+    regs_raise<HIGH>();
     // ---------------- softmax and epilogue: a row per thread ----------------
     const int t = warp >> 2, quarter = warp & 3;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;

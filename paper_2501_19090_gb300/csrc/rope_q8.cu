@@ -5,6 +5,12 @@
 // A block grows: the tokens that it held keep their elements while its scale stays, and are rounded anew, rne(q s_old / s),
 // when a new token raises it. With powers of two that loses nothing but in the subnormal range (a rounding there per rise), the
 // scale of a block does not depend on how its tokens were dealt to calls, and a float's relative precision does not depend on it.
+//
+// Bound by memory. The write: a stretch, the neighbouring rows of one block, and one head go to one or some warps, which hold all its
+// elements in registers from the rotation over the maximum to the rounding: every element is read and written once. CTAs of their own
+// turn queries in the same launch. Few tokens (decode): a chain of latencies, slots and cosines, rows, scale.
+// Measured, head_dim 128, bf16: 8192 tokens of 64 + 8 + 8 heads (318 MB) 59 us, 5.4 TB/s (the queries alone 47); 200 sequences in decode
+// 6.0, 8 sequences, 32 + 32 + 32 heads, 3.6; reading back 50001 tokens of 8 heads (307 MB) 50.5 us, 6.1 TB/s.
 #include <cmath>
 
 #include "q8.cuh"
