@@ -228,18 +228,42 @@ __global__ void __launch_bounds__(THREADS, 1)
       const uint8_t* buf = ring + stage * STAGE_BYTES;
       cp_wait<STAGES - 1>();
       __syncwarp();
-      float sc[2][4] = {};
+      // four sums of products in turn: an MMA's result is some thirty cycles away, and eight in a row would wait for each other
+      uint4 kk[KC][2];
 #pragma unroll
       for (int i = 0; i < KC; ++i)
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb) {
-          const uint4 k = *reinterpret_cast<const uint4*>(buf + place<D>(key_of<D>(gr + 8 * nb), c4 + 4 * i));
-          const uint32_t w[4] = {k.x, k.y, k.z, k.w};
+        for (int nb = 0; nb < 2; ++nb) kk[i][nb] = *reinterpret_cast<const uint4*>(buf + place<D>(key_of<D>(gr + 8 * nb), c4 + 4 * i));
+      float part_sc[KC][2][4] = {};
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            mma_m16n8k16_f16(sc[nb], q[0][i][2 * j], q[1][i][2 * j], q[0][i][2 * j + 1], q[1][i][2 * j + 1], halves_of(w[j] & 0xffffu),
-                             halves_of(w[j] >> 16));
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < KC; ++i)
+#pragma unroll
+          for (int nb = 0; nb < 2; ++nb) {
+            const uint32_t w = (&kk[i][nb].x)[j];
+            mma_m16n8k16_f16(part_sc[i][nb], q[0][i][2 * j], q[1][i][2 * j], q[0][i][2 * j + 1], q[1][i][2 * j + 1], halves_of(w & 0xffffu),
+                             halves_of(w >> 16));
+          }
+      // this lane's columns of four keys
+      const int group = D == 128 ? (gr >> 1) | (gr & 1) << 2 : gr;
+      uint32_t w[4][VC / 4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int key = key_of<D>(c4 * 2 + (k & 1) + 8 * (k >> 1));
+        if constexpr (D == 128) {
+          const uint4 u = *reinterpret_cast<const uint4*>(buf + STEP * D + place<D>(key, group));
+          w[k][0] = u.x, w[k][1] = u.y, w[k][2] = u.z, w[k][3] = u.w;
+        } else {
+          const uint2 u = *reinterpret_cast<const uint2*>(buf + STEP * D + place<D>(key, group >> 1) + 8 * (group & 1));
+          w[k][0] = u.x, w[k][1] = u.y;
         }
+      }
+      float sc[2][4];
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[nb][k] = KC == 2 ? part_sc[0][nb][k] + part_sc[KC - 1][nb][k] : part_sc[0][nb][k];
       // exponents of the weights times their value's scale, relative to m; keys that a row does not see
       float v[2][4];
       bool grows = false;
@@ -288,20 +312,6 @@ __global__ void __launch_bounds__(THREADS, 1)
         l[r] = fmaf((e[0] + e[1]) + (e[2] + e[3]), inverse, l[r]);
         p[r][0] = pack<true>(e[0], e[1]);
         p[r][1] = pack<true>(e[2], e[3]);
-      }
-      // this lane's columns of four keys: VC from `from` on
-      const int group = D == 128 ? (gr >> 1) | (gr & 1) << 2 : gr;
-      uint32_t w[4][VC / 4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int key = key_of<D>(c4 * 2 + (k & 1) + 8 * (k >> 1));
-        if constexpr (D == 128) {
-          const uint4 u = *reinterpret_cast<const uint4*>(buf + STEP * D + place<D>(key, group));
-          w[k][0] = u.x, w[k][1] = u.y, w[k][2] = u.z, w[k][3] = u.w;
-        } else {
-          const uint2 u = *reinterpret_cast<const uint2*>(buf + STEP * D + place<D>(key, group >> 1) + 8 * (group & 1));
-          w[k][0] = u.x, w[k][1] = u.y;
-        }
       }
 #pragma unroll
       for (int i = 0; i < VC / 4; ++i)
