@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int rows = x.n * g.group;
     const int32_t* pages = g.table + b * g.ldt;
     const int n_pages = (x.L + g.page_size - 1) >> g.page_shift;
-    // Lane i holds the page of step i of 32, and what its scales come to: of those that are being loaded and the next, of those
+    // Lane i holds the place of step i of 32, and what its scales come to: of those that are being loaded and the next, of those
     // that are being computed and the next. A page comes 32 steps, its scales some steps, before what needs them.
     auto page_of = [&](int s) {
       const int p = (s * STEP) >> g.page_shift;
@@ -116,38 +116,49 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int64_t from = id * c8.scale_page + ((s * STEP & (g.page_size - 1)) / PIFA_Q8_BLOCK) * c8.scale_block + head * c8.scale_head;
       return (int)c8.ks[from] | (int)c8.vs[from] << 8;
     };
-    int known = s0, ids = page_of(s0 + lane), ids_next = page_of(s0 + 32 + lane);
-    int scales_next = scales_of(s0 + lane, ids);
+    // where a step's first key of this head lies; -1: in no page
+    auto base_of = [&](int s, int id) {
+      return id < 0 || id >= g.pages ? (int64_t)-1
+                                     : id * g.page_stride + ((s * STEP) & (g.page_size - 1)) * g.token_stride + head * g.head_stride;
+    };
+    int known = s0, ids_next = page_of(s0 + 32 + lane), scales_next;
+    int64_t bases;
+    {
+      const int id = page_of(s0 + lane);
+      bases = base_of(s0 + lane, id);
+      scales_next = scales_of(s0 + lane, id);
+    }
+    // this lane's piece of every KEYS-th key: a warp's copy is whole rows
+    const int64_t mine = key0 * g.token_stride + piece * 16;
     auto load = [&](int s, int stage) {
       if (s == known + 32) {
         known = s;
-        ids = ids_next;
+        bases = base_of(s + lane, ids_next);
+        scales_next = scales_of(s + lane, ids_next);
         ids_next = page_of(s + 32 + lane);
-        scales_next = scales_of(s + lane, ids);
       }
-      const int id = __shfl_sync(0xffffffffu, ids, s - known);
-      const bool bad = id < 0 || id >= g.pages;
-      if (bad && x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
-      // this lane's piece of every KEYS-th key: a warp's copy is whole rows
-      const int64_t step = KEYS * g.token_stride;
-      int64_t from = (bad ? 0 : (int64_t)id) * g.page_stride + head * g.head_stride + ((s * STEP) & (g.page_size - 1)) * g.token_stride +
-                     key0 * g.token_stride + piece * 16;
+      const int64_t from = __shfl_sync(0xffffffffu, bases, s - known);
       const uint32_t dst = ring_at + stage * STAGE_BYTES;
-      if (bad || (s + 1) * STEP > x.L) {  // keys past the last one: zeros, that nothing is read for
-        const int left = bad ? 0 : x.L - s * STEP;
+      if (from >= 0 && (s + 1) * STEP <= x.L) {
+        const uint8_t *k = c8.k + from + mine, *v = c8.v + from + mine;
+#pragma unroll
+        for (int i = 0; i < STEP / KEYS; ++i) {
+          const int at = place<D>(key0 + i * KEYS, piece);
+          cp_async16_all(dst + at, k);
+          cp_async16_all(dst + STEP * D + at, v);
+          k += KEYS * g.token_stride;
+          v += KEYS * g.token_stride;
+        }
+      } else {  // keys past the last one, or of no page: zeros, that nothing is read for
+        if (from < 0 && x.L > 0) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
+        const int left = from < 0 ? 0 : x.L - s * STEP;
 #pragma unroll
         for (int i = 0; i < STEP / KEYS; ++i) {
           const int key = key0 + i * KEYS;
           const bool in = key < left;
-          cp_async16(dst + place<D>(key, piece), in ? c8.k + from + i * step : c8.k, in ? 16 : 0);
-          cp_async16(dst + STEP * D + place<D>(key, piece), in ? c8.v + from + i * step : c8.v, in ? 16 : 0);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < STEP / KEYS; ++i, from += step) {
-          const int at = place<D>(key0 + i * KEYS, piece);
-          cp_async16(dst + at, c8.k + from, 16);
-          cp_async16(dst + STEP * D + at, c8.v + from, 16);
+          const int64_t there = in ? from + mine + i * KEYS * g.token_stride : 0;
+          cp_async16(dst + place<D>(key, piece), c8.k + there, in ? 16 : 0);
+          cp_async16(dst + STEP * D + place<D>(key, piece), c8.v + there, in ? 16 : 0);
         }
       }
     };

@@ -167,6 +167,9 @@ __device__ __forceinline__ void cp_async4(uint32_t dst_smem, const void* src) {
 __device__ __forceinline__ void cp_async16(uint32_t dst_smem, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst_smem), "l"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void cp_async16_all(uint32_t dst_smem, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
+}
 // Waits for all of this thread's cp.async copies.
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // 32-bit store into the shared memory of a CTA of this cluster (shared::cluster address).
