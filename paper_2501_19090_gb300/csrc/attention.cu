@@ -56,6 +56,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Run steps_here = deal_steps(g, first, part, (int)gridDim.x * WARPS, MIN_STEPS);
   const int total = steps_here.total, run = steps_here.run;
+  if (blockIdx.x == 0) {  // written down for the join
+    for (int b = (int)threadIdx.x; b <= g.B; b += THREADS) g.sums[b] = first[b];
+    if (threadIdx.x == 0) g.sums[g.B + 1] = total == 0 ? 0 : run;
+  }
 
   // ---- this warp's run of steps: segments of one request and head each ----
   const int worker = warp * (int)gridDim.x + (int)blockIdx.x;  // neighbours on different SMs
@@ -244,9 +248,110 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   }
 }
 
+// Adds up the pieces of a request's head whose steps fell to several workers, in the order of the keys: `split` CTAs
+// for each, a share of the columns apiece, a thread for four columns of a row, up to 16 threads with every
+// so many-th piece where a CTA has fewer of those. Pieces and their weights are loaded together, four at a time: with few
+// pieces the kernel is two latencies long, and one long sequence (144 pieces of each head) spreads over the SMs (64
+// heads, 8 key / value heads, 16000 keys, both kernels: 63 us with one CTA a head, 34 with up to 8 shares and 8 threads,
+// 29 with 16 and 16, 30.5 with 32 and 32; eight pieces at a time cost 64 requests 3 %).
 template <bool F16, int D>
-cudaError_t launch_rows(const RowArgs& g, cudaStream_t stream) {
-  return launch_rows_and_join<F16, D, attention_rows<F16, D>>(g, (size_t)WARPS * kStages<D> * 2 * STEP * 2 * D, true, stream);
+__global__ void __launch_bounds__(THREADS) attention_join(const RowArgs g, int split) {
+  __shared__ float2 sh_ml[THREADS];
+  __shared__ float4 sh_o[THREADS];
+  pdl_launch_dependents();
+  const int item = (int)blockIdx.x / split, b = item / g.heads, head = item - b * g.heads;
+  const int quads = D / 4 / split, col0 = ((int)blockIdx.x - item * split) * quads * 4;  // of this CTA: fours of columns, first one
+  const int slots = g.max_rows * quads, groups = min(max(THREADS / slots, 1), 16);
+  const Lengths x = lengths_of(g, b);  // (before the wait: the kernel before lets this one begin when it has waited itself)
+  pdl_wait_primary();
+  const int run = g.sums[g.B + 1], steps = steps_of(x), from = g.sums[b] + head * steps;
+  if (steps == 0 || run == 0) return;
+  const int w0 = from / run, w1 = (from + steps - 1) / run;
+  if (w0 == w1) return;  // the worker has finished it
+  const int place = g.max_rows * (D + 2);  // a worker has two: the head that began before its run, and the last one
+  for (int slot = (int)threadIdx.x % (slots * groups); slot < slots * groups; slot += THREADS) {
+    const int group = slot / slots, row = (slot - group * slots) / quads, col = col0 + (slot - group * slots) % quads * 4;
+    const bool here = row < x.n * g.group && (int)threadIdx.x < slots * groups;
+    float top = -INFINITY, all = 0.0f;
+    float4 acc = make_float4(0, 0, 0, 0);
+    if (here) {
+      const float* base = g.partial + row * (D + 2);
+      for (int w = w0 + group; w <= w1; w += 4 * groups) {
+        float2 ml[4], lo[4], hi[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int v = min(w + i * groups, w1);
+          const float* p = base + ((int64_t)v * 2 + (v == w0 ? 1 : 0)) * place;
+          ml[i] = __ldcg(reinterpret_cast<const float2*>(p + D));
+          lo[i] = __ldcg(reinterpret_cast<const float2*>(p + col));
+          hi[i] = __ldcg(reinterpret_cast<const float2*>(p + col + 2));
+        }
+        float most = top;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (w + i * groups > w1) ml[i].y = 0.0f;  // a piece that is not there
+          if (ml[i].y != 0.0f) most = fmaxf(most, ml[i].x);
+        }
+        const float f = top > -INFINITY ? fast_exp2(top - most) : 0.0f;
+        all *= f;
+        acc.x *= f;
+        acc.y *= f;
+        acc.z *= f;
+        acc.w *= f;
+        top = most;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = ml[i].y != 0.0f ? fast_exp2(ml[i].x - top) : 0.0f;
+          all += ml[i].y * e;
+          acc.x += lo[i].x * e;
+          acc.y += lo[i].y * e;
+          acc.z += hi[i].x * e;
+          acc.w += hi[i].y * e;
+        }
+      }
+    }
+    if (groups > 1) {  // (then every thread has one slot at most)
+      sh_ml[threadIdx.x] = make_float2(top, all);
+      sh_o[threadIdx.x] = acc;
+      __syncthreads();
+      if (group > 0) return;
+      float most = top;
+      for (int k = 1; k < groups; ++k) most = fmaxf(most, sh_ml[slot + k * slots].x);
+      const float f = top > -INFINITY ? fast_exp2(top - most) : 0.0f;
+      all *= f;
+      acc.x *= f;
+      acc.y *= f;
+      acc.z *= f;
+      acc.w *= f;
+      for (int k = 1; k < groups; ++k) {
+        const float2 ml = sh_ml[slot + k * slots];
+        const float4 o = sh_o[slot + k * slots];
+        const float e = ml.y != 0.0f ? fast_exp2(ml.x - most) : 0.0f;
+        all += ml.y * e;
+        acc.x += o.x * e;
+        acc.y += o.y * e;
+        acc.z += o.z * e;
+        acc.w += o.w * e;
+      }
+    }
+    if (here) {
+      const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+      const int token = row / g.group;
+      uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + col;
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack<F16>(acc.x * inv, acc.y * inv), pack<F16>(acc.z * inv, acc.w * inv));
+    }
+  }
+}
+
+template <bool F16, int D>
+cudaError_t launch_rows_and_join(const RowArgs& g, cudaStream_t stream) {
+  const cudaError_t e =
+      launch_rows<attention_rows<F16, D>>(rows_grid(), (size_t)WARPS * kStages<D> * 2 * STEP * 2 * D + first_bytes(g), stream, g);
+  if (e != cudaSuccess) return e;
+  const int64_t items = (int64_t)g.B * g.heads;
+  int split = 1;
+  while (split < 16 && items * split * 2 <= 8 * pifa_sm_count() && g.max_rows * (D / 4) / (split * 2) >= THREADS / 16) split *= 2;
+  return launch_rows<attention_join<F16, D>>(items * split, 0, stream, g, split);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -334,8 +439,8 @@ int attend(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_he
   g.v = static_cast<const uint16_t*>(v_cache);
   const bool f16 = dtype == PIFA_DTYPE_FP16;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-  if (head_dim == 64) e = f16 ? launch_rows<true, 64>(g, stream) : launch_rows<false, 64>(g, stream);
-  else e = f16 ? launch_rows<true, 128>(g, stream) : launch_rows<false, 128>(g, stream);
+  if (head_dim == 64) e = f16 ? launch_rows_and_join<true, 64>(g, stream) : launch_rows_and_join<false, 64>(g, stream);
+  else e = f16 ? launch_rows_and_join<true, 128>(g, stream) : launch_rows_and_join<false, 128>(g, stream);
   if (e != cudaSuccess) return pifa_fail_cuda("attention launch", e);
   return PIFA_OK;
 }

@@ -32,19 +32,38 @@ struct RowsQ8 {
   const uint8_t *k, *v, *ks, *vs;
   int64_t scale_page, scale_block, scale_head;
   int whole;  // heads of a CTA; 0: an equal run of steps, wherever heads end
+  int4* cuts; // for each CTA, of the head that its run ends within: first row of Q, rows, its first and last CTA in 16 bits each, 1 + head
 };
+// Of partial sums a CTA has two places, for the head that began before its run and for the one that goes on behind it: of each row D
+// numbers, then of each row m and l, each place a multiple of 16 bytes. (The workspace has them for eight times as many.)
+template <int D>
+__host__ __device__ constexpr int64_t place_floats(int64_t max_rows) { return max_rows * (D + 4); }
+
+// One more piece of a row's sums: (m, l, four of O); l = 0: of no keys.
+__device__ __forceinline__ void add_piece(float& top, float& all, float4& acc, float2 ml, float4 o) {
+  const float most = ml.y != 0.0f ? fmaxf(top, ml.x) : top;
+  const float f = top > -INFINITY ? fast_exp2(top - most) : 0.0f, e = ml.y != 0.0f ? fast_exp2(ml.x - most) : 0.0f;
+  top = most;
+  all = fmaf(all, f, ml.y * e);
+  acc.x = fmaf(acc.x, f, o.x * e);
+  acc.y = fmaf(acc.y, f, o.y * e);
+  acc.z = fmaf(acc.z, f, o.z * e);
+  acc.w = fmaf(acc.w, f, o.w * e);
+}
 
 template <int D>
 constexpr int kStages = 512 / D;  // of 16 keys: 4 KB (D = 128) or 2 KB
 constexpr int LEAST = WARPS;      // steps of a CTA (one sequence of 351 keys, 32 heads: 11.7 us, with twice as many 12.4)
-// Where a CTA's share of the heads has at most so many keys, going by what the tables have room for, heads are not cut and nothing is
-// left to the join. (Measured, cut and whole: 1 sequence of 351 keys, 32 heads 11.7 and 8.3 us; 16 of 1000 to 2000, 8 heads 24.5 and 20.3;
-// 64 of 256 to 500, 8 heads 25.5 and 24.7; 64 of 480 to 940, 8 heads, 3840 keys a CTA, 31.3 and 34.6.)
-constexpr int WHOLE_KEYS = 2048;
+// Heads are not cut, and nothing is left to the join, where that gives no CTA much more than its equal share, going by what the tables
+// have room for: at most so many keys more, and no more in all than where requests shorter than the room, whose CTAs then wait
+// for the others', cost more than the join. (Measured, cut and whole: 1 sequence of 300 keys, 32 heads, 9.6 and 8.3 us; of 700 10.0 and 10.3;
+// of 2000 13.0 and 15.7; 18 sequences, 8 heads, of 700 15.4 and 11.3; of 500 to 2000 16.1 and 14.8; of 1000 to 4000 21.5 and 22.2. More heads than
+// CTAs: 40 sequences, 8 heads, of 300 16.0 and 15.2, of 175 to 700 17.3 and 18.7.)
+constexpr int WHOLE_MORE = 768, WHOLE_KEYS_ONE = 2048, WHOLE_KEYS = 1024;
 
 // What a warp has summed up of a head that it did not finish alone: in shared memory, for the CTA to add up.
 struct Piece {
-  int item, b, from, steps;  // (first step of the head) -1: none
+  int from, steps, q0, rows, head;  // the head's first step and its steps; its first row of Q and its rows (0: no piece)
 };
 
 // The 16-byte pieces of a key's row lie swizzled (its index xor the row's, in the 128 bytes that eight, or with D = 64 two rows of 64,
@@ -59,9 +78,9 @@ __device__ __forceinline__ int place(int key, int piece) {
   return D == 128 ? key * 128 + ((piece ^ (key & 7)) << 4) : key * 64 + ((piece ^ (key >> 1 & 3)) << 4);
 }
 
-template <bool F16, int D>
-__global__ void __launch_bounds__(THREADS, 1)
-    attention_rows_q8(const RowArgs g, const RowsQ8 c8) {
+template <bool F16, int D, bool SLIM>
+__global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g, const RowsQ8 c8) {
+  constexpr int ROWS = SLIM ? 8 : MAX_ROWS;
   constexpr int KC = D / 64, VC = D / 8;               // of a lane: 16-byte pieces of a key of K; columns of a key of V
   constexpr int PIECES = D / 16, KEYS = 32 / PIECES;   // of a key's row; keys that a warp copies at once
   constexpr int STAGE_BYTES = 2 * STEP * D;            // K and V of a step
@@ -70,10 +89,10 @@ __global__ void __launch_bounds__(THREADS, 1)
   // of each warp its first head's piece; its last one's takes the place of its stages when those are done
   float* sums = reinterpret_cast<float*>(smem + WARPS * STAGES * STAGE_BYTES);
   int* first = reinterpret_cast<int*>(sums + WARPS * g.max_rows * D);  // B + 1
-  static_assert(STAGES * STAGE_BYTES >= MAX_ROWS * D * 4, "a piece fits into a warp's stages");
+  static_assert(STAGES * STAGE_BYTES >= ROWS * D * 4, "a piece fits into a warp's stages");
   __shared__ int part[32];
   __shared__ Piece pieces[2 * WARPS];
-  __shared__ float2 ml[2 * WARPS][MAX_ROWS];
+  __shared__ float2 ml[2 * WARPS][ROWS];
   const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5);
   pdl_wait_primary();
   pdl_launch_dependents();  // (after the wait: the join reads the lengths before its own)
@@ -87,11 +106,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     return first[b] + ((int)k - b * g.heads) * steps_of(lengths_of(g, b));
   };
   const int c0 = begin_of(0), c1 = begin_of(1);
+  if (threadIdx.x == 0 && c8.whole == 0) c8.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (c0 == c1) return;
   const int share = (c1 - c0 + WARPS - 1) / WARPS;
   int at = min(c0 + warp * share, c1);
   const int stop = min(at + share, c1);
-  if (lane < 2) pieces[2 * warp + lane].item = -1;
+  if (lane < 2) pieces[2 * warp + lane].rows = 0;
   __syncwarp();
   const int gr = lane >> 2, c4 = lane & 3;
   const uint8_t* ring = smem + warp * STAGES * STAGE_BYTES;
@@ -103,6 +123,26 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int steps = steps_of(x), head = (at - first[b]) / steps, s0 = at - first[b] - head * steps;
     const int s1 = min(steps, s0 + stop - at);
     const int rows = x.n * g.group;
+    // The rows of Q: this lane's are gr (and gr + 8; SLIM: of the products' results, 2 c4 and 2 c4 + 1). Asked for before the copies, whose
+    // queue is some thousand cycles long when all SMs begin.
+    constexpr int QR = SLIM ? 1 : 2;
+    uint32_t q[QR][KC][8];
+#pragma unroll
+    for (int r = 0; r < QR; ++r) {
+      const int row = gr + 8 * r, token = row / g.group;
+      const uint4* from = reinterpret_cast<const uint4*>(g.q + (int64_t)(x.q0 + token) * g.ldq +
+                                                         (int64_t)(head * g.group + row - token * g.group) * D + c4 * 16);
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint4 w = row < rows ? from[8 * i + k] : make_uint4(0, 0, 0, 0);
+          q[r][i][4 * k] = w.x;
+          q[r][i][4 * k + 1] = w.y;
+          q[r][i][4 * k + 2] = w.z;
+          q[r][i][4 * k + 3] = w.w;
+        }
+    }
     const int32_t* pages = g.table + b * g.ldt;
     const int n_pages = (x.L + g.page_size - 1) >> g.page_shift;
     // Lane i holds the place of step i of 32, and what its scales come to: of those that are being loaded and the next, of those
@@ -167,27 +207,20 @@ __global__ void __launch_bounds__(THREADS, 1)
       if (s0 + i < s1) load(s0 + i, i);
       cp_commit();
     }
-    // the rows of Q: this lane's are gr and gr + 8; as fp16, times a power of two that brings bf16's into its range
-    uint32_t q[2][KC][8];
+    // Q as fp16, times a power of two that brings bf16's rows into its range
     int seen[2];
-    float c[2];
+    float c[2] = {g.c, g.c};
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int row = gr + 8 * r, token = row / g.group;
-      seen[r] = row < rows ? max(x.ahead + token, 0) : 0x7fffffff;
-      c[r] = g.c;
+      const int row = SLIM ? 2 * c4 + r : gr + 8 * r;
+      seen[r] = row < rows ? max(x.ahead + row / g.group, 0) : 0x7fffffff;
+    }
 #pragma unroll
-      for (int i = 0; i < KC; ++i) {
-        uint4 w[2] = {};
-        if (row < rows) {
-          const uint4* from = reinterpret_cast<const uint4*>(g.q + (int64_t)(x.q0 + token) * g.ldq +
-                                                             (int64_t)(head * g.group + row - token * g.group) * D + (c4 + 4 * i) * 16);
-          w[0] = from[0];
-          w[1] = from[1];
-        }
+    for (int r = 0; r < QR; ++r) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) q[r][i][k] = (&w[k / 4].x)[k % 4] ^ g.flip;
-      }
+      for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) q[r][i][k] ^= g.flip;
       if constexpr (!F16) {
         float most = 0.0f;
 #pragma unroll
@@ -198,8 +231,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const int e = row_exponent(most);
-        const float up = exponent_of_2(e);
-        c[r] *= exponent_of_2(-e);
+        const float up = exponent_of_2(e), down = exponent_of_2(-e);
+        if (SLIM) {
+          c[0] *= __shfl_sync(0xffffffffu, down, 8 * c4);
+          c[1] *= __shfl_sync(0xffffffffu, down, 8 * c4 + 4);
+        } else {
+          c[r] *= down;
+        }
 #pragma unroll
         for (int i = 0; i < KC; ++i)
 #pragma unroll
@@ -208,7 +246,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
     const int all_see = __reduce_min_sync(0xffffffffu, min(seen[0], seen[1]));  // keys before this are seen by every row
-    float o[VC][4] = {};
+    constexpr int OUT = SLIM ? VC / 2 : VC;
+    float o[OUT][4] = {};
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
     float base = NO_BASE;  // exponent that the values' scales are held against
     float key_scales = 0.0f, exponents = 0.0f, inverses = 0.0f;  // of step i of 32
@@ -226,7 +265,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (up > 0.0f) {  // the sums so far, in units of the larger exponent
           const float f = exponent_of_2(-(int)fminf(up, 126.0f));
 #pragma unroll
-          for (int i = 0; i < VC; ++i)
+          for (int i = 0; i < OUT; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) o[i][k] *= f;
         }
@@ -245,17 +284,20 @@ __global__ void __launch_bounds__(THREADS, 1)
       for (int i = 0; i < KC; ++i)
 #pragma unroll
         for (int nb = 0; nb < 2; ++nb) kk[i][nb] = *reinterpret_cast<const uint4*>(buf + place<D>(key_of<D>(gr + 8 * nb), c4 + 4 * i));
-      float part_sc[KC][2][4] = {};
+      float sums_qk[2][2][4] = {};
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < KC; ++i)
-#pragma unroll
-          for (int nb = 0; nb < 2; ++nb) {
-            const uint32_t w = (&kk[i][nb].x)[j];
-            mma_m16n8k16_f16(part_sc[i][nb], q[0][i][2 * j], q[1][i][2 * j], q[0][i][2 * j + 1], q[1][i][2 * j + 1], halves_of(w & 0xffffu),
-                             halves_of(w >> 16));
+        for (int i = 0; i < KC; ++i) {
+          const uint32_t w0 = (&kk[i][0].x)[j], w1 = (&kk[i][1].x)[j];
+          const uint32_t a = halves_of(w0 & 0xffffu), b2 = halves_of(w0 >> 16), a8 = halves_of(w1 & 0xffffu), b8 = halves_of(w1 >> 16);
+          if constexpr (SLIM) {  // keys gr and gr + 8 by rows 2 c4 and 2 c4 + 1
+            mma_m16n8k16_f16(sums_qk[KC == 2 ? i : j & 1][KC == 2 ? j & 1 : 0], a, a8, b2, b8, q[0][i][2 * j], q[0][i][2 * j + 1]);
+          } else {               // rows gr and gr + 8 by keys 2 c4 and 2 c4 + 1 (and 8 more)
+            mma_m16n8k16_f16(sums_qk[i][0], q[0][i][2 * j], q[QR - 1][i][2 * j], q[0][i][2 * j + 1], q[QR - 1][i][2 * j + 1], a, b2);
+            mma_m16n8k16_f16(sums_qk[i][1], q[0][i][2 * j], q[QR - 1][i][2 * j], q[0][i][2 * j + 1], q[QR - 1][i][2 * j + 1], a8, b8);
           }
+        }
       // this lane's columns of four keys
       const int group = D == 128 ? (gr >> 1) | (gr & 1) << 2 : gr;
       uint32_t w[4][VC / 4];
@@ -270,164 +312,254 @@ __global__ void __launch_bounds__(THREADS, 1)
           w[k][0] = u.x, w[k][1] = u.y;
         }
       }
-      float sc[2][4];
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sc[nb][k] = KC == 2 ? part_sc[0][nb][k] + part_sc[KC - 1][nb][k] : part_sc[0][nb][k];
-      // exponents of the weights times their value's scale, relative to m; keys that a row does not see
-      float v[2][4];
+      // exponents of the weights times their value's scale, relative to m; keys that a row does not see: v[r][k] is row r's of the lane
+      constexpr int EACH = SLIM ? 2 : 4;  // keys of a lane's row
+      auto key_at = [&](int k) { return s * STEP + key_of<D>(SLIM ? gr + 8 * k : 8 * (k >> 1) + c4 * 2 + (k & 1)); };
+      float v[2][EACH];
       bool grows = false;
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float cr = c[r] * key_scale;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[r][k] = fmaf(sc[k >> 1][2 * r + (k & 1)], cr, exponent);
+        for (int k = 0; k < EACH; ++k) {
+          float sum;
+          if constexpr (SLIM) {
+            const int at = 2 * k + r;
+            sum = KC == 2 ? (sums_qk[0][0][at] + sums_qk[0][1][at]) + (sums_qk[1][0][at] + sums_qk[1][1][at]) : sums_qk[0][0][at] + sums_qk[1][0][at];
+          } else {
+            const int at = 2 * r + (k & 1);
+            sum = KC == 2 ? sums_qk[0][k >> 1][at] + sums_qk[1][k >> 1][at] : sums_qk[0][k >> 1][at];
+          }
+          v[r][k] = fmaf(sum, cr, exponent);
+        }
       }
       if ((s + 1) * STEP > all_see) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (s * STEP + key_of<D>(8 * (k >> 1) + c4 * 2 + (k & 1)) >= seen[r]) v[r][k] = -INFINITY;
+          for (int k = 0; k < EACH; ++k)
+            if (key_at(k) >= seen[r]) v[r][k] = -INFINITY;
       }
       float top[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        top[r] = max3(v[r][0], v[r][1], fmaxf(v[r][2], v[r][3]));
+        top[r] = fmaxf(v[r][0], v[r][1]);
+        if constexpr (!SLIM) top[r] = max3(top[r], v[r][2], v[r][3]);
         grows |= top[r] > m[r] + 8.0f;
       }
       if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-          top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          if constexpr (SLIM) {
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 4));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 8));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 16));
+          } else {
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+          }
           top[r] = fmaxf(top[r], m[r]);
           const float f = top[r] > m[r] ? fast_exp2(m[r] - top[r]) : 1.0f;  // 0 where nothing was seen before
           m[r] = top[r];
           l[r] *= f;
 #pragma unroll
-          for (int i = 0; i < VC; ++i) {
-            o[i][2 * r] *= f;
-            o[i][2 * r + 1] *= f;
+          for (int i = 0; i < OUT; ++i) {
+            o[i][SLIM ? r : 2 * r] *= f;
+            o[i][SLIM ? r + 2 : 2 * r + 1] *= f;
           }
         }
       }
       uint32_t p[2][2];
+      float e[2][EACH];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const float from = m[r] > -INFINITY ? m[r] : 0.0f;
-        float e[4];
+        float sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) e[k] = fast_exp2(v[r][k] - from);
-        l[r] = fmaf((e[0] + e[1]) + (e[2] + e[3]), inverse, l[r]);
-        p[r][0] = pack<true>(e[0], e[1]);
-        p[r][1] = pack<true>(e[2], e[3]);
+        for (int k = 0; k < EACH; ++k) {
+          e[r][k] = fast_exp2(v[r][k] - from);
+          sum += e[r][k];
+        }
+        l[r] = fmaf(sum, inverse, l[r]);
+      }
+      if constexpr (SLIM) {  // from keys by rows to rows by keys: the second operand's order
+        p[0][0] = transposed(pack<true>(e[0][0], e[1][0]));
+        p[0][1] = transposed(pack<true>(e[0][1], e[1][1]));
+      } else {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          p[r][0] = pack<true>(e[r][0], e[r][1]);
+          p[r][1] = pack<true>(e[r][EACH - 2], e[r][EACH - 1]);
+        }
       }
 #pragma unroll
       for (int i = 0; i < VC / 4; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // columns 4 i + 2 h and the next
           const uint32_t lo = __byte_perm(w[0][i], w[1][i], h ? 0x7362 : 0x5140), hi = __byte_perm(w[2][i], w[3][i], h ? 0x7362 : 0x5140);
-          mma_m16n8k16_f16(o[4 * i + 2 * h], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo & 0xffffu), halves_of(hi & 0xffffu));
-          mma_m16n8k16_f16(o[4 * i + 2 * h + 1], p[0][0], p[1][0], p[0][1], p[1][1], halves_of(lo >> 16), halves_of(hi >> 16));
+          const uint32_t a = halves_of(lo & 0xffffu), a8 = halves_of(hi & 0xffffu), b2 = halves_of(lo >> 16), b8 = halves_of(hi >> 16);
+          if constexpr (SLIM) {
+            mma_m16n8k16_f16(o[2 * i + h], a, b2, a8, b8, p[0][0], p[0][1]);
+          } else {
+            mma_m16n8k16_f16(o[(4 * i + 2 * h) % OUT], p[0][0], p[1][0], p[0][1], p[1][1], a, a8);
+            mma_m16n8k16_f16(o[(4 * i + 2 * h + 1) % OUT], p[0][0], p[1][0], p[0][1], p[1][1], b2, b8);
+          }
         }
       stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
     cp_wait<0>();
-    // o[i][2 r + e]: row gr + 8 r, column VC group(2 c4 + e) + i, in units of 2^base
+    // o[i][2 r + e]: row gr + 8 r, column i of the VC of lane group 2 c4 + e; SLIM: o[i][2 e + r]: row 2 c4 + r, column 2 i + e of gr's.
+    // In units of 2^base.
     const float unit = base > NO_BASE ? exponent_of_2((int)base) : 1.0f;
     const bool alone = s0 == 0 && s1 == steps;
     const int which = 2 * warp + (at + s1 - s0 == stop ? 1 : 0);  // a piece's place: the warp's first, or what it ends with
     float* sum = which & 1 ? reinterpret_cast<float*>(smem + warp * STAGES * STAGE_BYTES) : sums + warp * g.max_rows * D;
     if (!alone) {
       __syncwarp();  // the stages have been read
-      if (lane == 0) pieces[which] = {b * g.heads + head, b, first[b] + head * steps, steps};
+      if (lane == 0) pieces[which] = {first[b] + head * steps, steps, x.q0, rows, head};
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-      const int row = gr + 8 * r, token = row / g.group;
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], SLIM ? 4 : 1);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], SLIM ? 8 : 2);
+      if (SLIM) l[r] += __shfl_xor_sync(0xffffffffu, l[r], 16);
+      const int row = SLIM ? 2 * c4 + r : gr + 8 * r, token = row / g.group;
       if (row >= rows) continue;
       const float inv = !alone ? 1.0f : l[r] == 0.0f ? 0.0f : 1.0f / l[r];
-      auto value = [&](int i, int e) { return o[i][2 * r + e] * inv * unit; };
-      if (!alone && c4 == 0) ml[which][row] = make_float2(m[r], l[r]);
+      if (!alone && (SLIM ? gr : c4) == 0) ml[which][row] = make_float2(m[r], l[r]);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int n = 2 * c4 + e, col = VC * (D == 128 ? (n >> 1) | (n & 1) << 2 : n);
+      for (int e = 0; e < (SLIM ? 1 : 2); ++e) {
+        const int n = SLIM ? gr : 2 * c4 + e, col = VC * (D == 128 ? (n >> 1) | (n & 1) << 2 : n);
+        auto value = [&](int i) { return (SLIM ? o[i / 2][2 * (i & 1) + r] : o[i % OUT][2 * r + e]) * inv * unit; };
         if (alone) {
           uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + col;
 #pragma unroll
           for (int i = 0; i < VC / 8; ++i) {
             uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = pack<F16>(value(8 * i + 2 * k, e), value(8 * i + 2 * k + 1, e));
+            for (int k = 0; k < 4; ++k) w[k] = pack<F16>(value(8 * i + 2 * k), value(8 * i + 2 * k + 1));
             *reinterpret_cast<uint4*>(out + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < VC / 4; ++i)
-            *reinterpret_cast<float4*>(sum + row * D + col + 4 * i) =
-                make_float4(value(4 * i, e), value(4 * i + 1, e), value(4 * i + 2, e), value(4 * i + 3, e));
+            *reinterpret_cast<float4*>(sum + row * D + col + 4 * i) = make_float4(value(4 * i), value(4 * i + 1), value(4 * i + 2), value(4 * i + 3));
         }
       }
     }
     at += s1 - s0;
   }
-  // ---- the CTA's pieces, those of one head added up in the order of the keys; heads of several CTAs are left to the join ----
+  // ---- the CTA's pieces, those of one head added up in the order of the keys; heads of several CTAs are left to the join. A warp for 128
+  // columns of a row ----
   __syncthreads();
-  for (int k0 = 0; k0 < 2 * WARPS;) {
+  Piece mine = {};  // lane i's: piece i
+  if (lane < 2 * WARPS) mine = pieces[lane];
+  const uint32_t valid = __ballot_sync(0xffffffffu, mine.rows > 0);
+  const int before = __shfl_sync(0xffffffffu, mine.from, 31 - __clz(valid & ((1u << lane) - 1) | 1u));
+  uint32_t starts = __ballot_sync(0xffffffffu, mine.rows > 0 && ((valid & ((1u << lane) - 1)) == 0 || mine.from != before));
+  int turn = warp;
+  while (starts) {
+    const int k0 = __ffs(starts) - 1;
+    starts &= starts - 1;
+    const uint32_t these = valid & ~((1u << k0) - 1) & (starts ? (starts & -starts) - 1 : 0xffffffffu);
     const Piece x = pieces[k0];
-    int k1 = k0 + 1;
-    while (k1 < 2 * WARPS && (pieces[k1].item == x.item || pieces[k1].item < 0)) ++k1;
-    if (x.item < 0) {
-      ++k0;
-      continue;
-    }
-    const int head = x.item - x.b * g.heads;
-    const Lengths len = lengths_of(g, x.b);
     const bool whole = x.from >= c0 && x.from + x.steps <= c1;
-    const int rows = len.n * g.group;
-    for (int slot = threadIdx.x; slot < rows * (D / 4); slot += THREADS) {
-      const int row = slot / (D / 4), col = slot % (D / 4) * 4;
-      float top = -INFINITY;
-      for (int k = k0; k < k1; ++k)
-        if (pieces[k].item >= 0 && ml[k][row].y != 0.0f) top = fmaxf(top, ml[k][row].x);
-      float all = 0.0f;
+    const int slots = x.rows * (D / 4);
+    for (; turn * 32 < slots; turn += WARPS) {
+      const int slot = turn * 32 + lane, row = slot / (D / 4), col = slot % (D / 4) * 4;
+      if (slot >= slots) continue;
+      float top = -INFINITY, all = 0.0f;
       float4 acc = make_float4(0, 0, 0, 0);
-      for (int k = k0; k < k1; ++k) {
-        if (pieces[k].item < 0) continue;
-        const float2 v = ml[k][row];
-        const float e = v.y != 0.0f ? fast_exp2(v.x - top) : 0.0f;
-        const float* from = k & 1 ? reinterpret_cast<const float*>(smem + (k >> 1) * STAGES * STAGE_BYTES) : sums + (k >> 1) * g.max_rows * D;
-        const float4 o = *reinterpret_cast<const float4*>(from + row * D + col);
-        all += v.y * e;
-        acc.x += o.x * e;
-        acc.y += o.y * e;
-        acc.z += o.z * e;
-        acc.w += o.w * e;
+      for (uint32_t rest = these; rest;) {
+        float2 v[4];
+        float4 o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = rest ? __ffs(rest) - 1 : k0;
+          v[i] = ml[k][row];
+          o[i] = *reinterpret_cast<const float4*>(
+              (k & 1 ? reinterpret_cast<const float*>(smem + (k >> 1) * STAGES * STAGE_BYTES) : sums + (k >> 1) * g.max_rows * D) + row * D + col);
+          if (rest == 0) {  // no piece
+            v[i].y = 0.0f;
+            o[i] = make_float4(0, 0, 0, 0);
+          }
+          rest &= rest - 1;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add_piece(top, all, acc, v[i], o[i]);
       }
       if (whole) {
         const float inv = all == 0.0f ? 0.0f : 1.0f / all;
         const int token = row / g.group;
-        uint16_t* out = g.o + (int64_t)(len.q0 + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + col;
+        uint16_t* out = g.o + (int64_t)(x.q0 + token) * g.ldo + (int64_t)(x.head * g.group + row - token * g.group) * D + col;
         *reinterpret_cast<uint2*>(out) = make_uint2(pack<F16>(acc.x * inv, acc.y * inv), pack<F16>(acc.z * inv, acc.w * inv));
-      } else {  // a head that began before this CTA's run: the first of its two places, else the second
-        float* to = g.partial + (((int64_t)blockIdx.x * 2 + (x.from < c0 ? 0 : 1)) * g.max_rows + row) * (D + 2);
-        if (col == 0) *reinterpret_cast<float2*>(to + D) = make_float2(top, all);
-        *reinterpret_cast<float2*>(to + col) = make_float2(acc.x, acc.y);
-        *reinterpret_cast<float2*>(to + col + 2) = make_float2(acc.z, acc.w);
+      } else {
+        float* to = g.partial + (2 * blockIdx.x + (x.from < c0 ? 0 : 1)) * place_floats<D>(g.max_rows);
+        if (col == 0) reinterpret_cast<float2*>(to + g.max_rows * D)[row] = make_float2(top, all);
+        *reinterpret_cast<float4*>(to + row * D + col) = acc;
       }
     }
-    k0 = k1;
+    turn -= (slots + 31) / 32;  // the next head's go on with the warps that had none of this one's
+    if (c8.whole == 0 && threadIdx.x == 0 && x.from + x.steps > c1)
+      c8.cuts[blockIdx.x] = make_int4(x.q0, x.rows, x.from / dealt.run << 16 | (x.from + x.steps - 1) / dealt.run, 1 + x.head);
   }
 }
 
+// Adds up the pieces of a head that several CTAs worked on, in the order of the keys. Two latencies and a launch, 2.5 us: a head of n + 1
+// pieces has n CTAs here, those whose run ends within it, and each takes its share of the columns, so that a hundred heads of two pieces and eight
+// of twenty spread alike, a load or two to a thread, over CTAs that have all begun before the pieces are there. (With CTAs for every
+// head and share of columns, cut or not, most of which begin after the others: 5 us; 16 sequences of 4000 keys, 8 heads, 39.0 and here 34.0 us.)
+template <bool F16, int D>
+__global__ void __launch_bounds__(THREADS) attention_join_q8(const RowArgs g, const RowsQ8 c8) {
+  __shared__ float2 sh_ml[THREADS];
+  __shared__ float4 sh_o[THREADS];
+  pdl_launch_dependents();
+  pdl_wait_primary();
+  const int w = (int)blockIdx.x;
+  const int4 x = __ldcg(c8.cuts + w);
+  if (x.w == 0) return;
+  const int w0 = x.z >> 16, w1 = x.z & 0xffff, n = w1 - w0, rows = x.y, head = x.w - 1;
+  const int slots = rows * (D / 4), share = (slots + n - 1) / n, end = min((w - w0 + 1) * share, slots);
+  const int64_t place = place_floats<D>(g.max_rows);
+  for (int from = (w - w0) * share; from < end; from += THREADS) {
+    const int here = min(end - from, THREADS), groups = min(THREADS / here, n + 1);
+    const int group = (int)threadIdx.x / here, slot = from + (int)threadIdx.x - group * here;
+    const int row = slot / (D / 4), col = slot % (D / 4) * 4;
+    float top = -INFINITY, all = 0.0f;
+    float4 acc = make_float4(0, 0, 0, 0);
+    if (group < groups) {
+      for (int v = w0 + group; v <= w1; v += groups) {
+        const float* p = g.partial + (2 * v + (v == w0 ? 1 : 0)) * place;
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(p + g.max_rows * D) + row);
+        const float4 o = __ldcg(reinterpret_cast<const float4*>(p + row * D + col));
+        add_piece(top, all, acc, ml, o);
+      }
+      sh_ml[threadIdx.x] = make_float2(top, all);
+      sh_o[threadIdx.x] = acc;
+    }
+    __syncthreads();
+    if (group == 0) {
+      for (int k = 1; k < groups; ++k) add_piece(top, all, acc, sh_ml[threadIdx.x + k * here], sh_o[threadIdx.x + k * here]);
+      const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+      const int token = row / g.group;
+      uint16_t* out = g.o + (int64_t)(x.x + token) * g.ldo + (int64_t)(head * g.group + row - token * g.group) * D + col;
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack<F16>(acc.x * inv, acc.y * inv), pack<F16>(acc.z * inv, acc.w * inv));
+    }
+    __syncthreads();
+  }
+}
+
+template <bool F16, int D, bool SLIM>
+cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
+  const int64_t ctas = rows_grid();
+  const size_t smem = (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4) + first_bytes(g);
+  const cudaError_t e = launch_rows<attention_rows_q8<F16, D, SLIM>>(ctas, smem, stream, g, c8);
+  if (e != cudaSuccess || c8.whole || ctas == 1) return e;
+  return launch_rows<attention_join_q8<F16, D>>(ctas - 1, 0, stream, g, c8);
+}
 template <bool F16, int D>
 cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
-  return launch_rows_and_join<F16, D, attention_rows_q8<F16, D>>(g, (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4),
-                                                                 c8.whole == 0, stream, c8);
+  return g.max_rows <= 8 ? launch_rows_q8<F16, D, true>(g, c8, stream) : launch_rows_q8<F16, D, false>(g, c8, stream);
 }
 
 }  // namespace
@@ -435,9 +567,12 @@ cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stre
 int launch_attention_rows_q8(const PifaAttention& a, int* status, cudaStream_t stream) {
   const RowArgs g = row_args(a, status);
   const int64_t heads = a.B * a.cache.heads, ctas = rows_grid();
-  const int64_t share = (heads + ctas - 1) / ctas, whole = share * a.cols * a.cache.page_size <= WHOLE_KEYS ? share : 0;
+  const int64_t share = (heads + ctas - 1) / ctas, room = a.cols * a.cache.page_size;
+  const bool uncut = share * room <= (share == 1 ? WHOLE_KEYS_ONE : WHOLE_KEYS) && (share * ctas - heads) * room <= WHOLE_MORE * ctas;
+  const int64_t places = 2 * MAX_CTAS * (a.cache.dim == 64 ? place_floats<64>(g.max_rows) : place_floats<128>(g.max_rows));
   const RowsQ8 c8 = {static_cast<const uint8_t*>(a.k), static_cast<const uint8_t*>(a.v), a.q8->k, a.q8->v, a.q8->shape.page_stride,
-                     a.q8->shape.block_stride, a.q8->shape.head_stride, (int)whole};
+                     a.q8->shape.block_stride, a.q8->shape.head_stride, uncut ? (int)share : 0,
+                     reinterpret_cast<int4*>(g.partial + places)};
   const bool f16 = a.dtype == PIFA_DTYPE_FP16;
   cudaError_t e;
   if (a.cache.dim == 64) e = f16 ? launch_rows_q8<true, 64>(g, c8, stream) : launch_rows_q8<false, 64>(g, c8, stream);
