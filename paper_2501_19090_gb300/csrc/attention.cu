@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
   pdl_wait_primary();
   pdl_launch_dependents();  // (after the wait: the join reads the lengths before its own)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Run steps_here = deal_steps(g, first, part, (int)gridDim.x * WARPS, MIN_STEPS);
+  const Run steps_here = deal_steps(g, first, part, (int)gridDim.x * WARPS, MIN_STEPS, [](int, const Lengths&) {});
   const int total = steps_here.total, run = steps_here.run;
   if (blockIdx.x == 0) {  // written down for the join
     for (int b = (int)threadIdx.x; b <= g.B; b += THREADS) g.sums[b] = first[b];

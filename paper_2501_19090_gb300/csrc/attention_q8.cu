@@ -21,6 +21,7 @@
 // the CTA 73 and 52; by TMA, scales of 32 steps at a time 69 and 51; copies by the warps' lanes again 65 and 47.
 // Not taken: the next step's scores beside this step's weights (71 and 53: a stage less in flight), copies that run over the ends of
 // segments (73 and 53: their bookkeeping is in every step).
+#include <algorithm>
 #include <cmath>
 
 #include "attention_rows.cuh"
@@ -61,6 +62,9 @@ constexpr int LEAST = WARPS;      // steps of a CTA (one sequence of 351 keys, 3
 // CTAs: 40 sequences, 8 heads, of 300 16.0 and 15.2, of 175 to 700 17.3 and 18.7.)
 constexpr int WHOLE_MORE = 768, WHOLE_KEYS_ONE = 2048, WHOLE_KEYS = 1024;
 
+// Lengths of so many requests are kept in shared memory (a look at them in memory takes 730 cycles each time).
+constexpr int KEPT = 512;
+
 // What a warp has summed up of a head that it did not finish alone: in shared memory, for the CTA to add up.
 struct Piece {
   int from, steps, q0, rows, head;  // the head's first step and its steps; its first row of Q and its rows (0: no piece)
@@ -88,24 +92,27 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
   extern __shared__ __align__(128) uint8_t smem[];
   // of each warp its first head's piece; its last one's takes the place of its stages when those are done
   float* sums = reinterpret_cast<float*>(smem + WARPS * STAGES * STAGE_BYTES);
-  int* first = reinterpret_cast<int*>(sums + WARPS * g.max_rows * D);  // B + 1
   static_assert(STAGES * STAGE_BYTES >= ROWS * D * 4, "a piece fits into a warp's stages");
+  Lengths* kept = reinterpret_cast<Lengths*>(sums + WARPS * g.max_rows * D);
+  int* first = reinterpret_cast<int*>(kept + min(g.B, KEPT));  // B + 1
   __shared__ int part[32];
   __shared__ Piece pieces[2 * WARPS];
   __shared__ float2 ml[2 * WARPS][ROWS];
   const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5);
   pdl_wait_primary();
   pdl_launch_dependents();  // (after the wait: the join reads the lengths before its own)
-  const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST);
+  const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST, [&](int b, const Lengths& x) {
+    if (b < KEPT) kept[b] = x;
+  });
+  auto lengths = [&](int b) { return b < KEPT ? kept[b] : lengths_of(g, b); };
 
   // ---- this CTA's run of steps, this warp's share of it: segments of one request and head each ----
-  auto begin_of = [&](int i) {  // this CTA's first step (i = 0), the next one's (1)
-    const int64_t k = (int64_t)(blockIdx.x + i) * (c8.whole ? c8.whole : dealt.run);
-    if (c8.whole == 0 || dealt.total == 0 || k >= g.B * g.heads) return (int)(c8.whole ? dealt.total : min(k, (int64_t)dealt.total));
-    const int b = (int)k / g.heads;
-    return first[b] + ((int)k - b * g.heads) * steps_of(lengths_of(g, b));
+  auto begin_of = [&](uint32_t cta) {  // a CTA's first step
+    if (c8.whole == 0) return (int)min(cta * (uint32_t)dealt.run, (uint32_t)dealt.total);
+    const uint32_t k = cta * (uint32_t)c8.whole, b = k / (uint32_t)g.heads;
+    return b >= (uint32_t)g.B || dealt.total == 0 ? dealt.total : first[b] + (int)(k - b * g.heads) * steps_of(lengths(b));
   };
-  const int c0 = begin_of(0), c1 = begin_of(1);
+  const int c0 = begin_of(blockIdx.x), c1 = begin_of(blockIdx.x + 1);
   if (threadIdx.x == 0 && c8.whole == 0) c8.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (c0 == c1) return;
   const int share = (c1 - c0 + WARPS - 1) / WARPS;
@@ -119,8 +126,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
   const int piece = lane % PIECES, key0 = lane / PIECES;
   while (at < stop) {
     const int b = find(first, g.B, at);
-    const Lengths x = lengths_of(g, b);
-    const int steps = steps_of(x), head = (at - first[b]) / steps, s0 = at - first[b] - head * steps;
+    const Lengths x = lengths(b);
+    const int steps = steps_of(x), head = (int)((uint32_t)(at - first[b]) / (uint32_t)steps), s0 = at - first[b] - head * steps;
     const int s1 = min(steps, s0 + stop - at);
     const int rows = x.n * g.group;
     // The rows of Q: this lane's are gr (and gr + 8; SLIM: of the products' results, 2 c4 and 2 c4 + 1). Asked for before the copies, whose
@@ -552,7 +559,7 @@ __global__ void __launch_bounds__(THREADS) attention_join_q8(const RowArgs g, co
 template <bool F16, int D, bool SLIM>
 cudaError_t launch_rows_q8(const RowArgs& g, const RowsQ8& c8, cudaStream_t stream) {
   const int64_t ctas = rows_grid();
-  const size_t smem = (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4) + first_bytes(g);
+  const size_t smem = (size_t)WARPS * (kStages<D> * 2 * STEP * D + g.max_rows * D * 4) + (size_t)std::min(g.B, KEPT) * sizeof(Lengths) + first_bytes(g);
   const cudaError_t e = launch_rows<attention_rows_q8<F16, D, SLIM>>(ctas, smem, stream, g, c8);
   if (e != cudaSuccess || c8.whole || ctas == 1) return e;
   return launch_rows<attention_join_q8<F16, D>>(ctas - 1, 0, stream, g, c8);

@@ -88,11 +88,12 @@ __device__ __forceinline__ int find(const int* first, int n, int v) {
 }
 
 // The requests' first steps, into first[0, B], how many there are, and the share of each worker, at least `least` (all threads of
-// the CTA).
+// the CTA); what `keep(b, lengths)` leaves in shared memory is there as well.
 struct Run {
   int total, run;
 };
-__device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* part, int workers, int least) {
+template <class Keep>
+__device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* part, int workers, int least, Keep keep) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int total = 0;
   bool over = false, falls = false;
@@ -104,6 +105,7 @@ __device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* par
       over |= g.kv_len[b] > (g.cols << g.page_shift) || (int64_t)g.q_start[b + 1] - g.q_start[b] > x.n;
       falls |= g.q_start[b + 1] < g.q_start[b];
       v = steps_of(x) * g.heads;
+      keep(b, x);
     }
     int a = v;
 #pragma unroll
