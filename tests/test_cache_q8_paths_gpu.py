@@ -84,6 +84,34 @@ def test_heads_that_are_not_cut(lens, hq, hk, d, dtype):
         check_attention(b, O, d ** -0.5)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hk,new", [(1, 1, 1), (7, 1, 1), (16, 2, 1), (18, 2, 1), (4, 2, 3), (5, 1, 3), (2, 1, 8), (16, 1, 1), (1, 1, 16)])
+def test_heads_that_are_cut(hq, hk, new, d):
+    """One to sixteen rows a key / value head, heads in two pieces and in many, beside short ones and one without keys."""
+    lens = [9000, 17, 0, 300, 2500, 16, 40000]
+    news = [min(new, n) for n in lens]
+    for pick in (slice(0, 7), slice(6, 7), slice(1, 5)):
+        a = make_q8(32, lens[pick], news[pick], hq, hk, d, 64, torch.bfloat16)
+        O = torch.full_like(a["Q"], math.nan)
+        attend(a, max_q=new, O=O)
+        check_attention(a, O, d ** -0.5)
+        again = attend(a, max_q=new, O=torch.full_like(O, math.nan))
+        assert torch.equal(O, again)
+
+
+@pytest.mark.parametrize("B", [511, 513, 4096])
+@pytest.mark.parametrize("cols", [None, 700])
+def test_many_requests(B, cols):
+    """More requests than there are CTAs, threads of one, and lengths that it keeps at hand; the long ones last."""
+    lens = [(7 * b * b + 3 * b) % 90 for b in range(B - 3)] + [2000, 1, 3000]
+    a = make_q8(33, lens, [min(n, 1) for n in lens], 4, 2, 128, 16, torch.float16)
+    if cols:
+        a = dict(a, table=torch.nn.functional.pad(a["table"], (0, cols - a["table"].shape[1]), value=-1).contiguous())
+    O = torch.full_like(a["Q"], math.nan)
+    attend(a, max_q=1, O=O)
+    check_attention(a, O, 128 ** -0.5)
+
+
 @pytest.fixture
 def _bound():
     yield
