@@ -6,21 +6,26 @@
 // Few rows (decode and its neighbours, up to 16 a key / value head) are here; more are attention_tc.cu's. Bound by the cache's bytes, of
 // which there are half as many as in 16 bits, so that the instructions a byte count twice: a step of 16 keys, one block of scales,
 // costs a warp 8 copies of 16 bytes a lane, 64 conversions of two e4m3 numbers to fp16 (at two cycles each, as all but plain fp32), 16
-// permutations that pair V's rows, 32 mma.sync, and as little as possible beside them: pages and scales are looked up for 32 steps
-// at once, a lane for each; keys are compared with what a row sees only in steps where some row does not see all; copies have bounds only in
-// a request's last step. The scales' part in softmax is in q8.cuh.
+// permutations that pair V's rows, 16 mma.sync (up to 8 rows, SLIM: they are the second operand's 8 columns, K's keys and V's columns
+// the first operand's 16 rows; with 9 to 16 rows, the first operand's, 32), and as little as possible beside them: pages and scales are looked
+// up for 32 steps at once, a lane for each; keys are compared with what a row sees only in steps where some row does not see all; copies
+// have bounds only in a request's last step. The scales' part in softmax is in q8.cuh.
 // All steps, in the order (request, head, step), are dealt to CTAs in equal runs, a run to the CTA's eight warps; each streams its steps by
 // itself. Pieces of heads that fell to several warps are added up in shared memory at the end, those of heads that fell to
 // several CTAs by the join.
 //
-// Measured, head_dim 128, bf16, 64 heads on 8 key / value heads: 64 sequences of 500 to 20000 keys (273 MB) 65 us, 4.2 TB/s; one of 100000
-// (205 MB) 47 us, 4.3 TB/s; one of 800000 (1.64 GB) 279 us, 5.9 TB/s. A kernel that only reads takes 43 to 47, 34 to 36 and 229 to
-// 256 us for as many bytes. About 5 us are the join, 5 to 7 the start (lengths, table, first copies), the rest SMs that get
-// less from memory than others (equal shares of a plain read end between 19 and 30 us). One sequence of 351 keys, 32 heads: 8.3 us.
-// Steps: a warp for each row 20.5 and 130 ms (first two cases); pieces of warps, joined by the second kernel 73 and 62 us; pieces added up in
-// the CTA 73 and 52; by TMA, scales of 32 steps at a time 69 and 51; copies by the warps' lanes again 65 and 47.
+// Measured, head_dim 128, bf16, 64 heads on 8 key / value heads: 64 sequences of 500 to 20000 keys (273 MB) 58 to 62 us, 4.4 to 4.7
+// TB/s; one of 100000 (205 MB) 40 us, 5.1 TB/s; one of 800000 (1.64 GB) 254 us, 6.5 TB/s. A kernel that only reads takes 43 to 47, 34 to
+// 36 and 229 to 256 us for as many bytes. One sequence of 351 keys, 32 heads: 6.7 us. Between the first data and the last, memory is the bound (100000
+// keys: 7.4 TB/s); before it are 9 to 10 thousand cycles of lengths, dealing, table, first copies, mostly their latencies and first fetches of
+// code, behind it 4 to 5 thousand of adding up, and the join, 2.5 us.
+// Steps (first two cases): a warp for each row 20.5 and 130 ms; pieces of warps, joined by the second kernel 73 and 62 us; pieces added up in
+// the CTA 73 and 52; by TMA, scales of 32 steps at a time 69 and 51; copies by the warps' lanes again 65 and 47; four sums of products in turn
+// and places of 32 steps 65 and 45; SLIM 63.8 and 44.0; a join of cut heads only 61.9 and 42.3; pieces added up by all warps without lengths,
+// Q asked for before the copies 61.4 and 40.5.
 // Not taken: the next step's scores beside this step's weights (71 and 53: a stage less in flight), copies that run over the ends of
-// segments (73 and 53: their bookkeeping is in every step).
+// segments (73 and 53: their bookkeeping is in every step), 12 warps of three stages or 10 of four (67.4 and 45.5, 69.6 and 49.0), five stages (66.1
+// and 45.6), a CTA's warps on neighbouring heads of the same tokens (46.2 for the second: DRAM's pages are not the bound).
 #include <algorithm>
 #include <cmath>
 
