@@ -120,9 +120,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
   const int c0 = begin_of(blockIdx.x), c1 = begin_of(blockIdx.x + 1);
   if (threadIdx.x == 0 && c8.whole == 0) c8.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
   if (c0 == c1) return;
-  const int share = (c1 - c0 + WARPS - 1) / WARPS;
-  int at = min(c0 + warp * share, c1);
-  const int stop = min(at + share, c1);
+  const uint32_t share = (uint32_t)(c1 - c0 + WARPS - 1) / WARPS;  // (c1 may be close to 2^31)
+  int at = (int)min((uint32_t)c0 + warp * share, (uint32_t)c1);
+  const int stop = (int)min((uint32_t)at + share, (uint32_t)c1);
   if (lane < 2) pieces[2 * warp + lane].rows = 0;
   __syncwarp();
   const int gr = lane >> 2, c4 = lane & 3;

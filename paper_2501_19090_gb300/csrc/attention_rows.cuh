@@ -27,8 +27,8 @@ struct RowArgs {
   const uint16_t *q, *k, *v;
   uint16_t* o;
   const int32_t *table, *q_start, *kv_len;
-  int* sums;          // B + 1: first step of each request (times heads), then the steps of one worker (0: nothing is done)
-  float* partial;     // for each worker, a warp or a CTA, two of max_rows x (D + 2): O, m, l
+  int* sums;          // (of a cache in 16 bits) B + 1: first step of each request (times heads), then the steps of one worker (0: nothing is done)
+  float* partial;     // for each worker, a warp or (8 bits) a CTA, two pieces of max_rows: O, m, l
   int64_t ldq, ldo, ldt, page_stride, token_stride, head_stride, pages;
   int T, heads, group, page_size, page_shift, cols, B, max_q, max_rows;
   float c;            // |scale| log2(e), with scale's sign in `flip`
@@ -129,7 +129,7 @@ __device__ __forceinline__ Run deal_steps(const RowArgs& g, int* first, int* par
   // requests that overlap: which of them a row belongs to is not said, so nothing is done
   const bool overlap = __syncthreads_or(falls);
   if (overlap) total = 0;
-  const int run = max((total + workers - 1) / workers, least);
+  const int run = max((total - 1) / workers + 1, least);  // (total may be close to 2^31)
   if (blockIdx.x == 0) {
     if (tid == 0 && overlap) latch_status(g.status, PIFA_ERR_DEVICE_INDEX);
     if (over) latch_status(g.status, PIFA_ERR_CAPACITY);
