@@ -8,9 +8,9 @@
 //
 // Bound by memory. The write: a stretch, the neighbouring rows of one block, and one head go to one or some warps, which hold all its
 // elements in registers from the rotation over the maximum to the rounding: every element is read and written once. CTAs of their own
-// turn queries in the same launch. Few tokens (decode): a chain of latencies, slots and cosines, rows, scale.
+// turn queries in the same launch. Few tokens (decode): a chain of latencies, slots and cosines, rows, scale, and rounds of CTAs.
 // Measured, head_dim 128, bf16: 8192 tokens of 64 + 8 + 8 heads (318 MB) 59 us, 5.4 TB/s (the queries alone 47); 200 sequences in decode
-// 6.0, 8 sequences, 32 + 32 + 32 heads, 3.6; reading back 50001 tokens of 8 heads (307 MB) 50.5 us, 6.1 TB/s.
+// 5.0, 8 sequences, 32 + 32 + 32 heads, 3.5; reading back 50001 tokens of 8 heads (307 MB) 50.5 us, 6.1 TB/s.
 #include <cmath>
 
 #include "q8.cuh"
@@ -417,6 +417,19 @@ int pifa_rope_cache_q8(const void* Q, int64_t ldq, const void* K, int64_t ldk, c
   const int windows = (t + g.window - 1) / g.window, heads = 2 * (int)kv_heads;
   int parts = (2 * sms + windows - 1) / windows;
   if (parts > (heads + 7) / 8) parts = (heads + 7) / 8;
+  if (t < FEW_TOKENS) {
+    // A second round of CTAs costs 2 us. So: no more that store than make a difference to their turns of eight warps, and where those of
+    // the queries do not begin in the first round beside them, two CTAs an SM, they take more tokens each if then they do. (200 sequences in
+    // decode, 64 + 8 + 8 heads: 5.9 us and 5.0; 64 of 32 + 32 + 32: 7.3 and 5.3.)
+    const int turns = ((heads + parts - 1) / parts + 7) / 8;
+    parts = (heads + 8 * turns - 1) / (8 * turns);
+    const int left = 2 * sms - windows * parts, q_ctas = (t + g.q.tokens - 1) / g.q.tokens * g.q_parts;
+    if (q_ctas > left && left >= (t + MAX_TOKENS - 1) / MAX_TOKENS) {
+      g.q.tokens = (t + left - 1) / left;
+      g.q.heads = (int)q_heads;
+      g.q_parts = 1;
+    }
+  }
   g.kv_heads = (heads + parts - 1) / parts;
   g.kv_parts = (heads + g.kv_heads - 1) / g.kv_heads;
   g.kv_ctas = windows * g.kv_parts;
