@@ -220,6 +220,30 @@ def test_write_of_many_tokens_equals_that_of_few(d, dtype):
         assert bool(((a == b) | (((a - b).abs() <= 2.0 ** -9) & (b.abs() <= 2.0 ** -6))).all())
 
 
+@pytest.mark.parametrize("hq,hk,d", [(64, 8, 128), (32, 32, 128), (40, 5, 64), (3, 1, 512)])
+@pytest.mark.parametrize("T", [33, 64, 100, 181, 200, 303, 607])
+def test_tokens_of_many_requests_equal_those_of_few(T, hq, hk, d):
+    """However tokens, heads and queries are dealt to CTAs: the bytes of the cache, and the queries, are those of calls of eight tokens."""
+    g = torch.Generator(DEV).manual_seed(T + hq)
+    x = torch.randn((T, hq + 2 * hk, d), device=DEV, generator=g)
+    x[:, hq:] *= torch.exp2(torch.randint(-6, 7, (T, 2 * hk, 1), device=DEV, generator=g).float())
+    x = x.to(torch.bfloat16)
+    Q, K, V = x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+    at = torch.randperm(T, device=DEV, generator=g) * 16 + torch.randint(0, 16, (T,), device=DEV, generator=g)  # a block each
+    pos = torch.randint(0, 100000, (T,), device=DEV, generator=g).int()
+    freq = P.pifa_rope_frequencies(d // 2, device=DEV)
+    one = empty_cache((T + 3) // 4, 64, hk, d, byte=0x35)
+    one[2].view(U8).random_(110, 140, generator=g)
+    one[3].view(U8).random_(110, 140, generator=g)
+    all_at_once = [c.clone() for c in one]
+    want = torch.cat([P.pifa_rope_cache_q8(Q[i:i + 8], K[i:i + 8], V[i:i + 8], pos[i:i + 8], at[i:i + 8], freq, *one) for i in range(0, T, 8)])
+    got = P.pifa_rope_cache_q8(Q, K, V, pos, at, freq, *all_at_once)
+    assert P.pifa_device_status() == P.PIFA_OK
+    assert torch.equal(got, want) and torch.equal(got, P.pifa_rope(Q, pos, freq))
+    for a, b in zip(one, all_at_once):
+        assert torch.equal(a.view(U8), b.view(U8))
+
+
 def test_calls_of_nothing():
     cache = empty_cache(3, 16, 2, 64)
     e = torch.empty
