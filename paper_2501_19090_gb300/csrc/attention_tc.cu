@@ -38,8 +38,9 @@
 // that leave little of shared memory's time; and instruction fetch: all of a warp's rows unrolled (10 KB more) took a tile's softmax from
 // 2650 to 3750 cycles. Chunks whose rows would convert the same keys several times have them converted once, by a kernel that makes
 // the plan too, and run as above. Measured, head_dim 128: 2048 tokens over 30000 cached, 64 heads on 8: 1.79 ms with conversion inside,
-// 1.35 to 1.40 with it before (36 us of it; 1.25 in 16 bits); a prompt of 1900, 32 heads, 69 and 53 us (9; 38.5); 512 rows a head
-// over 30000, 8 heads: 88 and 100.
+// 1.34 to 1.40 with it before (36 us of it; a cache in 16 bits of the same values 1.36); a prompt of 1900, 32 heads, 69 and 53 us (12; 48.5);
+// 512 rows a head over 30000, 8 heads: 88 and 100. These keys have a few large columns: on normal ones, whose running maxima
+// rise less often, 16 bits take 1.23 ms and 37.6 us.
 //
 // Measured, head_dim 128, bf16: 2048 tokens over 30000 cached, 64 heads on 8 key / value heads, pages of 64: 1.20 to 1.27 ms,
 // 1640 to 1740 TFLOP/s of the visible pairs (the measured bf16 rate is 1910 in a burst, 1702 for seconds: the power cap is what
