@@ -484,7 +484,8 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
  *   may reach the request's other new tokens too (0 times infinity). A K that is not finite stays with the tokens
  *   that see it.
  *   Numerics: fp32 scores, running maximum and sums; the weights enter the second product in dtype, at most 2^8 (the
- *   maximum that they refer to is raised when a score passes it by 8 in the exponent), O is rounded once. Results
+ *   maximum that they refer to is raised when a score passes it by 8 in the exponent; in fp16 those below 2^-14 of it are off by
+ *   2^-25 of it), O is rounded once. Results
  *   do not depend on the order in which blocks run; where the keys are cut, and with it the last bits, follows
  *   from the lengths of all requests of the call.
  */
@@ -552,9 +553,10 @@ int pifa_cache_read_q8(const void* k_cache, const void* v_cache, const void* k_s
  *   As there, but for: the caches and scales, as above; page_size a power of two from 16 to 256.
  *   Numerics: Q enters the first product in fp16, in bf16's case times a power of two for each row that brings its largest
  *   magnitude to [2^14, 2^15); keys and values enter as fp16, which holds e4m3 exactly, without their scales, which are applied in fp32
- *   (the keys') or as part of the weights' exponent (the values'). Weights are fp16, at most 2^8; scores, running maximum and sums fp32.
- *   Of long chunks, with room for it (pifa_paged_attention_q8_workspace_size), keys and values are rounded to dtype once, and all else
- *   is as in pifa_paged_attention.
+ *   (the keys') or as part of the weights' exponent (the values'). Weights are fp16, held so that the largest lie between 2^7 and 2^15
+ *   (those below 2^-21 of the largest are off by 2^-32 of it); scores, running maximum and sums fp32.
+ *   Of long chunks, with room for it (pifa_paged_attention_q8_workspace_size), keys and values are rounded to dtype once, the weights are
+ *   of dtype (fp16: held as said), and all else is as in pifa_paged_attention.
  */
 int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                             int dtype, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,

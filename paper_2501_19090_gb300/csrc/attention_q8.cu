@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
           w[k][0] = u.x, w[k][1] = u.y;
         }
       }
-      // exponents of the weights times their value's scale, relative to m; keys that a row does not see: v[r][k] is row r's of the lane
+      // exponents of the weights times their value's scale, relative to m (the maximum less LIFT); keys that a row does not see: v[r][k] is row r's of the lane
       constexpr int EACH = SLIM ? 2 : 4;  // keys of a lane's row
       auto key_at = [&](int k) { return s * STEP + key_of<D>(SLIM ? gr + 8 * k : 8 * (k >> 1) + c4 * 2 + (k & 1)); };
       float v[2][EACH];
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
       for (int r = 0; r < 2; ++r) {
         top[r] = fmaxf(v[r][0], v[r][1]);
         if constexpr (!SLIM) top[r] = max3(top[r], v[r][2], v[r][3]);
-        grows |= top[r] > m[r] + 8.0f;
+        grows |= top[r] > m[r] + RISE;
       }
       if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
             top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
             top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
           }
-          top[r] = fmaxf(top[r], m[r]);
+          top[r] = fmaxf(top[r] - LIFT, m[r]);
           const float f = top[r] > m[r] ? fast_exp2(m[r] - top[r]) : 1.0f;  // 0 where nothing was seen before
           m[r] = top[r];
           l[r] *= f;

@@ -124,6 +124,7 @@ struct TcArgs {
        most_keys, page_size, page_shift;  // most_keys: that the table has room for
   int token_at, head_at;             // their places among the tensor maps' coordinates 1 to 3; the page has the third
   float c;                           // |scale| log2(e)
+  float lift;                        // weights are held 2^lift times as large; 0 for a cache in 16 bits
   int negate;                        // scale < 0
   int wide;                          // rows of O start on 32-byte sectors
   int* status;
@@ -998,7 +999,7 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
             mbar_arrive(&p_full[2 * t + 1]);
           }
         } else if constexpr (Q8) {
-          // As below, but that m is in the exponents' units and holds the values' scale.
+          // As below, but that m is in the exponents' units, holds the values' scale, and is the maximum less LIFT.
           const int tile = tiles + j - it.j0;
           if (!wait(&scales_full[tile % SCALED], (uint32_t)(tile / SCALED) & 1u)) break;
           const TileScales sc = scales[tile % SCALED];
@@ -1044,10 +1045,10 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
               sum[0] = sum[1] = 0;
 #pragma unroll
               for (int i = 0; i < EARLY; ++i) weights(i);
-              if (!__any_sync(0xffffffffu, top - m > 8.0f)) break;
+              if (!__any_sync(0xffffffffu, top - m > RISE)) break;
             }
             fresh = false;
-            const float most = fmaxf(m, top);
+            const float most = fmaxf(m, top - LIFT);
             float f = m > -INFINITY ? fast_exp2(m - most) : 1.0f;  // (nothing was seen before: zeros)
             m = most;
             l *= f;
@@ -1075,7 +1076,7 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
           uint32_t w[4][16];
           const uint64_t c2 = f32x2(c, c);
           auto weights = [&](int i) {  // keys 32 i to 32 i + 31
-            const float mc = m > -INFINITY ? -m * c : 0.0f;
+            const float mc = m > -INFINITY ? fmaf(-m, c, g.lift) : 0.0f;
             const uint64_t mc2 = f32x2(mc, mc);
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
@@ -1378,6 +1379,7 @@ int launch_attention_tc(const PifaAttention& given, bool wide, int* status, uint
   g.wide = ((reinterpret_cast<uintptr_t>(a.o) | (uintptr_t)(a.ldo * 2)) & 31u) == 0;
   // equal weights for a scale of zero: the masked scores, -inf, still have to vanish
   g.c = a.scale_log2 == 0.0f ? 1e-30f : std::fabs(a.scale_log2);
+  g.lift = wide && a.dtype == PIFA_DTYPE_FP16 ? LIFT : 0.0f;
   g.status = status;
   g.timeout_ns = timeout_ns;
   CUtensorMap qmap, kmap, vmap;

@@ -18,6 +18,12 @@
 
 namespace pifa {
 
+// A running maximum is raised when a score passes it by 8 in the exponent, so that weights reach 2^8 of what it refers to, and fp16
+// goes to 2^15: weights are held 2^7 times as large (m is the maximum less 7; O and l are both in those units, which o = O / l is
+// rid of), and those below fp16's normal range are off by 2^-32 of the largest. They count: the tens of thousands of keys beside one
+// that has all but a millionth of the weight, and a value near zero, are all of o. (Without it, those 2^-25 of the largest and less were in l alone.)
+constexpr float LIFT = 7.0f, RISE = 8.0f + LIFT;
+
 constexpr float NO_BASE = -1000.0f;
 constexpr float FAR = 40.0f;
 
