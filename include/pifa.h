@@ -550,7 +550,8 @@ int pifa_cache_read_q8(const void* k_cache, const void* v_cache, const void* k_s
 
 /*
  * pifa_paged_attention_q8 -- pifa_paged_attention over a cache in 8 bits.
- *   As there, but for: the caches and scales, as above; page_size a power of two from 16 to 256.
+ *   As there, but for: the caches and scales, as above; page_size a power of two from 16 to 256. A scale that is NaN makes NaN of
+ *   the rows that see a token of its block, all columns, and of no others.
  *   Numerics: Q enters the first product in fp16, in bf16's case times a power of two for each row that brings its largest
  *   magnitude to [2^14, 2^15); keys and values enter as fp16, which holds e4m3 exactly, without their scales, which are applied in fp32
  *   (the keys') or as part of the weights' exponent (the values'). Weights are fp16, held so that the largest lie between 2^7 and 2^15

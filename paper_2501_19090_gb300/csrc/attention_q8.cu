@@ -346,6 +346,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
         }
       }
       if ((s + 1) * STEP > all_see) {
+        if (exponent != exponent) {  // the weights are NaN, where they are not zero: 0 times NaN must not be
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < VC / 4; ++i) w[k][i] = 0;
+        }
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll

@@ -400,18 +400,19 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan_widen(const TcArg
       if (h0 == 0 && token0 % WIDE_PAGE == 0) x.to_table[page] = page;
     }
     uint4 in[EACH];
-    float s[EACH];
+    int s[EACH];  // a row's scale, and from bit 8 on that of the values
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int row = (tid + i * PLAN_THREADS) / PIECES, piece = (tid + i * PLAN_THREADS) % PIECES;
       const int hh = h0 + row / PIFA_Q8_BLOCK, token = row % PIFA_Q8_BLOCK, head = hh < g.heads ? hh : hh - g.heads;
       in[i] = make_uint4(0, 0, 0, 0);
-      s[i] = 1.0f;
+      s[i] = 127 << 8 | 127;
       if (hh < 2 * g.heads && !bad) {
         const int in_page = token0 & (x.page_size - 1);
         const int64_t from = id * x.page_stride + (in_page + token) * x.token_stride + head * x.head_stride + piece * 16;
         in[i] = __ldg(reinterpret_cast<const uint4*>((hh < g.heads ? x.k : x.v) + from));
-        s[i] = scale_of((hh < g.heads ? g.ks : g.vs)[id * g.scale_page + in_page / PIFA_Q8_BLOCK * g.scale_block + head * g.scale_head]);
+        const int64_t scale = id * g.scale_page + in_page / PIFA_Q8_BLOCK * g.scale_block + head * g.scale_head;
+        s[i] = (int)(hh < g.heads ? g.ks : g.vs)[scale] | (int)g.vs[scale] << 8;
       }
     }
 #pragma unroll
@@ -419,11 +420,16 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan_widen(const TcArg
       const int row = (tid + i * PLAN_THREADS) / PIECES, piece = (tid + i * PLAN_THREADS) % PIECES;
       const int hh = h0 + row / PIFA_Q8_BLOCK, token = token0 + row % PIFA_Q8_BLOCK, head = hh < g.heads ? hh : hh - g.heads;
       if (hh >= 2 * g.heads) continue;
+      float f = scale_of(s[i] & 0xff);
+      if (s[i] >> 8 == 255) {  // of the values is NaN: the keys are, and the values zeros, as in the conversion of tiles
+        f = hh < g.heads ? __uint_as_float(0x7fffffffu) : 1.0f;
+        if (hh >= g.heads) in[i] = make_uint4(0, 0, 0, 0);
+      }
       uint32_t out[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const uint32_t w = (&in[i].x)[k / 2];
-        out[k] = scaled_from_e4m3x2<F16>(k & 1 ? w >> 16 : w & 0xffffu, s[i]);
+        out[k] = scaled_from_e4m3x2<F16>(k & 1 ? w >> 16 : w & 0xffffu, f);
       }
       uint16_t* to = (hh < g.heads ? x.to_k : x.to_v) + (((int64_t)page * g.heads + head) * WIDE_PAGE + token % WIDE_PAGE) * D + piece * 16;
       stg256(to, out);
@@ -793,10 +799,10 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&item_free[n & 1]);
         if (end) break;
-        // Lane i has the scale of the tile's block i (every warp of its own kind, the warp for K's scales the values' too, in lanes 8
-        // to 15); pages are read two tiles ahead, scales one.
+        // Lane i has the scale of the tile's block i (every warp of its own kind, K's the values' too, in lanes 8 to 15); pages are
+        // read two tiles ahead, scales one.
         const int32_t* pages = g.table + b * g.ldt;
-        const bool both = warp == 12;
+        const bool both = kv == 0;
         const uint8_t* from_scales = kv || lane >= 8 ? g.vs : g.ks;
         auto page_of = [&](int j) {
           const int key = j * BN + (lane & 7) * PIFA_Q8_BLOCK;
@@ -819,10 +825,14 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
           // Blocks are brought to the tile's largest scale by a power of two in fp16: exact unless that is below 2^-15, and
           // then off by 2^-25 at most, in units of which the tile's largest element is 224 or more.
           const int down = scale - most;
-          const uint32_t by = scale == NO_SCALE ? 0x3c00u : scale == 255 ? 0x7fffu : down >= -14 ? (uint32_t)(15 + down) << 10
-                              : down >= -24 ? 1u << (24 + down) : 0u;
+          uint32_t by = scale == NO_SCALE ? 0x3c00u : down >= -14 ? (uint32_t)(15 + down) << 10 : down >= -24 ? 1u << (24 + down) : 0u;
+          // A scale of NaN, of the values as well, makes the block's keys NaN, which is masked for rows that do not see them; its values are
+          // zeros (BLANK), since 0 times NaN is NaN.
+          constexpr uint32_t BLANK = 0x8000u;
+          const unsigned nan = __ballot_sync(0xffffffffu, scale == 255);
+          if (kv ? scale == 255 : ((nan | nan >> 8) >> (lane & 7) & 1u) != 0) by = kv ? BLANK : 0x7fffu;
           if (!wait(&empty[to], ((uint32_t)(fill / SLOTS) & 1u) ^ 1u)) break;
-          if (both) {
+          if (warp == 12) {
             // The scales of this tile take the place of those of four tiles ago: both tiles' S of the last K in this slot, or of a
             // later one, is done, and so is what their softmax did before.
             const int most_v = __reduce_max_sync(0xffffffffu, counts && lane >= 8 ? scale : -1);
@@ -847,6 +857,10 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) x[k] = *reinterpret_cast<const uint4*>(src + (i * PIFA_Q8_BLOCK + k * (32 / PIECES)) * D);
             const uint32_t f = __shfl_sync(0xffffffffu, by * 0x10001u, sub * BLOCKS + i);
+            if (f == BLANK * 0x10001u) {
+#pragma unroll
+              for (int k = 0; k < BATCH; ++k) x[k] = make_uint4(0, 0, 0, 0);
+            }
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
               uint32_t h[8];

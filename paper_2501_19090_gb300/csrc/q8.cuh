@@ -53,7 +53,7 @@ struct ValueScale {
   float exponent, inverse;  // log2 t - base, and 2^ the negative of it
 };
 // A block's scale byte against `base`. A scale of NaN gives weights of NaN to the keys that are seen, and leaves l alone where
-// none is.
+// none is. (Chunks make such a block's keys NaN instead, and its values zeros.)
 __device__ __forceinline__ ValueScale value_scale(int byte, float base) {
   if (byte == 255) return {__uint_as_float(0x7fffffffu), 0.0f};
   if (byte == NO_SCALE) return {0.0f, 1.0f};
