@@ -253,6 +253,7 @@ __device__ __forceinline__ void store_blocks(const StoreArgs& g, int wx, int par
       }
     }
     if (GW > 1) named_barrier_sync(1 + group, GW * 32);  // all have read the scale
+    else __syncwarp();
     if (l == 0) *scale = (uint8_t)byte;
   }
 }
