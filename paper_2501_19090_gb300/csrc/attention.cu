@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows(const RowArgs g) {
     const int b = find(first, g.B, at);
     const Lengths x = lengths_of(g, b);
     const int steps = steps_of(x), head = (at - first[b]) / steps, s0 = at - first[b] - head * steps;
-    const int s1 = min(steps, s0 + stop - at);
+    const int s1 = segment_end(steps, s0, at, stop);
     const int rows = x.n * g.group;
     // the rows of Q: this lane's are gr and gr + 8
     uint4 q[2][KC];

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
     const int b = find(first, g.B, at);
     const Lengths x = lengths(b);
     const int steps = steps_of(x), head = (int)((uint32_t)(at - first[b]) / (uint32_t)steps), s0 = at - first[b] - head * steps;
-    const int s1 = min(steps, s0 + stop - at);
+    const int s1 = segment_end(steps, s0, at, stop);
     const int rows = x.n * g.group;
     // The rows of Q: this lane's are gr (and gr + 8; SLIM: of the products' results, 2 c4 and 2 c4 + 1). Asked for before the copies, whose
     // queue is some thousand cycles long when all SMs begin.

@@ -11,6 +11,7 @@
 #include "pifa.h"
 #include "pifa_internal.h"
 #include "ptx.cuh"
+#include "steps.h"
 
 namespace {
 
