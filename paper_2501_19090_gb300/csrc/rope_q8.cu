@@ -367,10 +367,13 @@ int pifa_rope_cache_q8(const void* Q, int64_t ldq, const void* K, int64_t ldk, c
   // as in pifa_rope_cache: the caches, and the scales, may interleave, as may a row of Q that is turned in place with K and V
   bool bad = Qr == Q && ldqr == ldq ? pifa_rows_overlap(Q, qrow, ldq, K, krow, ldk, T) || pifa_rows_overlap(Q, qrow, ldq, V, krow, ldv, T)
                                     : pifa_spans_overlap(qr, in[0]) || pifa_spans_overlap(qr, in[1]) || pifa_spans_overlap(qr, in[2]);
+  const PifaSpan index[] = {pifa_span(positions, 1, T, T, 4), pifa_span(slots, 1, T, T, 8), pifa_span(freq, 1, rot_dim / 2, rot_dim / 2, 8)};
   for (const PifaSpan& o : out) {
     bad = bad || pifa_spans_overlap(o, qr);
     for (const PifaSpan& i : in) bad = bad || pifa_spans_overlap(o, i);
+    for (const PifaSpan& i : index) bad = bad || pifa_spans_overlap(o, i);
   }
+  for (const PifaSpan& i : index) bad = bad || pifa_spans_overlap(qr, i);
   if (bad || k_cache == v_cache || k_scale == v_scale) return pifa_fail(PIFA_ERR_INVALID_ARG, "an output overlaps another buffer");
   cudaError_t e = cudaSuccess;
   StoreArgs g = {};
