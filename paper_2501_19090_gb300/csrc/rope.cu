@@ -176,6 +176,8 @@ int pifa_rope_cache(const void* Q, int64_t ldq, const void* K, int64_t ldk, cons
   for (const PifaSpan& cache : {kc, vc})
     bad = bad || pifa_spans_overlap(cache, q) || pifa_spans_overlap(cache, in[0]) || pifa_spans_overlap(cache, in[1]) ||
           pifa_spans_overlap(cache, qr);
+  for (const PifaSpan& i : {pifa_span(positions, 1, T, T, 4), pifa_span(slots, 1, T, T, 8), pifa_span(freq, 1, rot_dim / 2, rot_dim / 2, 8)})
+    bad = bad || pifa_spans_overlap(kc, i) || pifa_spans_overlap(vc, i) || pifa_spans_overlap(qr, i);
   if (bad || k_cache == v_cache) return pifa_fail(PIFA_ERR_INVALID_ARG, "an output overlaps another buffer");
   RopeArgs g = {};
   g.q = static_cast<const uint16_t*>(Q);

@@ -22,7 +22,14 @@ def write_q8(lib, **kw):
     return lib.pifa_rope_cache_q8(*a.values(), None)
 
 
-WRITES = {"q8": (write_q8, 1, ("Qr", "kc", "vc", "ks", "vs"))}
+def write_16(lib, **kw):
+    a = dict(Q=Q, ldq=QROW, K=K, ldk=KROW, V=V, ldv=KROW, T=T, hq=2, hk=1, dim=128, dtype=0, pos=POS, slots=SLOTS, freq=FREQ, rot=128, layout=0,
+             scale=1.0, Qr=QR, ldqr=QROW, kc=KC, vc=VC, pages=PAGES, page=PAGE, ps=4096, ts=128, hs=128)
+    a.update(kw)
+    return lib.pifa_rope_cache(*a.values(), None)
+
+
+WRITES = {"q8": (write_q8, 1, ("Qr", "kc", "vc", "ks", "vs")), "16": (write_16, 2, ("Qr", "kc", "vc"))}
 
 
 def cases():
