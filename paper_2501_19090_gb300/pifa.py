@@ -1176,10 +1176,37 @@ def pifa_paged_attention_q8_workspace_size(T: int, q_heads: int, kv_heads: int, 
     return _attention_q8_workspace_size(int(T), int(q_heads), int(kv_heads), int(head_dim), int(B), int(max_q), int(cols), int(page_size))
 
 
+_no_room: dict = {}  # as _attention_workspaces: bytes that an allocation failed for, and the device's free memory then
+
+
+def _attention_q8_workspace(least, need, dev, run_on, stream):
+    """_attention_workspace of `need` bytes or, where there is no memory for them, of `least`."""
+    key = (dev, getattr(run_on, "value", run_on))
+    failed = _no_room.get(key)
+    # an allocation that fails gives back all that torch had kept for others: not tried again before as much has become free
+    if need > least and (failed is None or need < failed[0] or
+                         (not _captured(run_on) and _free_memory(dev) >= failed[1] + need)):
+        import torch
+        try:
+            ws = _attention_workspace(need, dev, run_on, stream)
+            if failed is not None and need >= failed[0]:
+                del _no_room[key]
+            return ws
+        except torch.OutOfMemoryError:
+            _no_room[key] = (need, 0 if _captured(run_on) else _free_memory(dev))
+    return _attention_workspace(least, dev, run_on, stream)
+
+
+def _free_memory(dev) -> int:
+    import torch
+    return torch.cuda.mem_get_info(dev)[0]
+
+
 def pifa_paged_attention_q8(Q, k_cache, v_cache, k_scale, v_scale, table, q_start, kv_len, max_q: int, scale=None, O=None,
                             workspace_tensor=None, stream=None):
     """pifa_paged_attention over a cache in 8 bits (pifa_paged_attention_q8): caches and scales as pifa_rope_cache_q8. Scratch as
-    there, of pifa_paged_attention_q8_workspace_size bytes; a workspace_tensor may be smaller, as that says."""
+    there, of pifa_paged_attention_q8_workspace_size bytes, up to a gigabyte more, which is done without where there is no memory for
+    it; a workspace_tensor may be smaller, as that says, and with one nothing is kept for the stream."""
     torch = sys.modules["torch"]
     run_on = _stream_ptr(stream)
     try:
@@ -1222,9 +1249,9 @@ def pifa_paged_attention_q8(Q, k_cache, v_cache, k_scale, v_scale, table, q_star
         if os_ != [T, h, d]:
             _refuse(f"O must be a tensor of shape {(T, h, d)}")
         dev = Q.get_device()
-    need = _attention_q8_workspace_size(T, h, hk, d, B, int(max_q), cols, size)
     if workspace_tensor is None:
-        ws_ptr, ws_bytes, _ = _attention_workspace(need, dev, run_on, stream)
+        need = _attention_q8_workspace_size(T, h, hk, d, B, int(max_q), cols, size)
+        ws_ptr, ws_bytes, _ = _attention_q8_workspace(_attention_workspace_size(T, h, hk, d, B, int(max_q)), need, dev, run_on, stream)
     else:
         ws = workspace_tensor
         if not isinstance(ws, torch.Tensor) or ws.get_device() != dev:
