@@ -124,7 +124,7 @@ struct TcArgs {
        most_keys, page_size, page_shift;  // most_keys: that the table has room for
   int token_at, head_at;             // their places among the tensor maps' coordinates 1 to 3; the page has the third
   float c;                           // |scale| log2(e)
-  float lift;                        // weights are held 2^lift times as large; 0 for a cache in 16 bits
+  float lift, rise;                  // 16 bits: m is the maximum less `lift`, and raised when a score passes it by `rise` in the exponent
   int negate;                        // scale < 0
   int wide;                          // rows of O start on 32-byte sectors
   int* status;
@@ -510,13 +510,11 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
   uint64_t* scales_full = raw_empty + C::RAWS;
   uint64_t* q_ready = scales_full + SCALED;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_ready + 2);
-  Item* items = reinterpret_cast<Item*>((reinterpret_cast<uintptr_t>(tmem_slot + 2) + 15) & ~uintptr_t(15));
+  constexpr uint32_t BARRIERS = 3 * SLOTS + 2 * C::RAWS + SCALED + 22;
+  constexpr uint32_t ITEMS_AT = ((2 + SLOTS) * TILE + C::RAWS * C::RAW + 8 * BARRIERS + 8 + 15) / 16 * 16;
+  Item* items = reinterpret_cast<Item*>(smem + ITEMS_AT);
   TileScales* scales = reinterpret_cast<TileScales*>(items + 2);
-  static_assert(C::SMEM >= 1024 + (2 + SLOTS) * TILE + C::RAWS * C::RAW + 8 * (3 * SLOTS + 2 * C::RAWS + SCALED + 22) + 8 + 16 +
-                               2 * sizeof(Item) + (Q8 ? SCALED * sizeof(TileScales) : 0), "what lies behind the tiles");
-  // what TMA fills
-  const uint32_t loads_at = smem_u32(Q8 ? raw : ring);
-  uint64_t *load_full = Q8 ? raw_full : full, *load_empty = Q8 ? raw_empty : empty;
+  static_assert(C::SMEM >= 1024 + ITEMS_AT + 2 * sizeof(Item) + (Q8 ? SCALED * sizeof(TileScales) : 0), "what lies behind the tiles");
 
   pdl_launch_dependents();
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -577,6 +575,8 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
   regs_lower<LOW>();
   // K (kv = 0) or V of an item's key tiles, fill after fill of the ring: K and V take its slots in turn. A lane
   // copies 64 columns of a page's rows (or of 128 of them). One warp issuing both was the bound for pages of 16.
+  // (Addresses that are computed before the warps part are kept by all: head_dim 64 spilled, and took 10% longer.)
+  uint64_t *load_full = Q8 ? raw_full : full, *load_empty = Q8 ? raw_empty : empty;
   auto stream = [&](int kv, int& tiles, int b, int L, int head, int j0, int j1, auto&& every) {
     const int per_tile = g.page_size >= BN ? 1 : BN / g.page_size, box_rows = min(g.page_size, BN);
     const int mine = Q8 ? lane : lane / (D / 64), half = Q8 ? 0 : lane % (D / 64);
@@ -605,8 +605,8 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
       if (lane == 0) mbar_arrive_expect_tx(&load_full[s], bytes);
       __syncwarp();
       if (has)
-        tma_load_4d(Q8 ? loads_at + (uint32_t)s * C::RAW + (uint32_t)(mine * box_rows) * (uint32_t)D
-                       : loads_at + (uint32_t)s * TILE + (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u,
+        tma_load_4d(Q8 ? smem_u32(raw) + (uint32_t)s * C::RAW + (uint32_t)(mine * box_rows) * (uint32_t)D
+                       : smem_u32(ring) + (uint32_t)s * TILE + (uint32_t)half * HALF + (uint32_t)(mine * box_rows) * 128u,
                     kv ? &vmap : &kmap, half * 64, y, z, w, &load_full[s]);
       ++tiles;
       id = next;
@@ -1007,142 +1007,142 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
             tmem_st_32x32b_x16(o_at + i * 16, o);
           }
         };
-        if (idle) {
-          if (lane == 0) {
-            mbar_arrive(&p_full[2 * t]);
-            mbar_arrive(&p_full[2 * t + 1]);
-          }
-        } else if constexpr (Q8) {
-          // As below, but that m is in the exponents' units, holds the values' scale, and is the maximum less LIFT.
-          const int tile = tiles + j - it.j0;
-          if (!wait(&scales_full[tile % SCALED], (uint32_t)(tile / SCALED) & 1u)) break;
-          const TileScales sc = scales[tile % SCALED];
-          base = sc.base;
-          tc_fence_after();
-          const float ct = fmaxf(c * sc.key, 1e-37f);  // (-inf times 0 is NaN)
-          const uint64_t c2 = f32x2(ct, ct);
-          const bool partly = __any_sync(0xffffffffu, lim < BN);
-          uint64_t sum[2];
-          uint32_t v[4][32], w[4][16];
-          auto weights = [&](int i) {  // keys 32 i to 32 i + 31
-            const float off = sc.exponent - (m > -INFINITY ? m : 0.0f);
-            const uint64_t off2 = f32x2(off, off);
+        if (!idle) {
+          if constexpr (Q8) {
+            // As below, but that m is in the exponents' units, holds the values' scale, and is the maximum less LIFT.
+            const int tile = tiles + j - it.j0;
+            if (!wait(&scales_full[tile % SCALED], (uint32_t)(tile / SCALED) & 1u)) break;
+            const TileScales sc = scales[tile % SCALED];
+            base = sc.base;
+            tc_fence_after();
+            const float ct = fmaxf(c * sc.key, 1e-37f);  // (-inf times 0 is NaN)
+            const uint64_t c2 = f32x2(ct, ct);
+            const bool partly = __any_sync(0xffffffffu, lim < BN);
+            uint64_t sum[2];
+            uint32_t v[4][32], w[4][16];
+            auto weights = [&](int i) {  // keys 32 i to 32 i + 31
+              const float off = sc.exponent - (m > -INFINITY ? m : 0.0f);
+              const uint64_t off2 = f32x2(off, off);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), c2, off2));
-              const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
-              sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
-              w[i][k] = pack<true>(p0, p1);
-            }
-          };
-          bool raised = sc.up > 0.0f;
+              for (int k = 0; k < 16; ++k) {
+                const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), c2, off2));
+                const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+                sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
+                w[i][k] = pack<true>(p0, p1);
+              }
+            };
+            bool raised = sc.up > 0.0f;
 #pragma unroll 1
-          while (true) {
+            while (true) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
-            tmem_ld_wait();
-            if (partly) {
+              for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
+              tmem_ld_wait();
+              if (partly) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
+                  for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
+              }
+              float mx[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
+#pragma unroll
+                for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
+              }
+              const float top = fmaf(max3(mx[0], mx[1], fmaxf(mx[2], mx[3])), ct, sc.exponent);
+              if (!fresh && !raised) {
+                sum[0] = sum[1] = 0;
+#pragma unroll
+                for (int i = 0; i < EARLY; ++i) weights(i);
+                if (!__any_sync(0xffffffffu, top - m > RISE)) break;
+              }
+              fresh = false;
+              const float most = fmaxf(m, top - LIFT);
+              float f = m > -INFINITY ? fast_exp2(m - most) : 1.0f;  // (nothing was seen before: zeros)
+              m = most;
+              l *= f;
+              if (raised) f *= exponent_of_2(-(int)fminf(sc.up, 126.0f));  // O, but not l, is in units of 2^base
+              raised = false;
+              if (j > it.j0) rescale(f);
             }
-            float mx[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
+            for (int i = 0; i < EARLY; ++i) tmem_st_32x32b_x16(s_at + i * 16, w[i]);
+            hand_over(0);
 #pragma unroll
-              for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
+            for (int i = EARLY; i < 4; ++i) {
+              weights(i);
+              tmem_st_32x32b_x16(s_at + i * 16, w[i]);
             }
-            const float top = fmaf(max3(mx[0], mx[1], fmaxf(mx[2], mx[3])), ct, sc.exponent);
-            if (!fresh && !raised) {
-              sum[0] = sum[1] = 0;
+            hand_over(1);
+            const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
+            l = fmaf(both.x + both.y, sc.inverse, l);
+          } else {
+            tc_fence_after();
+            uint32_t v[4][32];
+            // The weights of the first 64 keys with the maximum as it was, beside the search for the new one; they
+            // are computed again, from S, if that has grown too far, as it does for the first keys and seldom later.
+            uint64_t sum[2];
+            uint32_t w[4][16];
+            const uint64_t c2 = f32x2(c, c);
+            auto weights = [&](int i) {  // keys 32 i to 32 i + 31
+              const float mc = m > -INFINITY ? -m * c : 0.0f;
+              const uint64_t mc2 = f32x2(mc, mc);
 #pragma unroll
-              for (int i = 0; i < EARLY; ++i) weights(i);
-              if (!__any_sync(0xffffffffu, top - m > RISE)) break;
-            }
-            fresh = false;
-            const float most = fmaxf(m, top - LIFT);
-            float f = m > -INFINITY ? fast_exp2(m - most) : 1.0f;  // (nothing was seen before: zeros)
-            m = most;
-            l *= f;
-            if (raised) f *= exponent_of_2(-(int)fminf(sc.up, 126.0f));  // O, but not l, is in units of 2^base
-            raised = false;
-            if (j > it.j0) rescale(f);
-          }
-#pragma unroll
-          for (int i = 0; i < EARLY; ++i) tmem_st_32x32b_x16(s_at + i * 16, w[i]);
-          hand_over(0);
-#pragma unroll
-          for (int i = EARLY; i < 4; ++i) {
-            weights(i);
-            tmem_st_32x32b_x16(s_at + i * 16, w[i]);
-          }
-          hand_over(1);
-          const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
-          l = fmaf(both.x + both.y, sc.inverse, l);
-        } else {
-          tc_fence_after();
-          uint32_t v[4][32];
-          // The weights of the first 64 keys with the maximum as it was, beside the search for the new one; they
-          // are computed again, from S, if that has grown too far, as it does for the first keys and seldom later.
-          uint64_t sum[2];
-          uint32_t w[4][16];
-          const uint64_t c2 = f32x2(c, c);
-          auto weights = [&](int i) {  // keys 32 i to 32 i + 31
-            const float mc = m > -INFINITY ? fmaf(-m, c, g.lift) : 0.0f;
-            const uint64_t mc2 = f32x2(mc, mc);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), c2, mc2));
-              const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
-              sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
-              w[i][k] = pack<F16>(p0, p1);
-            }
-          };
+              for (int k = 0; k < 16; ++k) {
+                const float2 x = f32x2_parts(fma_f32x2(f32x2(__uint_as_float(v[i][2 * k]), __uint_as_float(v[i][2 * k + 1])), c2, mc2));
+                const float p0 = fast_exp2(x.x), p1 = fast_exp2(x.y);
+                sum[k & 1] = add_f32x2(sum[k & 1], f32x2(p0, p1));
+                w[i][k] = pack<F16>(p0, p1);
+              }
+            };
 #pragma unroll 1
-          while (true) {
+            while (true) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
-            tmem_ld_wait();
-            if (__any_sync(0xffffffffu, lim < BN)) {
+              for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_at + i * 32, v[i]);
+              tmem_ld_wait();
+              if (__any_sync(0xffffffffu, lim < BN)) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
+                  for (int k = 0; k < 32; ++k) v[i][k] = i * 32 + k < lim ? v[i][k] : 0xff800000u;
+              }
+              float mx[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
+#pragma unroll
+                for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
+              }
+              const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
+              if (!fresh) {
+                sum[0] = sum[1] = 0;
+#pragma unroll
+                for (int i = 0; i < EARLY; ++i) weights(i);
+                if (!__any_sync(0xffffffffu, (top - m) * c > g.rise)) break;
+              }
+              fresh = false;
+              const float up = fmaxf(m, top - g.lift);
+              const float f = m > -INFINITY ? fast_exp2((m - up) * c) : 1.0f;  // (nothing was seen before: zeros)
+              m = up;
+              l *= f;
+              if (j > it.j0) rescale(f);
             }
-            float mx[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              mx[i] = fmaxf(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]));
+            for (int i = 0; i < EARLY; ++i) tmem_st_32x32b_x16(s_at + i * 16, w[i]);
+            hand_over(0);
 #pragma unroll
-              for (int k = 2; k < 32; k += 2) mx[i] = max3(mx[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
+            for (int i = EARLY; i < 4; ++i) {
+              weights(i);
+              tmem_st_32x32b_x16(s_at + i * 16, w[i]);
             }
-            const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3]));
-            if (!fresh) {
-              sum[0] = sum[1] = 0;
-#pragma unroll
-              for (int i = 0; i < EARLY; ++i) weights(i);
-              if (!__any_sync(0xffffffffu, (top - m) * c > 8.0f)) break;
-            }
-            fresh = false;
-            const float up = fmaxf(m, top);
-            const float f = m > -INFINITY ? fast_exp2((m - up) * c) : 1.0f;  // (nothing was seen before: zeros)
-            m = up;
-            l *= f;
-            if (j > it.j0) rescale(f);
+            hand_over(1);
+            const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
+            l += both.x + both.y;
           }
-#pragma unroll
-          for (int i = 0; i < EARLY; ++i) tmem_st_32x32b_x16(s_at + i * 16, w[i]);
-          hand_over(0);
-#pragma unroll
-          for (int i = EARLY; i < 4; ++i) {
-            weights(i);
-            tmem_st_32x32b_x16(s_at + i * 16, w[i]);
-          }
-          hand_over(1);
-          const float2 both = f32x2_parts(add_f32x2(sum[0], sum[1]));
-          l += both.x + both.y;
+        } else if (lane == 0) {
+          mbar_arrive(&p_full[2 * t]);
+          mbar_arrive(&p_full[2 * t + 1]);
         }
       }
       tiles += it.j1 - it.j0;
@@ -1393,7 +1393,10 @@ int launch_attention_tc(const PifaAttention& given, bool wide, int* status, uint
   g.wide = ((reinterpret_cast<uintptr_t>(a.o) | (uintptr_t)(a.ldo * 2)) & 31u) == 0;
   // equal weights for a scale of zero: the masked scores, -inf, still have to vanish
   g.c = a.scale_log2 == 0.0f ? 1e-30f : std::fabs(a.scale_log2);
-  g.lift = wide && a.dtype == PIFA_DTYPE_FP16 ? LIFT : 0.0f;
+  // (weights of keys and values that were brought to fp16; with a scale near zero, by less)
+  const bool lifted = wide && a.dtype == PIFA_DTYPE_FP16;
+  g.lift = lifted ? std::fmin(LIFT / g.c, 1e37f) : 0.0f;
+  g.rise = lifted ? RISE : RISE - LIFT;
   g.status = status;
   g.timeout_ns = timeout_ns;
   CUtensorMap qmap, kmap, vmap;

@@ -42,15 +42,15 @@ def sink(n, d, dtype, nats, sink_scale=127):
     return a, float(v.max())
 
 
-def check(a, path, slack):
+def check(a, path, slack, scale=None):
     """The request, many times over the same pages, each against 64 bits."""
     n, B, room = PATHS[path]
     dtype, d = a["Q"].dtype, a["Q"].shape[2]
     many = dict(a, Q=a["Q"].repeat(B, 1, 1), table=a["table"].repeat(B, 1), kv_len=a["kv_len"].repeat(B),
                 q_start=torch.arange(B + 1, device=DEV, dtype=torch.int32) * n)
-    O = attend(many, max_q=n, room=room)
+    O = attend(many, max_q=n, room=room, scale=scale)
     assert P.pifa_device_status() == P.PIFA_OK and many["wide"] == (path == "long_chunk_widened")
-    want, size, _ = plain_attention(a, d ** -0.5)
+    want, size, _ = plain_attention(a, d ** -0.5 if scale is None else scale)
     w = U[dtype] if many["wide"] else 2.0 ** -11
     tol = U[dtype] * want.abs() + (1.1 * w + 2e-4) * size
     if not (many["wide"] and dtype is torch.bfloat16):
@@ -70,6 +70,14 @@ def test_many_small_weights_beside_a_large_one(path, dtype, d, nats):
     for sink_scale in (127, 100):
         a, most = sink(PATHS[path][0], d, dtype, nats, sink_scale)
         assert float(check(a, path, 2.0 ** -32 * L * most).min()) > 0.0
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-44, 1e-37, 1e-20])
+@pytest.mark.parametrize("path", list(PATHS))
+def test_equal_weights(path, scale):
+    """Scales so small that all weights are equal: what brings the reference 7 below the maximum must stay finite."""
+    a, most = sink(PATHS[path][0], 64, torch.float16, 4)
+    check(a, path, 2.0 ** -32 * L * most, scale)
 
 
 @pytest.mark.parametrize("path", list(PATHS))
