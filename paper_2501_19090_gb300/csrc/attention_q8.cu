@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
     }
     cp_wait<0>();
     // o[i][2 r + e]: row gr + 8 r, column i of the VC of lane group 2 c4 + e; SLIM: o[i][2 e + r]: row 2 c4 + r, column 2 i + e of gr's.
-    // In units of 2^base.
+    // In units of 2^base, and of UNLIFT.
     const float unit = base > NO_BASE ? exponent_of_2((int)base) : 1.0f;
     const bool alone = s0 == 0 && s1 == steps;
     const int which = 2 * warp + (at + s1 - s0 == stop ? 1 : 0);  // a piece's place: the warp's first, or what it ends with
@@ -443,8 +443,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
       if (SLIM) l[r] += __shfl_xor_sync(0xffffffffu, l[r], 16);
       const int row = SLIM ? 2 * c4 + r : gr + 8 * r, token = row / g.group;
       if (row >= rows) continue;
-      const float inv = !alone ? 1.0f : l[r] == 0.0f ? 0.0f : 1.0f / l[r];
-      if (!alone && (SLIM ? gr : c4) == 0) ml[which][row] = make_float2(m[r], l[r]);
+      const float inv = !alone ? UNLIFT : l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+      if (!alone && (SLIM ? gr : c4) == 0) ml[which][row] = make_float2(m[r], l[r] * UNLIFT);
 #pragma unroll
       for (int e = 0; e < (SLIM ? 1 : 2); ++e) {
         const int n = SLIM ? gr : 2 * c4 + e, col = VC * (D == 128 ? (n >> 1) | (n & 1) << 2 : n);

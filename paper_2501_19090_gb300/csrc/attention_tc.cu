@@ -1189,14 +1189,14 @@ __global__ void __launch_bounds__(kThreads<Q8>, 1)
             }
             if (Q8) {
 #pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * unit);
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * UNLIFT * unit);
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k)
               __stcg(reinterpret_cast<uint4*>(mine) + (w8 * (D / 4) + i * 8 + k) * 32 + lane,
                      make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]));
           }
-          __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, make_float2(Q8 ? m : m * c, l));
+          __stcg(reinterpret_cast<float2*>(mine + ROWS * D) + w8 * 32 + lane, Q8 ? make_float2(m, l * UNLIFT) : make_float2(m * c, l));
           __threadfence();
           __syncwarp();
         }

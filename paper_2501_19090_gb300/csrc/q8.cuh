@@ -23,6 +23,7 @@ namespace pifa {
 // rid of), and those below fp16's normal range are off by 2^-32 of the largest. They count: the tens of thousands of keys beside one
 // that has all but a millionth of the weight, and a value near zero, are all of o. (Without it, those 2^-25 of the largest and less were in l alone.)
 constexpr float LIFT = 7.0f, RISE = 8.0f + LIFT;
+constexpr float UNLIFT = 0x1p-7f;  // pieces that are written to be added up leave these units: values may be near fp32's largest
 
 constexpr float NO_BASE = -1000.0f;
 constexpr float FAR = 40.0f;

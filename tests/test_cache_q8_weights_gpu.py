@@ -80,6 +80,23 @@ def test_equal_weights(path, scale):
     check(a, path, 2.0 ** -32 * L * most, scale)
 
 
+@pytest.mark.parametrize("dtype,top", [(torch.bfloat16, 119), (torch.float16, 7)])
+@pytest.mark.parametrize("new", [1, 2, 60, 150])
+def test_values_near_the_largest_of_the_type(new, dtype, top):
+    """One key takes all, and its values are the largest that a block holds: sums that are cut along the keys stay finite."""
+    d = 128
+    a, _ = sink(new, d, dtype, 60)
+    page = int(a["table"][0, 0])
+    a["v8"].view(U8)[page, 0] = torch.full((HK, d), 448.0, device=DEV).to(E4M3).view(U8)
+    a["vs"].view(U8)[page, 0] = 127 + top
+    a["k_cache"], a["v_cache"] = values(a["k8"], a["ks"]), values(a["v8"], a["vs"])
+    want, _, _ = plain_attention(a, d ** -0.5)
+    for room in (False, True):
+        O = attend(a, room=room)                         # one request: its keys are cut
+        err = (O.double() - want).abs()
+        assert bool(O.isfinite().all()) and bool((err <= (U[dtype] + 1.1 * 2.0 ** -8 + 2e-4) * want).all()), float((err / want).max())
+
+
 @pytest.mark.parametrize("path", list(PATHS))
 def test_the_largest_weight_may_come_late_and_in_steps(path):
     """Maxima that rise by less than what raises the reference, so that weights reach the largest that they may: scores rise by 5 in
