@@ -558,7 +558,12 @@ int pifa_cache_read_q8(const void* k_cache, const void* v_cache, const void* k_s
  *   (the keys') or as part of the weights' exponent (the values'). Weights are fp16, held so that the largest lie between 2^7 and 2^15
  *   (those below 2^-21 of the largest are off by 2^-32 of it); scores, running maximum and sums fp32.
  *   Of long chunks, with room for it (pifa_paged_attention_q8_workspace_size), keys and values are rounded to dtype once, the weights are
- *   of dtype (fp16: held as said), and all else is as in pifa_paged_attention.
+ *   of dtype (fp16: held as said; a key or value beyond fp16's largest number becomes that), and all else is as in pifa_paged_attention.
+ *   A value whose scale is less than 2^-40 of the largest of its request and head may count with that scale instead: off by 2^-39 of the
+ *   largest value at most.
+ *   max_q and the workspace decide for all requests of a call: beside one long chunk, requests with one new token go to the tensor
+ *   cores too, and with room for it their whole contexts are brought to 16 bits, several times the bytes that they need. Where they
+ *   have much of the call's keys, give them a call of their own, or a workspace of pifa_paged_attention_workspace_size() bytes.
  */
 int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                             int dtype, const void* k_cache, const void* v_cache, const void* k_scale, const void* v_scale,
@@ -570,7 +575,8 @@ int pifa_paged_attention_q8(const void* Q, int64_t ldq, int64_t T, int64_t q_hea
 
 /* pifa_paged_attention_q8_workspace_size -- bytes of device scratch with which pifa_paged_attention_q8 is fastest:
  * pifa_paged_attention_workspace_size() is enough, more is room for the keys and values of long chunks in 16 bits (group max_q > 768
- * rows, and at most 1 GB for B requests of cols * page_size tokens). Negative pifa_status on bad arguments. Pure host arithmetic. */
+ * rows, and at most 1 GB for B requests of cols * page_size tokens, however short they are: tables no wider than need be keep it). Negative
+ * pifa_status on bad arguments. Pure host arithmetic. */
 int64_t pifa_paged_attention_q8_workspace_size(int64_t T, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t B,
                                                int64_t max_q, int64_t cols, int64_t page_size);
 

@@ -16,7 +16,9 @@
 //
 // Measured, head_dim 128, bf16, 64 heads on 8 key / value heads: 64 sequences of 500 to 20000 keys (273 MB) 58 to 62 us, 4.4 to 4.7
 // TB/s; one of 100000 (205 MB) 40 us, 5.1 TB/s; one of 800000 (1.64 GB) 254 us, 6.5 TB/s. A kernel that only reads takes 43 to 47, 34 to
-// 36 and 229 to 256 us for as many bytes. One sequence of 351 keys, 32 heads: 6.7 us. Between the first data and the last, memory is the bound (100000
+// 36 and 229 to 256 us for as many bytes. One sequence of 351 keys, 32 heads: 6.4 us; in a table with room for 32768, its heads cut, 7.1.
+// 9 to 16 rows: 64 heads on 4, 100000 keys (102 MB), 28.5 us, where 8 rows take 26.3; 2 new tokens of 64 sequences (1.15 GB) 205, where one takes 192;
+// head_dim 64, 64 heads on 4, 100000 keys 22.5 and 19.7. Between the first data and the last, memory is the bound (100000
 // keys: 7.4 TB/s); before it are 9 to 10 thousand cycles of lengths, dealing, table, first copies, mostly their latencies and first fetches of
 // code, behind it 4 to 5 thousand of adding up, and the join, 2.5 us.
 // Steps (first two cases): a warp for each row 20.5 and 130 ms; pieces of warps, joined by the second kernel 73 and 62 us; pieces added up in
@@ -105,7 +107,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_rows_q8(const RowArgs g,
   __shared__ float2 ml[2 * WARPS][ROWS];
   const int lane = threadIdx.x & 31, warp = uniform((int)threadIdx.x >> 5);
   pdl_wait_primary();
-  pdl_launch_dependents();  // (after the wait: the join reads the lengths before its own)
+  pdl_launch_dependents();  // (the join's CTAs begin beside these, and wait for their end)
   const Run dealt = deal_steps(g, first, part, (int)gridDim.x, LEAST, [&](int b, const Lengths& x) {
     if (b < KEPT) kept[b] = x;
   });

@@ -10,7 +10,8 @@
 // and sum need no exchange; p = exp2(c s - c m) goes back to tensor memory as bf16 or fp16 over S's columns
 // and is the first operand of O += P V. m is only raised, and O and l rescaled, when the row's maximum
 // has grown by more than 8 in the exponent (then O's columns are read and written by the row's warp);
-// until then weights reach 2^8 at most, which costs neither format precision. The rounding of the weights, which l
+// until then weights reach 2^8 at most, which costs neither format precision (but fp16's range: weights below 2^-14 of what they refer
+// to are off by 2^-25 of it; a cache in 8 bits holds them 2^7 times as large, q8.cuh). The rounding of the weights, which l
 // adds up as they were, takes the outputs' error from 0.0017 of their size to 0.0022 in bf16, from 0.00021 to 0.00026 in fp16; a
 // product of their lower parts as well, half as many MMAs again, was not taken.
 //
@@ -37,10 +38,13 @@
 // Q from bf16 to fp16. What bounds it is that work: a tile of K or V takes its two warps 2000 to 2300 cycles, next to 2048 of MMAs
 // that leave little of shared memory's time; and instruction fetch: all of a warp's rows unrolled (10 KB more) took a tile's softmax from
 // 2650 to 3750 cycles. Chunks whose rows would convert the same keys several times have them converted once, by a kernel that makes
-// the plan too, and run as above. Measured, head_dim 128: 2048 tokens over 30000 cached, 64 heads on 8: 1.79 ms with conversion inside,
-// 1.34 to 1.40 with it before (36 us of it; a cache in 16 bits of the same values 1.36); a prompt of 1900, 32 heads, 69 and 53 us (12; 48.5);
-// 512 rows a head over 30000, 8 heads: 88 and 100. These keys have a few large columns: on normal ones, whose running maxima
-// rise less often, 16 bits take 1.23 ms and 37.6 us.
+// the plan too, and run as above. Measured, head_dim 128: 2048 tokens over 30000 cached, 64 heads on 8: 1.78 ms with conversion inside,
+// 1.36 to 1.41 with it before (36 us of it; a cache in 16 bits of the same values 1.36); a prompt of 1900, 32 heads, 69 and 53 us (12; 47.5);
+// 512 rows a head over 30000, 8 heads: 85 and 100. These keys (but the last's) have a few large columns: on normal ones, whose running maxima
+// rise less often, conversion inside takes 1.60 ms and 59 us, before 1.09 and 49. The call decides, not the request: 30
+// requests with one new token over 8000 keys beside a chunk of 128 take 416 us converted before, 258 with conversion inside; the two
+// kinds as two calls 116 and 20. The instances that convert inside spill (bf16, head_dim 128: 84 bytes of stores, 68 of loads a thread; head_dim 64 52 and 32;
+// fp16 fewer): 128 registers a thread, moved to the softmax as far as they go.
 //
 // Measured, head_dim 128, bf16: 2048 tokens over 30000 cached, 64 heads on 8 key / value heads, pages of 64: 1.20 to 1.27 ms,
 // 1640 to 1740 TFLOP/s of the visible pairs (the measured bf16 rate is 1910 in a burst, 1702 for seconds: the power cap is what
